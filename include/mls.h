@@ -311,6 +311,160 @@ mls_status mls_junction_bwd(const mls_junction* j, const void* o, const void* e,
                             void* g_o, void* g_e, void* stream);
 
 /*
+ * Layer norm of hidden states in front of a head: per row x of d entries
+ *   y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias.
+ * Means and sums are fp32, taken from the deviations (not from a sum of squares).
+ */
+typedef struct mls_layer_norm {
+  int64_t T;            /* rows, >= 1 */
+  int64_t d;            /* width, 1..16384 (multiples of 8 (bf16) or 4 (f32) take wide accesses) */
+  int64_t ld_x;         /* elements between rows of x, >= d: x may be columns of a wider array */
+  int32_t act_dtype;    /* mls_dtype of x, y, g_y and g_x */
+  int32_t param_dtype;  /* mls_dtype of weight, bias and their gradients */
+  float eps;            /* finite and > 0 */
+  int32_t reserved;     /* 0 */
+} mls_layer_norm;
+
+/*
+ * Forward: y [T][d] from x ([T] rows of d entries, ld_x apart), weight [d] and bias
+ * [d] (may be NULL). stats (device float32 [2][T]: each row's mean, then its
+ * 1 / sqrt(variance + eps)) is what the backward reads; NULL if none follows. y
+ * must not overlap x. Pointers need their element's alignment; rows whose
+ * addresses, width and stride are multiples of 16 bytes are the fast ones.
+ * Asynchronous on stream.
+ */
+mls_status mls_layer_norm_fwd(const mls_layer_norm* n, const void* x, const void* weight,
+                              const void* bias, void* y, float* stats, void* stream);
+
+/* Workspace bytes of mls_layer_norm_bwd. */
+mls_status mls_layer_norm_workspace(const mls_layer_norm* n, size_t* bytes);
+
+/*
+ * Backward for the gradient g_y [T][d] of y: with xh the normalised row, r its
+ * 1 / sqrt(variance + eps) and u = g_y weight,
+ *   g_x = r (u - mean(u) - xh mean(u xh)),  g_weight = sum_t g_y xh,  g_bias = sum_t g_y.
+ * Each output may be NULL to skip it. The sums over t are fp32 and rounded once to
+ * param_dtype, in a fixed order. The workspace is needed for g_weight or g_bias only.
+ * g_x must not overlap x or g_y. Asynchronous on stream.
+ */
+mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void* weight,
+                              const float* stats, const void* g_y, void* g_x, void* g_weight,
+                              void* g_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log-probabilities of given tokens under one head, for post-training: with
+ * p->M = 1, temperature p->tau and the tokens in p->labels,
+ *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
+ *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
+ * as device float32 [T]. p->alpha and p->teacher do not matter. No [T, V] array is
+ * kept. stats and workspace as mls_query_sizes gives them; stats receives the
+ * rows' log-sum-exp (in the place of lset) for the backward and the device flags
+ * (mls_device_error; a token outside [0, V) is treated as ignored and raises
+ * MLS_DEVFLAG_LABEL_RANGE, a log-probability that is NaN or infinite
+ * MLS_DEVFLAG_NONFINITE); its valid-token count is 0. Asynchronous on stream.
+ */
+mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward for the gradient g_logp (device float32 [T]) of logp; the entropy is not
+ * differentiated. With G[t] = g_logp[t] / tau (onehot(tokens[t]) - softmax(W h[t] / tau)),
+ * 0 on ignored tokens (whose g_logp is not read):
+ *   grad_h = G W  [T, d] of p->grad_h_dtype,
+ *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
+ * Either may be NULL. The logits are recomputed one vocabulary chunk at a time and
+ * G is rounded to bfloat16 (bf16 inputs) in between, as in mls_distill_bwd, whose
+ * accumulation flags apply. stats: as mls_token_logp_fwd left it on the same
+ * inputs. Asynchronous on stream.
+ */
+mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp,
+                              void* grad_h, void* grad_W, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
+ * Clipped policy loss with a KL term on token log-probabilities. Per counted
+ * token with advantage A and r = exp(logp - old_logp),
+ *   L = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef k,
+ *   k = exp(ref_logp - logp) - (ref_logp - logp) - 1,
+ * and loss = sum of w L with w = 1 / (counted tokens), or with
+ * MLS_POLICY_MEAN_OF_SEQUENCES w = 1 / (sequences with a counted token x counted
+ * tokens of the token's own sequence). A token counts where mask is nonzero (NULL:
+ * everywhere) and, when sequences are given, it lies in one: sequence s is
+ * [cu_seqlens[s], cu_seqlens[s + 1]), offsets ascending (empty sequences are
+ * allowed; offsets outside [0, N] are taken as the nearest end). Values at tokens
+ * that do not count are not used, and their gradients are 0. All of it is computed
+ * in 64 bits from the float32 inputs; a tie between the two products counts as
+ * not clipped.
+ */
+enum mls_policy_flags {
+  MLS_POLICY_ADV_PER_SEQUENCE = 1u, /* advantages [S], one per sequence, instead of [N] */
+  MLS_POLICY_MEAN_OF_SEQUENCES = 2u /* mean over sequences of their tokens' means */
+};
+typedef struct mls_policy {
+  int64_t N;         /* tokens, 1..2^31 - 1 */
+  int64_t S;         /* sequences; 0: none are given */
+  double clip_low;   /* in [0, 1] */
+  double clip_high;  /* >= 0; may be infinite */
+  double kl_coef;    /* finite and >= 0 */
+  uint32_t flags;    /* mls_policy_flags */
+  int32_t reserved;  /* 0 */
+} mls_policy;
+
+/* Workspace bytes of mls_policy_loss_fwd. */
+mls_status mls_policy_loss_workspace(const mls_policy* p, size_t* bytes);
+
+/*
+ * Forward. Device arrays: logp, old_logp [N], advantages [N] or [S], ref_logp [N]
+ * (may be NULL when kl_coef is 0; k is reported where it is given), mask uint8 [N]
+ * (may be NULL), cu_seqlens int32 [S + 1] (NULL with S = 0), all float32 otherwise.
+ *   loss, kl, clipped  float32 [1]: the loss, the mean k and the share of clipped
+ *         tokens, each with the weights w above; 0 when nothing counts (kl and
+ *         clipped may be NULL)
+ *   grad  float32 [N + 1] (may be NULL): what the backward reads, the tokens' dL/dlogp
+ *         and 1 / (tokens or sequences counted)
+ * Asynchronous on stream.
+ */
+mls_status mls_policy_loss_fwd(const mls_policy* p, const float* logp, const float* old_logp,
+                               const float* advantages, const float* ref_logp, const uint8_t* mask,
+                               const int32_t* cu_seqlens, float* loss, float* kl, float* clipped,
+                               float* grad, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward: g_logp [N] = gradient of logp for the gradient g_loss (device float32
+ * [1]) of the loss, from the forward's grad. Asynchronous on stream.
+ */
+mls_status mls_policy_loss_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp,
+                               void* stream);
+
+/*
+ * Global L2 norm of a list of gradient tensors, and their clipping (the paper's
+ * recipe, section 3, clips at 1.0):
+ *   norm = sqrt(sum over all tensors and elements of x^2),  out = x * min(1, max_norm / norm).
+ * Squares are added in 64 bits, in a fixed order. A norm that is NaN or infinite
+ * scales nothing (the caller sees it in norm and skips the step).
+ */
+typedef struct mls_grad_tensor {
+  const void* data;  /* device, n elements */
+  void* out;         /* device, n elements of the same type: data itself (in place) or an
+                        array apart from it */
+  int64_t n;         /* elements, >= 0 */
+  int32_t dtype;     /* mls_dtype */
+  int32_t reserved;  /* 0 */
+} mls_grad_tensor;
+
+/* Workspace bytes of mls_clip_grad_norm for these tensors (their sizes matter). */
+mls_status mls_clip_grad_norm_workspace(int64_t count, const mls_grad_tensor* tensors, size_t* bytes);
+
+/*
+ * tensors: host array of `count` descriptors (read during the call). norm: device
+ * float32 [1]. max_norm = 0 computes the norm alone (no out is read or written);
+ * otherwise an out that overlaps another tensor of the list is an error. Asynchronous
+ * on stream.
+ */
+mls_status mls_clip_grad_norm(int64_t count, const mls_grad_tensor* tensors, double max_norm,
+                              float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Head step of nested speculative decoding (paper section 2, paragraph
  * "Speculative Decoding"; section 3 measures greedy and nucleus top-p 0.9
  * sampling at temperature 0.4). A smaller sub-model drafts gamma tokens and a

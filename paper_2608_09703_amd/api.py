@@ -15,11 +15,13 @@ on caller-visible buffers (used by the tests and the benchmark).
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -28,6 +30,9 @@ from . import binding as B
 # fields costs about as much as the launch.
 _make_junction = functools.lru_cache(maxsize=256)(B.make_junction)
 _make_sampling = functools.lru_cache(maxsize=256)(B.make_sampling)
+_make_layer_norm = functools.lru_cache(maxsize=256)(B.make_layer_norm)
+_layer_norm_workspace = functools.lru_cache(maxsize=256)(
+    lambda *key: B.layer_norm_workspace(_make_layer_norm(*key)))
 
 
 def _sampling(V, temperature, top_p, greedy) -> B.Sampling:
@@ -81,6 +86,14 @@ def _stream(dev) -> int:
     if _raw_stream is not None and isinstance(dev, torch.device) and dev.index is not None:
         return _raw_stream(dev.index)
     return torch.cuda.current_stream(dev).cuda_stream
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(dev: torch.device):
+    """The device the tensors live on as the current one, for the launches inside."""
+    return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
 class Buffers:
@@ -272,6 +285,303 @@ class _Junction(torch.autograd.Function):
 def junction(o: torch.Tensor, e: torch.Tensor, *, layout: str = "prev_first") -> torch.Tensor:
     """Inter-model junction of eq. (1) with autograd through the HIP kernels."""
     return _Junction.apply(o, e, layout)
+
+
+# ---------------------------------------------------------------------------
+# post-training: the norm in front of a head, token log-probabilities, the policy
+# loss on them and the clipping of the gradients
+# ---------------------------------------------------------------------------
+
+def _norm_rows(x: torch.Tensor):
+    """``x [..., d]`` as rows: (2-D view, elements between rows)."""
+    if x.dim() < 1 or x.numel() == 0 or (x.size(-1) > 1 and x.stride(-1) != 1):
+        raise ValueError("x must be a non-empty [..., d] tensor with neighbouring elements in a row")
+    try:
+        rows = x.view(-1, x.size(-1))
+    except RuntimeError as e:
+        raise ValueError("the rows of x must lie at one distance from each other") from e
+    ld = rows.stride(0) if rows.size(0) > 1 else rows.size(1)
+    if ld < rows.size(1):
+        raise ValueError("the rows of x must not overlap (an expanded x: call .contiguous())")
+    return rows, ld
+
+
+def _norm_desc(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], eps: float):
+    if not x.is_cuda or weight.device != x.device or (bias is not None and bias.device != x.device):
+        raise RuntimeError("layer_norm runs on the GPU only, on tensors of one device")
+    rows, ld = _norm_rows(x)
+    d = rows.size(1)
+    for p in (weight, bias):
+        if p is not None and (p.shape != (d,) or not p.is_contiguous() or p.dtype != weight.dtype):
+            raise ValueError("weight and bias must be contiguous [d] tensors of one dtype")
+    return rows, (rows.size(0), d, ld, _dtype_code(x.dtype), _dtype_code(weight.dtype),
+                  ctypes.c_float(eps).value)
+
+
+def layer_norm_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+                       eps: float = 1e-5, want_stats: bool = False):
+    """``y`` of :func:`layer_norm` (no autograd), and with ``want_stats`` the float32
+    ``[2, rows]`` means and inverse deviations that :func:`layer_norm_backward` reads."""
+    rows, key = _norm_desc(x, weight, bias, eps)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty(2, key[0], dtype=torch.float32, device=x.device) if want_stats else None
+    with _on(x.device):
+        B.layer_norm_fwd(_make_layer_norm(*key), rows.data_ptr(), weight.data_ptr(),
+                         bias.data_ptr() if bias is not None else None, y.data_ptr(),
+                         stats.data_ptr() if want_stats else None, _stream(x.device))
+    return (y, stats) if want_stats else y
+
+
+def layer_norm_backward(x: torch.Tensor, weight: torch.Tensor, stats: torch.Tensor, g_y: torch.Tensor, *,
+                        eps: float = 1e-5, want_x: bool = True, want_weight: bool = True,
+                        want_bias: bool = False):
+    """``(g_x, g_weight, g_bias)`` for the gradient ``g_y`` of ``y`` (None where not wanted)."""
+    rows, key = _norm_desc(x, weight, None, eps)
+    if g_y.shape != x.shape or g_y.dtype != x.dtype or g_y.device != x.device or not g_y.is_contiguous():
+        raise ValueError("g_y must be a contiguous tensor of x's shape, dtype and device")
+    if stats.shape != (2, key[0]) or stats.dtype != torch.float32 or stats.device != x.device \
+            or not stats.is_contiguous():
+        raise ValueError("stats must be the forward's [2, rows] float32 tensor")
+    n = _make_layer_norm(*key)
+    g_x = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
+    g_w = torch.empty_like(weight) if want_weight else None
+    g_b = torch.empty_like(weight) if want_bias else None
+    ws_bytes = _layer_norm_workspace(*key) if want_weight or want_bias else 0
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device) if ws_bytes else None
+    ptr = (lambda t: t.data_ptr() if t is not None else None)
+    with _on(x.device):
+        B.layer_norm_bwd(n, rows.data_ptr(), weight.data_ptr(), stats.data_ptr(), g_y.data_ptr(), ptr(g_x),
+                         ptr(g_w), ptr(g_b), ptr(ws), ws_bytes, _stream(x.device))
+    return g_x, g_w, g_b
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, stats = layer_norm_forward(x, weight, bias, eps=eps, want_stats=True)
+        ctx.save_for_backward(x, weight, stats)
+        ctx.eps = eps
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g_y):
+        x, weight, stats = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        g = layer_norm_backward(x, weight, stats, g_y.contiguous(), eps=ctx.eps, want_x=need[0],
+                                want_weight=need[1], want_bias=need[2])
+        return (*g, None)
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+               eps: float = 1e-5) -> torch.Tensor:
+    """Layer norm over the last dimension of ``x [..., d]`` with autograd through the HIP kernels.
+
+    ``x`` is bf16 or float32; its rows may be columns of a wider tensor (a nested
+    sub-model's channels). ``weight`` and ``bias [d]`` are bf16 or float32, whatever
+    ``x`` is; their gradients are summed in float32 and rounded once.
+    """
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                    (bias is not None and bias.requires_grad)):
+        return _LayerNorm.apply(x, weight, bias, eps)
+    return layer_norm_forward(x, weight, bias, eps=eps)
+
+
+class _TokenLogp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, opts, h, W):
+        logp, entropy, p, stats, ws = _token_logp_forward(h, W, tokens, opts)
+        ctx.p, ctx.stats, ctx.ws = p, stats, ws
+        ctx.save_for_backward(tokens, h, W)
+        ctx.mark_non_differentiable(entropy)
+        return logp, entropy
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g_logp, g_entropy):
+        # the saved tensors' addresses are taken anew, as in the loss's backward
+        tokens, h, W = (x.contiguous() for x in ctx.saved_tensors)
+        p = B.Problem.from_buffer_copy(ctx.p)
+        p.labels, p.h[0], p.W[0] = tokens.data_ptr(), h.data_ptr(), W.data_ptr()
+        g_logp = g_logp.to(torch.float32).contiguous()
+        need = ctx.needs_input_grad[2:]
+        gh = torch.empty_like(h) if need[0] else None
+        gW = torch.empty_like(W) if need[1] else None
+        with _on(h.device):
+            B.token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need[0] else None,
+                             gW.data_ptr() if need[1] else None, ctx.ws.data_ptr(), ctx.ws.numel(),
+                             _stream(h.device))
+        return None, None, gh, gW
+
+
+def _token_logp_forward(h, W, tokens, opts):
+    dev = h.device
+    p = make_problem([h], [W], tokens, grad_h_dtype=h.dtype,
+                     flags=B.MLS_GRAD_W_BF16 if h.dtype == torch.bfloat16 else 0, **opts)
+    ws_bytes, stats_bytes = B.query_sizes(p)
+    ws = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=dev)
+    stats = torch.empty(stats_bytes, dtype=torch.uint8, device=dev)
+    logp = torch.empty(p.T, dtype=torch.float32, device=dev)
+    entropy = torch.empty(p.T, dtype=torch.float32, device=dev)
+    with _on(dev):
+        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(), ws.data_ptr(), ws.numel(),
+                         _stream(dev))
+    return logp, entropy, p, stats, ws
+
+
+def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temperature: float = 1.0,
+               ignore_index: int = -100, vocab_chunk: int = 0):
+    """``(logp [T], entropy [T])`` (float32) of ``tokens [T]`` under the head ``W [V, d]`` on ``h [T, d]``.
+
+    ``logp[t] = log softmax(W h[t] / temperature)[tokens[t]]``, with autograd through
+    the HIP kernels for any gradient per token; ``entropy`` (of the same softmax) is
+    for monitoring and not differentiated. Both are 0 where the token is
+    ``ignore_index``. Nothing of size ``[T, V]`` is kept.
+    """
+    opts = dict(tau=temperature, ignore_index=ignore_index, vocab_chunk=vocab_chunk)
+    if torch.is_grad_enabled() and (h.requires_grad or W.requires_grad):
+        return _TokenLogp.apply(tokens, opts, h, W)
+    return _token_logp_forward(h, W, tokens, opts)[:2]
+
+
+_POLICY_REDUCTIONS = {"token": 0, "sequence": B.MLS_POLICY_MEAN_OF_SEQUENCES}
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, args):
+        old, adv, ref, mask, cu, desc = args
+        dev = logp.device
+        N = logp.numel()
+        need = ctx.needs_input_grad[0]
+        loss, kl, clipped = (torch.empty((), dtype=torch.float32, device=dev) for _ in range(3))
+        grad = torch.empty(N + 1, dtype=torch.float32, device=dev) if need else None
+        ws_bytes = B.policy_loss_workspace(desc)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        ptr = (lambda t: t.data_ptr() if t is not None else None)
+        with _on(dev):
+            B.policy_loss_fwd(desc, logp.data_ptr(), old.data_ptr(), adv.data_ptr(), ptr(ref), ptr(mask), ptr(cu),
+                              loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(), ptr(grad), ws.data_ptr(),
+                              ws_bytes, _stream(dev))
+        if need:
+            ctx.save_for_backward(grad)
+        ctx.shape = logp.shape
+        ctx.mark_non_differentiable(kl, clipped)
+        return loss, kl, clipped
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g_loss, g_kl, g_clipped):
+        grad, = ctx.saved_tensors
+        g_logp = torch.empty(ctx.shape, dtype=torch.float32, device=grad.device)
+        with _on(grad.device):
+            B.policy_loss_bwd(grad.numel() - 1, grad.data_ptr(), g_loss.contiguous().data_ptr(),
+                              g_logp.data_ptr(), _stream(grad.device))
+        return g_logp, None
+
+
+def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, *,
+                ref_logp: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                cu_seqlens: Optional[torch.Tensor] = None, per_sequence: bool = False, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, reduction: str = "token"):
+    """``(loss, kl, clipped)``: the clipped policy loss on token log-probabilities.
+
+    Per token with advantage ``A`` and ``r = exp(logp - old_logp)`` the loss is
+    ``-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef k`` with
+    ``k = exp(ref_logp - logp) - (ref_logp - logp) - 1``. ``reduction="token"`` takes
+    the mean over the tokens that count, ``"sequence"`` the mean over the sequences of
+    their tokens' means. ``kl`` is the same mean of ``k`` (0 without ``ref_logp``) and
+    ``clipped`` the share of clipped tokens. Only ``logp`` is differentiated, and only
+    in ``loss``.
+
+    ``logp``, ``old_logp``, ``ref_logp`` (float32) and ``mask`` (bool: the tokens that
+    count) are of one shape, ``[N]`` packed or ``[B, L]`` padded. Packed sequences are
+    ``cu_seqlens`` (int32 ``[S + 1]``, ascending; tokens outside of them do not count);
+    the rows of ``[B, L]`` are sequences by themselves. ``advantages`` is per token, or
+    with ``per_sequence`` one per sequence ``[S]``.
+    """
+    if not logp.is_cuda:
+        raise RuntimeError("policy_loss runs on the GPU only; got tensors on " + str(logp.device))
+    if reduction not in _POLICY_REDUCTIONS:
+        raise ValueError(f"reduction must be one of {sorted(_POLICY_REDUCTIONS)}, got {reduction!r}")
+    dev, N = logp.device, logp.numel()
+    for name, x in (("logp", logp), ("old_logp", old_logp), ("ref_logp", ref_logp)):
+        if x is not None and (x.dtype != torch.float32 or x.shape != logp.shape or x.device != dev or
+                              not x.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of logp's shape and device")
+    if mask is not None and (mask.dtype != torch.bool or mask.shape != logp.shape or mask.device != dev or
+                             not mask.is_contiguous()):
+        raise ValueError("mask must be a contiguous bool tensor of logp's shape and device")
+    flags = _POLICY_REDUCTIONS[reduction] | (B.MLS_POLICY_ADV_PER_SEQUENCE if per_sequence else 0)
+    if cu_seqlens is not None:
+        if logp.dim() != 1:
+            raise ValueError("cu_seqlens goes with packed [N] tokens")
+        if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2 or \
+                cu_seqlens.device != dev or not cu_seqlens.is_contiguous():
+            raise ValueError("cu_seqlens must be a contiguous int32 [S + 1] tensor on logp's device")
+    elif flags:
+        if logp.dim() != 2 or N == 0:
+            raise ValueError("sequences are cu_seqlens or the rows of a [B, L] logp")
+        cu_seqlens = torch.arange(0, N + 1, logp.size(1), dtype=torch.int32, device=dev)
+    S = cu_seqlens.numel() - 1 if cu_seqlens is not None else 0
+    if advantages.dtype != torch.float32 or advantages.device != dev or not advantages.is_contiguous() or \
+            advantages.shape != ((S,) if per_sequence else logp.shape):
+        raise ValueError("advantages must be a contiguous float32 tensor of " +
+                         ("[S]" if per_sequence else "logp's shape"))
+    desc = B.make_policy(N, S, clip_low, clip_high, kl_coef, flags)
+    return _PolicyLoss.apply(logp, (old_logp, advantages, ref_logp, mask, cu_seqlens, desc))
+
+
+def _grad_list(grads, out):
+    grads = [g for g in grads if g is not None] if out is None else list(grads)
+    if not grads:
+        raise ValueError("no gradients given")
+    out = grads if out is None else list(out)
+    if len(out) != len(grads):
+        raise ValueError("out must hold one tensor for each gradient")
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise RuntimeError("gradient norms run on the GPU only; got tensors on " + str(dev))
+    rows = []
+    for g, o in zip(grads, out):
+        if g.device != dev or not g.is_contiguous():
+            raise ValueError("gradients must be contiguous tensors on one device")
+        if o is not g and (o.device != dev or o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous()):
+            raise ValueError("each out must be contiguous and of its gradient's shape, dtype and device")
+        rows.append((g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g.dtype)))
+    return dev, rows
+
+
+def _clip(grads, max_norm: float, out) -> torch.Tensor:
+    dev, rows = _grad_list(grads, out)
+    tensors = B.make_grad_tensors(rows)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws_bytes = B.clip_grad_norm_workspace(len(rows), tensors)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        B.clip_grad_norm(len(rows), tensors, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
+    return norm
+
+
+@torch.no_grad()
+def grad_norm(grads: Sequence[Optional[torch.Tensor]]) -> torch.Tensor:
+    """The global L2 norm (float32, on the device) of a list of bf16 or float32 gradients."""
+    return _clip(grads, 0.0, None)
+
+
+@torch.no_grad()
+def clip_grad_norm(grads: Sequence[Optional[torch.Tensor]], max_norm: float, *,
+                   out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+    """Scales gradients by ``min(1, max_norm / norm)`` and returns their global L2 norm before.
+
+    The norm is a float32 scalar on the device: nothing waits for it. The gradients
+    (bf16 and float32 mixed; entries that are None are left out) are scaled in place,
+    or into the tensors ``out`` of the same shapes and dtypes. A norm that is NaN or
+    infinite scales nothing.
+    """
+    if not max_norm > 0:
+        raise ValueError(f"max_norm must be > 0, got {max_norm}")
+    return _clip(grads, max_norm, out)
 
 
 def head_logits(o: torch.Tensor, W: torch.Tensor, out: Optional[torch.Tensor] = None):

@@ -8,6 +8,7 @@ fails loudly otherwise.
 
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -40,6 +41,9 @@ MLS_ACCUMULATE_GRAD_H = 2
 MLS_FWD_BWD_RECOMPUTE = 4
 MLS_GRAD_W_BF16 = 8
 
+MLS_POLICY_ADV_PER_SEQUENCE = 1
+MLS_POLICY_MEAN_OF_SEQUENCES = 2
+
 MLS_DEVFLAG_LABEL_RANGE = 1
 MLS_DEVFLAG_NONFINITE = 2
 
@@ -52,6 +56,16 @@ EXPORTED = (
     "mls_diagnostics",
     "mls_junction_fwd",
     "mls_junction_bwd",
+    "mls_layer_norm_fwd",
+    "mls_layer_norm_workspace",
+    "mls_layer_norm_bwd",
+    "mls_token_logp_fwd",
+    "mls_token_logp_bwd",
+    "mls_policy_loss_workspace",
+    "mls_policy_loss_fwd",
+    "mls_policy_loss_bwd",
+    "mls_clip_grad_norm_workspace",
+    "mls_clip_grad_norm",
     "mls_head_logits",
     "mls_sample",
     "mls_spec_verify_workspace",
@@ -123,6 +137,40 @@ class Junction(ctypes.Structure):
     ]
 
 
+class LayerNorm(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64),
+        ("d", ctypes.c_int64),
+        ("ld_x", ctypes.c_int64),
+        ("act_dtype", ctypes.c_int32),
+        ("param_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class Policy(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int64),
+        ("S", ctypes.c_int64),
+        ("clip_low", ctypes.c_double),
+        ("clip_high", ctypes.c_double),
+        ("kl_coef", ctypes.c_double),
+        ("flags", ctypes.c_uint32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("n", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 _lib = None
 
 
@@ -148,6 +196,20 @@ def lib():
         J = ctypes.POINTER(Junction)
         L.mls_junction_fwd.argtypes = [J, vp, vp, vp, vp]
         L.mls_junction_bwd.argtypes = [J, vp, vp, vp, vp, vp, vp]
+        N = ctypes.POINTER(LayerNorm)
+        sz = ctypes.POINTER(ctypes.c_size_t)
+        L.mls_layer_norm_fwd.argtypes = [N, vp, vp, vp, vp, vp, vp]
+        L.mls_layer_norm_workspace.argtypes = [N, sz]
+        L.mls_layer_norm_bwd.argtypes = [N, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_token_logp_fwd.argtypes = [P, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_token_logp_bwd.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        Q = ctypes.POINTER(Policy)
+        L.mls_policy_loss_workspace.argtypes = [Q, sz]
+        L.mls_policy_loss_fwd.argtypes = [Q, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_policy_loss_bwd.argtypes = [ctypes.c_int64, vp, vp, vp, vp]
+        # the list of tensors: an array of GradTensor or the address of its bytes
+        L.mls_clip_grad_norm_workspace.argtypes = [ctypes.c_int64, vp, sz]
+        L.mls_clip_grad_norm.argtypes = [ctypes.c_int64, vp, ctypes.c_double, vp, vp, ctypes.c_size_t, vp]
         S = ctypes.POINTER(Sampling)
         L.mls_head_logits.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                       vp, vp, vp, vp]
@@ -276,6 +338,87 @@ def junction_fwd(j: Junction, o: int, e: int, x: int, stream: int):
 
 def junction_bwd(j: Junction, o: int, e: int, g_x: int, g_o: int, g_e: int, stream: int):
     check(lib().mls_junction_bwd(ctypes.byref(j), o, e, g_x, g_o, g_e, stream), "mls_junction_bwd")
+
+
+def make_layer_norm(T: int, d: int, ld_x: int, act_dtype: int, param_dtype: int, eps: float) -> LayerNorm:
+    n = LayerNorm()
+    n.T, n.d, n.ld_x, n.act_dtype, n.param_dtype, n.eps, n.reserved = T, d, ld_x, act_dtype, param_dtype, eps, 0
+    return n
+
+
+def layer_norm_fwd(n: LayerNorm, x: int, weight: int, bias: Optional[int], y: int, stats: Optional[int],
+                   stream: int):
+    check(lib().mls_layer_norm_fwd(ctypes.byref(n), x, weight, bias, y, stats, stream), "mls_layer_norm_fwd")
+
+
+def layer_norm_workspace(n: LayerNorm) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_layer_norm_workspace(ctypes.byref(n), ctypes.byref(b)), "mls_layer_norm_workspace")
+    return b.value
+
+
+def layer_norm_bwd(n: LayerNorm, x: int, weight: int, stats: int, g_y: int, g_x: Optional[int],
+                   g_weight: Optional[int], g_bias: Optional[int], ws: Optional[int], ws_bytes: int, stream: int):
+    check(lib().mls_layer_norm_bwd(ctypes.byref(n), x, weight, stats, g_y, g_x, g_weight, g_bias, ws, ws_bytes,
+                                   stream), "mls_layer_norm_bwd")
+
+
+def token_logp_fwd(p: Problem, stats: int, logp: int, entropy: Optional[int], ws: int, ws_bytes: int,
+                   stream: int):
+    check(lib().mls_token_logp_fwd(ctypes.byref(p), stats, logp, entropy, ws, ws_bytes, stream),
+          "mls_token_logp_fwd")
+
+
+def token_logp_bwd(p: Problem, stats: int, g_logp: int, grad_h: Optional[int], grad_W: Optional[int], ws: int,
+                   ws_bytes: int, stream: int):
+    check(lib().mls_token_logp_bwd(ctypes.byref(p), stats, g_logp, grad_h, grad_W, ws, ws_bytes, stream),
+          "mls_token_logp_bwd")
+
+
+def make_policy(N: int, S: int = 0, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                flags: int = 0) -> Policy:
+    p = Policy()
+    p.N, p.S, p.clip_low, p.clip_high, p.kl_coef, p.flags, p.reserved = N, S, clip_low, clip_high, kl_coef, flags, 0
+    return p
+
+
+def policy_loss_workspace(p: Policy) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_policy_loss_workspace(ctypes.byref(p), ctypes.byref(b)), "mls_policy_loss_workspace")
+    return b.value
+
+
+def policy_loss_fwd(p: Policy, logp: int, old_logp: int, advantages: int, ref_logp: Optional[int],
+                    mask: Optional[int], cu_seqlens: Optional[int], loss: int, kl: Optional[int],
+                    clipped: Optional[int], grad: Optional[int], ws: int, ws_bytes: int, stream: int):
+    check(lib().mls_policy_loss_fwd(ctypes.byref(p), logp, old_logp, advantages, ref_logp, mask, cu_seqlens, loss,
+                                    kl, clipped, grad, ws, ws_bytes, stream), "mls_policy_loss_fwd")
+
+
+def policy_loss_bwd(N: int, grad: int, g_loss: int, g_logp: int, stream: int):
+    check(lib().mls_policy_loss_bwd(N, grad, g_loss, g_logp, stream), "mls_policy_loss_bwd")
+
+
+def make_grad_tensors(tensors: Sequence[tuple]):
+    """The library's list of ``(data, out, elements, dtype)`` tensors, as bytes (one
+    conversion for the whole list: a structure's fields one by one take several times
+    as long)."""
+    flat = array.array("q")
+    for t in tensors:
+        flat.extend(t)  # dtype and the zero reserved field behind it are one little-endian word
+    return flat
+
+
+def clip_grad_norm_workspace(count: int, tensors) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_clip_grad_norm_workspace(count, tensors.buffer_info()[0], ctypes.byref(b)),
+          "mls_clip_grad_norm_workspace")
+    return b.value
+
+
+def clip_grad_norm(count: int, tensors, max_norm: float, norm: int, ws: int, ws_bytes: int, stream: int):
+    check(lib().mls_clip_grad_norm(count, tensors.buffer_info()[0], max_norm, norm, ws, ws_bytes, stream),
+          "mls_clip_grad_norm")
 
 
 def make_sampling(V: int, temperature: float = 1.0, top_p: float = 1.0,

@@ -11,6 +11,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -527,12 +528,14 @@ hipError_t sum_parts(const mls_problem* p, int splits, int64_t rows, const float
 
 // Label logits of every token and, when `count` is set, the valid-token count
 // into the statistics header (which the logit-gradient pass reads before the
-// loss mean is taken).
+// loss mean is taken). With logp the header is cleared, for token
+// log-probabilities' row merge.
 hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void* stats, bool count,
-                         hipStream_t s) {
+                         hipStream_t s, float* logp = nullptr) {
   RowArgs r;
   fill_rows(p, pl, r);
   r.lab = lab;
+  r.logp_row = logp;
   r.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
   hipError_t e;
   {
@@ -545,10 +548,11 @@ hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void*
 }
 
 // Forward of tokens [t0, t0 + tc): the tile kernel (partial records, and with
-// lslab the fp16 logits) and the row merge into the statistics.
+// lslab the fp16 logits) and the row merge into the statistics, or with logp into
+// token log-probabilities (and entropies).
 hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc,
                          float4* partials, const float* lab, uint16_t* lslab, void* stats,
-                         hipStream_t s) {
+                         hipStream_t s, float* logp = nullptr, float* entropy = nullptr) {
   FusedArgs a;
   fill_common(p, pl, a);
   for (int i = 0; i < pl.M; ++i)
@@ -580,6 +584,12 @@ hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64
   r.lab = const_cast<float*>(lab);
   r.stats = static_cast<float*>(stats);
   ProfScope ps("row_merge", s);
+  if (logp) {
+    r.logp_row = logp;
+    r.entropy_row = entropy;
+    r.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
+    return launch_finalize_logp(r, s);
+  }
   return launch_finalize_rows(r, s);
 }
 
@@ -597,131 +607,11 @@ hipError_t finish_losses(const mls_problem* p, const Plan& pl, void* stats, floa
   return launch_reduce_losses(r, s);
 }
 
-}  // namespace
-
-namespace mls {
-mls_status set_error(mls_status s, const char* what, const char* detail) {
-  return fail(s, detail && detail[0] ? "%s: %s" : "%s%s", what, detail ? detail : "");
-}
-}  // namespace mls
-
-extern "C" {
-
-const char* mls_version(void) { return "mls 0.1.0 (gfx950)"; }
-
-mls_status mls_device_info(int32_t* compute_units, int32_t* clock_khz, int32_t* mem_clock_khz,
-                           int32_t* mem_bus_bits) {
-  g_last_error.clear();
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-  struct Q {
-    int32_t* out;
-    hipDeviceAttribute_t attr;
-  } qs[] = {{compute_units, hipDeviceAttributeMultiprocessorCount},
-            {clock_khz, hipDeviceAttributeClockRate},
-            {mem_clock_khz, hipDeviceAttributeMemoryClockRate},
-            {mem_bus_bits, hipDeviceAttributeMemoryBusWidth}};
-  for (const Q& q : qs) {
-    if (!q.out) continue;
-    int v = 0;
-    if ((e = hipDeviceGetAttribute(&v, q.attr, dev)) != hipSuccess)
-      return hip_fail(e, "hipDeviceGetAttribute");
-    *q.out = v;
-  }
-  return MLS_OK;
-}
-
-const char* mls_last_error(void) { return g_last_error.c_str(); }
-
-const char* mls_status_string(mls_status s) {
-  switch (s) {
-    case MLS_OK: return "ok";
-    case MLS_INVALID_ARG: return "invalid argument";
-    case MLS_UNSUPPORTED: return "unsupported";
-    case MLS_WORKSPACE_TOO_SMALL: return "workspace too small";
-    case MLS_HIP_ERROR: return "HIP error";
-  }
-  return "unknown status";
-}
-
-mls_status mls_query_sizes(const mls_problem* p, size_t* workspace_bytes, size_t* stats_bytes) {
-  g_last_error.clear();
-  mls_status st = validate(p);
-  if (st != MLS_OK) return st;
-  Plan pl;
-  make_plan(p, pl);
-  if (workspace_bytes) *workspace_bytes = pl.ws_room;
-  if (stats_bytes) *stats_bytes = pl.stats_bytes;
-  return MLS_OK;
-}
-
-mls_status mls_coeffs(int32_t M, int32_t teacher, float alpha, float tau, int32_t mode,
-                      const float* w, float* g_ce, float* g_kl) {
-  g_last_error.clear();
-  if (M < 1 || M > MLS_MAX_MODELS) return fail(MLS_INVALID_ARG, "M=%d outside [1, %d]", M, MLS_MAX_MODELS);
-  if (teacher < -1 || teacher >= M) return fail(MLS_INVALID_ARG, "teacher=%d outside [-1, M)", teacher);
-  if (!g_ce || !g_kl) return fail(MLS_INVALID_ARG, "output pointer is NULL");
-  if (mode != MLS_MODE_PAPER && mode != MLS_MODE_ADDITIVE)
-    return fail(MLS_INVALID_ARG, "unknown mode %d", mode);
-  if (!(tau > 0.0f) || !isfinite(tau)) return fail(MLS_INVALID_ARG, "tau must be finite and > 0");
-  if (!isfinite(alpha) || alpha < 0.0f || alpha > 1.0f) return fail(MLS_INVALID_ARG, "alpha must be in [0, 1]");
-  host_coeffs(M, teacher < 0 ? M - 1 : teacher, alpha, tau, mode, w, g_ce, g_kl);
-  return MLS_OK;
-}
-
-mls_status mls_distill_fwd(const mls_problem* p, void* stats, float* ce, float* kl, float* entropy,
-                           void* workspace, size_t workspace_bytes, void* stream) {
-  g_last_error.clear();
-  mls_status st = validate(p);
-  if (st != MLS_OK) return st;
-  if (!stats || !ce || !kl || !workspace)
-    return fail(MLS_INVALID_ARG, "stats, ce, kl and workspace must be non-NULL");
-  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(ce, 4) || !aligned(kl, 4))
-    return fail(MLS_INVALID_ARG, "misaligned stats / workspace / loss pointer");
-  Plan pl;
-  make_plan(p, pl);
-  if (workspace_bytes < pl.fwd_bytes)
-    return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", pl.fwd_bytes,
-                workspace_bytes);
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  char* ws = static_cast<char*>(workspace);
-  float* lab = reinterpret_cast<float*>(ws + pl.off_lab);
-  hipError_t e = launch_labels(p, pl, lab, stats, false, s);
-  if (e != hipSuccess) return hip_fail(e, "label logits launch");
-  for (int c = 0; c < pl.fwd_nc; ++c) {
-    const int64_t t0 = (int64_t)c * pl.fwd_tc;
-    e = forward_chunk(p, pl, t0, std::min(pl.fwd_tc, pl.T - t0),
-                      reinterpret_cast<float4*>(ws + pl.off_partials), lab, nullptr, stats, s);
-    if (e != hipSuccess) return hip_fail(e, "forward launch");
-  }
-  e = finish_losses(p, pl, stats, ce, kl, entropy, s);
-  if (e != hipSuccess) return hip_fail(e, "loss reduction launch");
-  return MLS_OK;
-}
-
-mls_status mls_distill_bwd(const mls_problem* p, const void* stats, const float* g_ce,
-                           const float* g_kl, void* const* grad_h, float* const* grad_W,
-                           void* workspace, size_t workspace_bytes, void* stream) {
-  g_last_error.clear();
-  mls_status st = validate(p);
-  if (st != MLS_OK) return st;
-  if (!stats || !workspace || !grad_h || !grad_W)
-    return fail(MLS_INVALID_ARG, "stats, workspace, grad_h and grad_W must be non-NULL");
-  if ((g_ce == nullptr) != (g_kl == nullptr))
-    return fail(MLS_INVALID_ARG, "g_ce and g_kl must both be given or both be NULL");
-  if (!aligned(stats, 16) || !aligned(workspace, 16))
-    return fail(MLS_INVALID_ARG, "misaligned stats / workspace");
-  for (int i = 0; i < p->M; ++i) {
-    if ((grad_h[i] && !aligned(grad_h[i], p->grad_h_dtype == MLS_BF16 ? 2 : 4)) ||
-        (grad_W[i] && !aligned(grad_W[i], (p->flags & MLS_GRAD_W_BF16) ? 2 : 4)))
-      return fail(MLS_INVALID_ARG, "misaligned gradient pointer %d", i);
-  }
-  Plan pl;
-  make_plan(p, pl);
-  if (workspace_bytes < pl.bwd_bytes)
-    return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", pl.bwd_bytes,
-                workspace_bytes);
+// Launches of the backward: of the losses (g_ce, g_kl) or, with g_row, of token
+// log-probabilities.
+mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats, const float* g_ce,
+                        const float* g_kl, const float* g_row, void* const* grad_h, float* const* grad_W,
+                        void* workspace, size_t workspace_bytes, void* stream) {
   int splits = 1;  // K parts of the grad_h products
   int64_t ksplit = 0;
   if (pl.wide_bwd)
@@ -740,6 +630,7 @@ mls_status mls_distill_bwd(const mls_problem* p, const void* stats, const float*
   a.n_valid = reinterpret_cast<const int32_t*>(static_cast<const char*>(stats) + pl.header_off);
   a.g_ce = g_ce;
   a.g_kl = g_kl;
+  a.g_row = g_row;
   host_coeffs(pl.M, pl.s, p->alpha, p->tau, MLS_MODE_PAPER, nullptr, a.host_gce, a.host_gkl);
   a.slab = ws + pl.off_slab;
   const bool stored = pl.wide_bwd || pl.f32;  // products on the stored layouts
@@ -948,6 +839,134 @@ mls_status mls_distill_bwd(const mls_problem* p, const void* stats, const float*
     if (e != hipSuccess) return hip_fail(e, "grad_h sum launch");
   }
   return MLS_OK;
+}
+
+}  // namespace
+
+namespace mls {
+mls_status set_error(mls_status s, const char* what, const char* detail) {
+  return fail(s, detail && detail[0] ? "%s: %s" : "%s%s", what, detail ? detail : "");
+}
+}  // namespace mls
+
+extern "C" {
+
+const char* mls_version(void) { return "mls 0.1.0 (gfx950)"; }
+
+mls_status mls_device_info(int32_t* compute_units, int32_t* clock_khz, int32_t* mem_clock_khz,
+                           int32_t* mem_bus_bits) {
+  g_last_error.clear();
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  struct Q {
+    int32_t* out;
+    hipDeviceAttribute_t attr;
+  } qs[] = {{compute_units, hipDeviceAttributeMultiprocessorCount},
+            {clock_khz, hipDeviceAttributeClockRate},
+            {mem_clock_khz, hipDeviceAttributeMemoryClockRate},
+            {mem_bus_bits, hipDeviceAttributeMemoryBusWidth}};
+  for (const Q& q : qs) {
+    if (!q.out) continue;
+    int v = 0;
+    if ((e = hipDeviceGetAttribute(&v, q.attr, dev)) != hipSuccess)
+      return hip_fail(e, "hipDeviceGetAttribute");
+    *q.out = v;
+  }
+  return MLS_OK;
+}
+
+const char* mls_last_error(void) { return g_last_error.c_str(); }
+
+const char* mls_status_string(mls_status s) {
+  switch (s) {
+    case MLS_OK: return "ok";
+    case MLS_INVALID_ARG: return "invalid argument";
+    case MLS_UNSUPPORTED: return "unsupported";
+    case MLS_WORKSPACE_TOO_SMALL: return "workspace too small";
+    case MLS_HIP_ERROR: return "HIP error";
+  }
+  return "unknown status";
+}
+
+mls_status mls_query_sizes(const mls_problem* p, size_t* workspace_bytes, size_t* stats_bytes) {
+  g_last_error.clear();
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  Plan pl;
+  make_plan(p, pl);
+  if (workspace_bytes) *workspace_bytes = pl.ws_room;
+  if (stats_bytes) *stats_bytes = pl.stats_bytes;
+  return MLS_OK;
+}
+
+mls_status mls_coeffs(int32_t M, int32_t teacher, float alpha, float tau, int32_t mode,
+                      const float* w, float* g_ce, float* g_kl) {
+  g_last_error.clear();
+  if (M < 1 || M > MLS_MAX_MODELS) return fail(MLS_INVALID_ARG, "M=%d outside [1, %d]", M, MLS_MAX_MODELS);
+  if (teacher < -1 || teacher >= M) return fail(MLS_INVALID_ARG, "teacher=%d outside [-1, M)", teacher);
+  if (!g_ce || !g_kl) return fail(MLS_INVALID_ARG, "output pointer is NULL");
+  if (mode != MLS_MODE_PAPER && mode != MLS_MODE_ADDITIVE)
+    return fail(MLS_INVALID_ARG, "unknown mode %d", mode);
+  if (!(tau > 0.0f) || !isfinite(tau)) return fail(MLS_INVALID_ARG, "tau must be finite and > 0");
+  if (!isfinite(alpha) || alpha < 0.0f || alpha > 1.0f) return fail(MLS_INVALID_ARG, "alpha must be in [0, 1]");
+  host_coeffs(M, teacher < 0 ? M - 1 : teacher, alpha, tau, mode, w, g_ce, g_kl);
+  return MLS_OK;
+}
+
+mls_status mls_distill_fwd(const mls_problem* p, void* stats, float* ce, float* kl, float* entropy,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  if (!stats || !ce || !kl || !workspace)
+    return fail(MLS_INVALID_ARG, "stats, ce, kl and workspace must be non-NULL");
+  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(ce, 4) || !aligned(kl, 4))
+    return fail(MLS_INVALID_ARG, "misaligned stats / workspace / loss pointer");
+  Plan pl;
+  make_plan(p, pl);
+  if (workspace_bytes < pl.fwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", pl.fwd_bytes,
+                workspace_bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  float* lab = reinterpret_cast<float*>(ws + pl.off_lab);
+  hipError_t e = launch_labels(p, pl, lab, stats, false, s);
+  if (e != hipSuccess) return hip_fail(e, "label logits launch");
+  for (int c = 0; c < pl.fwd_nc; ++c) {
+    const int64_t t0 = (int64_t)c * pl.fwd_tc;
+    e = forward_chunk(p, pl, t0, std::min(pl.fwd_tc, pl.T - t0),
+                      reinterpret_cast<float4*>(ws + pl.off_partials), lab, nullptr, stats, s);
+    if (e != hipSuccess) return hip_fail(e, "forward launch");
+  }
+  e = finish_losses(p, pl, stats, ce, kl, entropy, s);
+  if (e != hipSuccess) return hip_fail(e, "loss reduction launch");
+  return MLS_OK;
+}
+
+mls_status mls_distill_bwd(const mls_problem* p, const void* stats, const float* g_ce,
+                           const float* g_kl, void* const* grad_h, float* const* grad_W,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  if (!stats || !workspace || !grad_h || !grad_W)
+    return fail(MLS_INVALID_ARG, "stats, workspace, grad_h and grad_W must be non-NULL");
+  if ((g_ce == nullptr) != (g_kl == nullptr))
+    return fail(MLS_INVALID_ARG, "g_ce and g_kl must both be given or both be NULL");
+  if (!aligned(stats, 16) || !aligned(workspace, 16))
+    return fail(MLS_INVALID_ARG, "misaligned stats / workspace");
+  for (int i = 0; i < p->M; ++i) {
+    if ((grad_h[i] && !aligned(grad_h[i], p->grad_h_dtype == MLS_BF16 ? 2 : 4)) ||
+        (grad_W[i] && !aligned(grad_W[i], (p->flags & MLS_GRAD_W_BF16) ? 2 : 4)))
+      return fail(MLS_INVALID_ARG, "misaligned gradient pointer %d", i);
+  }
+  Plan pl;
+  make_plan(p, pl);
+  if (workspace_bytes < pl.bwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", pl.bwd_bytes,
+                workspace_bytes);
+  return run_backward(p, pl, stats, g_ce, g_kl, nullptr, grad_h, grad_W, workspace, workspace_bytes, stream);
 }
 
 mls_status mls_query_fwd_bwd_workspace(const mls_problem* p, size_t* workspace_bytes) {
@@ -1237,6 +1256,55 @@ mls_status mls_diagnostics(const mls_problem* p, float* kl_pair, float* agree, i
   return MLS_OK;
 }
 
+mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
+  if (!stats || !logp || !workspace) return fail(MLS_INVALID_ARG, "stats, logp and workspace must be non-NULL");
+  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(logp, 4) || !aligned(entropy, 4))
+    return fail(MLS_INVALID_ARG, "misaligned stats / workspace / output pointer");
+  Plan pl;
+  make_plan(p, pl);
+  if (workspace_bytes < pl.fwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", pl.fwd_bytes,
+                workspace_bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  float* lab = reinterpret_cast<float*>(ws + pl.off_lab);
+  hipError_t e = launch_labels(p, pl, lab, stats, false, s, logp);
+  if (e != hipSuccess) return hip_fail(e, "label logits launch");
+  for (int c = 0; c < pl.fwd_nc; ++c) {
+    const int64_t t0 = (int64_t)c * pl.fwd_tc;
+    e = forward_chunk(p, pl, t0, std::min(pl.fwd_tc, pl.T - t0),
+                      reinterpret_cast<float4*>(ws + pl.off_partials), lab, nullptr, stats, s, logp, entropy);
+    if (e != hipSuccess) return hip_fail(e, "forward launch");
+  }
+  return MLS_OK;
+}
+
+mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp, void* grad_h,
+                              void* grad_W, void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
+  if (!stats || !g_logp || !workspace)
+    return fail(MLS_INVALID_ARG, "stats, g_logp and workspace must be non-NULL");
+  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(g_logp, 4) ||
+      !aligned(grad_h, p->grad_h_dtype == MLS_BF16 ? 2 : 4) || !aligned(grad_W, (p->flags & MLS_GRAD_W_BF16) ? 2 : 4))
+    return fail(MLS_INVALID_ARG, "misaligned stats / workspace / gradient pointer");
+  Plan pl;
+  make_plan(p, pl);
+  if (workspace_bytes < pl.bwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", pl.bwd_bytes,
+                workspace_bytes);
+  void* const gh[1] = {grad_h};
+  float* const gW[1] = {static_cast<float*>(grad_W)};
+  return run_backward(p, pl, stats, nullptr, nullptr, g_logp, gh, gW, workspace, workspace_bytes, stream);
+}
+
 }  // extern "C"
 
 namespace {
@@ -1342,6 +1410,402 @@ mls_status mls_junction_bwd(const mls_junction* j, const void* o, const void* e,
     err = launch_junction_bwd(a, j->act_dtype == MLS_F32, j->grad_dtype == MLS_F32, s);
   }
   if (err != hipSuccess) return hip_fail(err, "junction backward launch");
+  return MLS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+mls_status validate_norm(const mls_layer_norm* n) {
+  if (!n) return fail(MLS_INVALID_ARG, "layer norm descriptor is NULL");
+  if (n->T < 1 || n->T > (1ll << 31)) return fail(MLS_INVALID_ARG, "T=%lld out of range", (long long)n->T);
+  if (n->d < 1 || n->d > norm_max_width())
+    return fail(MLS_UNSUPPORTED, "d=%lld outside [1, %lld]", (long long)n->d, (long long)norm_max_width());
+  if (n->ld_x < n->d || n->ld_x > (1ll << 31))
+    return fail(MLS_INVALID_ARG, "ld_x=%lld outside [d, 2^31]", (long long)n->ld_x);
+  if ((n->act_dtype != MLS_BF16 && n->act_dtype != MLS_F32) ||
+      (n->param_dtype != MLS_BF16 && n->param_dtype != MLS_F32))
+    return fail(MLS_UNSUPPORTED, "layer norm dtypes %d / %d unsupported", n->act_dtype, n->param_dtype);
+  if (!(n->eps > 0.f) || !isfinite(n->eps)) return fail(MLS_INVALID_ARG, "eps must be finite and > 0");
+  if (n->reserved != 0) return fail(MLS_INVALID_ARG, "reserved field must be 0");
+  return MLS_OK;
+}
+
+NormArgs norm_args(const mls_layer_norm* n, const NormShape& sh) {
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.T = n->T;
+  a.d = (int32_t)n->d;
+  a.ld_x = n->ld_x;
+  a.waves = sh.waves;
+  a.param_f32 = n->param_dtype == MLS_F32 ? 1 : 0;
+  a.eps = n->eps;
+  return a;
+}
+
+// Rows of 16-byte chunks: the row length and stride and every row array's address.
+bool norm_vec(const mls_layer_norm* n, const void* x, const void* p, const void* q) {
+  const int64_t ve = n->act_dtype == MLS_F32 ? 4 : 8;
+  return n->d % ve == 0 && n->ld_x % ve == 0 && aligned(x, 16) && aligned(p, 16) && aligned(q, 16);
+}
+
+size_t norm_part_bytes(const mls_layer_norm* n) {
+  const bool f32 = n->act_dtype == MLS_F32;
+  const int blocks = std::max(norm_shape(n->T, n->d, f32, true, true).blocks,
+                              norm_shape(n->T, n->d, f32, false, true).blocks);
+  return align256((size_t)blocks * 2 * n->d * sizeof(float));
+}
+
+}  // namespace
+
+extern "C" {
+
+mls_status mls_layer_norm_fwd(const mls_layer_norm* n, const void* x, const void* weight, const void* bias,
+                              void* y, float* stats, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_norm(n);
+  if (st != MLS_OK) return st;
+  if (!x || !weight || !y) return fail(MLS_INVALID_ARG, "x, weight and y must be non-NULL");
+  const size_t es = n->act_dtype == MLS_F32 ? 4 : 2, ps = n->param_dtype == MLS_F32 ? 4 : 2;
+  if (!aligned(x, es) || !aligned(y, es) || !aligned(weight, ps) || !aligned(bias, ps) || !aligned(stats, 4))
+    return fail(MLS_INVALID_ARG, "misaligned layer norm operand");
+  if (!disjoint(y, (size_t)n->T * n->d * es, x, ((size_t)(n->T - 1) * n->ld_x + n->d) * es))
+    return fail(MLS_INVALID_ARG, "y overlaps x");
+  const bool f32 = n->act_dtype == MLS_F32;
+  const NormShape sh = norm_shape(n->T, n->d, f32, norm_vec(n, x, y, nullptr), false);
+  NormArgs a = norm_args(n, sh);
+  a.x = x;
+  a.weight = weight;
+  a.bias = bias;
+  a.y = y;
+  a.stats = stats;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope pr("layer_norm_fwd", s);
+    e = launch_layer_norm_fwd(a, sh, f32, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "layer norm forward launch");
+  return MLS_OK;
+}
+
+mls_status mls_layer_norm_workspace(const mls_layer_norm* n, size_t* bytes) {
+  g_last_error.clear();
+  mls_status st = validate_norm(n);
+  if (st != MLS_OK) return st;
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  *bytes = norm_part_bytes(n);
+  return MLS_OK;
+}
+
+mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void* weight, const float* stats,
+                              const void* g_y, void* g_x, void* g_weight, void* g_bias, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_norm(n);
+  if (st != MLS_OK) return st;
+  if (!x || !weight || !stats || !g_y) return fail(MLS_INVALID_ARG, "x, weight, stats and g_y must be non-NULL");
+  const size_t es = n->act_dtype == MLS_F32 ? 4 : 2, ps = n->param_dtype == MLS_F32 ? 4 : 2;
+  if (!aligned(x, es) || !aligned(g_y, es) || !aligned(g_x, es) || !aligned(weight, ps) ||
+      !aligned(g_weight, ps) || !aligned(g_bias, ps) || !aligned(stats, 4) || !aligned(workspace, 16))
+    return fail(MLS_INVALID_ARG, "misaligned layer norm operand");
+  const size_t nb = (size_t)n->T * n->d * es;
+  if (g_x && (!disjoint(g_x, nb, x, ((size_t)(n->T - 1) * n->ld_x + n->d) * es) || !disjoint(g_x, nb, g_y, nb)))
+    return fail(MLS_INVALID_ARG, "g_x overlaps x or g_y");
+  const bool params = g_weight || g_bias;
+  if (!g_x && !params) return MLS_OK;
+  if (params && (!workspace || workspace_bytes < norm_part_bytes(n)))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "layer norm backward needs %zu workspace bytes, got %zu",
+                norm_part_bytes(n), workspace ? workspace_bytes : (size_t)0);
+  const bool f32 = n->act_dtype == MLS_F32;
+  const NormShape sh = norm_shape(n->T, n->d, f32, norm_vec(n, x, g_y, g_x), true);
+  NormArgs a = norm_args(n, sh);
+  a.x = x;
+  a.weight = weight;
+  a.stats = const_cast<float*>(stats);
+  a.g_y = g_y;
+  a.g_x = g_x;
+  a.g_weight = g_weight;
+  a.g_bias = g_bias;
+  a.part = params ? static_cast<float*>(workspace) : nullptr;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope pr("layer_norm_bwd", s);
+    e = launch_layer_norm_bwd(a, sh, f32, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "layer norm backward launch");
+  if (!params) return MLS_OK;
+  {
+    ProfScope pr("layer_norm_params", s);
+    e = launch_layer_norm_params(a, sh.blocks, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "layer norm parameter gradient launch");
+  return MLS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+mls_status validate_policy(const mls_policy* p) {
+  if (!p) return fail(MLS_INVALID_ARG, "policy loss descriptor is NULL");
+  if (p->N < 1 || p->N > (1ll << 31) - 1) return fail(MLS_INVALID_ARG, "N=%lld out of range", (long long)p->N);
+  if (p->S < 0 || p->S > (1ll << 31) - 1) return fail(MLS_INVALID_ARG, "S=%lld out of range", (long long)p->S);
+  if (p->flags & ~(uint32_t)(MLS_POLICY_ADV_PER_SEQUENCE | MLS_POLICY_MEAN_OF_SEQUENCES))
+    return fail(MLS_INVALID_ARG, "unknown policy loss flags 0x%x", p->flags);
+  if (p->flags && p->S < 1) return fail(MLS_INVALID_ARG, "sequence-wise terms need sequences, got S=0");
+  // clip_high may be infinite: no bound above
+  if (!(p->clip_low >= 0.0) || p->clip_low > 1.0) return fail(MLS_INVALID_ARG, "clip_low must be in [0, 1]");
+  if (!(p->clip_high >= 0.0)) return fail(MLS_INVALID_ARG, "clip_high must be >= 0");
+  if (!(p->kl_coef >= 0.0) || !isfinite(p->kl_coef))
+    return fail(MLS_INVALID_ARG, "kl_coef must be finite and >= 0");
+  if (p->reserved != 0) return fail(MLS_INVALID_ARG, "reserved field must be 0");
+  return MLS_OK;
+}
+
+size_t policy_ws_bytes(const mls_policy* p) {
+  const size_t parts = align256(policy_part_bytes(p->N));
+  return parts + ((p->flags & MLS_POLICY_MEAN_OF_SEQUENCES) ? align256((size_t)p->S * sizeof(int32_t)) : 0);
+}
+
+}  // namespace
+
+extern "C" {
+
+mls_status mls_policy_loss_workspace(const mls_policy* p, size_t* bytes) {
+  g_last_error.clear();
+  mls_status st = validate_policy(p);
+  if (st != MLS_OK) return st;
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  *bytes = policy_ws_bytes(p);
+  return MLS_OK;
+}
+
+mls_status mls_policy_loss_fwd(const mls_policy* p, const float* logp, const float* old_logp,
+                               const float* advantages, const float* ref_logp, const uint8_t* mask,
+                               const int32_t* cu_seqlens, float* loss, float* kl, float* clipped, float* grad,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_policy(p);
+  if (st != MLS_OK) return st;
+  if (!logp || !old_logp || !advantages || !loss || !workspace)
+    return fail(MLS_INVALID_ARG, "logp, old_logp, advantages, loss and workspace must be non-NULL");
+  if ((p->S > 0) != (cu_seqlens != nullptr))
+    return fail(MLS_INVALID_ARG, "cu_seqlens must be given with S > 0 and be NULL with S = 0");
+  if (p->kl_coef > 0.0 && !ref_logp) return fail(MLS_INVALID_ARG, "a KL term needs ref_logp");
+  if (!aligned(logp, 4) || !aligned(old_logp, 4) || !aligned(advantages, 4) || !aligned(ref_logp, 4) ||
+      !aligned(cu_seqlens, 4) || !aligned(loss, 4) || !aligned(kl, 4) || !aligned(clipped, 4) ||
+      !aligned(grad, 4) || !aligned(workspace, 16))
+    return fail(MLS_INVALID_ARG, "misaligned policy loss operand");
+  if (workspace_bytes < policy_ws_bytes(p))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "policy loss needs %zu workspace bytes, got %zu", policy_ws_bytes(p),
+                workspace_bytes);
+  PolicyArgs a;
+  memset(&a, 0, sizeof(a));
+  a.N = p->N;
+  a.S = p->S;
+  a.logp = logp;
+  a.old_logp = old_logp;
+  a.adv = advantages;
+  a.ref = ref_logp;
+  a.mask = mask;
+  a.cu = cu_seqlens;
+  a.per_seq = (p->flags & MLS_POLICY_ADV_PER_SEQUENCE) ? 1 : 0;
+  a.by_seq = (p->flags & MLS_POLICY_MEAN_OF_SEQUENCES) ? 1 : 0;
+  a.lo = 1.0 - p->clip_low;
+  a.hi = 1.0 + p->clip_high;
+  a.beta = p->kl_coef;
+  a.loss = loss;
+  a.kl = kl;
+  a.clipped = clipped;
+  a.grad = grad;
+  a.part = static_cast<double*>(workspace);
+  a.counts = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + align256(policy_part_bytes(p->N)));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (a.by_seq && mask) {
+    ProfScope pr("policy_count", s);
+    e = launch_policy_count(a, s);
+    if (e != hipSuccess) return hip_fail(e, "policy count launch");
+  }
+  {
+    ProfScope pr("policy_fwd", s);
+    e = launch_policy_fwd(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "policy loss launch");
+  {
+    ProfScope pr("policy_finish", s);
+    e = launch_policy_finish(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "policy sums launch");
+  return MLS_OK;
+}
+
+mls_status mls_policy_loss_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp, void* stream) {
+  g_last_error.clear();
+  if (N < 1 || N > (1ll << 31) - 1) return fail(MLS_INVALID_ARG, "N=%lld out of range", (long long)N);
+  if (!grad || !g_loss || !g_logp) return fail(MLS_INVALID_ARG, "grad, g_loss and g_logp must be non-NULL");
+  if (!aligned(grad, 4) || !aligned(g_loss, 4) || !aligned(g_logp, 4))
+    return fail(MLS_INVALID_ARG, "misaligned policy loss operand");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope pr("policy_bwd", s);
+    e = launch_policy_bwd(N, grad, g_loss, g_logp, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "policy gradient launch");
+  return MLS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+mls_status validate_grads(int64_t count, const mls_grad_tensor* g, bool scale) {
+  if (count < 0 || count > (1 << 20)) return fail(MLS_INVALID_ARG, "count=%lld out of range", (long long)count);
+  if (count > 0 && !g) return fail(MLS_INVALID_ARG, "tensor list is NULL");
+  for (int64_t i = 0; i < count; ++i) {
+    if (g[i].dtype != MLS_BF16 && g[i].dtype != MLS_F32)
+      return fail(MLS_UNSUPPORTED, "tensor %lld: dtype=%d unsupported", (long long)i, g[i].dtype);
+    if (g[i].reserved != 0) return fail(MLS_INVALID_ARG, "reserved field must be 0");
+    if (g[i].n < 0 || g[i].n > (1ll << 40))
+      return fail(MLS_INVALID_ARG, "tensor %lld: n=%lld out of range", (long long)i, (long long)g[i].n);
+    if (g[i].n == 0) continue;
+    const size_t es = g[i].dtype == MLS_F32 ? 4 : 2;
+    if (!g[i].data || (scale && !g[i].out))
+      return fail(MLS_INVALID_ARG, "tensor %lld: NULL pointer", (long long)i);
+    if (!aligned(g[i].data, es) || (scale && !aligned(g[i].out, es)))
+      return fail(MLS_INVALID_ARG, "tensor %lld: misaligned pointer", (long long)i);
+    const size_t nb = (size_t)g[i].n * es;
+    if (scale && g[i].out != g[i].data && !disjoint(g[i].out, nb, g[i].data, nb))
+      return fail(MLS_INVALID_ARG, "tensor %lld: out overlaps its input in part", (long long)i);
+  }
+  return MLS_OK;
+}
+
+// No output may overlap another tensor (a gradient listed twice would be scaled
+// twice, or once and once in part).
+mls_status validate_grad_outputs(int64_t count, const mls_grad_tensor* g) {
+  struct Span {
+    uintptr_t begin, end;
+    bool out;
+  };
+  std::vector<Span> spans;
+  try {
+    spans.reserve(2 * (size_t)count);
+    for (int64_t i = 0; i < count; ++i) {
+      if (g[i].n == 0) continue;
+      const size_t nb = (size_t)g[i].n * (g[i].dtype == MLS_F32 ? 4 : 2);
+      const uintptr_t d = (uintptr_t)g[i].data, o = (uintptr_t)g[i].out;
+      spans.push_back({o, o + nb, true});
+      if (o != d) spans.push_back({d, d + nb, false});
+    }
+  } catch (const std::bad_alloc&) {
+    return fail(MLS_INVALID_ARG, "out of host memory for %lld tensors", (long long)count);
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  uintptr_t end_out = 0, end_any = 0;
+  for (const Span& x : spans) {
+    if (x.begin < (x.out ? end_any : end_out))
+      return fail(MLS_INVALID_ARG, "an output overlaps another tensor of the list");
+    end_any = std::max(end_any, x.end);
+    if (x.out) end_out = std::max(end_out, x.end);
+  }
+  return MLS_OK;
+}
+
+// Fills one launch with tensors from *next on; false when none are left. A launch
+// takes at most Args' tensors and fewer than 2^31 tiles.
+template <class Args, class Put>
+bool next_launch(int64_t count, const mls_grad_tensor* g, int per, int64_t* next, Args& a, Put put) {
+  memset(&a, 0, sizeof(a));
+  int64_t tiles = 0;
+  for (; *next < count && a.count < per; ++*next) {
+    const mls_grad_tensor& x = g[*next];
+    if (x.n == 0) continue;
+    const int64_t k = clip_tiles(x.n);
+    if (tiles + k >= (1ll << 31) - 1 && a.count > 0) break;
+    a.data[a.count] = x.data;
+    a.n[a.count] = x.n | (x.dtype == MLS_F32 ? kClipF32 : 0);
+    a.tile_begin[a.count] = (int32_t)tiles;
+    put(a, a.count, x);
+    tiles += k;
+    ++a.count;
+  }
+  a.tiles = (int32_t)tiles;
+  return a.count > 0;
+}
+
+int64_t norm_parts(int64_t count, const mls_grad_tensor* g) {
+  GradNormArgs a;
+  int64_t parts = 0;
+  for (int64_t next = 0; next_launch(count, g, kNormTensors, &next, a, [](GradNormArgs&, int, const mls_grad_tensor&) {});)
+    parts += clip_blocks(a.tiles);
+  return parts;
+}
+
+size_t clip_ws_bytes(int64_t count, const mls_grad_tensor* g) {
+  return 256 + align256((size_t)norm_parts(count, g) * sizeof(double));
+}
+
+}  // namespace
+
+extern "C" {
+
+mls_status mls_clip_grad_norm_workspace(int64_t count, const mls_grad_tensor* tensors, size_t* bytes) {
+  g_last_error.clear();
+  mls_status st = validate_grads(count, tensors, false);
+  if (st != MLS_OK) return st;
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  *bytes = clip_ws_bytes(count, tensors);
+  return MLS_OK;
+}
+
+mls_status mls_clip_grad_norm(int64_t count, const mls_grad_tensor* tensors, double max_norm, float* norm,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  const bool scale = max_norm != 0.0;
+  mls_status st = validate_grads(count, tensors, scale);
+  if (st != MLS_OK) return st;
+  if (!(max_norm >= 0.0)) return fail(MLS_INVALID_ARG, "max_norm must be >= 0");
+  if (!norm || !workspace) return fail(MLS_INVALID_ARG, "norm and workspace must be non-NULL");
+  if (!aligned(norm, 4) || !aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned norm / workspace");
+  if (scale && (st = validate_grad_outputs(count, tensors)) != MLS_OK) return st;
+  if (workspace_bytes < clip_ws_bytes(count, tensors))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "gradient norm needs %zu workspace bytes, got %zu",
+                clip_ws_bytes(count, tensors), workspace_bytes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  float* coef = static_cast<float*>(workspace);
+  double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
+  int n_parts = 0;
+  hipError_t e;
+  {
+    GradNormArgs a;
+    for (int64_t next = 0;
+         next_launch(count, tensors, kNormTensors, &next, a, [](GradNormArgs&, int, const mls_grad_tensor&) {});) {
+      a.part = part + n_parts;
+      n_parts += clip_blocks(a.tiles);
+      ProfScope pr("grad_norm", s);
+      e = launch_grad_norm(a, s);
+      if (e != hipSuccess) return hip_fail(e, "gradient norm launch");
+    }
+  }
+  {
+    ProfScope pr("grad_norm_finish", s);
+    e = launch_grad_norm_finish(part, n_parts, max_norm, norm, scale ? coef : nullptr, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "gradient norm launch");
+  if (!scale) return MLS_OK;
+  GradScaleArgs a;
+  for (int64_t next = 0; next_launch(count, tensors, kScaleTensors, &next, a,
+                                     [](GradScaleArgs& q, int k, const mls_grad_tensor& x) { q.out[k] = x.out; });) {
+    a.coef = coef;
+    ProfScope pr("grad_scale", s);
+    e = launch_grad_scale(a, s);
+    if (e != hipSuccess) return hip_fail(e, "gradient scaling launch");
+  }
   return MLS_OK;
 }
 

@@ -263,7 +263,10 @@ __device__ __forceinline__ void store4<F32>(float* p, float a0, float a1, float 
 
 // Backward tile kernel of the fp32 path (one slab, token-major) and of the
 // general bf16 path (both slab layouts).
-template <class Mma, typename E, bool TAU1>
+// ROWG (one sub-model): the gradient of the tokens' log-probabilities at
+// temperature tau, G = g_row / tau (onehot - softmax(l / tau)), in place of the
+// losses'.
+template <class Mma, typename E, bool TAU1, bool ROWG = false>
 __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
   constexpr int BN = Mma::kBN;
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   const int64_t vbase = a.v0 + vloc;      // absolute vocabulary row
   const int64_t tbase = (int64_t)tt * BN;
   const bool full = vbase + BM <= a.V;
-  const int nv = *a.n_valid;
+  const int nv = ROWG ? 0 : *a.n_valid;
   const float invN = nv > 0 ? 1.0f / (float)nv : 0.0f;
 
   int64_t tok[FN];
@@ -310,8 +313,8 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
     const int64_t kb = a.d[i] * E::kBytes;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
             kb, tbase, a.T, kb, smem, tid);
-    const float gce = a.g_ce ? a.g_ce[i] : a.host_gce[i];
-    const float gkl = a.g_kl ? a.g_kl[i] : a.host_gkl[i];
+    const float gce = ROWG ? 0.f : a.g_ce ? a.g_ce[i] : a.host_gce[i];
+    const float gkl = ROWG ? 0.f : a.g_kl ? a.g_kl[i] : a.host_gkl[i];
     S* slab = static_cast<S*>(a.slab) + (int64_t)i * a.T_pad * a.Vc;
     S* slabT = static_cast<S*>(a.slabT) + (int64_t)i * a.T_pad * a.Vc;
 
@@ -319,10 +322,10 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
     for (int fn = 0; fn < FN; ++fn) {
       const int64_t t = tok[fn];
       // invalid rows: +inf log-normalisers make every probability 0
-      const float l1 = rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
+      const float l1 = !ROWG && rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
       const float lt = rv[fn] ? a.lset[(int64_t)i * a.T + t] : INFINITY;
-      const float cg = rv[fn] ? gce * invN : 0.f;
-      const float ck = (rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
+      const float cg = !rv[fn] ? 0.f : ROWG ? -a.g_row[t] * a.inv_tau : gce * invN;
+      const float ck = (!ROWG && rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
       const float l1s = l1 * kLog2e;
       const float lts = lt * kLog2e;
       const float ct = kLog2e * a.inv_tau;
@@ -338,7 +341,9 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
             const bool ok = full || vbase + row < a.V;
             const float l = mma.acc[fm][fn][r];
             const float oh = row == ylab[fn] ? 1.f : 0.f;
-            if (oi == 0) {
+            if (ROWG) {
+              g[rr] = cg * ((ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f) - oh);
+            } else if (oi == 0) {
               const float q = ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f;
               q_t.set(fm, fn, r, q);
               const float p1 = TAU1 ? q : (ok ? fast_exp2(fmaf(l, kLog2e, -l1s)) : 0.f);
@@ -368,7 +373,7 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
 // [token][vocabulary] (16-byte chunks XOR-swizzled with the token index) and
 // leaves the block as 16-byte coalesced stores of token-major slab rows. The
 // gradient GEMMs read this one layout for both products.
-template <class Mma, bool TAU1, int MINB>
+template <class Mma, bool TAU1, int MINB, bool ROWG = false>
 __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;  // vocabulary rows
   constexpr int BN = Mma::kBN;  // tokens
@@ -395,7 +400,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
   const int64_t vbase = a.v0 + vloc;
   const int64_t tbase = (int64_t)tt * BN;
   const bool full = vbase + BM <= a.V;
-  const int nv = *a.n_valid;
+  const int nv = ROWG ? 0 : *a.n_valid;
   const float invN = nv > 0 ? 1.0f / (float)nv : 0.0f;
   const float ct = kLog2e * a.inv_tau;
 
@@ -420,17 +425,17 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
     const int64_t kb = a.d[i] * 2;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
             kb, tbase, a.T, kb, smem, tid);
-    const float gce = a.g_ce ? a.g_ce[i] : a.host_gce[i];
-    const float gkl = a.g_kl ? a.g_kl[i] : a.host_gkl[i];
+    const float gce = ROWG ? 0.f : a.g_ce ? a.g_ce[i] : a.host_gce[i];
+    const float gkl = ROWG ? 0.f : a.g_kl ? a.g_kl[i] : a.host_gkl[i];
 
     // 1. logit gradient -> bf16 tile in LDS
 #pragma unroll
     for (int fn = 0; fn < FN; ++fn) {
       const int64_t t = tbase + tcol[fn];
-      const float l1 = rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
+      const float l1 = !ROWG && rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
       const float lt = rv[fn] ? a.lset[(int64_t)i * a.T + t] : INFINITY;
-      const float cg = rv[fn] ? gce * invN : 0.f;
-      const float ck = (rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
+      const float cg = !rv[fn] ? 0.f : ROWG ? -a.g_row[t] * a.inv_tau : gce * invN;
+      const float ck = (!ROWG && rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
       const float l1s = l1 * kLog2e;
       const float lts = lt * kLog2e;
       const int trow = tcol[fn];
@@ -446,7 +451,9 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
             const bool ok = full || vbase + row < a.V;
             const float l = mma.acc[fm][fn][r];
             const float oh = row == ylab[fn] ? 1.f : 0.f;
-            if (oi == 0) {
+            if (ROWG) {
+              g[rr] = cg * ((ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f) - oh);
+            } else if (oi == 0) {
               const float q = ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f;
               q_t.set(fm, fn, r, q);
               const float p1 = TAU1 ? q : (ok ? fast_exp2(fmaf(l, kLog2e, -l1s)) : 0.f);
@@ -508,17 +515,24 @@ hipError_t launch_fwd_wide(const FusedArgs& a, hipStream_t stream) {
 template <class Mma>
 hipError_t launch_bwd_wide(const FusedArgs& a, hipStream_t stream) {
   dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt);
-  if (a.tau == 1.0f)
+  if (a.g_row)
+    hipLaunchKernelGGL((fused_bwd_wide_kernel<Mma, true, 2, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else if (a.tau == 1.0f)
     hipLaunchKernelGGL((fused_bwd_wide_kernel<Mma, true, 2>), grid, dim3(Mma::NT), 0, stream, a);
   else
     hipLaunchKernelGGL((fused_bwd_wide_kernel<Mma, false, 2>), grid, dim3(Mma::NT), 0, stream, a);
   return hipGetLastError();
 }
 
-template <class Mma, typename E, bool TAU1>
+template <class Mma, typename E>
 hipError_t launch_bwd_t(const FusedArgs& a, hipStream_t stream) {
   dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt);
-  hipLaunchKernelGGL((fused_bwd_kernel<Mma, E, TAU1>), grid, dim3(Mma::NT), 0, stream, a);
+  if (a.g_row)
+    hipLaunchKernelGGL((fused_bwd_kernel<Mma, E, true, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else if (a.tau == 1.0f)
+    hipLaunchKernelGGL((fused_bwd_kernel<Mma, E, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else
+    hipLaunchKernelGGL((fused_bwd_kernel<Mma, E, false>), grid, dim3(Mma::NT), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -546,14 +560,11 @@ hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
 }
 
 hipError_t launch_fused_bwd(const FusedArgs& a, bool f32, hipStream_t stream) {
-  const bool tau1 = a.tau == 1.0f;
-  if (f32)
-    return tau1 ? launch_bwd_t<MmaF32, F32, true>(a, stream)
-                : launch_bwd_t<MmaF32, F32, false>(a, stream);
+  if (a.g_row && a.M != 1) return hipErrorInvalidValue;
+  if (f32) return launch_bwd_t<MmaF32, F32>(a, stream);
   if (a.wide)
     return a.ktail ? launch_bwd_wide<WideFusedTail>(a, stream) : launch_bwd_wide<WideFused>(a, stream);
-  return tau1 ? launch_bwd_t<GenMmaBf16, Bf16, true>(a, stream)
-              : launch_bwd_t<GenMmaBf16, Bf16, false>(a, stream);
+  return launch_bwd_t<GenMmaBf16, Bf16>(a, stream);
 }
 
 }  // namespace mls

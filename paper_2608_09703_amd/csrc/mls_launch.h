@@ -63,6 +63,9 @@ struct FusedArgs {
   const int32_t* n_valid;
   const float* g_ce;  // device [M] or null
   const float* g_kl;
+  // backward of token log-probabilities (M = 1): upstream gradient of each
+  // token's log-probability at temperature tau; null for the losses
+  const float* g_row;  // [T]
   float host_gce[kMaxModels];
   float host_gkl[kMaxModels];
   void* slab;   // [M][T_pad][Vc]  dJ/dlogits, token-major
@@ -169,6 +172,9 @@ struct RowArgs {
   float* ce;
   float* kl;
   float* entropy;
+  // token log-probabilities (M = 1): per token, at temperature tau; null for the losses
+  float* logp_row;     // [T]
+  float* entropy_row;  // [T] or null
 };
 
 // Logit gradient of one token chunk from its stored logits (fused forward +
@@ -252,6 +258,85 @@ struct JunctionArgs {
   void* g_o;        // [T][d_prev]
   void* g_e;        // [T][d_fresh]
 };
+
+// Layer norm in front of a head.
+struct NormArgs {
+  int64_t T;
+  int64_t ld_x;         // elements between rows of x
+  int32_t d;
+  int32_t waves;        // waves of one row
+  int32_t param_f32;    // weight, bias and their gradients: fp32 (else bf16)
+  float eps;
+  const void* x;        // [T] rows of d, ld_x apart
+  const void* weight;   // [d]
+  const void* bias;     // [d] or null
+  void* y;              // [T][d]
+  float* stats;         // mean [T], 1 / deviation [T]; null: not kept
+  const void* g_y;      // [T][d]
+  void* g_x;            // [T][d] or null
+  float* part;          // [blocks][2][d] fp32 parts of the parameters' gradients, or null
+  void* g_weight;       // [d] or null
+  void* g_bias;         // [d] or null
+};
+// How a norm is laid over the chip: waves per row, 16-byte chunks per lane, rows
+// a block takes at a time, blocks, and whether rows take 16-byte accesses.
+struct NormShape {
+  int cpl;
+  int waves;
+  int groups;
+  int blocks;
+  bool vec;
+};
+
+// Clipped policy loss.
+struct PolicyArgs {
+  int64_t N;              // tokens
+  int64_t S;              // sequences (0 without cu)
+  const float* logp;      // [N]
+  const float* old_logp;  // [N]
+  const float* adv;       // [N], or [S] with per_seq
+  const float* ref;       // [N] or null
+  const uint8_t* mask;    // [N] (nonzero: counted) or null
+  const int32_t* cu;      // [S + 1] or null
+  int32_t per_seq;
+  int32_t by_seq;         // mean over sequences of their tokens' means
+  double lo;              // 1 - clip_low
+  double hi;              // 1 + clip_high
+  double beta;
+  float* loss;
+  float* kl;              // or null
+  float* clipped;         // or null
+  // null, or [N + 1]: dL/dlogp before the division by the number of tokens or
+  // sequences, then 1 / that number
+  float* grad;
+  double* part;           // [blocks][4]
+  int32_t* counts;        // [S], with by_seq and a mask
+};
+
+// Gradient norm and clipping. The tensors of one launch lie in the kernel's
+// arguments (below 4 KiB); n carries the type in its top bit.
+constexpr int64_t kClipF32 = (int64_t)1 << 62;
+constexpr int64_t kClipCountMask = kClipF32 - 1;
+constexpr int kNormTensors = 192;
+constexpr int kScaleTensors = 136;
+struct GradNormArgs {
+  const void* data[kNormTensors];
+  int64_t n[kNormTensors];
+  int32_t tile_begin[kNormTensors];
+  int32_t count;
+  int32_t tiles;
+  double* part;  // [blocks]
+};
+struct GradScaleArgs {
+  const void* data[kScaleTensors];
+  void* out[kScaleTensors];
+  int64_t n[kScaleTensors];
+  int32_t tile_begin[kScaleTensors];
+  int32_t count;
+  int32_t tiles;
+  const float* coef;
+};
+static_assert(sizeof(GradNormArgs) <= 4096 && sizeof(GradScaleArgs) <= 4096, "kernel argument size");
 
 // Speculative-decoding head step.
 struct HeadArgs {
@@ -347,6 +432,23 @@ bool junction_shape(int64_t width, int* tpr, int* cpl);
 int64_t junction_max_width();
 hipError_t launch_junction_fwd(const JunctionArgs& a, bool act_f32, hipStream_t stream);
 hipError_t launch_junction_bwd(const JunctionArgs& a, bool act_f32, bool grad_f32, hipStream_t stream);
+int64_t norm_max_width();
+NormShape norm_shape(int64_t T, int64_t d, bool f32, bool vec, bool bwd);
+hipError_t launch_layer_norm_fwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
+hipError_t launch_layer_norm_bwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
+hipError_t launch_layer_norm_params(const NormArgs& a, int n_parts, hipStream_t stream);
+int64_t policy_blocks(int64_t N);
+size_t policy_part_bytes(int64_t N);
+hipError_t launch_policy_count(const PolicyArgs& a, hipStream_t stream);
+hipError_t launch_policy_fwd(const PolicyArgs& a, hipStream_t stream);
+hipError_t launch_policy_finish(const PolicyArgs& a, hipStream_t stream);
+hipError_t launch_policy_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp, hipStream_t stream);
+int64_t clip_tiles(int64_t n);
+int clip_blocks(int64_t tiles);
+hipError_t launch_grad_norm(const GradNormArgs& a, hipStream_t stream);
+hipError_t launch_grad_norm_finish(const double* part, int n, double max_norm, float* norm, float* coef,
+                                   hipStream_t stream);
+hipError_t launch_grad_scale(const GradScaleArgs& a, hipStream_t stream);
 // wide: bf16; vocabulary rows and token columns of a head tile over T rows of V logits
 void head_tile(bool wide, int64_t T, int64_t V, int* rows, int* cols);
 int row_elems_per_thread(int64_t V);
@@ -357,6 +459,7 @@ hipError_t launch_row_params(const RowParamArgs& a, int ept, hipStream_t stream)
 hipError_t launch_verify(const VerifyArgs& a, int ept, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_finalize_rows(const RowArgs& a, hipStream_t stream);
+hipError_t launch_finalize_logp(const RowArgs& a, hipStream_t stream);
 hipError_t launch_reduce_losses(const RowArgs& a, hipStream_t stream);
 hipError_t launch_count_valid(const RowArgs& a, hipStream_t stream);
 hipError_t launch_grad_logits(const GradArgs& a, hipStream_t stream);

@@ -1,0 +1,223 @@
+// Clipped policy loss with a KL term on token log-probabilities, and its gradient.
+// Per counted token t with advantage A and ratio r = exp(logp - old):
+//   L = -min(r A, clip(r, 1 - lo, 1 + hi) A) + beta k,
+//   k = exp(ref - logp) - (ref - logp) - 1        (an estimate of KL(policy || reference), >= 0)
+//   dL/dlogp = -r A  where r A <= clip(r) A, else 0,  plus beta (1 - exp(ref - logp)).
+// loss = sum_t w_t L_t with w = 1 / N over the N counted tokens, or with
+// w = 1 / (S n_s) over the S sequences that have a counted token, n_s of them in
+// sequence s.
+//
+// 13 to 17 bytes read and 4 written per token: bound by memory for many tokens
+// and by launches for few. Everything is computed in 64 bits from the fp32
+// inputs, so that whether a ratio is clipped does not depend on a rounding (the
+// two exponentials of a million tokens take the chip a few microseconds). The
+// gradient is written by the forward, without the 1 / N or 1 / S that is known
+// only once every token has been counted; the backward multiplies that and the
+// upstream gradient in. Sums leave the blocks as 64-bit parts that one block adds
+// in block order: results are bitwise reproducible.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mls_device.h"
+#include "mls_launch.h"
+#include "mls_wave.h"
+
+namespace mls {
+
+namespace {
+
+constexpr int kPolThreads = 256;
+constexpr int kPolTok = 4;                        // tokens per thread
+constexpr int kPolTile = kPolThreads * kPolTok;   // tokens per block
+constexpr int kPolSums = 4;                       // loss, KL, clipped, counted (tokens or sequences)
+constexpr int kPolFinThreads = 1024;
+
+__device__ __forceinline__ double wave_total(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// Start of sequence s inside [0, N]: offsets out of range are clamped, so that a
+// bad one reads no memory outside the arrays.
+__device__ __forceinline__ int64_t seq_begin(const PolicyArgs& a, int64_t s) {
+  const int64_t c = a.cu[s];
+  return c < 0 ? 0 : c > a.N ? a.N : c;
+}
+
+// Sequence of token t: the last one that begins at or before t (t lies inside
+// [begin of the first, end of the last)).
+__device__ __forceinline__ int64_t seq_of(const PolicyArgs& a, int64_t t) {
+  int64_t lo = 0, hi = a.S;  // begin(lo) <= t < begin(hi)
+  while (hi - lo > 1) {
+    const int64_t m = (lo + hi) >> 1;
+    if (a.cu[m] <= t)
+      lo = m;
+    else
+      hi = m;
+  }
+  return lo;
+}
+
+// Counted tokens of every sequence under a mask, one block a sequence.
+__global__ __launch_bounds__(kPolThreads) void policy_count_kernel(PolicyArgs a) {
+  __shared__ int part[kPolThreads / 64];
+  const int64_t b = seq_begin(a, blockIdx.x), e = seq_begin(a, (int64_t)blockIdx.x + 1);
+  int n = 0;
+  for (int64_t t = b + threadIdx.x; t < e; t += kPolThreads) n += a.mask[t] ? 1 : 0;
+  n = wave_sum(n);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    n = 0;
+    for (int k = 0; k < kPolThreads / 64; ++k) n += part[k];
+    a.counts[blockIdx.x] = n;
+  }
+}
+
+__device__ __forceinline__ int64_t seq_count(const PolicyArgs& a, int64_t s) {
+  if (a.mask) return a.counts[s];
+  const int64_t n = seq_begin(a, s + 1) - seq_begin(a, s);
+  return n > 0 ? n : 0;
+}
+
+// The loss and its companions from the sums over all tokens; thread 0 of a block.
+__device__ __forceinline__ void write_losses(const PolicyArgs& a, const double* s) {
+  const double inv = s[3] > 0.0 ? 1.0 / s[3] : 0.0;
+  *a.loss = (float)(s[0] * inv);
+  if (a.kl) *a.kl = (float)(s[1] * inv);
+  if (a.clipped) *a.clipped = (float)(s[2] * inv);
+  if (a.grad) a.grad[a.N] = (float)inv;
+}
+
+// Sum over the block of each of kPolSums values; valid in thread 0. red: one row per wave.
+template <int NT>
+__device__ __forceinline__ void block_totals(double* v, double (*red)[kPolSums]) {
+#pragma unroll
+  for (int q = 0; q < kPolSums; ++q) v[q] = wave_total(v[q]);
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int q = 0; q < kPolSums; ++q) red[threadIdx.x >> 6][q] = v[q];
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int q = 0; q < kPolSums; ++q) {
+    v[q] = 0.0;
+    for (int w = 0; w < NT / 64; ++w) v[q] += red[w][q];
+  }
+}
+
+// Number of sequences with a counted token, this thread's share.
+template <int NT>
+__device__ __forceinline__ double live_sequences(const PolicyArgs& a) {
+  double n = 0.0;
+  for (int64_t s = threadIdx.x; s < a.S; s += NT) n += seq_count(a, s) > 0 ? 1.0 : 0.0;
+  return n;
+}
+
+__global__ __launch_bounds__(kPolThreads) void policy_fwd_kernel(PolicyArgs a) {
+  __shared__ double red[kPolThreads / 64][kPolSums];
+  double sum[kPolSums] = {0.0, 0.0, 0.0, 0.0};
+  // tokens that belong to a sequence
+  const int64_t begin = a.cu ? seq_begin(a, 0) : 0, end = a.cu ? seq_begin(a, a.S) : a.N;
+  int64_t s = -1, s_end = 0;
+  double seq_w = 1.0, seq_a = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPolTok; ++i) {
+    const int64_t t = (int64_t)blockIdx.x * kPolTile + i * kPolThreads + threadIdx.x;
+    if (t >= a.N) break;
+    float g = 0.f;
+    if (t >= begin && t < end && (!a.mask || a.mask[t])) {
+      if ((a.per_seq || a.by_seq) && (s < 0 || t >= s_end)) {
+        s = seq_of(a, t);
+        s_end = a.cu[s + 1];
+        if (a.per_seq) seq_a = a.adv[s];
+        if (a.by_seq) seq_w = 1.0 / (double)seq_count(a, s);
+      }
+      const double lp = a.logp[t];
+      const double adv = a.per_seq ? seq_a : (double)a.adv[t];
+      const double r = exp(lp - (double)a.old_logp[t]);
+      const double free = r * adv, bound = fmin(fmax(r, a.lo), a.hi) * adv;
+      const bool take = !(free > bound);
+      double l = take ? -free : -bound, dl = take ? -free : 0.0, k = 0.0;
+      if (a.ref) {
+        const double x = (double)a.ref[t] - lp, ex = exp(x);
+        k = ex - x - 1.0;
+        l += a.beta * k;
+        dl += a.beta * (1.0 - ex);
+      }
+      sum[0] += seq_w * l;
+      sum[1] += seq_w * k;
+      sum[2] += take ? 0.0 : seq_w;
+      sum[3] += 1.0;
+      g = (float)(seq_w * dl);
+    }
+    if (a.grad) a.grad[t] = g;
+  }
+  if (a.by_seq) sum[3] = gridDim.x == 1 ? live_sequences<kPolThreads>(a) : 0.0;
+  block_totals<kPolThreads>(sum, red);
+  if (threadIdx.x != 0) return;
+  if (gridDim.x == 1) {
+    write_losses(a, sum);
+  } else {
+#pragma unroll
+    for (int q = 0; q < kPolSums; ++q) a.part[(int64_t)blockIdx.x * kPolSums + q] = sum[q];
+  }
+}
+
+__global__ __launch_bounds__(kPolFinThreads) void policy_finish_kernel(PolicyArgs a, int n_parts) {
+  __shared__ double red[kPolFinThreads / 64][kPolSums];
+  double sum[kPolSums] = {0.0, 0.0, 0.0, 0.0};
+  for (int k = threadIdx.x; k < n_parts; k += kPolFinThreads)
+#pragma unroll
+    for (int q = 0; q < kPolSums; ++q) sum[q] += a.part[(int64_t)k * kPolSums + q];
+  if (a.by_seq) sum[3] = live_sequences<kPolFinThreads>(a);
+  block_totals<kPolFinThreads>(sum, red);
+  if (threadIdx.x == 0) write_losses(a, sum);
+}
+
+// g_logp = grad * upstream / (tokens or sequences counted)
+// (a token without a gradient keeps its exact zero, whatever the upstream one is)
+__global__ __launch_bounds__(kPolThreads) void policy_bwd_kernel(int64_t N, const float* grad, const float* g_loss,
+                                                                 float* g_logp) {
+  const float c = grad[N] * g_loss[0];
+#pragma unroll
+  for (int i = 0; i < kPolTok; ++i) {
+    const int64_t t = (int64_t)blockIdx.x * kPolTile + i * kPolThreads + threadIdx.x;
+    if (t < N) {
+      const float g = grad[t];
+      g_logp[t] = g == 0.f ? 0.f : g * c;
+    }
+  }
+}
+
+}  // namespace
+
+int64_t policy_blocks(int64_t N) { return (N + kPolTile - 1) / kPolTile; }
+size_t policy_part_bytes(int64_t N) { return (size_t)policy_blocks(N) * kPolSums * sizeof(double); }
+
+hipError_t launch_policy_count(const PolicyArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(policy_count_kernel, dim3((unsigned)a.S), dim3(kPolThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_policy_fwd(const PolicyArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(policy_fwd_kernel, dim3((unsigned)policy_blocks(a.N)), dim3(kPolThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_policy_finish(const PolicyArgs& a, hipStream_t stream) {
+  const int n = (int)policy_blocks(a.N);
+  if (n == 1) return hipSuccess;  // the forward's one block has finished
+  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kPolFinThreads), 0, stream, a, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_policy_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp, hipStream_t stream) {
+  hipLaunchKernelGGL(policy_bwd_kernel, dim3((unsigned)policy_blocks(N)), dim3(kPolThreads), 0, stream, N, grad,
+                     g_loss, g_logp);
+  return hipGetLastError();
+}
+
+}  // namespace mls

@@ -1,0 +1,201 @@
+"""The clipped policy loss on the GPU against the float64 oracle.
+
+The kernels compute in 64 bits. The three means are rounded to fp32 once: 2^-24 of
+themselves, plus 1e-12 of the terms' absolute mean for the 64-bit sums. A token's
+gradient is rounded when it is kept, multiplied by a rounded product of a rounded
+reciprocal count and the upstream gradient, and rounded: 5 * 2^-24 of itself.
+"""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import post as P
+from paper_2608_09703_amd import api as D
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def _draw(n, seed, S=None, per_sequence=False):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    old = -3 * torch.rand(n, generator=g, device=DEV)
+    logp = old + 0.2 * torch.randn(n, generator=g, device=DEV)
+    ref = old + 0.4 * torch.randn(n, generator=g, device=DEV)
+    adv = torch.randn(S if per_sequence else n, generator=g, device=DEV)
+    mask = torch.rand(n, generator=g, device=DEV) < 0.7
+    return logp, old, adv, ref, mask
+
+
+def _np(x):
+    return None if x is None else x.detach().double().cpu().numpy().reshape(-1)
+
+
+def _check(logp, old, adv, upstream=1.0, ref=None, mask=None, cu=None, oracle_cu=None, **kw):
+    leaf = logp.detach().requires_grad_(True)
+    loss, kl, clipped = D.policy_loss(leaf, old, adv, ref_logp=ref, mask=mask, cu_seqlens=cu, **kw)
+    (loss * upstream).backward()
+    cu_n = oracle_cu if oracle_cu is not None else None if cu is None else cu.cpu().numpy()
+    kw = {k: v for k, v in kw.items()}
+    want = P.policy(_np(logp), _np(old), _np(adv), ref=_np(ref), mask=None if mask is None else
+                    mask.cpu().numpy().reshape(-1), cu=cu_n, **kw)
+    scale = np.abs(np.nan_to_num(_np(adv), posinf=0, neginf=0)).max(initial=0) * 10 + 10
+    for got, ref_v, name in ((loss, want[0], "loss"), (kl, want[1], "kl"), (clipped, want[2], "clipped")):
+        assert got.shape == () and abs(float(got) - ref_v) <= U * abs(ref_v) + 1e-12 * scale, (name, float(got), ref_v)
+    got = _np(leaf.grad)
+    assert np.all(np.abs(got - upstream * want[3]) <= 5 * U * np.abs(upstream * want[3]) + 1e-45)
+    return leaf.grad, want
+
+
+SIZES = [1, 2, 63, 64, 255, 257, 1023, 1024, 1025, 2048, 5000]
+
+
+@pytest.mark.parametrize("n", SIZES)
+@pytest.mark.parametrize("masked", [False, True])
+def test_plain_tokens(n, masked):
+    logp, old, adv, ref, mask = _draw(n, n)
+    _check(logp, old, adv, mask=mask if masked else None)
+    _check(logp, old, adv, ref=ref, mask=mask if masked else None, kl_coef=0.1, clip_low=0.1, clip_high=0.3)
+
+
+def _sequences(lens, before=0, after=0):
+    cu = np.concatenate([[0], np.cumsum(lens)]) + before
+    return torch.tensor(cu, dtype=torch.int32, device=DEV), int(cu[-1]) + after
+
+
+LENS = [[1], [5], [0, 3], [3, 0], [0, 0, 7, 0], [1, 1, 1, 1], [1500], [1, 2000, 3], [700, 0, 900, 1, 60, 1024],
+        list(range(40))]
+
+
+@pytest.mark.parametrize("lens", LENS, ids=lambda v: f"{len(v)}x{sum(v)}")
+@pytest.mark.parametrize("reduction", ["token", "sequence"])
+@pytest.mark.parametrize("per_sequence", [False, True])
+@pytest.mark.parametrize("masked", [False, True])
+def test_packed_sequences(lens, reduction, per_sequence, masked):
+    for before, after in ((0, 0), (3, 1100)):
+        cu, n = _sequences(lens, before, after)
+        logp, old, adv, ref, mask = _draw(n, n, len(lens), per_sequence)
+        # what lies outside of the sequences, and what the mask takes out, is not used
+        out = torch.zeros(n, dtype=torch.bool, device=DEV)
+        out[:before] = True
+        out[n - after:] = True
+        if masked:
+            out |= ~mask
+        dirty = [t.clone() for t in (logp, old, ref)]
+        for t, v in zip(dirty, (float("nan"), float("-inf"), float("inf"))):
+            t[out] = v
+        if not per_sequence:
+            adv[out] = float("nan")
+        kw = dict(cu=cu, mask=mask if masked else None, per_sequence=per_sequence, reduction=reduction, kl_coef=0.05)
+        g, _ = _check(dirty[0], dirty[1], adv, ref=dirty[2], **kw)
+        assert not g[out].any()
+
+
+def test_padded_batch_equals_its_packed_form():
+    B_, L = 5, 70
+    logp, old, adv, ref, mask = (t.view(B_, L) if t.numel() == B_ * L else t for t in _draw(B_ * L, 1, B_, True))
+    cu = np.arange(0, B_ * L + 1, L)
+    g, _ = _check(logp, old, adv, ref=ref, mask=mask, oracle_cu=cu, per_sequence=True, reduction="sequence",
+                  kl_coef=0.1)
+    assert g.shape == (B_, L)
+    flat = [t.reshape(-1) for t in (logp, old, ref, mask)]
+    leaf = flat[0].detach().requires_grad_(True)
+    loss, _, _ = D.policy_loss(leaf, flat[1], adv, ref_logp=flat[2], mask=flat[3], per_sequence=True,
+                               cu_seqlens=torch.tensor(cu, dtype=torch.int32, device=DEV), reduction="sequence",
+                               kl_coef=0.1)
+    loss.backward()
+    assert torch.equal(leaf.grad.view(B_, L), g)
+
+
+def test_nothing_counts():
+    logp, old, adv, ref, _ = _draw(100, 2)
+    none = torch.zeros(100, dtype=torch.bool, device=DEV)
+    for kw in (dict(mask=none), dict(mask=none, reduction="sequence", cu_seqlens=_sequences([40, 60])[0]),
+               dict(cu_seqlens=_sequences([0, 0], before=7)[0])):
+        leaf = logp.detach().requires_grad_(True)
+        loss, kl, clipped = D.policy_loss(leaf, old, adv, ref_logp=ref, kl_coef=0.1, **kw)
+        loss.backward()
+        assert float(loss) == float(kl) == float(clipped) == 0.0 and not leaf.grad.any()
+
+
+def test_borders_of_the_clip():
+    """Ratios at and one fp32 step around both borders; the decision is that of 64 bits."""
+    lo, hi = math.log(0.8), math.log(1.2)
+    x = np.array([lo, hi, 0.0], dtype=np.float32)
+    x = np.concatenate([x, np.nextafter(x, np.float32(9)), np.nextafter(x, np.float32(-9))])
+    logp = torch.tensor(np.tile(x, 2), device=DEV)
+    adv = torch.cat([torch.ones(9), -torch.ones(9)]).to(DEV)
+    _check(logp, torch.zeros_like(logp), adv)
+    _check(logp, torch.zeros_like(logp), adv, clip_low=0.0, clip_high=0.0)
+    _check(logp, torch.zeros_like(logp), adv, clip_low=1.0, clip_high=float("inf"))
+
+
+@pytest.mark.parametrize("upstream", [1.0, -0.3, 1e-6])
+def test_upstream_gradient(upstream):
+    logp, old, adv, ref, mask = _draw(3000, 4)
+    up = float(np.float32(upstream))
+    _check(logp, old, adv, upstream=up, ref=ref, mask=mask, kl_coef=0.02)
+
+
+def test_gradients_of_masked_tokens_stay_zero_under_a_bad_upstream():
+    logp, old, adv, _, mask = _draw(2000, 5)
+    leaf = logp.detach().requires_grad_(True)
+    loss, _, _ = D.policy_loss(leaf, old, adv, mask=mask)
+    loss.backward(torch.tensor(float("nan"), device=DEV))
+    assert not leaf.grad[~mask].any()
+
+
+def test_far_ratios():
+    """Log-ratios of +-100: the loss of a token that is not held back grows, nothing turns NaN."""
+    logp = torch.tensor([0.0, -100.0, 0.0, -100.0], device=DEV)
+    old = torch.tensor([-80.0, 0.0, -80.0, 0.0], device=DEV)
+    adv = torch.tensor([1.0, 1.0, -1.0, -1.0], device=DEV)
+    _check(logp, old, adv)
+
+
+def test_bad_offsets_stay_inside():
+    """Offsets beyond the tokens are taken as their ends: no read or write outside."""
+    logp, old, adv, _, _ = _draw(50, 6)
+    for cu in ([0, 20, 500], [-5, 20, 50], [0, 60, 70], [0, 0, 0]):
+        for reduction in ("token", "sequence"):
+            leaf = logp.detach().requires_grad_(True)
+            loss, _, _ = D.policy_loss(leaf, old, adv, cu_seqlens=torch.tensor(cu, dtype=torch.int32, device=DEV),
+                                       reduction=reduction)
+            loss.backward()
+            clamped = np.clip(cu, 0, 50)
+            want = P.policy(_np(logp), _np(old), _np(adv), cu=clamped, reduction=reduction)
+            assert abs(float(loss) - want[0]) <= U * abs(want[0]) + 1e-11
+
+
+def test_many_tokens_and_no_gradient():
+    n, S = 300000, 200
+    cu, n = _sequences([n // S] * S)
+    logp, old, adv, ref, mask = _draw(n, 7, S, True)
+    kw = dict(ref_logp=ref, mask=mask, cu_seqlens=cu, per_sequence=True, reduction="sequence", kl_coef=0.1)
+    _, want = _check(logp, old, adv, ref=ref, mask=mask, cu=cu, per_sequence=True, reduction="sequence", kl_coef=0.1)
+    a = D.policy_loss(logp, old, adv, **kw)
+    b = D.policy_loss(logp, old, adv, **kw)
+    assert all(torch.equal(x, y) for x, y in zip(a, b)) and not a[0].requires_grad
+    assert abs(float(a[0]) - want[0]) <= U * abs(want[0]) + 1e-11
+
+
+def test_refusals():
+    logp, old, adv, ref, mask = _draw(12, 8)
+    cu, _ = _sequences([5, 7])
+    bad = [dict(reduction="mean"), dict(reduction="sequence"), dict(per_sequence=True), dict(mask=mask.float()),
+           dict(mask=mask[:5]), dict(ref_logp=ref.double()), dict(cu_seqlens=cu.long()), dict(cu_seqlens=cu[:1]),
+           dict(cu_seqlens=cu, per_sequence=True), dict(cu_seqlens=cu.cpu())]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            D.policy_loss(logp, old, adv, **kw)
+    for args in ((logp[::2], old[::2], adv[::2]), (logp.double(), old, adv), (logp, old[:3], adv),
+                 (logp, old, adv[:3]), (logp, old, adv.cpu())):
+        with pytest.raises(ValueError):
+            D.policy_loss(*args)
+    for kw in (dict(kl_coef=0.1), dict(clip_low=2.0), dict(clip_high=-1.0)):
+        with pytest.raises(RuntimeError):
+            D.policy_loss(logp, old, adv, **kw)

@@ -1,0 +1,189 @@
+"""Token log-probabilities of a head on the GPU against the float64 oracle.
+
+Forward: fp32 rows, the statistics' tolerance of the fused loss (5e-5 for a
+log-sum-exp and a logit of fp32 sums). Gradients: every row within the fused loss's
+gradient bounds (the logit gradient is bf16 in between on the bf16 path), and
+element by element within what the roundings allow: with G the exact logit gradient,
+2^-8 sum |G| |W| for its rounding, as much again of the result for the output's, and
+2^-12 sum |G| |W| for the recomputed logits (a logit of fp32 sums is off by less than
+2^-13 here, and exp turns that into a relative error of G's softmax part).
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import post as P
+from paper_2608_09703_amd import api as D
+from paper_2608_09703_amd import binding as B
+from tests.grad_checks import assert_grad_rows
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _np(x):
+    return x.detach().double().cpu().numpy()
+
+
+def _draw(T, d, V, dtype, seed, ignore=0.2):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    h = torch.randn(T, d, generator=g, device=DEV).to(dtype)
+    W = (torch.randn(V, d, generator=g, device=DEV) * (2.0 / d ** 0.5)).to(dtype)
+    tokens = torch.randint(0, V, (T,), generator=g, device=DEV)
+    tokens[torch.rand(T, generator=g, device=DEV) < ignore] = -100
+    gl = torch.randn(T, generator=g, device=DEV)
+    return h, W, tokens, gl
+
+
+def _check(h, W, tokens, gl, temperature, got, what):
+    logp, entropy, gh, gW = got
+    hn, Wn, tn, gn = _np(h), _np(W), tokens.cpu().numpy(), _np(gl)
+    lp, en = P.token_logp(hn, Wn, tn, temperature)
+    np.testing.assert_allclose(_np(logp), lp, rtol=1e-5, atol=5e-5, err_msg=what)
+    np.testing.assert_allclose(_np(entropy), en, rtol=1e-5, atol=5e-5, err_msg=what)
+    rh, rW = P.token_logp_backward(hn, Wn, tn, gn, temperature)
+    bf16 = h.dtype == torch.bfloat16
+    rows = np.flatnonzero((tn != -100) & (tn >= 0) & (tn < len(Wn)))
+    G = np.zeros((len(hn), len(Wn)))
+    if rows.size:
+        z = hn[rows] @ Wn.T / temperature
+        p = np.exp(z - z.max(1, keepdims=True))
+        G[rows] = p / p.sum(1, keepdims=True)
+        G[rows, tn[rows]] = 1 - G[rows, tn[rows]]
+        G[rows] *= np.abs(gn[rows])[:, None] / temperature
+    rel = 2.0 ** -8 + 2.0 ** -12 if bf16 else 2.0 ** -12
+    half = 2.0 ** -8 if bf16 else 2.0 ** -24
+    for g, r, s, name in ((gh, rh, G @ np.abs(Wn), "grad_h"), (gW, rW, G.T @ np.abs(hn), "grad_W")):
+        if g is None:
+            continue
+        gn_ = _np(g)
+        bad = ~(np.abs(gn_ - r) <= rel * s + half * np.abs(r))
+        assert not bad.any(), f"{what} {name}: {bad.sum()} off, first at {np.argwhere(bad)[0]}"
+        assert_grad_rows(gn_, r, f"{what} {name}")
+    return rh, rW
+
+
+def _run(h, W, tokens, gl, **kw):
+    h, W = h.detach().requires_grad_(True), W.detach().requires_grad_(True)
+    logp, entropy = D.token_logp(h, W, tokens, **kw)
+    gh, gW = torch.autograd.grad(logp, (h, W), gl)
+    return logp, entropy, gh, gW
+
+
+SHAPES = [(1, 8, 2), (1, 64, 300), (2, 64, 128), (127, 64, 129), (128, 72, 1000), (129, 200, 515), (300, 128, 2000),
+          (257, 520, 4097), (700, 1024, 3001)]
+
+
+@pytest.mark.parametrize("T,d,V", SHAPES)
+@pytest.mark.parametrize("temperature", [1.0, 0.7])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_shapes(T, d, V, temperature, dtype):
+    h, W, tokens, gl = _draw(T, d, V, dtype, T + d)
+    _check(h, W, tokens, gl, temperature, _run(h, W, tokens, gl, temperature=temperature), f"{T} {d} {V}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kept", [[], [0], [299], [5, 130, 299], list(range(0, 300, 2)), list(range(200, 300))])
+def test_ignored_tokens(kept, dtype):
+    """From every token ignored to half of them in turn; the others' values do not matter."""
+    h, W, tokens, gl = _draw(300, 96, 700, dtype, 3, ignore=0.0)
+    ignored = torch.ones(300, dtype=torch.bool, device=DEV)
+    ignored[kept] = False
+    tokens[ignored] = -100
+    got = _run(h, W, tokens, gl)
+    _check(h, W, tokens, gl, 1.0, got, f"{len(kept)} kept")
+    for g in (got[0], got[1], got[2]):
+        assert not g[ignored].any()
+
+
+def test_tokens_out_of_range_are_ignored_and_flagged():
+    h, W, tokens, gl = _draw(200, 64, 500, torch.bfloat16, 4)
+    tokens[3], tokens[7] = 500, -1
+    got = _run(h, W, tokens, gl)
+    _check(h, W, tokens, gl, 1.0, got, "out of range")
+    p = D.make_problem([h], [W], tokens)
+    buf = D.Buffers(p, h.device)
+    logp = torch.empty(200, device=DEV)
+
+    def flags():
+        B.token_logp_fwd(p, buf.stats.data_ptr(), logp.data_ptr(), None, buf.workspace.data_ptr(),
+                         buf.workspace.numel(), D._stream(h.device))
+        return B.device_error(p, buf.stats.data_ptr(), D._stream(h.device))
+    assert flags() == B.MLS_DEVFLAG_LABEL_RANGE
+    tokens[3] = tokens[7] = 1
+    assert flags() == 0
+    h[11] = float("nan")
+    tokens[11] = 5
+    assert flags() == B.MLS_DEVFLAG_NONFINITE and torch.isnan(logp[11])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_vocabulary_chunks(dtype):
+    """One chunk, and chunks that the vocabulary does not fill: the same gradients."""
+    h, W, tokens, gl = _draw(200, 128, 3000, dtype, 5)
+    for chunk in (256, 1024, 1 << 20):
+        _check(h, W, tokens, gl, 0.9, _run(h, W, tokens, gl, temperature=0.9, vocab_chunk=chunk), f"chunk {chunk}")
+
+
+def test_wide_logits():
+    """Logits from -200 to 200: log-probabilities far below what exp represents."""
+    h, W, tokens, gl = _draw(64, 64, 1000, torch.float32, 6, ignore=0.0)
+    W = W * 30
+    logp, entropy, gh, gW = _run(h, W, tokens, gl)
+    lp, en = P.token_logp(_np(h), _np(W), tokens.cpu().numpy())
+    assert lp.min() < -100
+    np.testing.assert_allclose(_np(logp), lp, rtol=1e-6, atol=1e-4)
+    np.testing.assert_allclose(_np(entropy), en, atol=1e-4)
+    assert torch.isfinite(gh).all() and torch.isfinite(gW).all()
+
+
+def test_one_gradient_alone_and_no_gradient():
+    h, W, tokens, gl = _draw(150, 64, 900, torch.bfloat16, 7)
+    logp, entropy, gh, gW = _run(h, W, tokens, gl)
+    h1 = h.detach().requires_grad_(True)
+    assert torch.equal(torch.autograd.grad(D.token_logp(h1, W, tokens)[0], h1, gl)[0], gh)
+    W1 = W.detach().requires_grad_(True)
+    assert torch.equal(torch.autograd.grad(D.token_logp(h, W1, tokens)[0], W1, gl)[0], gW)
+    with torch.no_grad():
+        lp, en = D.token_logp(h1, W1, tokens)
+    assert not lp.requires_grad and torch.equal(lp, logp) and torch.equal(en, entropy)
+
+
+def test_a_head_used_twice_collects_both_gradients():
+    h, W, tokens, gl = _draw(150, 64, 900, torch.float32, 8)
+    h2 = torch.roll(h, 3, 0)
+    W1 = W.detach().requires_grad_(True)
+    a, b = D.token_logp(h, W1, tokens)[0], D.token_logp(h2, W1, tokens)[0]
+    (a @ gl + b @ gl).backward()
+    ref = P.token_logp_backward(_np(h), _np(W), tokens.cpu().numpy(), _np(gl))[1] + \
+        P.token_logp_backward(_np(h2), _np(W), tokens.cpu().numpy(), _np(gl))[1]
+    assert_grad_rows(_np(W1.grad), ref, "shared head")
+
+
+def test_gradient_against_differences():
+    """Along random directions, in float32: (f(h + e v) - f(h - e v)) / 2e is v . grad.
+    A difference of sums of about 40 fp32 log-probabilities of size 8 is off by at most
+    40 * 8 * 2^-20 / 2e, the third derivative costs e^2."""
+    h, W, tokens, gl = _draw(40, 64, 300, torch.float32, 9)
+    _, _, gh, gW = _run(h, W, tokens, gl, temperature=0.8)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    f = lambda a, b: float((D.token_logp(a, b, tokens, temperature=0.8)[0].double() * gl.double()).sum())  # noqa: E731
+    for x, grad, at in ((h, gh, lambda v: f(v, W)), (W, gW, lambda v: f(h, v))):
+        v = torch.randn(x.shape, generator=g, device=DEV)
+        v /= v.norm()
+        e = 0.05
+        num = (at(x + e * v) - at(x - e * v)) / (2 * e)
+        assert abs(num - float((grad.double() * v.double()).sum())) <= 40 * 8 * 2.0 ** -20 / (2 * e) + 10 * e * e
+
+
+def test_refusals():
+    h, W, tokens, _ = _draw(10, 64, 50, torch.bfloat16, 10)
+    for bad in (dict(h=h.float()), dict(h=h[:, :32]), dict(h=h.t()), dict(W=W[:, ::2]), dict(tokens=tokens.int()),
+                dict(tokens=tokens[:5]), dict(h=h[0])):
+        with pytest.raises((ValueError, RuntimeError)):
+            D.token_logp(**{"h": h, "W": W, "tokens": tokens, **bad})
+    for t in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(B.MlsError):
+            D.token_logp(h, W, tokens, temperature=t)
