@@ -358,19 +358,42 @@ def layer_norm_backward(x: torch.Tensor, weight: torch.Tensor, stats: torch.Tens
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, stats = layer_norm_forward(x, weight, bias, eps=eps, want_stats=True)
+        rows, key = _norm_desc(x, weight, bias, eps)
+        dev = x.device
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        stats = torch.empty(2, key[0], dtype=torch.float32, device=dev)
+        n = _make_layer_norm(*key)
+        with _on(dev):
+            B.layer_norm_fwd(n, rows.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None,
+                             y.data_ptr(), stats.data_ptr(), _stream(dev))
         ctx.save_for_backward(x, weight, stats)
-        ctx.eps = eps
+        ctx.n, ctx.ws_bytes = n, _layer_norm_workspace(*key)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g_y):
+        # The engine calls this on a thread of its own, where every step costs about
+        # twice what it does on the caller's: what the forward has checked is not
+        # checked again. Only the layout of x may be another, behind saved-tensor hooks.
         x, weight, stats = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        g = layer_norm_backward(x, weight, stats, g_y.contiguous(), eps=ctx.eps, want_x=need[0],
-                                want_weight=need[1], want_bias=need[2])
-        return (*g, None)
+        g_y = g_y.contiguous()
+        dev, n = g_y.device, ctx.n
+        if x.dim() != 2 or x.stride() != (n.ld_x, 1):
+            x, ld = _norm_rows(x)
+            if ld != n.ld_x:
+                n = B.make_layer_norm(n.T, n.d, ld, n.act_dtype, n.param_dtype, n.eps)
+        need_x, need_w, need_b, _ = ctx.needs_input_grad
+        g_x = torch.empty_like(g_y) if need_x else None
+        g_w = torch.empty_like(weight) if need_w else None
+        g_b = torch.empty_like(weight) if need_b else None
+        ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=dev) if need_w or need_b else None
+        with _on(dev):
+            B.layer_norm_bwd(n, x.data_ptr(), weight.data_ptr(), stats.data_ptr(), g_y.data_ptr(),
+                             g_x.data_ptr() if need_x else None, g_w.data_ptr() if need_w else None,
+                             g_b.data_ptr() if need_b else None, ws.data_ptr() if ws is not None else None,
+                             ctx.ws_bytes, _stream(dev))
+        return g_x, g_w, g_b, None
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
@@ -387,33 +410,6 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     return layer_norm_forward(x, weight, bias, eps=eps)
 
 
-class _TokenLogp(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, tokens, opts, h, W):
-        logp, entropy, p, stats, ws = _token_logp_forward(h, W, tokens, opts)
-        ctx.p, ctx.stats, ctx.ws = p, stats, ws
-        ctx.save_for_backward(tokens, h, W)
-        ctx.mark_non_differentiable(entropy)
-        return logp, entropy
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, g_logp, g_entropy):
-        # the saved tensors' addresses are taken anew, as in the loss's backward
-        tokens, h, W = (x.contiguous() for x in ctx.saved_tensors)
-        p = B.Problem.from_buffer_copy(ctx.p)
-        p.labels, p.h[0], p.W[0] = tokens.data_ptr(), h.data_ptr(), W.data_ptr()
-        g_logp = g_logp.to(torch.float32).contiguous()
-        need = ctx.needs_input_grad[2:]
-        gh = torch.empty_like(h) if need[0] else None
-        gW = torch.empty_like(W) if need[1] else None
-        with _on(h.device):
-            B.token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need[0] else None,
-                             gW.data_ptr() if need[1] else None, ctx.ws.data_ptr(), ctx.ws.numel(),
-                             _stream(h.device))
-        return None, None, gh, gW
-
-
 def _token_logp_forward(h, W, tokens, opts):
     dev = h.device
     p = make_problem([h], [W], tokens, grad_h_dtype=h.dtype,
@@ -427,6 +423,37 @@ def _token_logp_forward(h, W, tokens, opts):
         B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(), ws.data_ptr(), ws.numel(),
                          _stream(dev))
     return logp, entropy, p, stats, ws
+
+
+class _TokenLogp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, opts, h, W):
+        logp, entropy, ctx.p, ctx.stats, ctx.ws = _token_logp_forward(h, W, tokens, opts)
+        ctx.save_for_backward(tokens, h, W)
+        ctx.mark_non_differentiable(entropy)
+        ctx.set_materialize_grads(False)  # no zeros for the entropy
+        return logp, entropy
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g_logp, g_entropy):
+        if g_logp is None:
+            return None, None, None, None
+        # the saved tensors' addresses are taken anew, as in the loss's backward
+        tokens, h, W = (x.contiguous() for x in ctx.saved_tensors)
+        g_logp = g_logp.contiguous()
+        p = ctx.p
+        if (p.labels, p.h[0], p.W[0]) != (tokens.data_ptr(), h.data_ptr(), W.data_ptr()):
+            p = B.Problem.from_buffer_copy(p)
+            p.labels, p.h[0], p.W[0] = tokens.data_ptr(), h.data_ptr(), W.data_ptr()
+        _, _, need_h, need_W = ctx.needs_input_grad
+        gh = torch.empty_like(h) if need_h else None
+        gW = torch.empty_like(W) if need_W else None
+        with _on(h.device):
+            B.token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need_h else None,
+                             gW.data_ptr() if need_W else None, ctx.ws.data_ptr(), ctx.ws.numel(),
+                             _stream(h.device))
+        return None, None, gh, gW
 
 
 def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temperature: float = 1.0,
@@ -447,36 +474,43 @@ def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temper
 _POLICY_REDUCTIONS = {"token": 0, "sequence": B.MLS_POLICY_MEAN_OF_SEQUENCES}
 
 
+def _policy_forward(logp, args, want_grad):
+    old, adv, ref, mask, cu, desc = args
+    dev = logp.device
+    loss, kl, clipped = (torch.empty((), dtype=torch.float32, device=dev) for _ in range(3))
+    grad = torch.empty(desc.N + 1, dtype=torch.float32, device=dev) if want_grad else None
+    ws_bytes = B.policy_loss_workspace(desc)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        B.policy_loss_fwd(desc, logp.data_ptr(), old.data_ptr(), adv.data_ptr(),
+                          ref.data_ptr() if ref is not None else None,
+                          mask.data_ptr() if mask is not None else None,
+                          cu.data_ptr() if cu is not None else None, loss.data_ptr(), kl.data_ptr(),
+                          clipped.data_ptr(), grad.data_ptr() if want_grad else None, ws.data_ptr(), ws_bytes,
+                          _stream(dev))
+    return loss, kl, clipped, grad
+
+
 class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logp, args):
-        old, adv, ref, mask, cu, desc = args
-        dev = logp.device
-        N = logp.numel()
-        need = ctx.needs_input_grad[0]
-        loss, kl, clipped = (torch.empty((), dtype=torch.float32, device=dev) for _ in range(3))
-        grad = torch.empty(N + 1, dtype=torch.float32, device=dev) if need else None
-        ws_bytes = B.policy_loss_workspace(desc)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-        ptr = (lambda t: t.data_ptr() if t is not None else None)
-        with _on(dev):
-            B.policy_loss_fwd(desc, logp.data_ptr(), old.data_ptr(), adv.data_ptr(), ptr(ref), ptr(mask), ptr(cu),
-                              loss.data_ptr(), kl.data_ptr(), clipped.data_ptr(), ptr(grad), ws.data_ptr(),
-                              ws_bytes, _stream(dev))
-        if need:
-            ctx.save_for_backward(grad)
+        loss, kl, clipped, grad = _policy_forward(logp, args, True)
+        ctx.save_for_backward(grad)
         ctx.shape = logp.shape
         ctx.mark_non_differentiable(kl, clipped)
+        ctx.set_materialize_grads(False)  # no zeros for the other two
         return loss, kl, clipped
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g_loss, g_kl, g_clipped):
+        if g_loss is None:
+            return None, None
         grad, = ctx.saved_tensors
-        g_logp = torch.empty(ctx.shape, dtype=torch.float32, device=grad.device)
-        with _on(grad.device):
-            B.policy_loss_bwd(grad.numel() - 1, grad.data_ptr(), g_loss.contiguous().data_ptr(),
-                              g_logp.data_ptr(), _stream(grad.device))
+        dev = grad.device
+        g_logp = torch.empty(ctx.shape, dtype=torch.float32, device=dev)
+        with _on(dev):
+            B.policy_loss_bwd(g_logp.numel(), grad.data_ptr(), g_loss.data_ptr(), g_logp.data_ptr(), _stream(dev))
         return g_logp, None
 
 
@@ -504,9 +538,9 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Te
         raise RuntimeError("policy_loss runs on the GPU only; got tensors on " + str(logp.device))
     if reduction not in _POLICY_REDUCTIONS:
         raise ValueError(f"reduction must be one of {sorted(_POLICY_REDUCTIONS)}, got {reduction!r}")
-    dev, N = logp.device, logp.numel()
+    dev, shape, N = logp.device, logp.shape, logp.numel()
     for name, x in (("logp", logp), ("old_logp", old_logp), ("ref_logp", ref_logp)):
-        if x is not None and (x.dtype != torch.float32 or x.shape != logp.shape or x.device != dev or
+        if x is not None and (x.dtype != torch.float32 or x.shape != shape or x.device != dev or
                               not x.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 tensor of logp's shape and device")
     if mask is not None and (mask.dtype != torch.bool or mask.shape != logp.shape or mask.device != dev or
@@ -529,7 +563,10 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Te
         raise ValueError("advantages must be a contiguous float32 tensor of " +
                          ("[S]" if per_sequence else "logp's shape"))
     desc = B.make_policy(N, S, clip_low, clip_high, kl_coef, flags)
-    return _PolicyLoss.apply(logp, (old_logp, advantages, ref_logp, mask, cu_seqlens, desc))
+    args = (old_logp, advantages, ref_logp, mask, cu_seqlens, desc)
+    if torch.is_grad_enabled() and logp.requires_grad:
+        return _PolicyLoss.apply(logp, args)
+    return _policy_forward(logp, args, False)[:3]
 
 
 def _grad_list(grads, out):
