@@ -357,25 +357,30 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
  * as device float32 [T]. p->alpha and p->teacher do not matter. No [T, V] array is
- * kept. stats and workspace as mls_query_sizes gives them; stats receives the
- * rows' log-sum-exp (in the place of lset) for the backward and the device flags
- * (mls_device_error; a token outside [0, V) is treated as ignored and raises
+ * kept. Tokens with ignore_index cost no product: the others' hidden states are
+ * packed first, and those of ignored tokens are not used, whatever they hold.
+ * stats: mls_query_sizes' stats_bytes; it receives what the backward needs, the
+ * number of tokens that count and the device flags (mls_read_stats_header,
+ * mls_device_error): a token outside [0, V) is treated as ignored and raises
  * MLS_DEVFLAG_LABEL_RANGE, a log-probability that is NaN or infinite
- * MLS_DEVFLAG_NONFINITE); its valid-token count is 0. Asynchronous on stream.
+ * MLS_DEVFLAG_NONFINITE. workspace: fwd_bytes of mls_token_logp_workspace (contents
+ * are not kept between calls). Asynchronous on stream.
  */
+mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes);
 mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Backward for the gradient g_logp (device float32 [T]) of logp; the entropy is not
  * differentiated. With G[t] = g_logp[t] / tau (onehot(tokens[t]) - softmax(W h[t] / tau)),
- * 0 on ignored tokens (whose g_logp is not read):
- *   grad_h = G W  [T, d] of p->grad_h_dtype,
+ * 0 on ignored tokens (whose g_logp is not used):
+ *   grad_h = G W  [T, d] of p->grad_h_dtype (0 on ignored tokens),
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
  * Either may be NULL. The logits are recomputed one vocabulary chunk at a time and
  * G is rounded to bfloat16 (bf16 inputs) in between, as in mls_distill_bwd, whose
- * accumulation flags apply. stats: as mls_token_logp_fwd left it on the same
- * inputs. Asynchronous on stream.
+ * accumulation flags apply (an accumulated grad_h is added to in fp32). stats: as
+ * mls_token_logp_fwd left it on the same inputs. workspace: bwd_bytes of
+ * mls_token_logp_workspace. Asynchronous on stream.
  */
 mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp,
                               void* grad_h, void* grad_W, void* workspace, size_t workspace_bytes,

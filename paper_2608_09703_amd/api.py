@@ -414,21 +414,21 @@ def _token_logp_forward(h, W, tokens, opts):
     dev = h.device
     p = make_problem([h], [W], tokens, grad_h_dtype=h.dtype,
                      flags=B.MLS_GRAD_W_BF16 if h.dtype == torch.bfloat16 else 0, **opts)
-    ws_bytes, stats_bytes = B.query_sizes(p)
-    ws = torch.empty(max(ws_bytes, 256), dtype=torch.uint8, device=dev)
-    stats = torch.empty(stats_bytes, dtype=torch.uint8, device=dev)
+    ws_bytes, bwd_bytes = B.token_logp_workspace(p)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    stats = torch.empty(B.query_sizes(p)[1], dtype=torch.uint8, device=dev)
     logp = torch.empty(p.T, dtype=torch.float32, device=dev)
     entropy = torch.empty(p.T, dtype=torch.float32, device=dev)
     with _on(dev):
-        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(), ws.data_ptr(), ws.numel(),
+        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), entropy.data_ptr(), ws.data_ptr(), ws_bytes,
                          _stream(dev))
-    return logp, entropy, p, stats, ws
+    return logp, entropy, p, stats, bwd_bytes
 
 
 class _TokenLogp(torch.autograd.Function):
     @staticmethod
     def forward(ctx, tokens, opts, h, W):
-        logp, entropy, ctx.p, ctx.stats, ctx.ws = _token_logp_forward(h, W, tokens, opts)
+        logp, entropy, ctx.p, ctx.stats, ctx.ws_bytes = _token_logp_forward(h, W, tokens, opts)
         ctx.save_for_backward(tokens, h, W)
         ctx.mark_non_differentiable(entropy)
         ctx.set_materialize_grads(False)  # no zeros for the entropy
@@ -449,10 +449,10 @@ class _TokenLogp(torch.autograd.Function):
         _, _, need_h, need_W = ctx.needs_input_grad
         gh = torch.empty_like(h) if need_h else None
         gW = torch.empty_like(W) if need_W else None
+        ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=h.device)
         with _on(h.device):
             B.token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need_h else None,
-                             gW.data_ptr() if need_W else None, ctx.ws.data_ptr(), ctx.ws.numel(),
-                             _stream(h.device))
+                             gW.data_ptr() if need_W else None, ws.data_ptr(), ctx.ws_bytes, _stream(h.device))
         return None, None, gh, gW
 
 

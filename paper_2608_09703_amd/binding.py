@@ -59,6 +59,7 @@ EXPORTED = (
     "mls_layer_norm_fwd",
     "mls_layer_norm_workspace",
     "mls_layer_norm_bwd",
+    "mls_token_logp_workspace",
     "mls_token_logp_fwd",
     "mls_token_logp_bwd",
     "mls_policy_loss_workspace",
@@ -201,6 +202,7 @@ def lib():
         L.mls_layer_norm_fwd.argtypes = [N, vp, vp, vp, vp, vp, vp]
         L.mls_layer_norm_workspace.argtypes = [N, sz]
         L.mls_layer_norm_bwd.argtypes = [N, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_token_logp_workspace.argtypes = [P, sz, sz]
         L.mls_token_logp_fwd.argtypes = [P, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.mls_token_logp_bwd.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         Q = ctypes.POINTER(Policy)
@@ -361,6 +363,14 @@ def layer_norm_bwd(n: LayerNorm, x: int, weight: int, stats: int, g_y: int, g_x:
                    g_weight: Optional[int], g_bias: Optional[int], ws: Optional[int], ws_bytes: int, stream: int):
     check(lib().mls_layer_norm_bwd(ctypes.byref(n), x, weight, stats, g_y, g_x, g_weight, g_bias, ws, ws_bytes,
                                    stream), "mls_layer_norm_bwd")
+
+
+def token_logp_workspace(p: Problem):
+    """``(forward, backward)`` workspace bytes."""
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    check(lib().mls_token_logp_workspace(ctypes.byref(p), ctypes.byref(f), ctypes.byref(b)),
+          "mls_token_logp_workspace")
+    return f.value, b.value
 
 
 def token_logp_fwd(p: Problem, stats: int, logp: int, entropy: Optional[int], ws: int, ws_bytes: int,

@@ -528,14 +528,12 @@ hipError_t sum_parts(const mls_problem* p, int splits, int64_t rows, const float
 
 // Label logits of every token and, when `count` is set, the valid-token count
 // into the statistics header (which the logit-gradient pass reads before the
-// loss mean is taken). With logp the header is cleared, for token
-// log-probabilities' row merge.
+// loss mean is taken).
 hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void* stats, bool count,
-                         hipStream_t s, float* logp = nullptr) {
+                         hipStream_t s) {
   RowArgs r;
   fill_rows(p, pl, r);
   r.lab = lab;
-  r.logp_row = logp;
   r.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
   hipError_t e;
   {
@@ -547,12 +545,11 @@ hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void*
   return launch_count_valid(r, s);
 }
 
-// Forward of tokens [t0, t0 + tc): the tile kernel (partial records, and with
-// lslab the fp16 logits) and the row merge into the statistics, or with logp into
-// token log-probabilities (and entropies).
-hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc,
-                         float4* partials, const float* lab, uint16_t* lslab, void* stats,
-                         hipStream_t s, float* logp = nullptr, float* entropy = nullptr) {
+// Tile kernel of the forward of tokens [t0, t0 + tc): partial records, and with
+// lslab the fp16 logits. n_rows: of token log-probabilities' rows, as many of these
+// as the device counts.
+hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc, float4* partials,
+                         uint16_t* lslab, const int32_t* n_rows, hipStream_t s) {
   FusedArgs a;
   fill_common(p, pl, a);
   for (int i = 0; i < pl.M; ++i)
@@ -570,11 +567,18 @@ hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64
   a.partials = partials;
   a.lslab = lslab;
   a.ld_lslab = pl.fb_ld;
-  hipError_t e;
-  {
-    ProfScope ps("fused_fwd", s);
-    e = launch_fused_fwd(a, pl.f32, s);
-  }
+  a.n_rows = n_rows;
+  a.row0 = t0;
+  ProfScope ps("fused_fwd", s);
+  return launch_fused_fwd(a, pl.f32, s);
+}
+
+// Forward of tokens [t0, t0 + tc): the tile kernel and the row merge into the
+// statistics.
+hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc,
+                         float4* partials, const float* lab, uint16_t* lslab, void* stats,
+                         hipStream_t s) {
+  hipError_t e = forward_tiles(p, pl, t0, tc, partials, lslab, nullptr, s);
   if (e != hipSuccess) return e;
   RowArgs r;
   fill_rows(p, pl, r);
@@ -584,12 +588,6 @@ hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64
   r.lab = const_cast<float*>(lab);
   r.stats = static_cast<float*>(stats);
   ProfScope ps("row_merge", s);
-  if (logp) {
-    r.logp_row = logp;
-    r.entropy_row = entropy;
-    r.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
-    return launch_finalize_logp(r, s);
-  }
   return launch_finalize_rows(r, s);
 }
 
@@ -608,7 +606,8 @@ hipError_t finish_losses(const mls_problem* p, const Plan& pl, void* stats, floa
 }
 
 // Launches of the backward: of the losses (g_ce, g_kl) or, with g_row, of token
-// log-probabilities.
+// log-probabilities, whose problem p holds the packed rows and whose number of rows
+// the header has.
 mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats, const float* g_ce,
                         const float* g_kl, const float* g_row, void* const* grad_h, float* const* grad_W,
                         void* workspace, size_t workspace_bytes, void* stream) {
@@ -631,6 +630,7 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   a.g_ce = g_ce;
   a.g_kl = g_kl;
   a.g_row = g_row;
+  a.n_rows = g_row ? a.n_valid : nullptr;
   host_coeffs(pl.M, pl.s, p->alpha, p->tau, MLS_MODE_PAPER, nullptr, a.host_gce, a.host_gkl);
   a.slab = ws + pl.off_slab;
   const bool stored = pl.wide_bwd || pl.f32;  // products on the stored layouts
@@ -724,6 +724,7 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
     // the transposed operands.
     GemmArgs ga;
     memset(&ga, 0, sizeof(ga));
+    ga.n_rows = a.n_rows;
     int tiles = 0;
     for (int i = 0; i < pl.M; ++i) {
       if (!grad_h[i]) continue;
@@ -839,6 +840,63 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
     if (e != hipSuccess) return hip_fail(e, "grad_h sum launch");
   }
   return MLS_OK;
+}
+
+mls_status validate_tokens(const mls_problem* p) {
+  mls_status st = validate(p);
+  if (st != MLS_OK) return st;
+  if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
+  return MLS_OK;
+}
+
+// Workspaces of token log-probabilities: the packed rows, then what the tile kernels
+// and products need.
+struct TokenPlan {
+  Plan pl;         // of the packed rows
+  mls_problem q;   // p with the rows' grad_h (the scatter adds to an output)
+  size_t off_hc = 0, off_tokens = 0, off_lab = 0, off_part = 0, off_gh = 0, off_work = 0;
+  size_t fwd_bytes = 0, bwd_bytes = 0, bwd_room = 0;  // room: see Plan
+};
+
+void token_plan(const mls_problem* p, TokenPlan& tp) {
+  tp.q = *p;
+  // what is added to an output is added in fp32
+  if (p->flags & MLS_ACCUMULATE_GRAD_H) tp.q.grad_h_dtype = MLS_F32;
+  tp.q.flags &= ~(uint32_t)MLS_ACCUMULATE_GRAD_H;
+  make_plan(&tp.q, tp.pl);
+  const Plan& pl = tp.pl;
+  size_t off = align256((size_t)pl.T_pad * p->d[0] * pl.es);
+  tp.off_tokens = off;
+  off = align256(off + (size_t)pl.T * sizeof(int64_t));
+  tp.off_lab = off;  // forward: own logits; backward: gradients
+  off = align256(off + (size_t)pl.T * sizeof(float));
+  tp.off_part = tp.off_gh = off;
+  tp.fwd_bytes = off + pl.off_lab;  // the forward's partial records
+  off = align256(off + (size_t)pl.T * p->d[0] * (tp.q.grad_h_dtype == MLS_F32 ? 4 : 2));
+  tp.off_work = off;
+  tp.bwd_bytes = off + pl.bwd_bytes;
+  tp.bwd_room = off + pl.bwd_room;
+}
+
+TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
+  TokenArgs a;
+  memset(&a, 0, sizeof(a));
+  a.T = pl.T;
+  a.T_pad = pl.T_pad;
+  a.V = pl.V;
+  a.d = p->d[0];
+  a.h = p->h[0];
+  a.W = p->W[0];
+  a.tokens = p->labels;
+  a.ignore_index = p->ignore_index;
+  a.tau = p->tau;
+  // the statistics' rows of the losses (mls_query_sizes), taken over
+  float* sf = static_cast<float*>(stats);
+  a.rank = reinterpret_cast<int32_t*>(sf);           // lse1
+  a.lse = sf + pl.T;                                 // lset
+  a.index = reinterpret_cast<int32_t*>(sf + 2 * pl.T);  // ce_row
+  a.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
+  return a;
 }
 
 }  // namespace
@@ -1256,30 +1314,62 @@ mls_status mls_diagnostics(const mls_problem* p, float* kl_pair, float* agree, i
   return MLS_OK;
 }
 
+mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes) {
+  g_last_error.clear();
+  mls_status st = validate_tokens(p);
+  if (st != MLS_OK) return st;
+  TokenPlan tp;
+  token_plan(p, tp);
+  if (fwd_bytes) *fwd_bytes = tp.fwd_bytes;
+  if (bwd_bytes) *bwd_bytes = tp.bwd_room;
+  return MLS_OK;
+}
+
 mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
                               void* workspace, size_t workspace_bytes, void* stream) {
   g_last_error.clear();
-  mls_status st = validate(p);
+  mls_status st = validate_tokens(p);
   if (st != MLS_OK) return st;
-  if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
   if (!stats || !logp || !workspace) return fail(MLS_INVALID_ARG, "stats, logp and workspace must be non-NULL");
   if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(logp, 4) || !aligned(entropy, 4))
     return fail(MLS_INVALID_ARG, "misaligned stats / workspace / output pointer");
-  Plan pl;
-  make_plan(p, pl);
-  if (workspace_bytes < pl.fwd_bytes)
-    return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", pl.fwd_bytes,
+  TokenPlan tp;
+  token_plan(p, tp);
+  const Plan& pl = tp.pl;
+  if (workspace_bytes < tp.fwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", tp.fwd_bytes,
                 workspace_bytes);
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  float* lab = reinterpret_cast<float*>(ws + pl.off_lab);
-  hipError_t e = launch_labels(p, pl, lab, stats, false, s, logp);
-  if (e != hipSuccess) return hip_fail(e, "label logits launch");
+  TokenArgs a = token_args(p, pl, stats);
+  a.logp = logp;
+  a.entropy = entropy;
+  a.hc = ws + tp.off_hc;
+  a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
+  a.lab = reinterpret_cast<float*>(ws + tp.off_lab);
+  a.n_rec = pl.n_vt_fwd * kFusedFwdParts;
+  a.partials = reinterpret_cast<const float4*>(ws + tp.off_part);
+  hipError_t e;
+  {
+    ProfScope ps("token_pack", s);
+    e = launch_token_pack(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "token list launch");
+  {
+    ProfScope ps("token_gather", s);
+    e = launch_token_gather(a, pl.f32, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "token rows launch");
+  tp.q.h[0] = a.hc;
+  tp.q.labels = a.tokens_c;
   for (int c = 0; c < pl.fwd_nc; ++c) {
-    const int64_t t0 = (int64_t)c * pl.fwd_tc;
-    e = forward_chunk(p, pl, t0, std::min(pl.fwd_tc, pl.T - t0),
-                      reinterpret_cast<float4*>(ws + pl.off_partials), lab, nullptr, stats, s, logp, entropy);
+    a.t0 = (int64_t)c * pl.fwd_tc;
+    a.Tc = std::min(pl.fwd_tc, pl.T - a.t0);
+    e = forward_tiles(&tp.q, pl, a.t0, a.Tc, const_cast<float4*>(a.partials), nullptr, a.header, s);
     if (e != hipSuccess) return hip_fail(e, "forward launch");
+    ProfScope ps("token_merge", s);
+    e = launch_token_merge(a, s);
+    if (e != hipSuccess) return hip_fail(e, "row merge launch");
   }
   return MLS_OK;
 }
@@ -1287,22 +1377,52 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
 mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp, void* grad_h,
                               void* grad_W, void* workspace, size_t workspace_bytes, void* stream) {
   g_last_error.clear();
-  mls_status st = validate(p);
+  mls_status st = validate_tokens(p);
   if (st != MLS_OK) return st;
-  if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
   if (!stats || !g_logp || !workspace)
     return fail(MLS_INVALID_ARG, "stats, g_logp and workspace must be non-NULL");
   if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(g_logp, 4) ||
-      !aligned(grad_h, p->grad_h_dtype == MLS_BF16 ? 2 : 4) || !aligned(grad_W, (p->flags & MLS_GRAD_W_BF16) ? 2 : 4))
+      !aligned(grad_h, p->grad_h_dtype == MLS_BF16 ? 8 : 16) ||
+      !aligned(grad_W, (p->flags & MLS_GRAD_W_BF16) ? 2 : 4))
     return fail(MLS_INVALID_ARG, "misaligned stats / workspace / gradient pointer");
-  Plan pl;
-  make_plan(p, pl);
-  if (workspace_bytes < pl.bwd_bytes)
-    return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", pl.bwd_bytes,
+  TokenPlan tp;
+  token_plan(p, tp);
+  const Plan& pl = tp.pl;
+  if (workspace_bytes < tp.bwd_bytes)
+    return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", tp.bwd_bytes,
                 workspace_bytes);
-  void* const gh[1] = {grad_h};
+  if (!grad_h && !grad_W) return MLS_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  TokenArgs a = token_args(p, pl, const_cast<void*>(stats));
+  a.hc = ws + tp.off_hc;
+  a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
+  a.g = g_logp;
+  a.g_c = reinterpret_cast<float*>(ws + tp.off_lab);
+  hipError_t e;
+  {
+    ProfScope ps("token_gather", s);
+    e = launch_token_gather(a, pl.f32, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "token rows launch");
+  tp.q.h[0] = a.hc;
+  tp.q.labels = a.tokens_c;
+  void* const gh[1] = {grad_h ? ws + tp.off_gh : nullptr};
   float* const gW[1] = {static_cast<float*>(grad_W)};
-  return run_backward(p, pl, stats, nullptr, nullptr, g_logp, gh, gW, workspace, workspace_bytes, stream);
+  st = run_backward(&tp.q, pl, stats, nullptr, nullptr, a.g_c, gh, gW, ws + tp.off_work,
+                    workspace_bytes - tp.off_work, stream);
+  if (st != MLS_OK || !grad_h) return st;
+  a.gh_c = gh[0];
+  a.gh_f32 = tp.q.grad_h_dtype == MLS_F32 ? 1 : 0;
+  a.out_f32 = p->grad_h_dtype == MLS_F32 ? 1 : 0;
+  a.accumulate = (p->flags & MLS_ACCUMULATE_GRAD_H) ? 1 : 0;
+  a.grad_h = grad_h;
+  {
+    ProfScope ps("token_scatter", s);
+    e = launch_token_scatter(a, s);
+  }
+  if (e != hipSuccess) return hip_fail(e, "token gradient launch");
+  return MLS_OK;
 }
 
 }  // extern "C"

@@ -72,6 +72,12 @@ struct TeacherTile<FM, FN, true> {
   }
 };
 
+// Rows of a launch over the tokens that count (see FusedArgs::n_rows).
+__device__ __forceinline__ int64_t live_rows(const FusedArgs& a) {
+  const int64_t n = *a.n_rows - a.row0;
+  return n < 0 ? 0 : n < a.T ? n : a.T;
+}
+
 // Forward tile kernel: for each sub-model (the teacher first) the logit tile
 // of BM vocabulary rows x BN tokens, reduced in registers to one partial record
 // (max, sum exp, sum exp at tau, teacher-weighted logit sum) per token and wave
@@ -81,7 +87,9 @@ struct TeacherTile<FM, FN, true> {
 // fp16 of its distance to the record's maximum (at most 0; 2^-11 relative, so
 // the entries that carry the softmax's mass, near the maximum, are the most
 // exact), token-major, for the logit gradient pass.
-template <class Mma, typename E, bool TAU1, int MINB = 1, bool STORE = false>
+// ROWS (token log-probabilities): the number of rows is read from the device;
+// with one temperature, TAU1's single sum at a.tau.
+template <class Mma, typename E, bool TAU1, int MINB = 1, bool STORE = false, bool ROWS = false>
 __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
   constexpr int BN = Mma::kBN;
@@ -98,16 +106,20 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   const int wm = wave % WGM;
   const int wn = wave / WGM;
   const int hi = lane >> 5;
-  const int bl = xcd_remap(blockIdx.x, gridDim.x);
+  const int64_t T = ROWS ? live_rows(a) : a.T;
+  const int n_tt = ROWS ? (int)((T + BN - 1) / BN) : a.n_tt;
+  const int nb = ROWS ? a.n_vt * n_tt : gridDim.x;
+  if (ROWS && (int)blockIdx.x >= nb) return;
+  const int bl = xcd_remap(blockIdx.x, nb);
   int vt, tt;
-  tile_coords(bl, a.n_vt, a.n_tt, a.group_v, vt, tt);
+  tile_coords(bl, a.n_vt, n_tt, a.group_v, vt, tt);
   const int64_t vbase = (int64_t)vt * BM;
   const int64_t tbase = (int64_t)tt * BN;
   const bool full = vbase + BM <= a.V;
   const float ct = kLog2e * a.inv_tau;
   // records of sub-model order[oi] and token group tbase / kFusedBN: [n_vt * WGM][kFusedBN]
   const int64_t n_rec = (int64_t)a.n_vt * WGM;
-  const int64_t n_tg = (a.T + kFusedBN - 1) / kFusedBN;
+  const int64_t n_tg = (T + kFusedBN - 1) / kFusedBN;
   const int64_t rec = (int64_t)vt * WGM + wm;
 
   // teacher weights exp((l_s - max_s) / tau); 0 outside V
@@ -118,7 +130,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
     const int i = a.order[oi];
     const int64_t kb = a.d[i] * E::kBytes;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
-            kb, tbase, a.T, kb, smem, tid);
+            kb, tbase, T, kb, smem, tid);
 
 #pragma unroll
     for (int fn = 0; fn < FN; ++fn) {
@@ -238,7 +250,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
 
       // 3. the wave's partial record of this token
       const int c = Mma::col_of(wn, fn, lane);
-      if (hi == 0 && tbase + c < a.T)
+      if (hi == 0 && tbase + c < T)
         a.partials[((oi * n_tg + tbase / kFusedBN) * n_rec + rec) * kFusedBN + tbase % kFusedBN + c] =
             make_float4(mb, s1, st, xr);
     }
@@ -263,9 +275,9 @@ __device__ __forceinline__ void store4<F32>(float* p, float a0, float a1, float 
 
 // Backward tile kernel of the fp32 path (one slab, token-major) and of the
 // general bf16 path (both slab layouts).
-// ROWG (one sub-model): the gradient of the tokens' log-probabilities at
+// ROWG (one sub-model): the gradient of the rows' log-probabilities at
 // temperature tau, G = g_row / tau (onehot - softmax(l / tau)), in place of the
-// losses'.
+// losses', over the rows that the device counts.
 template <class Mma, typename E, bool TAU1, bool ROWG = false>
 __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
@@ -281,9 +293,15 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   const int wave = tid >> 6;
   const int wm = wave % WGM;
   const int wn = wave / WGM;
-  const int bl = xcd_remap(blockIdx.x, gridDim.x);
+  const int64_t T = ROWG ? live_rows(a) : a.T;
+  // (the general bf16 products read every row of the slab: zeros behind the last)
+  constexpr bool kSkip = ROWG && E::kBytes == 4;
+  const int n_tt = kSkip ? (int)((T + BN - 1) / BN) : a.n_tt;
+  const int nb = kSkip ? a.n_vt * n_tt : gridDim.x;
+  if (kSkip && (int)blockIdx.x >= nb) return;
+  const int bl = xcd_remap(blockIdx.x, nb);
   int vt, tt;
-  tile_coords(bl, a.n_vt, a.n_tt, a.group_v, vt, tt);
+  tile_coords(bl, a.n_vt, n_tt, a.group_v, vt, tt);
   const int64_t vloc = (int64_t)vt * BM;  // row offset inside the chunk
   const int64_t vbase = a.v0 + vloc;      // absolute vocabulary row
   const int64_t tbase = (int64_t)tt * BN;
@@ -298,8 +316,8 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   for (int fn = 0; fn < FN; ++fn) {
     const int64_t t = tbase + Mma::col_of(wn, fn, lane);
     tok[fn] = t;
-    const int64_t y = t < a.T ? a.labels[t] : a.ignore_index;
-    rv[fn] = t < a.T && y != a.ignore_index && y >= 0 && y < a.V;
+    const int64_t y = t < T ? a.labels[t] : a.ignore_index;
+    rv[fn] = t < T && y != a.ignore_index && y >= 0 && y < a.V;
     const int64_t rel = y - vbase;
     ylab[fn] = (rv[fn] && rel >= 0 && rel < BM) ? (int)rel : -1;
   }
@@ -312,7 +330,7 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
     const int i = a.order[oi];
     const int64_t kb = a.d[i] * E::kBytes;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
-            kb, tbase, a.T, kb, smem, tid);
+            kb, tbase, T, kb, smem, tid);
     const float gce = ROWG ? 0.f : a.g_ce ? a.g_ce[i] : a.host_gce[i];
     const float gkl = ROWG ? 0.f : a.g_kl ? a.g_kl[i] : a.host_gkl[i];
     S* slab = static_cast<S*>(a.slab) + (int64_t)i * a.T_pad * a.Vc;
@@ -393,9 +411,13 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
   const int wave = tid >> 6;
   const int wm = wave % WGM;
   const int wn = wave / WGM;
-  const int bl = xcd_remap(blockIdx.x, gridDim.x);
+  const int64_t T = ROWG ? live_rows(a) : a.T;
+  const int n_tt = ROWG ? (int)((T + BN - 1) / BN) : a.n_tt;
+  const int nb = ROWG ? a.n_vt * n_tt : gridDim.x;
+  if (ROWG && (int)blockIdx.x >= nb) return;
+  const int bl = xcd_remap(blockIdx.x, nb);
   int vt, tt;
-  tile_coords(bl, a.n_vt, a.n_tt, a.group_v, vt, tt);
+  tile_coords(bl, a.n_vt, n_tt, a.group_v, vt, tt);
   const int64_t vloc = (int64_t)vt * BM;
   const int64_t vbase = a.v0 + vloc;
   const int64_t tbase = (int64_t)tt * BN;
@@ -411,8 +433,8 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
   for (int fn = 0; fn < FN; ++fn) {
     tcol[fn] = Mma::col_of(wn, fn, lane);
     const int64_t t = tbase + tcol[fn];
-    const int64_t y = t < a.T ? a.labels[t] : a.ignore_index;
-    rv[fn] = t < a.T && y != a.ignore_index && y >= 0 && y < a.V;
+    const int64_t y = t < T ? a.labels[t] : a.ignore_index;
+    rv[fn] = t < T && y != a.ignore_index && y >= 0 && y < a.V;
     const int64_t rel = y - vbase;
     ylab[fn] = (rv[fn] && rel >= 0 && rel < BM) ? (int)rel : -1;
   }
@@ -424,7 +446,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
     const int i = a.order[oi];
     const int64_t kb = a.d[i] * 2;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
-            kb, tbase, a.T, kb, smem, tid);
+            kb, tbase, T, kb, smem, tid);
     const float gce = ROWG ? 0.f : a.g_ce ? a.g_ce[i] : a.host_gce[i];
     const float gkl = ROWG ? 0.f : a.g_kl ? a.g_kl[i] : a.host_gkl[i];
 
@@ -493,17 +515,24 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
   }
 }
 
-template <class Mma, typename E, bool TAU1>
+template <class Mma, typename E>
 hipError_t launch_fwd_t(const FusedArgs& a, hipStream_t stream) {
   dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt);
-  hipLaunchKernelGGL((fused_fwd_kernel<Mma, E, TAU1>), grid, dim3(Mma::NT), 0, stream, a);
+  if (a.n_rows)
+    hipLaunchKernelGGL((fused_fwd_kernel<Mma, E, true, 1, false, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else if (a.tau == 1.0f)
+    hipLaunchKernelGGL((fused_fwd_kernel<Mma, E, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else
+    hipLaunchKernelGGL((fused_fwd_kernel<Mma, E, false>), grid, dim3(Mma::NT), 0, stream, a);
   return hipGetLastError();
 }
 
 template <class Mma, bool STORE>
 hipError_t launch_fwd_wide(const FusedArgs& a, hipStream_t stream) {
   dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt);
-  if (a.tau == 1.0f)
+  if (!STORE && a.n_rows)
+    hipLaunchKernelGGL((fused_fwd_kernel<Mma, Bf16, true, 2, false, true>), grid, dim3(Mma::NT), 0, stream, a);
+  else if (a.tau == 1.0f)
     hipLaunchKernelGGL((fused_fwd_kernel<Mma, Bf16, true, 2, STORE>), grid, dim3(Mma::NT), 0, stream,
                        a);
   else
@@ -543,10 +572,8 @@ int fused_tile_rows(bool f32) { return f32 ? kFusedF32 : kFusedBM; }
 int fused_tile_cols(bool f32) { return f32 ? kFusedF32 : kFusedBN; }
 
 hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
-  const bool tau1 = a.tau == 1.0f;
-  if (f32)
-    return tau1 ? launch_fwd_t<MmaF32, F32, true>(a, stream)
-                : launch_fwd_t<MmaF32, F32, false>(a, stream);
+  if (a.n_rows && (a.M != 1 || a.lslab)) return hipErrorInvalidValue;
+  if (f32) return launch_fwd_t<MmaF32, F32>(a, stream);
   // bf16: the wide core for every width. K tails (widths that are not multiples
   // of 64) have their own form, so that the loads of the others carry no masks:
   // at T = 1,531, widths 200 / 408 / 1,000, V = 32,003, tau = 2 the forward
@@ -560,7 +587,7 @@ hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
 }
 
 hipError_t launch_fused_bwd(const FusedArgs& a, bool f32, hipStream_t stream) {
-  if (a.g_row && a.M != 1) return hipErrorInvalidValue;
+  if (a.g_row && (a.M != 1 || !a.n_rows)) return hipErrorInvalidValue;
   if (f32) return launch_bwd_t<MmaF32, F32>(a, stream);
   if (a.wide)
     return a.ktail ? launch_bwd_wide<WideFusedTail>(a, stream) : launch_bwd_wide<WideFused>(a, stream);

@@ -127,7 +127,8 @@ struct F32Loader {
 };
 
 template <int BM, int BN, int KS, bool AMC>
-__device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, char* smem, int tid) {
+__device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, int64_t mext, int64_t K, char* smem,
+                                         int tid) {
   constexpr int BK = 32 * KS;
   using Tile = F32Tile<BM, BN, BK>;
   Tile* stage = reinterpret_cast<Tile*>(smem);
@@ -138,7 +139,7 @@ __device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, cha
   const int kw = KS > 1 ? wave * 32 : 0;  // the wave's part of a K-tile
   const int64_t m0 = (int64_t)tm * BM;
   const int64_t n0 = (int64_t)tn * BN;
-  const int64_t mext = g.ldc_rows, next = g.ldc, K = g.K;
+  const int64_t next = g.ldc;
   const float* A = static_cast<const float*>(g.A);
   const float* B = static_cast<const float*>(g.B);
   f32x16_t acc;
@@ -196,7 +197,8 @@ __device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, cha
   }
 }
 
-template <int BM, int BN, int KS>
+// ROWS: the number of tokens (rows of grad_h, K of grad_W) comes from the device.
+template <int BM, int BN, int KS, bool ROWS = false>
 __global__ __launch_bounds__(kThreads) void gemm_f32_kernel(GemmArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[2 * sizeof(F32Tile<BM, BN, 32 * KS>)];
   const int b = blockIdx.x;
@@ -207,10 +209,12 @@ __global__ __launch_bounds__(kThreads) void gemm_f32_kernel(GemmArgs a) {
   const int local = b - g.tile_begin;
   const int tn = local % g.tiles_n;
   const int tm = local / g.tiles_n;
+  const int rows = ROWS ? *a.n_rows : 0;
+  if (ROWS && g.kind == 0 && (int64_t)tm * BM >= rows) return;
   if (g.kind == 0)
-    f32_tile<BM, BN, KS, false>(g, tm, tn, smem, threadIdx.x);
+    f32_tile<BM, BN, KS, false>(g, tm, tn, ROWS ? rows : g.ldc_rows, g.K, smem, threadIdx.x);
   else
-    f32_tile<BM, BN, KS, true>(g, tm, tn, smem, threadIdx.x);
+    f32_tile<BM, BN, KS, true>(g, tm, tn, g.ldc_rows, ROWS ? rows : g.K, smem, threadIdx.x);
 }
 
 // bf16 path: 256 x 256 tiles, 8 waves (2 per SIMD) of 128 x 64, direct-to-LDS
@@ -359,10 +363,12 @@ struct TileIo {
   }
 };
 
-// Tile (tm, tn) of group g, over its K part `part_k` (kind 0 groups in parts).
+// Tile (tm, tn) of group g, over its K part `part_k` (kind 0 groups in parts), with
+// the group's rows, cols and K (see GemmGroup).
 template <class Mma>
-__device__ __forceinline__ void wide_tile(const GemmGroup& g, int tm, int tn, int part_k,
-                                          int64_t mext, int64_t next, char* smem, int tid) {
+__device__ __forceinline__ void wide_tile(const GemmGroup& g, int tm, int tn, int part_k, int64_t mext,
+                                          int64_t next, int64_t g_rows, int64_t g_cols, int64_t g_K, char* smem,
+                                          int tid) {
   constexpr int FM = Mma::FM;
   constexpr int FN = Mma::FN;
   const int lane = tid & 63;
@@ -377,7 +383,7 @@ __device__ __forceinline__ void wide_tile(const GemmGroup& g, int tm, int tn, in
   const int64_t rows = mext - m0 < Mma::kBM ? mext - m0 : Mma::kBM;
   const bool out16 = g.Cb != nullptr;
   const int64_t k0 = part_k * g.ksplit;
-  const int64_t K = g.splits > 1 && g.K - k0 > g.ksplit ? g.ksplit : g.K - k0;
+  const int64_t K = g.splits > 1 && g_K - k0 > g.ksplit ? g.ksplit : g_K - k0;
   float* const C = g.C + part_k * g.csplit;
   const __amdgpu_buffer_rsrc_t rc =
       out16 ? uniform_rsrc(reinterpret_cast<const char*>(g.Cb + m0 * g.ldc), (int)(rows * g.ldc * 2))
@@ -404,8 +410,8 @@ __device__ __forceinline__ void wide_tile(const GemmGroup& g, int tm, int tn, in
   // so the product is added to it there and the epilogue only stores; the
   // reads' latency overlaps the first K-tile's loads.
   Mma mma;
-  mma.run_pipelined(static_cast<const char*>(g.A) + k0 * 2, g.lda * 2, m0, g.rows,
-               static_cast<const char*>(g.B) + k0 * g.ldb * 2, g.ldb * 2, n0, g.cols - k0, K * 2,
+  mma.run_pipelined(static_cast<const char*>(g.A) + k0 * 2, g.lda * 2, m0, g_rows,
+               static_cast<const char*>(g.B) + k0 * g.ldb * 2, g.ldb * 2, n0, g_cols - k0, K * 2,
                smem, tid, [&]() {
                  if (!part && !acc_old)
                    mma.zero();
@@ -418,6 +424,46 @@ __device__ __forceinline__ void wide_tile(const GemmGroup& g, int tm, int tn, in
     TileIo<Mma, true>::store(mma.acc, rc, coff, ok, ldc, out16);
   else
     TileIo<Mma, false>::store(mma.acc, rc, coff, ok, ldc, out16);
+}
+
+// A launch over the tokens that count (GemmArgs::n_rows): tiles of group k, and
+// of the whole launch, once the number of rows is known.
+__device__ __forceinline__ int live_tiles(const GemmGroup& g, int rows, int bm) {
+  const int tm = g.kind == 0 ? (rows + bm - 1) / bm : g.tiles_m;
+  return tm * g.tiles_n * (g.splits > 1 ? g.splits : 1);
+}
+__device__ __forceinline__ int live_total(const GemmArgs& a, int rows, int bm) {
+  int n = 0;
+  for (int k = 0; k < a.ngroups; ++k) n += live_tiles(a.g[k], rows, bm);
+  return n;
+}
+
+// ROWS: the groups' sizes in tokens come from the device. Their tiles are dealt out
+// anew, so that the XCDs share what is left evenly; blocks past them end at once.
+template <class MmaH, class MmaW>
+__global__ __launch_bounds__(MmaH::NT, 1) void gemm_wide_rows_kernel(GemmArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[MmaH::kSmemBytes];
+  const int rows = *a.n_rows;
+  const int first = live_tiles(a.g[0], rows, MmaH::kBM), nb = live_total(a, rows, MmaH::kBM);
+  if ((int)blockIdx.x >= nb) return;
+  const int b = xcd_remap_phased(blockIdx.x, nb, a.ngroups > 1 ? first : 0);
+  const int gi = a.ngroups > 1 && b >= first ? 1 : 0;
+  const GemmGroup& g = a.g[gi];
+  int local = b - (gi ? first : 0);
+  if (g.kind == 0) {
+    const int tiles_m = (rows + MmaH::kBM - 1) / MmaH::kBM;
+    int part = 0, tm, tn;
+    if (g.splits > 1) {
+      part = local / (tiles_m * g.tiles_n);
+      local -= part * tiles_m * g.tiles_n;
+    }
+    tile_coords(local, tiles_m, g.tiles_n, g.group_m, tm, tn);
+    wide_tile<MmaH>(g, tm, tn, part, rows, g.ldc, g.rows, g.cols, g.K, smem, threadIdx.x);
+  } else {
+    // K: the rows, in whole K-tiles; h reads as zero past them
+    const int64_t K = ((int64_t)rows + MmaW::BK - 1) / MmaW::BK * MmaW::BK;
+    wide_tile<MmaW>(g, local / g.tiles_n, local % g.tiles_n, 0, g.ldc_rows, g.ldc, K, rows, K, smem, threadIdx.x);
+  }
 }
 
 template <class MmaH, class MmaW>
@@ -447,9 +493,9 @@ __global__ __launch_bounds__(MmaH::NT, 1) void gemm_wide_kernel(GemmArgs a, int 
   const int64_t mext = g.ldc_rows;
   const int64_t next = g.ldc;
   if (g.kind == 0)
-    wide_tile<MmaH>(g, tm, tn, part, mext, next, smem, threadIdx.x);
+    wide_tile<MmaH>(g, tm, tn, part, mext, next, g.rows, g.cols, g.K, smem, threadIdx.x);
   else
-    wide_tile<MmaW>(g, tm, tn, 0, mext, next, smem, threadIdx.x);
+    wide_tile<MmaW>(g, tm, tn, 0, mext, next, g.rows, g.cols, g.K, smem, threadIdx.x);
 }
 
 // Adds the K parts of grad_h (fixed order, so results are reproducible).
@@ -508,6 +554,13 @@ int gemm_wide_k_tile() { return WideGemmH::BK; }
 
 hipError_t launch_gemm_wide(const GemmArgs& a, int total_tiles, hipStream_t stream) {
   if (total_tiles <= 0) return hipSuccess;
+  if (a.n_rows) {
+    const bool order = a.ngroups == 1 || (a.ngroups == 2 && a.g[0].kind == 0 && a.g[1].kind == 1);
+    if (!order) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemm_wide_rows_kernel<WideGemmH, WideGemmW>), dim3(total_tiles), dim3(WideGemmH::NT), 0,
+                       stream, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL((gemm_wide_kernel<WideGemmH, WideGemmW>), dim3(total_tiles),
                      dim3(WideGemmH::NT), 0, stream, a, total_tiles);
   return hipGetLastError();
@@ -524,15 +577,21 @@ hipError_t launch_split_sum(const SplitSumArgs& a, hipStream_t stream) {
 
 hipError_t launch_gemm_f32(const GemmArgs& a, int tile, int total_tiles, hipStream_t stream) {
   if (total_tiles <= 0) return hipSuccess;
-  if (tile == 64)
-    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 1>), dim3(total_tiles), dim3(kThreads), 0, stream, a);
+  const dim3 grid(total_tiles), block(kThreads);
+  if (tile == 64 && a.n_rows)
+    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 1, true>), grid, block, 0, stream, a);
+  else if (tile == 64)
+    hipLaunchKernelGGL((gemm_f32_kernel<64, 64, 1>), grid, block, 0, stream, a);
+  else if (tile == 32 && a.n_rows)
+    hipLaunchKernelGGL((gemm_f32_kernel<32, 32, 4, true>), grid, block, 0, stream, a);
   else if (tile == 32)
-    hipLaunchKernelGGL((gemm_f32_kernel<32, 32, 4>), dim3(total_tiles), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((gemm_f32_kernel<32, 32, 4>), grid, block, 0, stream, a);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();
 }
 
+// (n_rows is not needed: slab and operands hold zeros behind the last row)
 hipError_t launch_gemm_nt(const GemmArgs& a, int total_tiles, hipStream_t stream) {
   if (total_tiles <= 0) return hipSuccess;
   hipLaunchKernelGGL(gemm_nt_kernel, dim3(total_tiles), dim3(kThreads), 0, stream, a);

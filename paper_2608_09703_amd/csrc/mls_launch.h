@@ -63,8 +63,12 @@ struct FusedArgs {
   const int32_t* n_valid;
   const float* g_ce;  // device [M] or null
   const float* g_kl;
-  // backward of token log-probabilities (M = 1): upstream gradient of each
-  // token's log-probability at temperature tau; null for the losses
+  // token log-probabilities (M = 1); null for the losses. The rows are the tokens
+  // that count, *n_rows of them: this launch's are [row0, min(row0 + T, *n_rows)),
+  // and T and n_tt only bound them. g_row (backward): upstream gradient of each
+  // row's log-probability at temperature tau
+  const int32_t* n_rows;
+  int64_t row0;
   const float* g_row;  // [T]
   float host_gce[kMaxModels];
   float host_gkl[kMaxModels];
@@ -116,6 +120,10 @@ struct GemmArgs {
   // Tiles [0, phase_tiles) and [phase_tiles, total) have different costs (K);
   // each phase is spread evenly over the XCDs. 0 = one phase.
   int32_t phase_tiles;
+  // token log-probabilities: the number of tokens that count (rows of grad_h's
+  // groups, K of grad_W's); null: as the groups say. At most one group of each kind,
+  // grad_h's first
+  const int32_t* n_rows;
   GemmGroup g[kMaxGemmGroups];
 };
 
@@ -172,9 +180,41 @@ struct RowArgs {
   float* ce;
   float* kl;
   float* entropy;
-  // token log-probabilities (M = 1): per token, at temperature tau; null for the losses
-  float* logp_row;     // [T]
-  float* entropy_row;  // [T] or null
+};
+
+// Token log-probabilities: the tokens that count, packed.
+struct TokenArgs {
+  int64_t T;
+  int64_t T_pad;          // rows of hc
+  int64_t V;
+  int64_t d;
+  const void* h;          // [T][d]
+  const void* W;          // [V][d]
+  const int64_t* tokens;  // [T]
+  int64_t ignore_index;
+  float tau;
+  int32_t* header;        // number of tokens that count, device flags
+  int32_t* rank;          // [T] row of each token, -1 where it does not count
+  int32_t* index;         // [T] token of each row
+  float* logp;            // [T]
+  float* entropy;         // [T] or null
+  void* hc;               // [T_pad][d] their hidden states; zeros behind the last
+  int64_t* tokens_c;      // [T] their ids
+  float* lab;             // [T] forward: their own logits
+  const float* g;         // [T] backward: gradients by token
+  float* g_c;             // [T] and by row
+  // row merge of rows [t0, t0 + Tc)
+  int64_t t0;
+  int64_t Tc;
+  int32_t n_rec;
+  const float4* partials;
+  float* lse;             // [T] by row
+  // grad_h by token from the rows' one
+  const void* gh_c;       // [T][d] in the type gh_f32 says
+  int32_t gh_f32;
+  int32_t out_f32;
+  int32_t accumulate;
+  void* grad_h;           // [T][d]
 };
 
 // Logit gradient of one token chunk from its stored logits (fused forward +
@@ -459,7 +499,10 @@ hipError_t launch_row_params(const RowParamArgs& a, int ept, hipStream_t stream)
 hipError_t launch_verify(const VerifyArgs& a, int ept, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_finalize_rows(const RowArgs& a, hipStream_t stream);
-hipError_t launch_finalize_logp(const RowArgs& a, hipStream_t stream);
+hipError_t launch_token_pack(const TokenArgs& a, hipStream_t stream);
+hipError_t launch_token_gather(const TokenArgs& a, bool f32, hipStream_t stream);
+hipError_t launch_token_merge(const TokenArgs& a, hipStream_t stream);
+hipError_t launch_token_scatter(const TokenArgs& a, hipStream_t stream);
 hipError_t launch_reduce_losses(const RowArgs& a, hipStream_t stream);
 hipError_t launch_count_valid(const RowArgs& a, hipStream_t stream);
 hipError_t launch_grad_logits(const GradArgs& a, hipStream_t stream);

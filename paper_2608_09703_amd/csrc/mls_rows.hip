@@ -9,18 +9,17 @@
 
 #include "mls_device.h"
 #include "mls_launch.h"
+#include "mls_merge.h"
 
 namespace mls {
 
 namespace {
 
-// ROWS: also clears the statistics header, for the row merge that sets flags in it.
-template <typename E, bool ROWS>
+template <typename E>
 __global__ __launch_bounds__(kThreads) void label_logits_kernel(RowArgs a) {
   using S = typename E::storage;
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (ROWS && blockIdx.x == 0 && threadIdx.x < 2) a.header[threadIdx.x] = 0;
   if (w >= (int64_t)a.M * a.T) return;
   const int i = (int)(w / a.T);
   const int64_t t = w % a.T;
@@ -51,44 +50,6 @@ __global__ __launch_bounds__(kThreads) void label_logits_kernel(RowArgs a) {
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) a.lab[(int64_t)i * a.T + t] = s;
 }
-
-// Running merge of partial rows. Every sub-model keeps its own max m,
-// sum exp(l - m) (s1) and sum exp((l - m) / tau) (st); the cross terms xr of
-// every sub-model are weighted by the teacher's exponentials, so they are
-// rescaled with the teacher's max. Slots follow the processing order, slot 0
-// being the teacher; MM (the number of sub-models) is a compile-time constant,
-// so every array is indexed with constants and stays in registers.
-template <int MM>
-struct RowState {
-  float m[MM];
-  float s1[MM];
-  float st[MM];
-  float xr[MM];
-};
-
-// rec[k] = partial of slot k over one vocabulary range (the same for all k)
-template <int MM>
-__device__ __forceinline__ void absorb(RowState<MM>& st, float ct, const float4* rec) {
-  const float ms_new = fmaxf(st.m[0], rec[0].x);
-  const float wa = fast_exp2((st.m[0] - ms_new) * ct);
-  const float wb = fast_exp2((rec[0].x - ms_new) * ct);
-#pragma unroll
-  for (int k = 0; k < MM; ++k) {
-    const float mo = st.m[k];
-    const float mn = fmaxf(mo, rec[k].x);
-    st.s1[k] = st.s1[k] * fast_exp2((mo - mn) * kLog2e) + rec[k].y * fast_exp2((rec[k].x - mn) * kLog2e);
-    st.st[k] = st.st[k] * fast_exp2((mo - mn) * ct) + rec[k].z * fast_exp2((rec[k].x - mn) * ct);
-    st.xr[k] = st.xr[k] * wa + rec[k].w * wb;
-    st.m[k] = mn;
-  }
-}
-
-// 4 tokens x 64 groups: 25 records per thread at the headline shape rather than
-// 49 with 8 x 32 (row merge 39 -> 34 us per launch)
-constexpr int kRowTok = 4;    // tokens per block
-constexpr int kRowGrp = 64;   // partial groups per token, merged pairwise in a fixed tree
-static_assert(kRowTok * kRowGrp == kThreads && (kRowGrp & (kRowGrp - 1)) == 0, "row merge shape");
-static_assert(kFusedBN % kRowTok == 0, "a block's tokens lie in one token tile");
 
 // Tokens [t0, t0 + Tc) of one forward chunk: its partial records are indexed
 // by the token inside the chunk, the statistics by the token itself.
@@ -166,53 +127,6 @@ __global__ __launch_bounds__(kThreads) void finalize_rows_kernel(RowArgs a) {
     kl_row[i * T + t] = (valid && k != 0) ? (xr_s - st.xr[k]) / den - lset_s + lt : 0.f;
   }
   h_row[t] = valid ? lset_s - xr_s / den : 0.f;
-}
-
-// Row merge of token log-probabilities (one sub-model):
-//   logp = l_y / tau - logsumexp(l / tau),  entropy = logsumexp(l / tau) - mean_p(l) / tau
-// and the device flags of rows that a caller must know of. The label logit and
-// the flags' zero come from label_logits_kernel.
-__global__ __launch_bounds__(kThreads) void finalize_logp_kernel(RowArgs a) {
-  __shared__ float4 sh[kRowGrp][kRowTok];
-  const int tl = threadIdx.x % kRowTok;
-  const int grp = threadIdx.x / kRowTok;
-  const int64_t tc = (int64_t)blockIdx.x * kRowTok + tl;
-  const float inv_tau = 1.0f / a.tau;
-  const float ct = kLog2e * inv_tau;
-  RowState<1> st = {{-INFINITY}, {0.f}, {0.f}, {0.f}};
-  if (tc < a.Tc) {
-    const float4* part = a.partials + (tc / kFusedBN) * a.n_rec * kFusedBN + tc % kFusedBN;
-#pragma unroll 4
-    for (int j = grp; j < a.n_rec; j += kRowGrp) {
-      const float4 rec = part[(int64_t)j * kFusedBN];
-      if (rec.x != -INFINITY) absorb<1>(st, ct, &rec);
-    }
-  }
-  sh[grp][tl] = make_float4(st.m[0], st.s1[0], st.st[0], st.xr[0]);
-#pragma unroll
-  for (int w = kRowGrp / 2; w >= 1; w >>= 1) {
-    __syncthreads();
-    if (grp < w) {
-      const float4 rec = sh[grp + w][tl];
-      if (rec.x != -INFINITY) {
-        absorb<1>(st, ct, &rec);
-        if (w > 1) sh[grp][tl] = make_float4(st.m[0], st.s1[0], st.st[0], st.xr[0]);
-      }
-    }
-  }
-  if (grp != 0 || tc >= a.Tc) return;
-  const int64_t t = a.t0 + tc;
-  const int64_t y = a.labels[t];
-  const bool counts = y != a.ignore_index;
-  const bool valid = counts && y >= 0 && y < a.V;
-  const float lse = st.m[0] * inv_tau + logf(st.st[0]);
-  const float lp = fmaf(a.lab[t], inv_tau, -lse);
-  a.stats[a.T + t] = lse;  // the statistics' lset row
-  a.logp_row[t] = valid ? lp : 0.f;
-  if (a.entropy_row) a.entropy_row[t] = valid ? lse - st.xr[0] / (a.tau * st.st[0]) : 0.f;
-  const int flags = (counts && !valid ? MLS_DEVFLAG_LABEL_RANGE : 0) |
-                    (valid && !isfinite(lp) ? MLS_DEVFLAG_NONFINITE : 0);
-  if (flags) atomicOr(a.header + 1, flags);  // order does not matter to an OR
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -423,22 +337,10 @@ hipError_t launch_grad_logits(const GradArgs& a, hipStream_t stream) {
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream) {
   const int64_t waves = (int64_t)a.M * a.T;
   dim3 grid((unsigned)((waves + 3) / 4));
-  if (a.logp_row) {
-    if (f32)
-      hipLaunchKernelGGL((label_logits_kernel<F32, true>), grid, dim3(kThreads), 0, stream, a);
-    else
-      hipLaunchKernelGGL((label_logits_kernel<Bf16, true>), grid, dim3(kThreads), 0, stream, a);
-  } else if (f32) {
-    hipLaunchKernelGGL((label_logits_kernel<F32, false>), grid, dim3(kThreads), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL((label_logits_kernel<Bf16, false>), grid, dim3(kThreads), 0, stream, a);
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_finalize_logp(const RowArgs& a, hipStream_t stream) {
-  dim3 grid((unsigned)((a.Tc + kRowTok - 1) / kRowTok));
-  hipLaunchKernelGGL(finalize_logp_kernel, grid, dim3(kThreads), 0, stream, a);
+  if (f32)
+    hipLaunchKernelGGL(label_logits_kernel<F32>, grid, dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(label_logits_kernel<Bf16>, grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -1,0 +1,227 @@
+// Token log-probabilities: what stands around the tile kernels (mls_fused.hip) and
+// the gradient products (mls_gemm.hip).
+//
+// Only the tokens that count are computed: prompt and padding tokens, a quarter to
+// two thirds of a post-training batch, are left out of every product. Their
+// positions are packed in order (pack), the hidden states of the others copied
+// together (gather) and the products run on those rows, whose number they read from
+// the device; log-probabilities (merge) and grad_h (scatter) go back to the tokens'
+// places. What an ignored token's hidden state holds does not matter, NaN included.
+// The copies are T d elements in and out, memory-bound, against 2 T V d operations
+// a product: at T = 4,096, d = 4,352, V = 49,152 they are 1 % of the time.
+#include <math.h>
+
+#include "mls_device.h"
+#include "mls_launch.h"
+#include "mls_merge.h"
+#include "mls_vec.h"
+#include "mls_wave.h"
+
+namespace mls {
+
+namespace {
+
+constexpr int kPackThreads = 1024;
+constexpr int kPackTok = 4;  // tokens per thread and round
+
+// One block walks the tokens in order: rank[t] = number of counting tokens before t
+// (or -1), index = its inverse. Ignored tokens get their zeros here.
+__global__ __launch_bounds__(kPackThreads) void token_pack_kernel(TokenArgs a) {
+  __shared__ int wave_n[kPackThreads / 64];
+  __shared__ int bad_any[kPackThreads / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int base = 0;
+  int bad = 0;
+  for (int64_t t0 = 0; t0 < a.T; t0 += kPackThreads * kPackTok) {
+    const int64_t t = t0 + (int64_t)threadIdx.x * kPackTok;
+    bool ok[kPackTok];
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kPackTok; ++i) {
+      const int64_t y = t + i < a.T ? a.tokens[t + i] : a.ignore_index;
+      ok[i] = y != a.ignore_index && y >= 0 && y < a.V;
+      bad |= y != a.ignore_index && !ok[i];
+      n += ok[i] ? 1 : 0;
+    }
+    const int incl = wave_incl_scan(n);
+    if (lane == 63) wave_n[wave] = incl;
+    __syncthreads();
+    int before = base;
+    for (int w = 0; w < kPackThreads / 64; ++w) {
+      before += w < wave ? wave_n[w] : 0;
+      base += wave_n[w];
+    }
+    int r = before + incl - n;
+#pragma unroll
+    for (int i = 0; i < kPackTok; ++i) {
+      if (t + i >= a.T) continue;
+      a.rank[t + i] = ok[i] ? r : -1;
+      if (ok[i]) {
+        a.index[r++] = (int32_t)(t + i);
+      } else {
+        a.logp[t + i] = 0.f;
+        if (a.entropy) a.entropy[t + i] = 0.f;
+      }
+    }
+    __syncthreads();  // wave_n is written again
+  }
+  bad = wave_sum(bad);
+  if (lane == 0) bad_any[wave] = bad;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  bad = 0;
+  for (int w = 0; w < kPackThreads / 64; ++w) bad |= bad_any[w];
+  a.header[0] = base;
+  a.header[1] = bad ? MLS_DEVFLAG_LABEL_RANGE : 0;
+}
+
+// One wave per token and, for the rows behind the last one, per row: copies the
+// token's hidden state to its row and its id and gradient along, and takes its own
+// logit <h, W[y]> on the way (forward).
+template <typename E>
+__global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
+  using S = typename E::storage;
+  constexpr int kPer = 16 / E::kBytes;  // elements per 16-byte access
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= a.T_pad) return;
+  S* hc = static_cast<S*>(a.hc);
+  if (t >= a.header[0]) {
+    for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer)
+      *reinterpret_cast<uint4*>(hc + t * a.d + k) = make_uint4(0, 0, 0, 0);
+  }
+  if (t >= a.T) return;
+  const int64_t r = a.rank[t];
+  if (r < 0) return;
+  const int64_t y = a.tokens[t];
+  const S* h = static_cast<const S*>(a.h) + t * a.d;
+  const S* w = static_cast<const S*>(a.W) + y * a.d;
+  float s = 0.f;
+  for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer) {
+    const uint4 hv = *reinterpret_cast<const uint4*>(h + k);
+    *reinterpret_cast<uint4*>(hc + r * a.d + k) = hv;
+    if (!a.lab) continue;
+    const uint4 wv = *reinterpret_cast<const uint4*>(w + k);
+    const uint32_t hu[4] = {hv.x, hv.y, hv.z, hv.w};
+    const uint32_t wu[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (E::kBytes == 2) {
+        s = fmaf(__uint_as_float(hu[q] << 16), __uint_as_float(wu[q] << 16), s);
+        s = fmaf(__uint_as_float(hu[q] & 0xffff0000u), __uint_as_float(wu[q] & 0xffff0000u), s);
+      } else {
+        s = fmaf(__uint_as_float(hu[q]), __uint_as_float(wu[q]), s);
+      }
+    }
+  }
+  if (a.lab) s = wave_sum(s);
+  if (lane != 0) return;
+  a.tokens_c[r] = y;
+  if (a.lab) a.lab[r] = s;
+  if (a.g) a.g_c[r] = a.g[t];
+}
+
+// Row merge (one sub-model, temperature tau):
+//   logp = l_y / tau - logsumexp(l / tau),  entropy = logsumexp(l / tau) - mean_p(l) / tau
+__global__ __launch_bounds__(kThreads) void token_merge_kernel(TokenArgs a) {
+  __shared__ float4 sh[kRowGrp][kRowTok];
+  const int tl = threadIdx.x % kRowTok;
+  const int grp = threadIdx.x / kRowTok;
+  const int64_t tc = (int64_t)blockIdx.x * kRowTok + tl;
+  const int64_t live = (int64_t)a.header[0] - a.t0;
+  const int64_t Tc = live < a.Tc ? live : a.Tc;
+  if ((int64_t)blockIdx.x * kRowTok >= Tc) return;
+  const float inv_tau = 1.0f / a.tau;
+  const float ct = kLog2e * inv_tau;
+  RowState<1> st = {{-INFINITY}, {0.f}, {0.f}, {0.f}};
+  if (tc < Tc) {
+    const float4* part = a.partials + (tc / kFusedBN) * a.n_rec * kFusedBN + tc % kFusedBN;
+#pragma unroll 4
+    for (int j = grp; j < a.n_rec; j += kRowGrp) {
+      const float4 rec = part[(int64_t)j * kFusedBN];
+      if (rec.x != -INFINITY) absorb<1>(st, ct, &rec);  // else rows all beyond V
+    }
+  }
+  sh[grp][tl] = make_float4(st.m[0], st.s1[0], st.st[0], st.xr[0]);
+#pragma unroll
+  for (int w = kRowGrp / 2; w >= 1; w >>= 1) {
+    __syncthreads();
+    if (grp < w) {
+      const float4 rec = sh[grp + w][tl];
+      if (rec.x != -INFINITY) {
+        absorb<1>(st, ct, &rec);
+        if (w > 1) sh[grp][tl] = make_float4(st.m[0], st.s1[0], st.st[0], st.xr[0]);
+      }
+    }
+  }
+  if (grp != 0 || tc >= Tc) return;
+  const int64_t r = a.t0 + tc;
+  const int64_t t = a.index[r];
+  const float lse = st.m[0] * inv_tau + logf(st.st[0]);
+  const float lp = fmaf(a.lab[r], inv_tau, -lse);
+  a.lse[r] = lse;
+  a.logp[t] = lp;
+  if (a.entropy) a.entropy[t] = lse - st.xr[0] / (a.tau * st.st[0]);
+  if (!isfinite(lp)) atomicOr(a.header + 1, MLS_DEVFLAG_NONFINITE);
+}
+
+// grad_h by token: its row's, or zeros (with accumulate, nothing) where it does not
+// count. One wave per token, 4 elements per lane and step (both widths' granularity).
+template <typename G, typename O>
+__global__ __launch_bounds__(kThreads) void token_scatter_kernel(TokenArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= a.T) return;
+  const int64_t r = a.rank[t];
+  if (r < 0 && a.accumulate) return;
+  const typename Elt<G>::type* src = static_cast<const typename Elt<G>::type*>(a.gh_c) + r * a.d;
+  typename Elt<O>::type* out = static_cast<typename Elt<O>::type*>(a.grad_h) + t * a.d;
+  for (int64_t k = (int64_t)lane * 4; k < a.d; k += 64 * 4) {
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r >= 0) load4<false>(src + k, v);
+    if (a.accumulate) {
+      float o[4];
+      load4<false>(out + k, o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += o[i];
+    }
+    store4<false>(out + k, v);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_token_pack(const TokenArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(token_pack_kernel, dim3(1), dim3(kPackThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_token_gather(const TokenArgs& a, bool f32, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.T_pad + 3) / 4));
+  if (f32)
+    hipLaunchKernelGGL(token_gather_kernel<F32>, grid, dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(token_gather_kernel<Bf16>, grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_token_merge(const TokenArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.Tc + kRowTok - 1) / kRowTok));
+  hipLaunchKernelGGL(token_merge_kernel, grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_token_scatter(const TokenArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.T + 3) / 4));
+  if (a.gh_f32 && a.out_f32)
+    hipLaunchKernelGGL((token_scatter_kernel<F32, F32>), grid, dim3(kThreads), 0, stream, a);
+  else if (a.gh_f32)
+    hipLaunchKernelGGL((token_scatter_kernel<F32, Bf16>), grid, dim3(kThreads), 0, stream, a);
+  else if (!a.out_f32)
+    hipLaunchKernelGGL((token_scatter_kernel<Bf16, Bf16>), grid, dim3(kThreads), 0, stream, a);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace mls

@@ -44,7 +44,7 @@ def _check(logp, old, adv, upstream=1.0, ref=None, mask=None, cu=None, oracle_cu
     want = P.policy(_np(logp), _np(old), _np(adv), ref=_np(ref), mask=None if mask is None else
                     mask.cpu().numpy().reshape(-1), cu=cu_n, **kw)
     scale = np.abs(np.nan_to_num(_np(adv), posinf=0, neginf=0)).max(initial=0) * 10 + 10
-    for got, ref_v, name in ((loss, want[0], "loss"), (kl, want[1], "kl"), (clipped, want[2], "clipped")):
+    for got, ref_v, name in ((loss.detach(), want[0], "loss"), (kl, want[1], "kl"), (clipped, want[2], "clipped")):
         assert got.shape == () and abs(float(got) - ref_v) <= U * abs(ref_v) + 1e-12 * scale, (name, float(got), ref_v)
     got = _np(leaf.grad)
     assert np.all(np.abs(got - upstream * want[3]) <= 5 * U * np.abs(upstream * want[3]) + 1e-45)
@@ -168,7 +168,7 @@ def test_bad_offsets_stay_inside():
             loss.backward()
             clamped = np.clip(cu, 0, 50)
             want = P.policy(_np(logp), _np(old), _np(adv), cu=clamped, reduction=reduction)
-            assert abs(float(loss) - want[0]) <= U * abs(want[0]) + 1e-11
+            assert abs(float(loss.detach()) - want[0]) <= U * abs(want[0]) + 1e-11
 
 
 def test_many_tokens_and_no_gradient():

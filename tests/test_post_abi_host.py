@@ -85,9 +85,9 @@ def _problem(**kw):
 
 def test_token_logp_refusals():
     p = _problem()
-    ws, st = B.query_sizes(p)
+    ws, wb = B.token_logp_workspace(p)
     fwd = lambda q=p, s=_at(4), lp=_at(5), en=None, w=_at(6), nb=ws: B.token_logp_fwd(q, s, lp, en, w, nb, None)  # noqa: E731
-    bwd = lambda q=p, s=_at(4), g=_at(5), gh=_at(7), gW=_at(8), w=_at(6), nb=ws: B.token_logp_bwd(  # noqa: E731
+    bwd = lambda q=p, s=_at(4), g=_at(5), gh=_at(7), gW=_at(8), w=_at(6), nb=wb: B.token_logp_bwd(  # noqa: E731
         q, s, g, gh, gW, w, nb, None)
     for call in (fwd, bwd):
         _refused(B.MLS_INVALID_ARG, lambda: call(q=_problem(M=2)), text="one sub-model")
@@ -104,6 +104,15 @@ def test_token_logp_refusals():
         _refused(B.MLS_INVALID_ARG, lambda: fwd(**kw))
     for kw in (dict(g=None), dict(g=_at(5, 2)), dict(gh=_at(7, 2)), dict(gW=_at(8, 2))):
         _refused(B.MLS_INVALID_ARG, lambda: bwd(**kw))
+
+
+def test_a_token_logp_workspace_for_the_longest_batch_serves_the_shorter_ones():
+    last = (0, 0)
+    for T in (1, 127, 128, 129, 300, 512, 1000, 2000, 4096, 9000):
+        now = B.token_logp_workspace(_problem(T=T, V=50000, d=512, grad_h_dtype=B.MLS_BF16))
+        assert now[0] >= last[0] and now[1] >= last[1]
+        assert now[0] < T * 50000 * 4 // 2 + (1 << 26)
+        last = now
 
 
 # -- policy loss -----------------------------------------------------------------

@@ -96,6 +96,11 @@ def test_ignored_tokens(kept, dtype):
     _check(h, W, tokens, gl, 1.0, got, f"{len(kept)} kept")
     for g in (got[0], got[1], got[2]):
         assert not g[ignored].any()
+    h[ignored] = float("nan")
+    h[ignored.nonzero()[::2, 0]] = float("-inf")
+    gl[ignored] = float("inf")
+    for a, b in zip(got, _run(h, W, tokens, gl)):
+        assert torch.equal(a, b)
 
 
 def test_tokens_out_of_range_are_ignored_and_flagged():
@@ -105,12 +110,16 @@ def test_tokens_out_of_range_are_ignored_and_flagged():
     _check(h, W, tokens, gl, 1.0, got, "out of range")
     p = D.make_problem([h], [W], tokens)
     buf = D.Buffers(p, h.device)
+    ws = torch.empty(B.token_logp_workspace(p)[0], dtype=torch.uint8, device=DEV)
     logp = torch.empty(200, device=DEV)
 
     def flags():
-        B.token_logp_fwd(p, buf.stats.data_ptr(), logp.data_ptr(), None, buf.workspace.data_ptr(),
-                         buf.workspace.numel(), D._stream(h.device))
-        return B.device_error(p, buf.stats.data_ptr(), D._stream(h.device))
+        B.token_logp_fwd(p, buf.stats.data_ptr(), logp.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                         D._stream(h.device))
+        n, f = B.read_stats_header(p, buf.stats.data_ptr(), D._stream(h.device))
+        assert n == int(((tokens >= 0) & (tokens < 500)).sum()) and f == B.device_error(
+            p, buf.stats.data_ptr(), D._stream(h.device))
+        return f
     assert flags() == B.MLS_DEVFLAG_LABEL_RANGE
     tokens[3] = tokens[7] = 1
     assert flags() == 0
@@ -151,6 +160,38 @@ def test_one_gradient_alone_and_no_gradient():
     assert not lp.requires_grad and torch.equal(lp, logp) and torch.equal(en, entropy)
 
 
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                       (torch.bfloat16, torch.float32)])
+def test_accumulated_gradients(dtype, out):
+    """grad_h and grad_W += : the sum's own rounding once, ignored tokens' rows as they were."""
+    h, W, tokens, gl = _draw(300, 64, 900, dtype, 11)
+    flags = B.MLS_GRAD_W_BF16 if out == torch.bfloat16 else 0
+    g0 = [torch.randn(x.shape, device=DEV).to(out) for x in (h, W)]
+
+    def grads(acc):
+        p = D.make_problem([h], [W], tokens, grad_h_dtype=out, flags=flags | acc)
+        stats = torch.empty(B.query_sizes(p)[1], dtype=torch.uint8, device=DEV)
+        logp, s = torch.empty(300, device=DEV), D._stream(h.device)
+        ws = torch.full((max(B.token_logp_workspace(p)),), 255, dtype=torch.uint8, device=DEV)
+        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), None, ws.data_ptr(), ws.numel(), s)
+        g = [x.clone() if acc else torch.full_like(x, float("nan")) for x in g0]
+        ws.fill_(255)
+        B.token_logp_bwd(p, stats.data_ptr(), gl.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), ws.data_ptr(),
+                         ws.numel(), s)
+        torch.cuda.synchronize()
+        return g
+    plain, acc = grads(0), grads(B.MLS_ACCUMULATE_GRAD_H | B.MLS_ACCUMULATE_GRAD_W)
+    half = 2.0 ** -8 if out == torch.bfloat16 else 2.0 ** -24
+    for a, b, c in zip(plain, g0, acc):
+        a, b, c = a.double(), b.double(), c.double()
+        # the plain gradient's rounding and the sum's; an fp32 grad_W starts its sum over 300 tokens at the old
+        # value, so each of its 19 products of 16 tokens rounds at that value's size, twice at most: 2^-24 * 40
+        n = 40 if out == torch.float32 else 4
+        assert bool(((c - (a + b)).abs() <= n * half * (a.abs() + b.abs() + c.abs())).all())
+    ignored = tokens == -100
+    assert torch.equal(acc[0][ignored], g0[0][ignored]) and not plain[0][ignored].any()
+
+
 def test_a_head_used_twice_collects_both_gradients():
     h, W, tokens, gl = _draw(150, 64, 900, torch.float32, 8)
     h2 = torch.roll(h, 3, 0)
@@ -160,6 +201,33 @@ def test_a_head_used_twice_collects_both_gradients():
     ref = P.token_logp_backward(_np(h), _np(W), tokens.cpu().numpy(), _np(gl))[1] + \
         P.token_logp_backward(_np(h2), _np(W), tokens.cpu().numpy(), _np(gl))[1]
     assert_grad_rows(_np(W1.grad), ref, "shared head")
+
+
+def test_hidden_states_of_4_gib():
+    """Packed rows that reach 4 GiB take the general gradient kernels (64-bit addresses)."""
+    T, d, V = 131200, 16384, 260
+    g = torch.Generator(device=DEV).manual_seed(12)
+    h = torch.empty(T, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    W = (torch.randn(V, d, generator=g, device=DEV) * 0.01).bfloat16()
+    tokens = torch.randint(0, V, (T,), generator=g, device=DEV)
+    tokens[::3] = -100
+    h[::3] = float("nan")
+    gl = torch.randn(T, generator=g, device=DEV)
+    logp, entropy, gh, gW = _run(h, W, tokens, gl, temperature=0.8)
+    Wd, rW = W.double(), torch.zeros(V, d, dtype=torch.float64, device=DEV)
+    for t0 in range(0, T, 16384):
+        rows = t0 + (tokens[t0:t0 + 16384] != -100).nonzero()[:, 0]
+        hd, y = h[rows].double(), tokens[rows]
+        lp = torch.log_softmax(hd @ Wd.t() / 0.8, 1)
+        assert (logp[rows] - lp.gather(1, y[:, None])[:, 0]).abs().max() <= 1e-4
+        G = -lp.exp()
+        G[torch.arange(rows.numel(), device=DEV), y] += 1
+        G *= (gl[rows].double() / 0.8)[:, None]
+        rh = G @ Wd
+        assert (gh[rows].double() - rh).norm() <= 2e-2 * rh.norm()
+        rW += G.t() @ hd
+    assert not gh[::3].any() and not logp[::3].any()
+    assert (gW.double() - rW).norm() <= 2e-2 * rW.norm()
 
 
 def test_gradient_against_differences():
