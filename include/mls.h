@@ -356,7 +356,7 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  * p->M = 1, temperature p->tau and the tokens in p->labels,
  *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
- * as device float32 [T]. p->alpha and p->teacher do not matter. No [T, V] array is
+ * as device float32 [T]. p->alpha and p->teacher do not matter. No logits are
  * kept. Tokens with ignore_index cost no product: the others' hidden states are
  * packed first, and those of ignored tokens are not used, whatever they hold.
  * stats: mls_query_sizes' stats_bytes; it receives what the backward needs, the
@@ -376,8 +376,9 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
  * 0 on ignored tokens (whose g_logp is not used):
  *   grad_h = G W  [T, d] of p->grad_h_dtype (0 on ignored tokens),
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
- * Either may be NULL. The logits are recomputed one vocabulary chunk at a time and
- * G is rounded to bfloat16 (bf16 inputs) in between, as in mls_distill_bwd, whose
+ * Either may be NULL. The logits are recomputed one vocabulary chunk at a time
+ * (p->vocab_chunk = 0: as few chunks as keep a chunk's G within 256 MiB) and G is
+ * rounded to bfloat16 (bf16 inputs) in between, as in mls_distill_bwd, whose
  * accumulation flags apply (an accumulated grad_h is added to in fp32). stats: as
  * mls_token_logp_fwd left it on the same inputs. workspace: bwd_bytes of
  * mls_token_logp_workspace. Asynchronous on stream.

@@ -463,7 +463,10 @@ def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temper
     ``logp[t] = log softmax(W h[t] / temperature)[tokens[t]]``, with autograd through
     the HIP kernels for any gradient per token; ``entropy`` (of the same softmax) is
     for monitoring and not differentiated. Both are 0 where the token is
-    ``ignore_index``. Nothing of size ``[T, V]`` is kept.
+    ``ignore_index``. No logits are kept between the passes: the backward computes
+    them again, a chunk of the vocabulary at a time (``vocab_chunk`` columns, or as many
+    as fit 256 MiB). Ignored tokens cost no product, and what their rows of ``h`` hold
+    does not matter.
     """
     opts = dict(tau=temperature, ignore_index=ignore_index, vocab_chunk=vocab_chunk)
     if torch.is_grad_enabled() and (h.requires_grad or W.requires_grad):

@@ -545,6 +545,20 @@ hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void*
   return launch_count_valid(r, s);
 }
 
+// Tile core of token log-probabilities: 256 x 256 tiles, one block per CU, or the
+// losses' 128 x 128, two per CU. The larger one reads less per product and has
+// twice the tile epilogue in one piece, which counts for little in long products:
+// forward / backward tiles in us, 256 against 128, with a fifth of T ignored, at
+// d = 4,352, V = 128,256: 538 / 536 against 595 / 594 (T = 512), 3,074 / 3,368
+// against 3,498 / 3,669 (T = 4,096); d = 2,048: 502 / 515 against 496 / 510
+// (T = 1,024), 1,569 / 1,756 against 1,677 / 1,811 (T = 4,096); d = 1,024, where
+// neither wins throughout: 299 / 292 against 281 / 292 (T = 1,024), 928 / 1,057
+// against 956 / 1,042. It takes whole K-tiles of 32; up to 128 tokens half of its
+// columns would be empty.
+bool rows_core(const mls_problem* p, const Plan& pl) {
+  return pl.wide_bwd && p->d[0] % 32 == 0 && p->d[0] >= 2048 && p->T > 128;
+}
+
 // Tile kernel of the forward of tokens [t0, t0 + tc): partial records, and with
 // lslab the fp16 logits. n_rows: of token log-probabilities' rows, as many of these
 // as the device counts.
@@ -569,6 +583,10 @@ hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64
   a.ld_lslab = pl.fb_ld;
   a.n_rows = n_rows;
   a.row0 = t0;
+  if (n_rows && rows_core(p, pl)) {
+    a.tile_v = kRowsTile;
+    a.n_vt = (int)((pl.V + kRowsTile - 1) / kRowsTile);
+  }
   ProfScope ps("fused_fwd", s);
   return launch_fused_fwd(a, pl.f32, s);
 }
@@ -622,8 +640,6 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   FusedArgs a;
   fill_common(p, pl, a);
   a.wide = pl.wide_bwd ? 1 : 0;
-  const int fbm = fused_tile_rows(pl.f32);
-  a.n_vt = (int)(pl.Vc / fbm);
   a.lse1 = sf;
   a.lset = sf + (int64_t)pl.M * pl.T;
   a.n_valid = reinterpret_cast<const int32_t*>(static_cast<const char*>(stats) + pl.header_off);
@@ -631,6 +647,10 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   a.g_kl = g_kl;
   a.g_row = g_row;
   a.n_rows = g_row ? a.n_valid : nullptr;
+  const bool rows_tiles = g_row && rows_core(p, pl);
+  const int fbm = rows_tiles ? kRowsTile : fused_tile_rows(pl.f32);
+  if (rows_tiles) a.tile_v = kRowsTile;
+  a.n_vt = (int)(pl.Vc / fbm);
   host_coeffs(pl.M, pl.s, p->alpha, p->tau, MLS_MODE_PAPER, nullptr, a.host_gce, a.host_gkl);
   a.slab = ws + pl.off_slab;
   const bool stored = pl.wide_bwd || pl.f32;  // products on the stored layouts
@@ -849,6 +869,14 @@ mls_status validate_tokens(const mls_problem* p) {
   return MLS_OK;
 }
 
+// Logit gradients of one vocabulary chunk of token log-probabilities' backward.
+// A head of one sub-model needs no four chunks to stay far below its [T, V]: what
+// few chunks save is launches and the part-filled last round of each. T = 4,096
+// (3,071 counted), d = 4,352, V = 49,152, us for 12,288 / 24,576 / 49,152 columns:
+// 4,756 / 4,594 / 4,686; T = 1,531, d = 1,000, V = 32,003, for 8,192 / 32,256: 590 /
+// 485; fp32, T = 256, d = 256, V = 4,096, for 1,024 / 4,096: 183 / 117.
+constexpr int64_t kTokenSlabBytes = 256ll << 20;
+
 // Workspaces of token log-probabilities: the packed rows, then what the tile kernels
 // and products need.
 struct TokenPlan {
@@ -863,6 +891,12 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   // what is added to an output is added in fp32
   if (p->flags & MLS_ACCUMULATE_GRAD_H) tp.q.grad_h_dtype = MLS_F32;
   tp.q.flags &= ~(uint32_t)MLS_ACCUMULATE_GRAD_H;
+  const int64_t es = p->in_dtype == MLS_F32 ? 4 : 2, T_pad = round_up(p->T, kFusedBN);
+  const int64_t whole = T_pad * round_up(p->V, 256) * es;
+  if (tp.q.vocab_chunk == 0) {
+    const int64_t n = (whole + kTokenSlabBytes - 1) / kTokenSlabBytes;
+    tp.q.vocab_chunk = (p->V + n - 1) / n;
+  }
   make_plan(&tp.q, tp.pl);
   const Plan& pl = tp.pl;
   size_t off = align256((size_t)pl.T_pad * p->d[0] * pl.es);
@@ -875,7 +909,8 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   off = align256(off + (size_t)pl.T * p->d[0] * (tp.q.grad_h_dtype == MLS_F32 ? 4 : 2));
   tp.off_work = off;
   tp.bwd_bytes = off + pl.bwd_bytes;
-  tp.bwd_room = off + pl.bwd_room;
+  // (the slab alone may be smaller for more tokens, where chunks get narrower)
+  tp.bwd_room = off + std::max<size_t>(pl.bwd_room, align256((size_t)std::min(whole, kTokenSlabBytes)));
 }
 
 TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
@@ -1347,7 +1382,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   a.hc = ws + tp.off_hc;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
   a.lab = reinterpret_cast<float*>(ws + tp.off_lab);
-  a.n_rec = pl.n_vt_fwd * kFusedFwdParts;
+  a.n_rec = (rows_core(p, pl) ? (int)((pl.V + kRowsTile - 1) / kRowsTile) : pl.n_vt_fwd) * kFusedFwdParts;
   a.partials = reinterpret_cast<const float4*>(ws + tp.off_part);
   hipError_t e;
   {

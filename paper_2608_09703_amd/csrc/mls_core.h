@@ -338,6 +338,11 @@ struct WideMma {
                                       int64_t b_row0, int64_t b_rows, int64_t kbytes,
                                       char* smem, int tid) {
     static_assert(ALAY == kLayoutKC && BLAY == kLayoutKC, "K-contiguous operands");
+    if constexpr (KSTEPS == 2) {
+      run_pipelined(A, lda_bytes, a_row0, a_rows, B, ldb_bytes, b_row0, b_rows, kbytes, smem, tid,
+                    [&]() { zero(); });
+      return;
+    }
     const int lane = tid & 63;
     const int wave = tid >> 6;
     const int wm = wave % WGM;
@@ -438,7 +443,7 @@ struct WideMma {
                                                 const char* __restrict__ B, int64_t ldb_bytes,
                                                 int64_t b_row0, int64_t b_rows, int64_t kbytes,
                                                 char* smem, int tid, Init&& init) {
-    static_assert(KSTEPS == 2 && !KTAIL && STAGES == 5, "K-tiles of two K-steps, five stages");
+    static_assert(KSTEPS == 2 && !KTAIL && STAGES >= 3, "K-tiles of two K-steps, three stages or more");
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WGM;

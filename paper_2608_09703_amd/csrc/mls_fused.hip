@@ -41,6 +41,9 @@ using WideFused = WideMma<kFusedWideBM, kFusedBN, 2, 2, 2>;  // 2 blocks per CU
 using WideFusedTail =
     WideMma<kFusedWideBM, kFusedBN, 2, 2, 2, 128, kLayoutKC, kLayoutKC, true>;
 
+// Token log-probabilities (one sub-model, no teacher's tile to keep): 256 x 256.
+using WideRows = WideMma<kRowsTile, kRowsTile, 2, 4, 5, 64>;
+
 // Per-lane copy of the teacher's tile values (its softmax weights), laid out
 // like the accumulators. The bf16 paths keep them as packed fp16 pairs (half
 // the registers; probabilities lie in [0, 1], where fp16 rounds to 2^-11
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   constexpr int FM = Mma::FM;
   constexpr int FN = Mma::FN;
   static_assert(WGM == kFusedFwdParts, "one partial record per wave row");
-  static_assert(kFusedBN % BN == 0, "a tile's tokens lie in one record group");
+  static_assert(kFusedBN % BN == 0 || BN % kFusedBN == 0, "tiles hold whole record groups or parts of one");
   __shared__ __attribute__((aligned(16))) char smem[Mma::kSmemBytes];
 
   const int tid = threadIdx.x;
@@ -126,8 +129,8 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   TeacherTile<FM, FN, false> e_t;
   Mma mma;
 
-  for (int oi = 0; oi < a.M; ++oi) {
-    const int i = a.order[oi];
+  for (int oi = 0; oi < (ROWS ? 1 : a.M); ++oi) {
+    const int i = ROWS ? 0 : a.order[oi];
     const int64_t kb = a.d[i] * E::kBytes;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
             kb, tbase, T, kb, smem, tid);
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
             const float l = mma.acc[fm][fn][r];
             const float x = l - mb;
             const float e = ok ? fast_exp2(x * ct) : 0.f;
-            e_t.set(fm, fn, r, e);
+            if (!ROWS) e_t.set(fm, fn, r, e);
             st += e;
             xr = fmaf(e, l, xr);
             if (!TAU1) s1 += ok ? fast_exp2(x * kLog2e) : 0.f;
@@ -250,8 +253,9 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
 
       // 3. the wave's partial record of this token
       const int c = Mma::col_of(wn, fn, lane);
+      const int64_t tb = tbase + (BN > kFusedBN ? c / kFusedBN * kFusedBN : 0);
       if (hi == 0 && tbase + c < T)
-        a.partials[((oi * n_tg + tbase / kFusedBN) * n_rec + rec) * kFusedBN + tbase % kFusedBN + c] =
+        a.partials[((oi * n_tg + tb / kFusedBN) * n_rec + rec) * kFusedBN + (tbase + c) % kFusedBN] =
             make_float4(mb, s1, st, xr);
     }
   }
@@ -326,8 +330,8 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   TeacherTile<FM, FN, E::kBytes == 2> q_t;
   Mma mma;
 
-  for (int oi = 0; oi < a.M; ++oi) {
-    const int i = a.order[oi];
+  for (int oi = 0; oi < (ROWG ? 1 : a.M); ++oi) {
+    const int i = ROWG ? 0 : a.order[oi];
     const int64_t kb = a.d[i] * E::kBytes;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
             kb, tbase, T, kb, smem, tid);
@@ -442,8 +446,8 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
   TeacherTile<FM, FN, true> q_t;
   Mma mma;
 
-  for (int oi = 0; oi < a.M; ++oi) {
-    const int i = a.order[oi];
+  for (int oi = 0; oi < (ROWG ? 1 : a.M); ++oi) {
+    const int i = ROWG ? 0 : a.order[oi];
     const int64_t kb = a.d[i] * 2;
     mma.run(static_cast<const char*>(a.W[i]), kb, vbase, a.V, static_cast<const char*>(a.h[i]),
             kb, tbase, T, kb, smem, tid);
@@ -580,6 +584,11 @@ hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
   // takes 266 us instead of 471 on the register-staged core, the four backward
   // tile launches 394 instead of 652, and the gradient GEMMs need no transposed
   // copies (117 us).
+  if (a.n_rows && a.tile_v == kRowsTile) {
+    hipLaunchKernelGGL((fused_fwd_kernel<WideRows, Bf16, true, 1, false, true>),
+                       dim3((unsigned)a.n_tt * (unsigned)a.n_vt), dim3(WideRows::NT), 0, stream, a);
+    return hipGetLastError();
+  }
   if (a.lslab)  // the stored-logit plan takes multiples of 64 only
     return a.ktail ? hipErrorInvalidValue : launch_fwd_wide<WideFused, true>(a, stream);
   return a.ktail ? launch_fwd_wide<WideFusedTail, false>(a, stream)
@@ -589,6 +598,11 @@ hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
 hipError_t launch_fused_bwd(const FusedArgs& a, bool f32, hipStream_t stream) {
   if (a.g_row && (a.M != 1 || !a.n_rows)) return hipErrorInvalidValue;
   if (f32) return launch_bwd_t<MmaF32, F32>(a, stream);
+  if (a.n_rows && a.tile_v == kRowsTile) {
+    hipLaunchKernelGGL((fused_bwd_wide_kernel<WideRows, true, 1, true>),
+                       dim3((unsigned)a.n_tt * (unsigned)a.n_vt), dim3(WideRows::NT), 0, stream, a);
+    return hipGetLastError();
+  }
   if (a.wide)
     return a.ktail ? launch_bwd_wide<WideFusedTail>(a, stream) : launch_bwd_wide<WideFused>(a, stream);
   return launch_bwd_t<GenMmaBf16, Bf16>(a, stream);

@@ -15,6 +15,7 @@ constexpr int kMaxModels = 8;
 constexpr int kFusedBM = 128;      // general core
 constexpr int kFusedWideBM = 128;  // wide bf16 core
 constexpr int kFusedF32 = 64;      // fp32 core, rows and columns
+constexpr int kRowsTile = 256;     // core of token log-probabilities, rows and columns
 // forward partial records per (vocabulary tile, token, sub-model): one per
 // wave row of the tile, each over its own half of the tile's rows; their
 // records are grouped by kFusedBN tokens whatever the tile's columns
@@ -69,6 +70,7 @@ struct FusedArgs {
   // row's log-probability at temperature tau
   const int32_t* n_rows;
   int64_t row0;
+  int32_t tile_v;  // kRowsTile: that core's tiles; else 0
   const float* g_row;  // [T]
   float host_gce[kMaxModels];
   float host_gkl[kMaxModels];

@@ -73,7 +73,7 @@ def _run(h, W, tokens, gl, **kw):
 
 
 SHAPES = [(1, 8, 2), (1, 64, 300), (2, 64, 128), (127, 64, 129), (128, 72, 1000), (129, 200, 515), (300, 128, 2000),
-          (257, 520, 4097), (700, 1024, 3001)]
+          (257, 520, 4097), (700, 1024, 3001), (129, 2048, 255), (300, 2080, 1029)]
 
 
 @pytest.mark.parametrize("T,d,V", SHAPES)
@@ -84,11 +84,12 @@ def test_shapes(T, d, V, temperature, dtype):
     _check(h, W, tokens, gl, temperature, _run(h, W, tokens, gl, temperature=temperature), f"{T} {d} {V}")
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("kept", [[], [0], [299], [5, 130, 299], list(range(0, 300, 2)), list(range(200, 300))])
-def test_ignored_tokens(kept, dtype):
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 96), (torch.bfloat16, 2048), (torch.float32, 96)])
+@pytest.mark.parametrize("kept", [[], [0], [299], [5, 130, 299], list(range(0, 300, 2)), list(range(200, 300))],
+                         ids=lambda v: f"{len(v)}kept")
+def test_ignored_tokens(kept, dtype, d):
     """From every token ignored to half of them in turn; the others' values do not matter."""
-    h, W, tokens, gl = _draw(300, 96, 700, dtype, 3, ignore=0.0)
+    h, W, tokens, gl = _draw(300, d, 700, dtype, 3, ignore=0.0)
     ignored = torch.ones(300, dtype=torch.bool, device=DEV)
     ignored[kept] = False
     tokens[ignored] = -100
@@ -128,10 +129,10 @@ def test_tokens_out_of_range_are_ignored_and_flagged():
     assert flags() == B.MLS_DEVFLAG_NONFINITE and torch.isnan(logp[11])
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_vocabulary_chunks(dtype):
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.bfloat16, 2048), (torch.float32, 128)])
+def test_vocabulary_chunks(dtype, d):
     """One chunk, and chunks that the vocabulary does not fill: the same gradients."""
-    h, W, tokens, gl = _draw(200, 128, 3000, dtype, 5)
+    h, W, tokens, gl = _draw(200, d, 3000, dtype, 5)
     for chunk in (256, 1024, 1 << 20):
         _check(h, W, tokens, gl, 0.9, _run(h, W, tokens, gl, temperature=0.9, vocab_chunk=chunk), f"chunk {chunk}")
 
