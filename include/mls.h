@@ -317,7 +317,7 @@ mls_status mls_junction_bwd(const mls_junction* j, const void* o, const void* e,
  */
 typedef struct mls_layer_norm {
   int64_t T;            /* rows, >= 1 */
-  int64_t d;            /* width, 1..16384 (multiples of 8 (bf16) or 4 (f32) take wide accesses) */
+  int64_t d;            /* width, 1..16384 */
   int64_t ld_x;         /* elements between rows of x, >= d: x may be columns of a wider array */
   int32_t act_dtype;    /* mls_dtype of x, y, g_y and g_x */
   int32_t param_dtype;  /* mls_dtype of weight, bias and their gradients */
@@ -329,9 +329,8 @@ typedef struct mls_layer_norm {
  * Forward: y [T][d] from x ([T] rows of d entries, ld_x apart), weight [d] and bias
  * [d] (may be NULL). stats (device float32 [2][T]: each row's mean, then its
  * 1 / sqrt(variance + eps)) is what the backward reads; NULL if none follows. y
- * must not overlap x. Pointers need their element's alignment; rows whose
- * addresses, width and stride are multiples of 16 bytes are the fast ones.
- * Asynchronous on stream.
+ * must not overlap x. Pointers need their element's alignment only. Asynchronous on
+ * stream.
  */
 mls_status mls_layer_norm_fwd(const mls_layer_norm* n, const void* x, const void* weight,
                               const void* bias, void* y, float* stats, void* stream);

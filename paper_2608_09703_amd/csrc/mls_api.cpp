@@ -1599,17 +1599,9 @@ NormArgs norm_args(const mls_layer_norm* n, const NormShape& sh) {
   return a;
 }
 
-// Rows of 16-byte chunks: the row length and stride and every row array's address.
-bool norm_vec(const mls_layer_norm* n, const void* x, const void* p, const void* q) {
-  const int64_t ve = n->act_dtype == MLS_F32 ? 4 : 8;
-  return n->d % ve == 0 && n->ld_x % ve == 0 && aligned(x, 16) && aligned(p, 16) && aligned(q, 16);
-}
-
 size_t norm_part_bytes(const mls_layer_norm* n) {
-  const bool f32 = n->act_dtype == MLS_F32;
-  const int blocks = std::max(norm_shape(n->T, n->d, f32, true, true).blocks,
-                              norm_shape(n->T, n->d, f32, false, true).blocks);
-  return align256((size_t)blocks * 2 * n->d * sizeof(float));
+  const NormShape sh = norm_shape(n->T, n->d, n->act_dtype == MLS_F32, true);
+  return align256((size_t)sh.blocks * 2 * n->d * sizeof(float));
 }
 
 }  // namespace
@@ -1628,7 +1620,7 @@ mls_status mls_layer_norm_fwd(const mls_layer_norm* n, const void* x, const void
   if (!disjoint(y, (size_t)n->T * n->d * es, x, ((size_t)(n->T - 1) * n->ld_x + n->d) * es))
     return fail(MLS_INVALID_ARG, "y overlaps x");
   const bool f32 = n->act_dtype == MLS_F32;
-  const NormShape sh = norm_shape(n->T, n->d, f32, norm_vec(n, x, y, nullptr), false);
+  const NormShape sh = norm_shape(n->T, n->d, f32, false);
   NormArgs a = norm_args(n, sh);
   a.x = x;
   a.weight = weight;
@@ -1674,7 +1666,7 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
     return fail(MLS_WORKSPACE_TOO_SMALL, "layer norm backward needs %zu workspace bytes, got %zu",
                 norm_part_bytes(n), workspace ? workspace_bytes : (size_t)0);
   const bool f32 = n->act_dtype == MLS_F32;
-  const NormShape sh = norm_shape(n->T, n->d, f32, norm_vec(n, x, g_y, g_x), true);
+  const NormShape sh = norm_shape(n->T, n->d, f32, true);
   NormArgs a = norm_args(n, sh);
   a.x = x;
   a.weight = weight;

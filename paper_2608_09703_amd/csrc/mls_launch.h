@@ -320,14 +320,15 @@ struct NormArgs {
   void* g_weight;       // [d] or null
   void* g_bias;         // [d] or null
 };
-// How a norm is laid over the chip: waves per row, 16-byte chunks per lane, rows
-// a block takes at a time, blocks, and whether rows take 16-byte accesses.
+// How a norm is laid over the chip: 16-byte chunks per lane, waves per row, groups
+// of such waves in a block, rows a group takes at a time, blocks, cache policy.
 struct NormShape {
   int cpl;
   int waves;
   int groups;
+  int rows;
   int blocks;
-  bool vec;
+  bool nt;  // non-temporal accesses
 };
 
 // Clipped policy loss.
@@ -475,7 +476,7 @@ int64_t junction_max_width();
 hipError_t launch_junction_fwd(const JunctionArgs& a, bool act_f32, hipStream_t stream);
 hipError_t launch_junction_bwd(const JunctionArgs& a, bool act_f32, bool grad_f32, hipStream_t stream);
 int64_t norm_max_width();
-NormShape norm_shape(int64_t T, int64_t d, bool f32, bool vec, bool bwd);
+NormShape norm_shape(int64_t T, int64_t d, bool f32, bool bwd);
 hipError_t launch_layer_norm_fwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
 hipError_t launch_layer_norm_bwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
 hipError_t launch_layer_norm_params(const NormArgs& a, int n_parts, hipStream_t stream);

@@ -5,14 +5,18 @@
 //   gw = sum_t gy xh,   gb = sum_t gy.
 //
 // Memory-bound: a pass reads and writes each row once. The W waves of a row hold
-// it in registers, CPL chunks of 16 bytes a lane, so the deviations are taken
-// from the mean itself (no sum of squares to cancel against). Each wave centres
-// its own part first and the parts are joined by the pairwise formula
+// it in registers as it was loaded, CPL chunks of 16 bytes a lane, so the deviations
+// are taken from the mean itself (no sum of squares to cancel against). Each wave
+// centres its own part first and the parts are joined by the pairwise formula
 //   sum (x - mu)^2 = sum_w [ M_w + n_w (mu_w - mu)^2 ],
-// which costs one barrier a row. A block takes G rows at a time and goes on by
-// gridDim.x * G, with w and b (backward: w and the running sums of gw and gb) in
-// registers; a block's parts of gw and gb leave once, in fp32, and a second
-// kernel adds them in block order, so the results are bitwise reproducible.
+// which costs one barrier. R rows go through it together, so that enough loads are
+// in flight for each. A block takes G * R rows at a time and goes on by gridDim.x *
+// G * R, with w and b (backward: w and the running sums of gw and gb) in registers;
+// a block's parts of gw and gb leave once, in fp32, and a second kernel adds them in
+// block order, so the results are bitwise reproducible.
+//
+// Rows may begin at any element: 16-byte accesses need no 16-byte address here. Only
+// a width that is no multiple of the chunk has a last, partial chunk (TAIL).
 #include <math.h>
 
 #include <algorithm>
@@ -26,224 +30,326 @@ namespace mls {
 
 namespace {
 
-constexpr int kNormMaxWaves = 16;
-constexpr int kNormLaneElts = 16;  // entries of a row per lane: more spill in the backward's 128 registers
+constexpr int kNormMaxWaves = 16;  // of a row, and of a block
+constexpr int kNormMaxRows = 4;    // a group takes together
 constexpr int64_t kNormMaxWidth = 16384;
 constexpr int kNormRedCols = 64;
 constexpr int kNormRedRows = 16;
 
-// Which entries of a row a lane holds: element i of chunk c of lane j among the
-// row's L lanes. VEC: 16 consecutive bytes a chunk. Otherwise (a width, stride or
-// address that is no multiple of 16 bytes) single entries, neighbours in
-// neighbouring lanes.
-template <typename A, bool VEC>
-struct RowMap {
-  static constexpr int VE = 16 / A::kBytes;
-  __device__ __forceinline__ static int at(int c, int i, int j, int L) {
-    return VEC ? (c * L + j) * VE + i : (c * VE + i) * L + j;
+// 16 bytes at an element's address
+typedef unsigned int u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+template <bool NT>
+__device__ __forceinline__ uint4 load16_any(const void* p) {
+  const u32x4_any_t* q = static_cast<const u32x4_any_t*>(p);
+  const u32x4_any_t v = NT ? __builtin_nontemporal_load(q) : *q;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool NT>
+__device__ __forceinline__ void store16_any(void* p, uint4 v) {
+  const u32x4_any_t w = {v.x, v.y, v.z, v.w};
+  if (NT)
+    __builtin_nontemporal_store(w, static_cast<u32x4_any_t*>(p));
+  else
+    *static_cast<u32x4_any_t*>(p) = w;
+}
+
+// A chunk of 16 bytes: kN elements.
+template <typename A>
+struct Chunk;
+template <>
+struct Chunk<Bf16> {
+  static constexpr int kN = 8;
+  __device__ __forceinline__ static void unpack(uint4 r, float* v) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ static uint4 pack(const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (uint32_t)to_storage<Bf16>(v[2 * i]) | ((uint32_t)to_storage<Bf16>(v[2 * i + 1]) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Chunk<F32> {
+  static constexpr int kN = 4;
+  __device__ __forceinline__ static void unpack(uint4 r, float* v) {
+    v[0] = __uint_as_float(r.x);
+    v[1] = __uint_as_float(r.y);
+    v[2] = __uint_as_float(r.z);
+    v[3] = __uint_as_float(r.w);
+  }
+  __device__ __forceinline__ static uint4 pack(const float* v) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
   }
 };
 
 __device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float widen(float v) { return v; }
 
-template <bool NT>
-__device__ __forceinline__ void load_chunk(const uint16_t* p, float* v) { load8<NT>(p, v); }
-template <bool NT>
-__device__ __forceinline__ void load_chunk(const float* p, float* v) { load4<NT>(p, v); }
-template <bool NT>
-__device__ __forceinline__ void store_chunk(uint16_t* p, const float* v) { store8<NT>(p, v); }
-template <bool NT>
-__device__ __forceinline__ void store_chunk(float* p, const float* v) { store4<NT>(p, v); }
+// Chunk c of lane j holds entries [at, at + kN) of a row of L lanes.
+template <typename A>
+__device__ __forceinline__ int chunk_at(int c, int j, int L) {
+  return (c * L + j) * Chunk<A>::kN;
+}
 
-// A row's entries of this lane; zeros past the row's end and on dead rows.
-template <typename A, int CPL, bool VEC>
+// A row's chunks of this lane, as stored; zeros past the row's end and on dead rows.
+template <typename A, int CPL, bool NT>
 __device__ __forceinline__ void load_row(const typename Elt<A>::type* p, int d, int j, int L, bool live,
-                                         float (&v)[CPL][RowMap<A, VEC>::VE]) {
-  using M = RowMap<A, VEC>;
+                                         uint4 (&v)[CPL]) {
+  constexpr int N = Chunk<A>::kN;
 #pragma unroll
   for (int c = 0; c < CPL; ++c) {
-    if (VEC) {
-      const int k = M::at(c, 0, j, L);
-      if (live && k < d) {
-        load_chunk<false>(p + k, v[c]);
+    const int k = chunk_at<A>(c, j, L);
+    v[c] = make_uint4(0, 0, 0, 0);
+    if (live && k + N <= d) {
+      v[c] = load16_any<NT>(p + k);
+    } else if (live && k < d) {
+      float e[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) e[i] = k + i < d ? widen(p[k + i]) : 0.f;
+      v[c] = Chunk<A>::pack(e);  // exact: the values are of the type
+    }
+  }
+}
+
+template <typename A, bool NT>
+__device__ __forceinline__ void store_chunk(typename Elt<A>::type* p, int d, int k, const float* v) {
+  constexpr int N = Chunk<A>::kN;
+  if (k + N <= d) {
+    store16_any<NT>(p + k, Chunk<A>::pack(v));
+  } else if (k < d) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (k + i < d) p[k + i] = to_storage<A>(v[i]);
+  }
+}
+
+// Where the waves of a row leave their parts: wave k of group g puts row q's at slot
+// (q, its own), and lane 16 q + k of every wave of the group reads it back, so that
+// one read and a sum over 16 lanes join up to four rows.
+struct RowSlots {
+  int W, wave, first, lane, k, q;
+  __device__ __forceinline__ RowSlots(int waves, int g)
+      : W(waves), wave(threadIdx.x >> 6), first(g * waves), lane(threadIdx.x & 63), k(lane & 15), q(lane >> 4) {}
+  __device__ __forceinline__ int mine(int row) const { return row * kNormMaxWaves + wave; }
+  __device__ __forceinline__ bool live(int rows) const { return k < W && q < rows; }
+  __device__ __forceinline__ int theirs() const { return q * kNormMaxWaves + first + k; }
+};
+
+// Entries of a parameter (bf16 or fp32) in the lane's layout; zeros past the end.
+// Wide loads: a block's first rows wait for these.
+template <typename A, int CPL>
+__device__ __forceinline__ void load_param(const void* p, bool f32, int d, int j, int L,
+                                           float (&v)[CPL][Chunk<A>::kN]) {
+  constexpr int N = Chunk<A>::kN;
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) {
+    const int k = chunk_at<A>(c, j, L);
+    if (k + N <= d) {
+      uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+      if (f32) {
+#pragma unroll
+        for (int h = 0; h < N / 4; ++h) raw[h] = load16_any<false>(static_cast<const float*>(p) + k + 4 * h);
+      } else if (N == 8) {
+        raw[0] = load16_any<false>(static_cast<const uint16_t*>(p) + k);
       } else {
-#pragma unroll
-        for (int i = 0; i < M::VE; ++i) v[c][i] = 0.f;
+        typedef unsigned int u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
+        const u32x2_any_t r = *reinterpret_cast<const u32x2_any_t*>(static_cast<const uint16_t*>(p) + k);
+        raw[0].x = r.x;
+        raw[0].y = r.y;
       }
+      float x[8], y[8];
+      Chunk<F32>::unpack(raw[0], x);
+      Chunk<F32>::unpack(raw[1], x + 4);
+      Chunk<Bf16>::unpack(raw[0], y);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[c][i] = f32 ? x[i] : y[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) {
-        const int k = M::at(c, i, j, L);
-        v[c][i] = (live && k < d) ? widen(p[k]) : 0.f;
-      }
+      for (int i = 0; i < N; ++i)
+        v[c][i] = k + i >= d ? 0.f
+                  : f32      ? static_cast<const float*>(p)[k + i]
+                             : widen(static_cast<const uint16_t*>(p)[k + i]);
     }
   }
 }
 
-template <typename A, int CPL, bool VEC>
-__device__ __forceinline__ void store_row(typename Elt<A>::type* p, int d, int j, int L,
-                                          const float (&v)[CPL][RowMap<A, VEC>::VE]) {
-  using M = RowMap<A, VEC>;
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) {
-    if (VEC) {
-      const int k = M::at(c, 0, j, L);
-      if (k < d) store_chunk<false>(p + k, v[c]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < M::VE; ++i) {
-        const int k = M::at(c, i, j, L);
-        if (k < d) p[k] = to_storage<A>(v[c][i]);
-      }
-    }
-  }
-}
-
-// Entries of a parameter (bf16 or fp32) in the lane's layout; `fill` past the end.
-template <typename A, int CPL, bool VEC>
-__device__ __forceinline__ void load_param(const void* p, bool f32, int d, int j, int L, float fill,
-                                           float (&v)[CPL][RowMap<A, VEC>::VE]) {
-  using M = RowMap<A, VEC>;
-#pragma unroll
-  for (int c = 0; c < CPL; ++c)
-#pragma unroll
-    for (int i = 0; i < M::VE; ++i) {
-      const int k = M::at(c, i, j, L);
-      v[c][i] = k >= d ? fill : f32 ? static_cast<const float*>(p)[k] : widen(static_cast<const uint16_t*>(p)[k]);
-    }
-}
-
-template <typename A, int CPL, bool VEC, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 512) void layer_norm_fwd_kernel(NormArgs a) {
-  using M = RowMap<A, VEC>;
+template <typename A, int CPL, int R, bool TAIL, bool MULTI, bool NT>
+__global__ __launch_bounds__(MULTI ? 1024 : 256) void layer_norm_fwd_kernel(NormArgs a) {
   typedef typename Elt<A>::type TA;
-  __shared__ float4 red[2][kNormMaxWaves];
+  constexpr int N = Chunk<A>::kN;
+  __shared__ float4 red[2][kNormMaxWaves * kNormMaxRows];
   const int d = a.d, W = a.waves, L = W * 64, G = blockDim.x / L;
   const int g = threadIdx.x / L, j = threadIdx.x % L;
-  const int wave = threadIdx.x >> 6, first = g * W;
-  float w[CPL][M::VE], b[CPL][M::VE], x[CPL][M::VE];
-  load_param<A, CPL, VEC>(a.weight, a.param_f32, d, j, L, 0.f, w);
+  const RowSlots sl(W, g);
+  float w[CPL][N], b[CPL][N];
+  load_param<A, CPL>(a.weight, a.param_f32, d, j, L, w);
   if (a.bias)
-    load_param<A, CPL, VEC>(a.bias, a.param_f32, d, j, L, 0.f, b);
+    load_param<A, CPL>(a.bias, a.param_f32, d, j, L, b);
   else
 #pragma unroll
     for (int c = 0; c < CPL; ++c)
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) b[c][i] = 0.f;
+      for (int i = 0; i < N; ++i) b[c][i] = 0.f;
   float n = 0.f;  // entries of this wave
 #pragma unroll
-  for (int c = 0; c < CPL; ++c)
-#pragma unroll
-    for (int i = 0; i < M::VE; ++i) n += M::at(c, i, j, L) < d ? 1.f : 0.f;
+  for (int c = 0; c < CPL; ++c) n += (float)min(N, max(0, d - chunk_at<A>(c, j, L)));
   n = wave_sum(n);
   // means by division: exact where the sum is (a constant row has no deviations)
   const float fn = n > 0.f ? n : 1.f, fd = (float)d;
   int par = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * G; t0 < a.T; t0 += (int64_t)gridDim.x * G, par ^= 1) {
-    const int64_t t = t0 + g;
-    const bool live = t < a.T;  // dead rows still join the barriers
-    load_row<A, CPL, VEC>(static_cast<const TA*>(a.x) + t * a.ld_x, d, j, L, live, x);
-    float s = 0.f;
+  for (int64_t t0 = (int64_t)blockIdx.x * G * R; t0 < a.T; t0 += (int64_t)gridDim.x * G * R, par ^= 1) {
+    uint4 x[R][CPL];
+    float mu[R], var[R];
 #pragma unroll
-    for (int c = 0; c < CPL; ++c)
+    for (int q = 0; q < R; ++q) {
+      const int64_t t = t0 + q * G + g;  // dead rows still join the barrier
+      load_row<A, CPL, NT>(static_cast<const TA*>(a.x) + t * a.ld_x, d, j, L, t < a.T, x[q]);
+    }
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) s += x[c][i];
-    s = wave_sum(s);
-    const float mw = s / fn;
-    float q = 0.f;
+    for (int q = 0; q < R; ++q) {
+      float v[CPL][N], s = 0.f, m2 = 0.f;
 #pragma unroll
-    for (int c = 0; c < CPL; ++c)
+      for (int c = 0; c < CPL; ++c) {
+        Chunk<A>::unpack(x[q][c], v[c]);
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) {
-        const float e = M::at(c, i, j, L) < d ? x[c][i] - mw : 0.f;
-        q = fmaf(e, e, q);
+        for (int i = 0; i < N; ++i) s += v[c][i];
       }
-    q = wave_sum(q);
-    float mu = mw, var = q;
+      s = wave_sum(s);
+      const float mw = s / fn;
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        const int k = chunk_at<A>(c, j, L);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float e = k + (TAIL ? i : 0) < d ? v[c][i] - mw : 0.f;
+          m2 = fmaf(e, e, m2);
+        }
+      }
+      m2 = wave_sum(m2);
+      mu[q] = mw;
+      var[q] = m2;
+      if (MULTI && sl.lane == 0) red[par][sl.mine(q)] = make_float4(s, m2, n, mw);
+    }
     if (MULTI) {
-      if ((threadIdx.x & 63) == 0) red[par][wave] = make_float4(s, q, n, mw);
       __syncthreads();
-      float tot = 0.f;
-      for (int k = 0; k < W; ++k) tot += red[par][first + k].x;
-      mu = tot / fd;
-      var = 0.f;
-      for (int k = 0; k < W; ++k) {
-        const float4 p = red[par][first + k];
-        const float e = p.w - mu;
-        var += fmaf(p.z * e, e, p.y);
+      const float4 p = sl.live(R) ? red[par][sl.theirs()] : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float m = row16_sum(p.x) / fd;
+      const float e = p.w - m;
+      const float v = row16_sum(fmaf(p.z * e, e, p.y));
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        mu[q] = lane_read(m, 16 * q);
+        var[q] = lane_read(v, 16 * q);
       }
     }
-    const float r = 1.f / sqrtf(var / fd + a.eps);
-    if (!live) continue;
-    if (a.stats && j == 0) {
-      a.stats[t] = mu;
-      a.stats[a.T + t] = r;
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const int64_t t = t0 + q * G + g;
+      if (t >= a.T) continue;
+      const float r = 1.f / sqrtf(var[q] / fd + a.eps);
+      if (a.stats && j == 0) {
+        a.stats[t] = mu[q];
+        a.stats[a.T + t] = r;
+      }
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        float v[N];
+        Chunk<A>::unpack(x[q][c], v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = fmaf((v[i] - mu[q]) * r, w[c][i], b[c][i]);
+        store_chunk<A, NT>(static_cast<TA*>(a.y) + t * d, d, chunk_at<A>(c, j, L), v);
+      }
     }
-#pragma unroll
-    for (int c = 0; c < CPL; ++c)
-#pragma unroll
-      for (int i = 0; i < M::VE; ++i) x[c][i] = fmaf((x[c][i] - mu) * r, w[c][i], b[c][i]);
-    store_row<A, CPL, VEC>(static_cast<TA*>(a.y) + t * d, d, j, L, x);
   }
 }
 
-template <typename A, int CPL, bool VEC, bool MULTI>
+template <typename A, int CPL, int R, bool MULTI, bool NT>
 __global__ __launch_bounds__(MULTI ? 1024 : 512) void layer_norm_bwd_kernel(NormArgs a) {
-  using M = RowMap<A, VEC>;
   typedef typename Elt<A>::type TA;
-  __shared__ float2 red[2][kNormMaxWaves];
+  constexpr int N = Chunk<A>::kN;
+  __shared__ float2 red[2][kNormMaxWaves * kNormMaxRows];
   extern __shared__ float sums[];  // [2][d], only with G > 1
   const int d = a.d, W = a.waves, L = W * 64, G = blockDim.x / L;
   const int g = threadIdx.x / L, j = threadIdx.x % L;
-  const int wave = threadIdx.x >> 6, first = g * W;
+  const RowSlots sl(W, g);
   const float inv_d = 1.f / (float)d;
-  float w[CPL][M::VE], gw[CPL][M::VE], gb[CPL][M::VE], x[CPL][M::VE], u[CPL][M::VE];
-  load_param<A, CPL, VEC>(a.weight, a.param_f32, d, j, L, 0.f, w);
+  float w[CPL][N], gw[CPL][N], gb[CPL][N];
+  load_param<A, CPL>(a.weight, a.param_f32, d, j, L, w);
 #pragma unroll
   for (int c = 0; c < CPL; ++c)
 #pragma unroll
-    for (int i = 0; i < M::VE; ++i) gw[c][i] = gb[c][i] = 0.f;
+    for (int i = 0; i < N; ++i) gw[c][i] = gb[c][i] = 0.f;
   int par = 0;
-  for (int64_t t0 = (int64_t)blockIdx.x * G; t0 < a.T; t0 += (int64_t)gridDim.x * G, par ^= 1) {
-    const int64_t t = t0 + g;
-    const bool live = t < a.T;
-    load_row<A, CPL, VEC>(static_cast<const TA*>(a.x) + t * a.ld_x, d, j, L, live, x);
-    load_row<A, CPL, VEC>(static_cast<const TA*>(a.g_y) + t * d, d, j, L, live, u);
-    const float mu = live ? a.stats[t] : 0.f, r = live ? a.stats[a.T + t] : 0.f;
-    float s0 = 0.f, s1 = 0.f;
+  for (int64_t t0 = (int64_t)blockIdx.x * G * R; t0 < a.T; t0 += (int64_t)gridDim.x * G * R, par ^= 1) {
+    uint4 x[R][CPL], y[R][CPL];
+    float mu[R], r[R], s0[R], s1[R];
 #pragma unroll
-    for (int c = 0; c < CPL; ++c)
+    for (int q = 0; q < R; ++q) {
+      const int64_t t = t0 + q * G + g;
+      const bool live = t < a.T;
+      load_row<A, CPL, NT>(static_cast<const TA*>(a.x) + t * a.ld_x, d, j, L, live, x[q]);
+      load_row<A, CPL, NT>(static_cast<const TA*>(a.g_y) + t * d, d, j, L, live, y[q]);
+      mu[q] = live ? a.stats[t] : 0.f;
+      r[q] = live ? a.stats[a.T + t] : 0.f;
+    }
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) {
-        // past the end of a row u and w are 0
-        const float xh = (x[c][i] - mu) * r, gy = u[c][i];
-        gw[c][i] = fmaf(gy, xh, gw[c][i]);
-        gb[c][i] += gy;
-        x[c][i] = xh;
-        u[c][i] = gy * w[c][i];
-        s0 += u[c][i];
-        s1 = fmaf(u[c][i], xh, s1);
+    for (int q = 0; q < R; ++q) {
+      s0[q] = s1[q] = 0.f;
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        float xv[N], gv[N];
+        Chunk<A>::unpack(x[q][c], xv);
+        Chunk<A>::unpack(y[q][c], gv);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          // past the end of a row gy and w are 0
+          const float xh = (xv[i] - mu[q]) * r[q], u = gv[i] * w[c][i];
+          gw[c][i] = fmaf(gv[i], xh, gw[c][i]);
+          gb[c][i] += gv[i];
+          s0[q] += u;
+          s1[q] = fmaf(u, xh, s1[q]);
+        }
       }
-    s0 = wave_sum(s0);
-    s1 = wave_sum(s1);
+      s0[q] = wave_sum(s0[q]);
+      s1[q] = wave_sum(s1[q]);
+      if (MULTI && sl.lane == 0) red[par][sl.mine(q)] = make_float2(s0[q], s1[q]);
+    }
     if (MULTI) {
-      if ((threadIdx.x & 63) == 0) red[par][wave] = make_float2(s0, s1);
       __syncthreads();
-      s0 = s1 = 0.f;
-      for (int k = 0; k < W; ++k) {
-        const float2 p = red[par][first + k];
-        s0 += p.x;
-        s1 += p.y;
+      const float2 p = sl.live(R) ? red[par][sl.theirs()] : make_float2(0.f, 0.f);
+      const float p0 = row16_sum(p.x), p1 = row16_sum(p.y);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        s0[q] = lane_read(p0, 16 * q);
+        s1[q] = lane_read(p1, 16 * q);
       }
     }
-    if (!live || !a.g_x) continue;
-    const float c0 = s0 * inv_d, c1 = s1 * inv_d;
+    if (!a.g_x) continue;
 #pragma unroll
-    for (int c = 0; c < CPL; ++c)
+    for (int q = 0; q < R; ++q) {
+      const int64_t t = t0 + q * G + g;
+      if (t >= a.T) continue;
+      const float c0 = s0[q] * inv_d, c1 = s1[q] * inv_d;
 #pragma unroll
-      for (int i = 0; i < M::VE; ++i) x[c][i] = r * (u[c][i] - fmaf(x[c][i], c1, c0));
-    store_row<A, CPL, VEC>(static_cast<TA*>(a.g_x) + t * d, d, j, L, x);
+      for (int c = 0; c < CPL; ++c) {
+        float xv[N], gv[N];
+        Chunk<A>::unpack(x[q][c], xv);
+        Chunk<A>::unpack(y[q][c], gv);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float xh = (xv[i] - mu[q]) * r[q];
+          gv[i] = r[q] * (fmaf(gv[i], w[c][i], -c0) - xh * c1);
+        }
+        store_chunk<A, NT>(static_cast<TA*>(a.g_x) + t * d, d, chunk_at<A>(c, j, L), gv);
+      }
+    }
   }
   // the block's parts: the groups' sums one after the other, in group order
   if (!a.part) return;
@@ -253,8 +359,8 @@ __global__ __launch_bounds__(MULTI ? 1024 : 512) void layer_norm_bwd_kernel(Norm
 #pragma unroll
       for (int c = 0; c < CPL; ++c)
 #pragma unroll
-        for (int i = 0; i < M::VE; ++i) {
-          const int e = M::at(c, i, j, L);
+        for (int i = 0; i < N; ++i) {
+          const int e = chunk_at<A>(c, j, L) + i;
           if (e >= d) continue;
           float vw = gw[c][i], vb = gb[c][i];
           if (k > 0) {
@@ -300,78 +406,86 @@ __global__ __launch_bounds__(kNormRedCols* kNormRedRows) void layer_norm_param_k
     static_cast<uint16_t*>(out)[k] = to_storage<Bf16>(s);
 }
 
-template <typename A, int CPL, bool VEC>
-hipError_t launch_fwd_shape(const NormArgs& a, const NormShape& sh, hipStream_t s) {
+template <typename A, int CPL, int R, bool MULTI, bool NT>
+hipError_t launch_shape(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
   const dim3 grid(sh.blocks), block(sh.waves * sh.groups * 64);
-  if (sh.waves > 1)
-    hipLaunchKernelGGL((layer_norm_fwd_kernel<A, CPL, VEC, true>), grid, block, 0, s, a);
+  const size_t lds = bwd && sh.groups > 1 && a.part ? 2 * (size_t)a.d * sizeof(float) : 0;
+  if (bwd)
+    hipLaunchKernelGGL((layer_norm_bwd_kernel<A, CPL, R, MULTI, NT>), grid, block, lds, s, a);
+  else if (a.d % Chunk<A>::kN)
+    hipLaunchKernelGGL((layer_norm_fwd_kernel<A, CPL, R, true, MULTI, NT>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((layer_norm_fwd_kernel<A, CPL, VEC, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((layer_norm_fwd_kernel<A, CPL, R, false, MULTI, NT>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
-template <typename A, int CPL, bool VEC>
-hipError_t launch_bwd_shape(const NormArgs& a, const NormShape& sh, hipStream_t s) {
-  const dim3 grid(sh.blocks), block(sh.waves * sh.groups * 64);
-  const size_t lds = sh.groups > 1 && a.part ? 2 * (size_t)a.d * sizeof(float) : 0;
-  if (sh.waves > 1)
-    hipLaunchKernelGGL((layer_norm_bwd_kernel<A, CPL, VEC, true>), grid, block, lds, s, a);
-  else
-    hipLaunchKernelGGL((layer_norm_bwd_kernel<A, CPL, VEC, false>), grid, block, lds, s, a);
-  return hipGetLastError();
-}
-
-template <typename A, bool VEC>
-hipError_t launch_norm_cpl(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
-  if (sh.cpl == 1) return bwd ? launch_bwd_shape<A, 1, VEC>(a, sh, s) : launch_fwd_shape<A, 1, VEC>(a, sh, s);
-  if (sh.cpl == 2) return bwd ? launch_bwd_shape<A, 2, VEC>(a, sh, s) : launch_fwd_shape<A, 2, VEC>(a, sh, s);
+template <typename A, bool MULTI, bool NT>
+hipError_t launch_rows(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
+  if (sh.cpl == 1 && sh.rows == 1) return launch_shape<A, 1, 1, MULTI, NT>(a, sh, bwd, s);
+  if (sh.cpl == 1 && sh.rows == 2) return launch_shape<A, 1, 2, MULTI, NT>(a, sh, bwd, s);
+  if (sh.cpl == 2 && sh.rows == 1) return launch_shape<A, 2, 1, MULTI, NT>(a, sh, bwd, s);
   if constexpr (A::kBytes == 4) {
-    if (sh.cpl == 3) return bwd ? launch_bwd_shape<A, 3, VEC>(a, sh, s) : launch_fwd_shape<A, 3, VEC>(a, sh, s);
-    if (sh.cpl == 4) return bwd ? launch_bwd_shape<A, 4, VEC>(a, sh, s) : launch_fwd_shape<A, 4, VEC>(a, sh, s);
+    if (sh.cpl == 4 && sh.rows == 1) return launch_shape<A, 4, 1, MULTI, NT>(a, sh, bwd, s);
   }
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_norm(const NormArgs& a, const NormShape& sh, bool f32, bool bwd, hipStream_t s) {
-  const int ve = f32 ? 4 : 8;
-  if (sh.waves < 1 || sh.waves * sh.groups > kNormMaxWaves || sh.blocks < 1 ||
-      (int64_t)sh.waves * 64 * sh.cpl * ve < a.d || a.waves != sh.waves)
+template <typename A>
+hipError_t launch_norm(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
+  if (sh.waves < 1 || sh.groups < 1 || sh.waves * sh.groups > (sh.waves > 1 ? kNormMaxWaves : bwd ? 8 : 4) ||
+      sh.blocks < 1 || (int64_t)sh.waves * 64 * sh.cpl * Chunk<A>::kN < a.d || a.waves != sh.waves)
     return hipErrorInvalidValue;
-  if (sh.vec)
-    return f32 ? launch_norm_cpl<F32, true>(a, sh, bwd, s) : launch_norm_cpl<Bf16, true>(a, sh, bwd, s);
-  return f32 ? launch_norm_cpl<F32, false>(a, sh, bwd, s) : launch_norm_cpl<Bf16, false>(a, sh, bwd, s);
+  if (sh.waves > 1)
+    return sh.nt ? launch_rows<A, true, true>(a, sh, bwd, s) : launch_rows<A, true, false>(a, sh, bwd, s);
+  return sh.nt ? launch_rows<A, false, true>(a, sh, bwd, s) : launch_rows<A, false, false>(a, sh, bwd, s);
 }
 
 }  // namespace
 
 int64_t norm_max_width() { return kNormMaxWidth; }
 
-NormShape norm_shape(int64_t T, int64_t d, bool f32, bool vec, bool bwd) {
+// Chosen by timing, forward / backward us (each pass in a process of its own order,
+// the least of two to four):
+// - waves: one chunk a lane while a row then has at most 4 (fp32: 8) waves, else two
+//   (fp32: up to four). 32768 x 4352 bf16, 9 waves of one chunk against 5 of two:
+//   144 / 187 and 127 / 162; 16384 x 2305 bf16, 5 against 3: 50 / 81 and 44 / 66;
+//   16384 x 4096 fp32, 8 of two against 4 of four: 93 / 136 and 93 / 143.
+// - rows: two at a time with one chunk a lane, where every block has them. 32768 x
+//   1024 bf16, four, two, one: 32 / 43, 28 / 40, 32 / 39; four spill at 16 entries a
+//   lane.
+// - blocks: at 32768 x 4352 the forward takes 115 to 124 us with 1024 to 3072 blocks
+//   and 197 with 16384, whose first rows wait for weight and bias; at 32768 x 1024 it
+//   takes 31 with 1024 and 28 with 3072. The backward's parts are read again: 512 or
+//   768 blocks 162 / 193.
+// - non-temporal accesses where a row array is 64 MiB or more (32768 x 4352: 153 -> 137
+//   us forward, 190 -> 162 backward with its shape; 16384 x 4096 fp32 backward 158 ->
+//   136) and the default below, where the caches still hold what comes next (4096 x
+//   2304 bf16: 20 -> 23 with them).
+// At 32768 x 4352 the two passes move 570 and 856 MB: 4.6 and 5.3 TB/s of the 5.1 that
+// a device copy of this size reaches.
+NormShape norm_shape(int64_t T, int64_t d, bool f32, bool bwd) {
+  constexpr int64_t kFwdBlocks = 3072, kBwdBlocks = 512, kNtBytes = 64ll << 20;
   NormShape sh;
-  const int ve = f32 ? 4 : 8;
-  const int chunks = (int)((d + ve - 1) / ve);
-  sh.cpl = sh.waves = 0;
-  for (int c = 1; c <= kNormLaneElts / ve; ++c) {
-    const int w = (chunks + 64 * c - 1) / (64 * c);
-    // fewest idle lanes, then the fewest waves
-    if (w <= kNormMaxWaves && (sh.cpl == 0 || c * w <= sh.cpl * sh.waves)) {
-      sh.cpl = c;
-      sh.waves = w;
-    }
+  const int n = f32 ? 4 : 8, max_waves = f32 ? 8 : 4;
+  const int chunks = (int)((d + n - 1) / n);
+  for (sh.cpl = 1; chunks > 64 * sh.cpl * max_waves && sh.cpl < 16 / n; sh.cpl *= 2) {
   }
-  sh.vec = vec;
-  sh.groups = sh.waves >= 4 ? 1 : sh.waves == 1 ? 4 : 2;
-  const int64_t most = bwd ? 512 : 2048;
-  sh.blocks = (int)std::min<int64_t>(most, (T + sh.groups - 1) / sh.groups);
+  sh.waves = (chunks + 64 * sh.cpl - 1) / (64 * sh.cpl);
+  sh.groups = std::max(1, (bwd ? 8 : 4) / sh.waves);
+  const int64_t most = bwd ? kBwdBlocks : kFwdBlocks;
+  sh.rows = sh.cpl == 1 && T >= most * sh.groups * 2 ? 2 : 1;
+  const int64_t step = (int64_t)sh.groups * sh.rows;
+  sh.blocks = (int)std::min<int64_t>(most, (T + step - 1) / step);
+  sh.nt = T * d * (f32 ? 4 : 2) >= kNtBytes;
   return sh;
 }
 
 hipError_t launch_layer_norm_fwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream) {
-  return launch_norm(a, sh, f32, false, stream);
+  return f32 ? launch_norm<F32>(a, sh, false, stream) : launch_norm<Bf16>(a, sh, false, stream);
 }
 
 hipError_t launch_layer_norm_bwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream) {
-  return launch_norm(a, sh, f32, true, stream);
+  return f32 ? launch_norm<F32>(a, sh, true, stream) : launch_norm<Bf16>(a, sh, true, stream);
 }
 
 hipError_t launch_layer_norm_params(const NormArgs& a, int n_parts, hipStream_t stream) {

@@ -9,7 +9,8 @@ K = 64 this bounds xh by K u s, s = |xh| + r mean|x|, and y by K u s |w| plus a
 rounding of the result. The backward's two row means pass as many additions, over
 terms |u| and |u| s. The parameters' gradients add T terms |gy| s in lanes, blocks
 and groups: no term passes more than 64 additions at the sizes here plus those of
-xh, so 2 K u sum |gy| s.
+xh (at most 40 rounds of a block's rows, 8 groups, 32 parts and 16 rows of them in
+the largest ones), so 2 K u sum |gy| s.
 """
 
 import numpy as np
@@ -86,11 +87,22 @@ def test_widths_and_types(d, act, par):
     _check(x, w, b, gy, 1e-5, _run(x, w, b, gy), f"d={d}")
 
 
-@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 127, 512, 513, 1025, 3000])
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 127, 512, 513, 1025, 3000, 8200])
 @pytest.mark.parametrize("d", [40, 600, 1100, 2500])
-def test_rows(T, d):
-    """Fewer rows than blocks, one more than a round of blocks, several rounds."""
-    x, w, b, gy = _draw(T, d, torch.bfloat16, torch.float32, T)
+@pytest.mark.parametrize("act", [torch.bfloat16, torch.float32])
+def test_rows(T, d, act):
+    """Fewer rows than blocks, one more than a round of blocks, several rounds of one and of two rows."""
+    x, w, b, gy = _draw(T, d, act, torch.float32, T)
+    _check(x, w, b, gy, 1e-5, _run(x, w, b, gy), f"T={T} d={d}")
+
+
+@pytest.mark.parametrize("T,d,act", [(25000, 1500, torch.bfloat16), (70000, 500, torch.bfloat16), (9000, 4352,
+                                     torch.bfloat16), (13000, 1303, torch.float32), (7000, 3001, torch.float32)])
+def test_large_arrays(T, d, act):
+    """Arrays of 64 MiB and more (streamed past the caches), where the sums over rows are long.
+    No value passes more additions than its block has rounds (below 40), 8 groups, 32 parts and 16 rows."""
+    x, w, b, gy = _draw(T, d, act, torch.bfloat16, d)
+    assert x.numel() * x.element_size() >= 64 << 20
     _check(x, w, b, gy, 1e-5, _run(x, w, b, gy), f"T={T} d={d}")
 
 
@@ -108,7 +120,7 @@ def test_columns_of_a_wider_array(act, d, ld, off):
     gy3 = torch.randn(x3.shape, generator=g, device=DEV).to(act)
     y, gx, gw, gb = _run(x3, w, b, gy3)
     assert y.shape == gx.shape == x3.shape
-    # (rows at odd addresses are summed in another order than those of a contiguous copy: no equal bits)
+    assert torch.equal(y, D.layer_norm(x3.contiguous(), w, b))
     _check(x3.reshape(36, d), w, b, gy3.view(36, d), 1e-5, (y.view(36, d), gx.view(36, d), gw, gb), "3-D")
 
 
@@ -124,8 +136,8 @@ def test_unaligned_addresses(off):
     got = _run(shifted(x), shifted(w), shifted(b), shifted(gy))
     _check(x, w, b, gy, 1e-5, got, "unaligned")
     _check(x, w, b, gy, 1e-5, ref, "aligned")
-    # a parameter's address alone does not change how rows are read: the same bits
-    for a, c in zip(ref, _run(x, shifted(w), shifted(b), gy)):
+    # an address does not change what is computed: the same bits
+    for a, c in zip(ref, got):
         assert torch.equal(a, c)
 
 
