@@ -21,7 +21,6 @@ import functools
 from typing import List, Optional, Sequence
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -94,6 +93,18 @@ _HERE = contextlib.nullcontext()
 def _on(dev: torch.device):
     """The device the tensors live on as the current one, for the launches inside."""
     return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+def _once(ctx_name: str):
+    """Backward passes run with gradients enabled only where their own are asked for."""
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{ctx_name}: gradients of gradients are not available")
+
+
+# Backward passes below run on the engine's thread, where every step costs about twice
+# what it does on the caller's. The engine has made the forward's device and stream the
+# current ones; what the forward has checked is not checked again, and the library is
+# called without a wrapper in between.
 
 
 class Buffers:
@@ -296,10 +307,12 @@ def _norm_rows(x: torch.Tensor):
     """``x [..., d]`` as rows: (2-D view, elements between rows)."""
     if x.dim() < 1 or x.numel() == 0 or (x.size(-1) > 1 and x.stride(-1) != 1):
         raise ValueError("x must be a non-empty [..., d] tensor with neighbouring elements in a row")
-    try:
-        rows = x.view(-1, x.size(-1))
-    except RuntimeError as e:
-        raise ValueError("the rows of x must lie at one distance from each other") from e
+    rows = x
+    if x.dim() != 2:
+        try:
+            rows = x.view(-1, x.size(-1))
+        except RuntimeError as e:
+            raise ValueError("the rows of x must lie at one distance from each other") from e
     ld = rows.stride(0) if rows.size(0) > 1 else rows.size(1)
     if ld < rows.size(1):
         raise ValueError("the rows of x must not overlap (an expanded x: call .contiguous())")
@@ -371,14 +384,13 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, g_y):
-        # The engine calls this on a thread of its own, where every step costs about
-        # twice what it does on the caller's: what the forward has checked is not
-        # checked again. Only the layout of x may be another, behind saved-tensor hooks.
+        _once("layer_norm")
         x, weight, stats = ctx.saved_tensors
-        g_y = g_y.contiguous()
+        if not g_y.is_contiguous():
+            g_y = g_y.contiguous()
         dev, n = g_y.device, ctx.n
+        # (behind saved-tensor hooks the layout of x may be another)
         if x.dim() != 2 or x.stride() != (n.ld_x, 1):
             x, ld = _norm_rows(x)
             if ld != n.ld_x:
@@ -388,11 +400,12 @@ class _LayerNorm(torch.autograd.Function):
         g_w = torch.empty_like(weight) if need_w else None
         g_b = torch.empty_like(weight) if need_b else None
         ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=dev) if need_w or need_b else None
-        with _on(dev):
-            B.layer_norm_bwd(n, x.data_ptr(), weight.data_ptr(), stats.data_ptr(), g_y.data_ptr(),
-                             g_x.data_ptr() if need_x else None, g_w.data_ptr() if need_w else None,
-                             g_b.data_ptr() if need_b else None, ws.data_ptr() if ws is not None else None,
-                             ctx.ws_bytes, _stream(dev))
+        st = B.lib().mls_layer_norm_bwd(
+            n, x.data_ptr(), weight.data_ptr(), stats.data_ptr(), g_y.data_ptr(),
+            g_x.data_ptr() if need_x else None, g_w.data_ptr() if need_w else None,
+            g_b.data_ptr() if need_b else None, ws.data_ptr() if ws is not None else None, ctx.ws_bytes, _stream(dev))
+        if st:
+            B.check(st, "mls_layer_norm_bwd")
         return g_x, g_w, g_b, None
 
 
@@ -435,12 +448,14 @@ class _TokenLogp(torch.autograd.Function):
         return logp, entropy
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, g_logp, g_entropy):
+        _once("token_logp")
         if g_logp is None:
             return None, None, None, None
         # the saved tensors' addresses are taken anew, as in the loss's backward
-        tokens, h, W = (x.contiguous() for x in ctx.saved_tensors)
+        tokens, h, W = ctx.saved_tensors
+        if not (tokens.is_contiguous() and h.is_contiguous() and W.is_contiguous()):
+            tokens, h, W = tokens.contiguous(), h.contiguous(), W.contiguous()
         g_logp = g_logp.contiguous()
         p = ctx.p
         if (p.labels, p.h[0], p.W[0]) != (tokens.data_ptr(), h.data_ptr(), W.data_ptr()):
@@ -450,9 +465,11 @@ class _TokenLogp(torch.autograd.Function):
         gh = torch.empty_like(h) if need_h else None
         gW = torch.empty_like(W) if need_W else None
         ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=h.device)
-        with _on(h.device):
-            B.token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need_h else None,
-                             gW.data_ptr() if need_W else None, ws.data_ptr(), ctx.ws_bytes, _stream(h.device))
+        st = B.lib().mls_token_logp_bwd(p, ctx.stats.data_ptr(), g_logp.data_ptr(), gh.data_ptr() if need_h else None,
+                                        gW.data_ptr() if need_W else None, ws.data_ptr(), ctx.ws_bytes,
+                                        _stream(h.device))
+        if st:
+            B.check(st, "mls_token_logp_bwd")
         return None, None, gh, gW
 
 
@@ -505,15 +522,17 @@ class _PolicyLoss(torch.autograd.Function):
         return loss, kl, clipped
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, g_loss, g_kl, g_clipped):
+        _once("policy_loss")
         if g_loss is None:
             return None, None
         grad, = ctx.saved_tensors
         dev = grad.device
         g_logp = torch.empty(ctx.shape, dtype=torch.float32, device=dev)
-        with _on(dev):
-            B.policy_loss_bwd(g_logp.numel(), grad.data_ptr(), g_loss.data_ptr(), g_logp.data_ptr(), _stream(dev))
+        st = B.lib().mls_policy_loss_bwd(grad.numel() - 1, grad.data_ptr(), g_loss.data_ptr(), g_logp.data_ptr(),
+                                         _stream(dev))
+        if st:
+            B.check(st, "mls_policy_loss_bwd")
         return g_logp, None
 
 
@@ -572,34 +591,40 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Te
     return _policy_forward(logp, args, False)[:3]
 
 
-def _grad_list(grads, out):
-    grads = [g for g in grads if g is not None] if out is None else list(grads)
-    if not grads:
-        raise ValueError("no gradients given")
-    out = grads if out is None else list(out)
-    if len(out) != len(grads):
-        raise ValueError("out must hold one tensor for each gradient")
-    dev = grads[0].device
-    if dev.type != "cuda":
-        raise RuntimeError("gradient norms run on the GPU only; got tensors on " + str(dev))
-    rows = []
-    for g, o in zip(grads, out):
-        if g.device != dev or not g.is_contiguous():
-            raise ValueError("gradients must be contiguous tensors on one device")
-        if o is not g and (o.device != dev or o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous()):
-            raise ValueError("each out must be contiguous and of its gradient's shape, dtype and device")
-        rows.append((g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g.dtype)))
-    return dev, rows
+_GRAD_CODES = {torch.bfloat16: B.MLS_BF16, torch.float32: B.MLS_F32}
 
 
 def _clip(grads, max_norm: float, out) -> torch.Tensor:
-    dev, rows = _grad_list(grads, out)
-    tensors = B.make_grad_tensors(rows)
+    # (one pass over the list for each property: hundreds of tensors, whose properties
+    # cost more than the launches when asked for one by one)
+    T = torch.Tensor
+    grads = [g for g in grads if g is not None] if out is None else list(grads)
+    if not grads:
+        raise ValueError("no gradients given")
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise RuntimeError("gradient norms run on the GPU only; got tensors on " + str(dev))
+    on = {grads[0].get_device()}
+    if {*map(T.get_device, grads)} != on or not all(map(T.is_contiguous, grads)):
+        raise ValueError("gradients must be contiguous tensors on one device")
+    dtypes = [g.dtype for g in grads]
+    codes = [*map(_GRAD_CODES.get, dtypes)]
+    if None in codes:
+        raise TypeError(f"unsupported dtype {dtypes[codes.index(None)]}; use bfloat16 or float32")
+    sizes, data = [*map(T.numel, grads)], [*map(T.data_ptr, grads)]
+    to = data
+    if out is not None:
+        out = list(out)
+        if [*map(T.numel, out)] != sizes or [o.dtype for o in out] != dtypes or {*map(T.get_device, out)} != on or \
+                not all(map(T.is_contiguous, out)):
+            raise ValueError("out must hold for each gradient one contiguous tensor of its size, dtype and device")
+        to = [*map(T.data_ptr, out)]
+    tensors = B.make_grad_tensors(data, to, sizes, codes)
     norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws_bytes = B.clip_grad_norm_workspace(len(rows), tensors)
+    ws_bytes = B.clip_grad_norm_workspace(len(data), tensors)
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
     with _on(dev):
-        B.clip_grad_norm(len(rows), tensors, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
+        B.clip_grad_norm(len(data), tensors, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
     return norm
 
 
@@ -616,7 +641,7 @@ def clip_grad_norm(grads: Sequence[Optional[torch.Tensor]], max_norm: float, *,
 
     The norm is a float32 scalar on the device: nothing waits for it. The gradients
     (bf16 and float32 mixed; entries that are None are left out) are scaled in place,
-    or into the tensors ``out`` of the same shapes and dtypes. A norm that is NaN or
+    or into the tensors ``out`` of the same sizes and dtypes. A norm that is NaN or
     infinite scales nothing.
     """
     if not max_norm > 0:

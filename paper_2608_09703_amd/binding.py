@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import itertools
 import os
 from typing import Optional, Sequence
 
@@ -409,14 +410,11 @@ def policy_loss_bwd(N: int, grad: int, g_loss: int, g_logp: int, stream: int):
     check(lib().mls_policy_loss_bwd(N, grad, g_loss, g_logp, stream), "mls_policy_loss_bwd")
 
 
-def make_grad_tensors(tensors: Sequence[tuple]):
-    """The library's list of ``(data, out, elements, dtype)`` tensors, as bytes (one
-    conversion for the whole list: a structure's fields one by one take several times
-    as long)."""
-    flat = array.array("q")
-    for t in tensors:
-        flat.extend(t)  # dtype and the zero reserved field behind it are one little-endian word
-    return flat
+def make_grad_tensors(data: Sequence[int], out: Sequence[int], n: Sequence[int], dtype: Sequence[int]):
+    """The library's list of tensors, as the bytes of GradTensor structures (one conversion
+    for the whole list: a structure's fields one by one take several times as long)."""
+    # dtype and the zero reserved field behind it are one little-endian word
+    return array.array("q", itertools.chain.from_iterable(zip(data, out, n, dtype)))
 
 
 def clip_grad_norm_workspace(count: int, tensors) -> int:

@@ -1872,7 +1872,7 @@ bool next_launch(int64_t count, const mls_grad_tensor* g, int per, int64_t* next
   for (; *next < count && a.count < per; ++*next) {
     const mls_grad_tensor& x = g[*next];
     if (x.n == 0) continue;
-    const int64_t k = clip_tiles(x.n);
+    const int64_t k = clip_tiles(x.n, x.dtype == MLS_F32);
     if (tiles + k >= (1ll << 31) - 1 && a.count > 0) break;
     a.data[a.count] = x.data;
     a.n[a.count] = x.n | (x.dtype == MLS_F32 ? kClipF32 : 0);

@@ -486,7 +486,7 @@ hipError_t launch_policy_count(const PolicyArgs& a, hipStream_t stream);
 hipError_t launch_policy_fwd(const PolicyArgs& a, hipStream_t stream);
 hipError_t launch_policy_finish(const PolicyArgs& a, hipStream_t stream);
 hipError_t launch_policy_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp, hipStream_t stream);
-int64_t clip_tiles(int64_t n);
+int64_t clip_tiles(int64_t n, bool f32);
 int clip_blocks(int64_t tiles);
 hipError_t launch_grad_norm(const GradNormArgs& a, hipStream_t stream);
 hipError_t launch_grad_norm_finish(const double* part, int n, double max_norm, float* norm, float* coef,

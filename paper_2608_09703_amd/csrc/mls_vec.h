@@ -6,6 +6,23 @@
 
 namespace mls {
 
+// 16 bytes at an element's address (bf16 or fp32: any even one)
+typedef unsigned int u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+template <bool NT>
+__device__ __forceinline__ uint4 load16_any(const void* p) {
+  const u32x4_any_t* q = static_cast<const u32x4_any_t*>(p);
+  const u32x4_any_t v = NT ? __builtin_nontemporal_load(q) : *q;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool NT>
+__device__ __forceinline__ void store16_any(void* p, uint4 v) {
+  const u32x4_any_t w = {v.x, v.y, v.z, v.w};
+  if (NT)
+    __builtin_nontemporal_store(w, static_cast<u32x4_any_t*>(p));
+  else
+    *static_cast<u32x4_any_t*>(p) = w;
+}
+
 typedef unsigned int u32x2j __attribute__((ext_vector_type(2)));
 template <bool NT>
 __device__ __forceinline__ uint2 ld8(const void* p) {
@@ -110,6 +127,45 @@ struct Elt<Bf16> {
 template <>
 struct Elt<F32> {
   typedef float type;
+};
+
+__device__ __forceinline__ float widen(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ float widen(float v) { return v; }
+
+// A chunk of 16 bytes: kN elements.
+template <typename A>
+struct Chunk;
+template <>
+struct Chunk<Bf16> {
+  static constexpr int kN = 8;
+  __device__ __forceinline__ static void unpack(uint4 r, float* v) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ static uint4 pack(const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (uint32_t)to_storage<Bf16>(v[2 * i]) | ((uint32_t)to_storage<Bf16>(v[2 * i + 1]) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Chunk<F32> {
+  static constexpr int kN = 4;
+  __device__ __forceinline__ static void unpack(uint4 r, float* v) {
+    v[0] = __uint_as_float(r.x);
+    v[1] = __uint_as_float(r.y);
+    v[2] = __uint_as_float(r.z);
+    v[3] = __uint_as_float(r.w);
+  }
+  __device__ __forceinline__ static uint4 pack(const float* v) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  }
 };
 
 }  // namespace mls

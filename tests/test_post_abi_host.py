@@ -148,7 +148,7 @@ def test_policy_pointers():
 # -- gradient clipping -----------------------------------------------------------
 
 def _clip(rows, max_norm=1.0, norm=_at(100), ws=_at(101), nb=None):
-    t = B.make_grad_tensors(rows)
+    t = B.make_grad_tensors(*zip(*rows))
     B.clip_grad_norm(len(rows), t, max_norm, norm, ws, (1 << 30) if nb is None else nb, None)
 
 
@@ -164,7 +164,7 @@ def test_clip_refusals():
     for kw in (dict(max_norm=-1.0), dict(max_norm=math.nan), dict(norm=None), dict(ws=None), dict(norm=_at(100, 2)),
                dict(ws=_at(101, 4))):
         _refused(B.MLS_INVALID_ARG, lambda: _clip([ok], **kw))
-    t = B.make_grad_tensors([ok])
+    t = B.make_grad_tensors(*zip(ok))
     need = B.clip_grad_norm_workspace(1, t)
     _refused(B.MLS_WORKSPACE_TOO_SMALL, lambda: _clip([ok], nb=need - 1))
 
@@ -183,7 +183,7 @@ def test_clip_outputs_that_overlap(rows):
 
 def test_clip_workspace_follows_the_launches():
     def need(*sizes):
-        return B.clip_grad_norm_workspace(len(sizes), B.make_grad_tensors([(_at(1), _at(1), n, 0) for n in sizes]))
+        return B.clip_grad_norm_workspace(len(sizes), B.make_grad_tensors([_at(1)] * len(sizes), [_at(1)] * len(sizes), sizes, [0] * len(sizes)))
     assert need() == need(0, 0) <= 512
     assert need(1) <= need(1 << 20) <= need(1 << 30) <= 2048 * 8 + 512
     assert need(*[1] * 500) <= 500 * 8 + 512

@@ -86,6 +86,18 @@ def test_step_against_64_bits(dtype):
     assert abs(total - s.max_norm) <= 1e-3 * s.max_norm
 
 
+def test_gradients_of_gradients_are_refused():
+    x = torch.randn(4, 64, device=DEV, requires_grad=True)
+    W = torch.randn(9, 64, device=DEV, requires_grad=True)
+    logp = torch.randn(4, device=DEV, requires_grad=True)
+    y = D.layer_norm(x, torch.ones(64, device=DEV))
+    lp, _ = D.token_logp(x, W, torch.zeros(4, dtype=torch.int64, device=DEV))
+    loss, _, _ = D.policy_loss(logp, torch.zeros(4, device=DEV), torch.ones(4, device=DEV))
+    for out, leaf in ((y.sum(), x), (lp.sum(), W), (loss, logp)):
+        with pytest.raises(RuntimeError, match="gradients of gradients"):
+            torch.autograd.grad(out, leaf, create_graph=True)
+
+
 def test_step_on_another_stream_has_the_same_bits():
     s = _Step(torch.bfloat16)
     ref = s.run()
