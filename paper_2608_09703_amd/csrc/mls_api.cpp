@@ -1782,7 +1782,7 @@ mls_status mls_policy_loss_fwd(const mls_policy* p, const float* logp, const flo
     e = launch_policy_fwd(a, s);
   }
   if (e != hipSuccess) return hip_fail(e, "policy loss launch");
-  {
+  if (!policy_finishes(a.N)) {
     ProfScope pr("policy_finish", s);
     e = launch_policy_finish(a, s);
   }

@@ -480,10 +480,10 @@ NormShape norm_shape(int64_t T, int64_t d, bool f32, bool bwd);
 hipError_t launch_layer_norm_fwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
 hipError_t launch_layer_norm_bwd(const NormArgs& a, const NormShape& sh, bool f32, hipStream_t stream);
 hipError_t launch_layer_norm_params(const NormArgs& a, int n_parts, hipStream_t stream);
-int64_t policy_blocks(int64_t N);
 size_t policy_part_bytes(int64_t N);
 hipError_t launch_policy_count(const PolicyArgs& a, hipStream_t stream);
 hipError_t launch_policy_fwd(const PolicyArgs& a, hipStream_t stream);
+bool policy_finishes(int64_t N);  // the forward writes the losses itself
 hipError_t launch_policy_finish(const PolicyArgs& a, hipStream_t stream);
 hipError_t launch_policy_bwd(int64_t N, const float* grad, const float* g_loss, float* g_logp, hipStream_t stream);
 int64_t clip_tiles(int64_t n, bool f32);

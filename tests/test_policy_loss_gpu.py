@@ -51,7 +51,7 @@ def _check(logp, old, adv, upstream=1.0, ref=None, mask=None, cu=None, oracle_cu
     return leaf.grad, want
 
 
-SIZES = [1, 2, 63, 64, 255, 257, 1023, 1024, 1025, 2048, 5000]
+SIZES = [1, 2, 3, 63, 64, 255, 257, 1023, 1024, 1025, 4095, 4096, 4097, 5000, 8193]
 
 
 @pytest.mark.parametrize("n", SIZES)
@@ -67,7 +67,7 @@ def _sequences(lens, before=0, after=0):
     return torch.tensor(cu, dtype=torch.int32, device=DEV), int(cu[-1]) + after
 
 
-LENS = [[1], [5], [0, 3], [3, 0], [0, 0, 7, 0], [1, 1, 1, 1], [1500], [1, 2000, 3], [700, 0, 900, 1, 60, 1024],
+LENS = [[1], [5], [15, 16, 17, 33], [0, 3], [3, 0], [0, 0, 7, 0], [1, 1, 1, 1], [1500], [1, 2000, 3], [700, 0, 900, 1, 60, 1024],
         list(range(40))]
 
 
@@ -119,7 +119,7 @@ def test_nothing_counts():
         leaf = logp.detach().requires_grad_(True)
         loss, kl, clipped = D.policy_loss(leaf, old, adv, ref_logp=ref, kl_coef=0.1, **kw)
         loss.backward()
-        assert float(loss) == float(kl) == float(clipped) == 0.0 and not leaf.grad.any()
+        assert float(loss.detach()) == float(kl) == float(clipped) == 0.0 and not leaf.grad.any()
 
 
 def test_borders_of_the_clip():
@@ -169,6 +169,15 @@ def test_bad_offsets_stay_inside():
             clamped = np.clip(cu, 0, 50)
             want = P.policy(_np(logp), _np(old), _np(adv), cu=clamped, reduction=reduction)
             assert abs(float(loss.detach()) - want[0]) <= U * abs(want[0]) + 1e-11
+
+
+def test_one_long_sequence_among_the_mask():
+    """Sequences whose masks are counted by the wide kernel, and what lies around them."""
+    lens = [70001, 140003, 3]
+    cu, n = _sequences(lens, before=5, after=9)
+    logp, old, adv, _, mask = _draw(n, 9, 3, True)
+    mask[100000:170000] = False
+    _check(logp, old, adv, mask=mask, cu=cu, per_sequence=True, reduction="sequence")
 
 
 def test_many_tokens_and_no_gradient():
