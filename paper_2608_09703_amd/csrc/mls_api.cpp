@@ -217,6 +217,23 @@ void grad_h_parts(const mls_problem* p, int64_t rows, int64_t vrows, size_t room
   }
 }
 
+// K parts of grad_h's products on the fp32 path of token log-probabilities, whose one
+// chunk has a K of all of V: as many as make 512 tiles of 32 x 32 of it, 256 of K or
+// more each (T = 256, d = 256, V = 4,096: 64 tiles of 4,096 took 50 us of a launch
+// whose other 1,024 tiles need half of that). ksplit is a multiple of the K-tile.
+constexpr int64_t kF32PartK = 256;
+int64_t f32_most_parts(int64_t T, int64_t V, int64_t d) {
+  const int64_t tiles = (T + 31) / 32 * ((d + 31) / 32);
+  return std::min<int64_t>({kMaxSplits, 512 / tiles, V / kF32PartK});
+}
+void f32_parts(const mls_problem* p, const Plan& pl, size_t room, int* splits, int64_t* ksplit) {
+  const int64_t V = std::min(pl.Vc, pl.V), out = pl.T * p->d[0] * 4;
+  const int64_t n = std::min<int64_t>(f32_most_parts(pl.T, V, p->d[0]), room / out);
+  if (n < 2) return;
+  *ksplit = ((V + n - 1) / n + 127) / 128 * 128;
+  *splits = (int)((V + *ksplit - 1) / *ksplit);
+}
+
 mls_status validate(const mls_problem* p) {
   if (!p) return fail(MLS_INVALID_ARG, "problem is NULL");
   if (p->M < 1 || p->M > MLS_MAX_MODELS)
@@ -633,6 +650,8 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   int64_t ksplit = 0;
   if (pl.wide_bwd)
     grad_h_parts(p, pl.T, std::min(pl.Vc, pl.V), workspace_bytes - pl.off_ghp, &splits, &ksplit);
+  else if (pl.f32 && g_row)
+    f32_parts(p, pl, workspace_bytes - pl.off_ghp, &splits, &ksplit);
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const float* sf = static_cast<const float*>(stats);
@@ -911,6 +930,7 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   tp.bwd_bytes = off + pl.bwd_bytes;
   // (the slab alone may be smaller for more tokens, where chunks get narrower)
   tp.bwd_room = off + std::max<size_t>(pl.bwd_room, align256((size_t)std::min(whole, kTokenSlabBytes)));
+  if (pl.f32) tp.bwd_room += align256((size_t)f32_most_parts(p->T, std::min(pl.Vc, pl.V), p->d[0]) * p->T * p->d[0] * 4);
 }
 
 TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
@@ -1864,7 +1884,7 @@ mls_status validate_grad_outputs(int64_t count, const mls_grad_tensor* g) {
 }
 
 // Fills one launch with tensors from *next on; false when none are left. A launch
-// takes at most Args' tensors and fewer than 2^31 tiles.
+// takes at most `per` tensors and about 2^30 tiles (32-bit tile counters with room).
 template <class Args, class Put>
 bool next_launch(int64_t count, const mls_grad_tensor* g, int per, int64_t* next, Args& a, Put put) {
   memset(&a, 0, sizeof(a));
@@ -1873,7 +1893,7 @@ bool next_launch(int64_t count, const mls_grad_tensor* g, int per, int64_t* next
     const mls_grad_tensor& x = g[*next];
     if (x.n == 0) continue;
     const int64_t k = clip_tiles(x.n, x.dtype == MLS_F32);
-    if (tiles + k >= (1ll << 31) - 1 && a.count > 0) break;
+    if (tiles + k >= (1ll << 30) && a.count > 0) break;
     a.data[a.count] = x.data;
     a.n[a.count] = x.n | (x.dtype == MLS_F32 ? kClipF32 : 0);
     a.tile_begin[a.count] = (int32_t)tiles;

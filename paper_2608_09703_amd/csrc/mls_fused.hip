@@ -512,6 +512,8 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
       const int idx = tid + NT * j;
       const int t = idx / kChunks;
       const int c = idx & kCMask;
+      // (the slab's rows are a multiple of kFusedBN: a wider tile may reach past them)
+      if (BN > kFusedBN && tbase + t >= a.T_pad) break;
       const uint4 v = *reinterpret_cast<const uint4*>(smem + t * kGRow + ((c ^ (t & kCMask)) << 4));
       store16_nt(slab + (tbase + t) * a.Vc + vloc + c * 8, v);
     }

@@ -14,13 +14,13 @@ namespace mls {
 namespace {
 
 // One output element: fp32 C (overwritten or accumulated) or bf16 Cb (see GemmGroup).
-__device__ __forceinline__ void store_out(const GemmGroup& g, int64_t idx, float v) {
+__device__ __forceinline__ void store_out(const GemmGroup& g, float* C, int64_t idx, float v) {
   if (g.Cb) {
     if (g.Cpart) v += g.Cpart[idx];
     if (g.accumulate) v += __uint_as_float((uint32_t)g.Cb[idx] << 16);
     g.Cb[idx] = to_storage<Bf16>(v);
   } else {
-    float* c = g.C + idx;
+    float* c = C + idx;
     *c = g.accumulate ? *c + v : v;
   }
 }
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_nt_kernel(GemmArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int64_t m = m0 + Mma::row_of(wm, fm, r, lane);
-        if (m < g.rows && n < g.cols) store_out(g, m * g.ldc + n, mma.acc[fm][fn][r]);
+        if (m < g.rows && n < g.cols) store_out(g, g.C, m * g.ldc + n, mma.acc[fm][fn][r]);
       }
     }
 }
@@ -127,8 +127,8 @@ struct F32Loader {
 };
 
 template <int BM, int BN, int KS, bool AMC>
-__device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, int64_t mext, int64_t K, char* smem,
-                                         int tid) {
+__device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, const float* A, const float* B, float* C,
+                                         int64_t mext, int64_t K, char* smem, int tid) {
   constexpr int BK = 32 * KS;
   using Tile = F32Tile<BM, BN, BK>;
   Tile* stage = reinterpret_cast<Tile*>(smem);
@@ -140,8 +140,6 @@ __device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, int
   const int64_t m0 = (int64_t)tm * BM;
   const int64_t n0 = (int64_t)tn * BN;
   const int64_t next = g.ldc;
-  const float* A = static_cast<const float*>(g.A);
-  const float* B = static_cast<const float*>(g.B);
   f32x16_t acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
@@ -193,7 +191,7 @@ __device__ __forceinline__ void f32_tile(const GemmGroup& g, int tm, int tn, int
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int64_t m = m0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-    if (m < mext) store_out(g, m * g.ldc + n, acc[r]);
+    if (m < mext) store_out(g, C, m * g.ldc + n, acc[r]);
   }
 }
 
@@ -206,15 +204,26 @@ __global__ __launch_bounds__(kThreads) void gemm_f32_kernel(GemmArgs a) {
   for (int k = 1; k < a.ngroups; ++k)
     if (b >= a.g[k].tile_begin) gi = k;
   const GemmGroup& g = a.g[gi];
-  const int local = b - g.tile_begin;
+  int local = b - g.tile_begin;
+  int part = 0;  // K part
+  if (ROWS && g.splits > 1) {
+    part = local / (g.tiles_m * g.tiles_n);
+    local -= part * g.tiles_m * g.tiles_n;
+  }
   const int tn = local % g.tiles_n;
   const int tm = local / g.tiles_n;
   const int rows = ROWS ? *a.n_rows : 0;
   if (ROWS && g.kind == 0 && (int64_t)tm * BM >= rows) return;
-  if (g.kind == 0)
-    f32_tile<BM, BN, KS, false>(g, tm, tn, ROWS ? rows : g.ldc_rows, g.K, smem, threadIdx.x);
-  else
-    f32_tile<BM, BN, KS, true>(g, tm, tn, g.ldc_rows, ROWS ? rows : g.K, smem, threadIdx.x);
+  const float* A = static_cast<const float*>(g.A);
+  const float* B = static_cast<const float*>(g.B);
+  if (g.kind == 0) {
+    const int64_t k0 = ROWS ? part * g.ksplit : 0;
+    const int64_t K = ROWS && g.splits > 1 && g.K - k0 > g.ksplit ? g.ksplit : g.K - k0;
+    f32_tile<BM, BN, KS, false>(g, tm, tn, A + k0, B + k0 * g.ldb, ROWS ? g.C + part * g.csplit : g.C,
+                                ROWS ? rows : g.ldc_rows, K, smem, threadIdx.x);
+  } else {
+    f32_tile<BM, BN, KS, true>(g, tm, tn, A, B, g.C, g.ldc_rows, ROWS ? rows : g.K, smem, threadIdx.x);
+  }
 }
 
 // bf16 path: 256 x 256 tiles, 8 waves (2 per SIMD) of 128 x 64, direct-to-LDS

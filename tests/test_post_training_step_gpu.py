@@ -133,6 +133,10 @@ def test_captured_step_replays(dtype):
         with torch.no_grad():
             s.x.mul_(1.01)
             s.adv.neg_()
+            # other tokens, and another number of them that count
+            s.tokens.copy_(torch.roll(s.tokens, 5))
+            s.tokens[rep * 11:rep * 30] = -100
+            s.mask.copy_(s.tokens != -100)
         ref = s.run()
         for g, out in graphs if rep % 2 else graphs[::-1]:
             g.replay()
