@@ -355,19 +355,24 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  * p->M = 1, temperature p->tau and the tokens in p->labels,
  *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
- * as device float32 [T]. p->alpha and p->teacher do not matter. No logits are
- * kept. Tokens with ignore_index cost no product: the others' hidden states are
+ * as device float32 [T]. p->alpha and p->teacher do not matter. Tokens with ignore_index cost no product: the others' hidden states are
  * packed first, and those of ignored tokens are not used, whatever they hold.
  * stats: mls_query_sizes' stats_bytes; it receives what the backward needs, the
  * number of tokens that count and the device flags (mls_read_stats_header,
  * mls_device_error): a token outside [0, V) is treated as ignored and raises
  * MLS_DEVFLAG_LABEL_RANGE, a log-probability that is NaN or infinite
- * MLS_DEVFLAG_NONFINITE. workspace: fwd_bytes of mls_token_logp_workspace (contents
- * are not kept between calls). Asynchronous on stream.
+ * MLS_DEVFLAG_NONFINITE.
+ * kept: NULL, or a device buffer of kept_bytes that receives the counted tokens'
+ * logits (fp16, each as its distance to a maximum over 64 or 128 vocabulary rows) for
+ * the backward, which then does not compute them again; about 2 T V bytes. kept_bytes
+ * is 0 where that is not done (fp32, or operands near 4 GiB).
+ * workspace: fwd_bytes of mls_token_logp_workspace (contents are not kept between
+ * calls). Any output of mls_token_logp_workspace may be NULL. Asynchronous on stream.
  */
-mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes);
+mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes,
+                                    size_t* kept_bytes);
 mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
-                              void* workspace, size_t workspace_bytes, void* stream);
+                              void* kept, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Backward for the gradient g_logp (device float32 [T]) of logp; the entropy is not
@@ -375,16 +380,17 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
  * 0 on ignored tokens (whose g_logp is not used):
  *   grad_h = G W  [T, d] of p->grad_h_dtype (0 on ignored tokens),
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
- * Either may be NULL. The logits are recomputed one vocabulary chunk at a time
- * (p->vocab_chunk = 0: as few chunks as keep a chunk's G within 256 MiB) and G is
- * rounded to bfloat16 (bf16 inputs) in between, as in mls_distill_bwd, whose
- * accumulation flags apply (an accumulated grad_h is added to in fp32). stats: as
- * mls_token_logp_fwd left it on the same inputs. workspace: bwd_bytes of
+ * Either may be NULL. G is formed one vocabulary chunk at a time (p->vocab_chunk = 0:
+ * as few chunks as keep a chunk's G within 256 MiB), from the kept logits or, with
+ * kept NULL, from logits computed again, and rounded to bfloat16 (bf16 inputs) in
+ * between, as in mls_distill_bwd, whose accumulation flags apply (an accumulated
+ * grad_h is added to in fp32). stats and kept: as mls_token_logp_fwd left them on the
+ * same inputs; neither is changed. workspace: bwd_bytes of
  * mls_token_logp_workspace. Asynchronous on stream.
  */
-mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp,
-                              void* grad_h, void* grad_W, void* workspace, size_t workspace_bytes,
-                              void* stream);
+mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const void* kept,
+                              const float* g_logp, void* grad_h, void* grad_W, void* workspace,
+                              size_t workspace_bytes, void* stream);
 
 /*
  * Clipped policy loss with a KL term on token log-probabilities. Per counted

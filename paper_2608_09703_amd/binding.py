@@ -203,9 +203,9 @@ def lib():
         L.mls_layer_norm_fwd.argtypes = [N, vp, vp, vp, vp, vp, vp]
         L.mls_layer_norm_workspace.argtypes = [N, sz]
         L.mls_layer_norm_bwd.argtypes = [N, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
-        L.mls_token_logp_workspace.argtypes = [P, sz, sz]
-        L.mls_token_logp_fwd.argtypes = [P, vp, vp, vp, vp, ctypes.c_size_t, vp]
-        L.mls_token_logp_bwd.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_token_logp_workspace.argtypes = [P, sz, sz, sz]
+        L.mls_token_logp_fwd.argtypes = [P, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_token_logp_bwd.argtypes = [P, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         Q = ctypes.POINTER(Policy)
         L.mls_policy_loss_workspace.argtypes = [Q, sz]
         L.mls_policy_loss_fwd.argtypes = [Q, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -367,22 +367,22 @@ def layer_norm_bwd(n: LayerNorm, x: int, weight: int, stats: int, g_y: int, g_x:
 
 
 def token_logp_workspace(p: Problem):
-    """``(forward, backward)`` workspace bytes."""
-    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    check(lib().mls_token_logp_workspace(ctypes.byref(p), ctypes.byref(f), ctypes.byref(b)),
+    """``(forward, backward, kept)``: workspace bytes, and those of the kept logits (0: not kept)."""
+    f, b, k = ctypes.c_size_t(0), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    check(lib().mls_token_logp_workspace(ctypes.byref(p), ctypes.byref(f), ctypes.byref(b), ctypes.byref(k)),
           "mls_token_logp_workspace")
-    return f.value, b.value
+    return f.value, b.value, k.value
 
 
-def token_logp_fwd(p: Problem, stats: int, logp: int, entropy: Optional[int], ws: int, ws_bytes: int,
-                   stream: int):
-    check(lib().mls_token_logp_fwd(ctypes.byref(p), stats, logp, entropy, ws, ws_bytes, stream),
+def token_logp_fwd(p: Problem, stats: int, logp: int, entropy: Optional[int], kept: Optional[int], ws: int,
+                   ws_bytes: int, stream: int):
+    check(lib().mls_token_logp_fwd(ctypes.byref(p), stats, logp, entropy, kept, ws, ws_bytes, stream),
           "mls_token_logp_fwd")
 
 
-def token_logp_bwd(p: Problem, stats: int, g_logp: int, grad_h: Optional[int], grad_W: Optional[int], ws: int,
-                   ws_bytes: int, stream: int):
-    check(lib().mls_token_logp_bwd(ctypes.byref(p), stats, g_logp, grad_h, grad_W, ws, ws_bytes, stream),
+def token_logp_bwd(p: Problem, stats: int, kept: Optional[int], g_logp: int, grad_h: Optional[int],
+                   grad_W: Optional[int], ws: int, ws_bytes: int, stream: int):
+    check(lib().mls_token_logp_bwd(ctypes.byref(p), stats, kept, g_logp, grad_h, grad_W, ws, ws_bytes, stream),
           "mls_token_logp_bwd")
 
 

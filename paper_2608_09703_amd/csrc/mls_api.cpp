@@ -562,6 +562,9 @@ hipError_t launch_labels(const mls_problem* p, const Plan& pl, float* lab, void*
   return launch_count_valid(r, s);
 }
 
+// Row length of kept logits: whole tiles of either core.
+int64_t kept_ld(const Plan& pl) { return round_up(pl.V, kRowsTile); }
+
 // Tile core of token log-probabilities: 256 x 256 tiles, one block per CU, or the
 // losses' 128 x 128, two per CU. The larger one reads less per product and has
 // twice the tile epilogue in one piece, which counts for little in long products:
@@ -597,7 +600,7 @@ hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64
   a.n_vt = pl.n_vt_fwd;
   a.partials = partials;
   a.lslab = lslab;
-  a.ld_lslab = pl.fb_ld;
+  a.ld_lslab = n_rows ? kept_ld(pl) : pl.fb_ld;
   a.n_rows = n_rows;
   a.row0 = t0;
   if (n_rows && rows_core(p, pl)) {
@@ -640,12 +643,13 @@ hipError_t finish_losses(const mls_problem* p, const Plan& pl, void* stats, floa
   return launch_reduce_losses(r, s);
 }
 
-// Launches of the backward: of the losses (g_ce, g_kl) or, with g_row, of token
-// log-probabilities, whose problem p holds the packed rows and whose number of rows
-// the header has.
+// Launches of the backward: of the losses (g_ce, g_kl) or, with rows, of token
+// log-probabilities, whose problem p holds the packed rows, whose number of rows the
+// header has and whose logits rows->kept may hold.
 mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats, const float* g_ce,
-                        const float* g_kl, const float* g_row, void* const* grad_h, float* const* grad_W,
+                        const float* g_kl, const TokenArgs* rows, void* const* grad_h, float* const* grad_W,
                         void* workspace, size_t workspace_bytes, void* stream) {
+  const float* g_row = rows ? rows->g_c : nullptr;
   int splits = 1;  // K parts of the grad_h products
   int64_t ksplit = 0;
   if (pl.wide_bwd)
@@ -751,7 +755,15 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
       // vocabulary tiles past the chunk end are skipped.
       a.n_vt = (int)((vrows + fbm - 1) / fbm);
     }
-    {
+    if (rows && rows->kept) {
+      TokenArgs k = *rows;
+      k.v0 = v0;
+      k.cols = (int64_t)a.n_vt * fbm;  // as far as there are records
+      k.slab = static_cast<uint16_t*>(a.slab);
+      k.ld_slab = pl.Vc;
+      ProfScope ps("token_grad", s);
+      e = launch_token_grad(k, s);
+    } else {
       ProfScope ps("fused_bwd", s);
       e = launch_fused_bwd(a, pl.f32, s);
     }
@@ -903,6 +915,10 @@ struct TokenPlan {
   mls_problem q;   // p with the rows' grad_h (the scatter adds to an output)
   size_t off_hc = 0, off_tokens = 0, off_lab = 0, off_part = 0, off_gh = 0, off_work = 0;
   size_t fwd_bytes = 0, bwd_bytes = 0, bwd_room = 0;  // room: see Plan
+  // kept logits (bf16 in one forward chunk): the rows' fp16 distances, then the
+  // partial records with the maxima they are relative to
+  int n_rec = 0;
+  size_t kept_rec = 0, kept_bytes = 0;
 };
 
 void token_plan(const mls_problem* p, TokenPlan& tp) {
@@ -925,6 +941,11 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   off = align256(off + (size_t)pl.T * sizeof(float));
   tp.off_part = tp.off_gh = off;
   tp.fwd_bytes = off + pl.off_lab;  // the forward's partial records
+  tp.n_rec = (rows_core(p, pl) ? (int)((pl.V + kRowsTile - 1) / kRowsTile) : pl.n_vt_fwd) * kFusedFwdParts;
+  if (pl.wide_bwd && pl.fwd_nc == 1 && pl.T_pad <= 4 * 65535ll) {
+    tp.kept_rec = align256((size_t)pl.T_pad * kept_ld(pl) * 2);
+    tp.kept_bytes = tp.kept_rec + align256((size_t)tp.n_rec * pl.T_pad * sizeof(float4));
+  }
   off = align256(off + (size_t)pl.T * p->d[0] * (tp.q.grad_h_dtype == MLS_F32 ? 4 : 2));
   tp.off_work = off;
   tp.bwd_bytes = off + pl.bwd_bytes;
@@ -1369,7 +1390,8 @@ mls_status mls_diagnostics(const mls_problem* p, float* kl_pair, float* agree, i
   return MLS_OK;
 }
 
-mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes) {
+mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, size_t* bwd_bytes,
+                                    size_t* kept_bytes) {
   g_last_error.clear();
   mls_status st = validate_tokens(p);
   if (st != MLS_OK) return st;
@@ -1377,16 +1399,17 @@ mls_status mls_token_logp_workspace(const mls_problem* p, size_t* fwd_bytes, siz
   token_plan(p, tp);
   if (fwd_bytes) *fwd_bytes = tp.fwd_bytes;
   if (bwd_bytes) *bwd_bytes = tp.bwd_room;
+  if (kept_bytes) *kept_bytes = tp.kept_bytes;
   return MLS_OK;
 }
 
-mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy,
+mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, float* entropy, void* kept,
                               void* workspace, size_t workspace_bytes, void* stream) {
   g_last_error.clear();
   mls_status st = validate_tokens(p);
   if (st != MLS_OK) return st;
   if (!stats || !logp || !workspace) return fail(MLS_INVALID_ARG, "stats, logp and workspace must be non-NULL");
-  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(logp, 4) || !aligned(entropy, 4))
+  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(kept, 16))
     return fail(MLS_INVALID_ARG, "misaligned stats / workspace / output pointer");
   TokenPlan tp;
   token_plan(p, tp);
@@ -1394,6 +1417,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   if (workspace_bytes < tp.fwd_bytes)
     return fail(MLS_WORKSPACE_TOO_SMALL, "forward needs %zu workspace bytes, got %zu", tp.fwd_bytes,
                 workspace_bytes);
+  if (kept && !tp.kept_bytes) return fail(MLS_UNSUPPORTED, "the logits of this problem cannot be kept");
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   TokenArgs a = token_args(p, pl, stats);
@@ -1402,8 +1426,9 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   a.hc = ws + tp.off_hc;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
   a.lab = reinterpret_cast<float*>(ws + tp.off_lab);
-  a.n_rec = (rows_core(p, pl) ? (int)((pl.V + kRowsTile - 1) / kRowsTile) : pl.n_vt_fwd) * kFusedFwdParts;
-  a.partials = reinterpret_cast<const float4*>(ws + tp.off_part);
+  a.n_rec = tp.n_rec;
+  uint16_t* const lslab = static_cast<uint16_t*>(kept);
+  a.partials = reinterpret_cast<const float4*>(kept ? static_cast<char*>(kept) + tp.kept_rec : ws + tp.off_part);
   hipError_t e;
   {
     ProfScope ps("token_pack", s);
@@ -1420,7 +1445,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   for (int c = 0; c < pl.fwd_nc; ++c) {
     a.t0 = (int64_t)c * pl.fwd_tc;
     a.Tc = std::min(pl.fwd_tc, pl.T - a.t0);
-    e = forward_tiles(&tp.q, pl, a.t0, a.Tc, const_cast<float4*>(a.partials), nullptr, a.header, s);
+    e = forward_tiles(&tp.q, pl, a.t0, a.Tc, const_cast<float4*>(a.partials), lslab, a.header, s);
     if (e != hipSuccess) return hip_fail(e, "forward launch");
     ProfScope ps("token_merge", s);
     e = launch_token_merge(a, s);
@@ -1429,14 +1454,14 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   return MLS_OK;
 }
 
-mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const float* g_logp, void* grad_h,
-                              void* grad_W, void* workspace, size_t workspace_bytes, void* stream) {
+mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const void* kept, const float* g_logp,
+                              void* grad_h, void* grad_W, void* workspace, size_t workspace_bytes, void* stream) {
   g_last_error.clear();
   mls_status st = validate_tokens(p);
   if (st != MLS_OK) return st;
   if (!stats || !g_logp || !workspace)
     return fail(MLS_INVALID_ARG, "stats, g_logp and workspace must be non-NULL");
-  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(g_logp, 4) ||
+  if (!aligned(stats, 16) || !aligned(workspace, 16) || !aligned(g_logp, 4) || !aligned(kept, 16) ||
       !aligned(grad_h, p->grad_h_dtype == MLS_BF16 ? 8 : 16) ||
       !aligned(grad_W, (p->flags & MLS_GRAD_W_BF16) ? 2 : 4))
     return fail(MLS_INVALID_ARG, "misaligned stats / workspace / gradient pointer");
@@ -1446,10 +1471,18 @@ mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const flo
   if (workspace_bytes < tp.bwd_bytes)
     return fail(MLS_WORKSPACE_TOO_SMALL, "backward needs %zu workspace bytes, got %zu", tp.bwd_bytes,
                 workspace_bytes);
+  if (kept && !tp.kept_bytes) return fail(MLS_UNSUPPORTED, "the logits of this problem cannot be kept");
   if (!grad_h && !grad_W) return MLS_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   TokenArgs a = token_args(p, pl, const_cast<void*>(stats));
+  if (kept) {
+    a.kept = static_cast<const uint16_t*>(kept);
+    a.ld_kept = kept_ld(pl);
+    a.n_rec = tp.n_rec;
+    a.rec_rows = (int32_t)((rows_core(p, pl) ? kRowsTile : kFusedBM) / kFusedFwdParts);
+    a.partials = reinterpret_cast<const float4*>(static_cast<const char*>(kept) + tp.kept_rec);
+  }
   a.hc = ws + tp.off_hc;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
   a.g = g_logp;
@@ -1464,7 +1497,7 @@ mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const flo
   tp.q.labels = a.tokens_c;
   void* const gh[1] = {grad_h ? ws + tp.off_gh : nullptr};
   float* const gW[1] = {static_cast<float*>(grad_W)};
-  st = run_backward(&tp.q, pl, stats, nullptr, nullptr, a.g_c, gh, gW, ws + tp.off_work,
+  st = run_backward(&tp.q, pl, stats, nullptr, nullptr, &a, gh, gW, ws + tp.off_work,
                     workspace_bytes - tp.off_work, stream);
   if (st != MLS_OK || !grad_h) return st;
   a.gh_c = gh[0];

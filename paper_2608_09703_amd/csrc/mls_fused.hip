@@ -162,8 +162,13 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
         // complete in order, so no barrier is needed here. The slab lines are
         // written with the non-temporal policy (forward 2.82 -> 2.78 ms per
         // step at the headline shape).
-        static_assert(Mma::kStageBytes >= Mma::NW * 32 * 128 && Mma::WTM == 64, "staging fits");
-        char* stg = smem + Mma::kStageBytes + wave * 32 * 128;
+        // (ROWS: one product a block, so every stage is idle.)
+        constexpr int kCh = Mma::WTM / 8;    // 16-byte chunks of a token's row
+        constexpr int kRow = Mma::WTM * 2;   // its bytes
+        constexpr int kTok = 64 / kCh;       // tokens per store instruction
+        constexpr int kBase = ROWS ? 0 : Mma::kStageBytes;
+        static_assert(kBase + Mma::NW * 32 * kRow <= Mma::kSmemBytes, "staging fits");
+        char* stg = smem + kBase + wave * 32 * kRow;
         const int c = lane & 31;  // token inside the 32-token block
 #pragma unroll
         for (int fm = 0; fm < FM; ++fm)
@@ -177,17 +182,19 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
               w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x0) |
                      ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x1) << 16);
             }
-            const int chunk = (fm * 4 + rg) ^ (c & 7);  // 8 vocabulary rows per chunk
-            *reinterpret_cast<uint2*>(stg + c * 128 + chunk * 16 + hi * 8) = make_uint2(w[0], w[1]);
+            const int chunk = (fm * 4 + rg) ^ (c & (kCh - 1));  // 8 vocabulary rows per chunk
+            *reinterpret_cast<uint2*>(stg + c * kRow + chunk * 16 + hi * 8) = make_uint2(w[0], w[1]);
           }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        uint16_t* rows = a.lslab + ((int64_t)i * a.n_tt * BN + tbase + wn * Mma::WTN + fn * 32) *
-                                       a.ld_lslab + vbase + wm * Mma::WTM;
+        const int64_t row0 = tbase + wn * Mma::WTN + fn * 32;
+        uint16_t* rows = a.lslab + ((int64_t)i * a.n_tt * BN + row0) * a.ld_lslab + vbase + wm * Mma::WTM;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int tr = q * 8 + (lane >> 3);
-          const int kk = lane & 7;
-          const uint4 v = *reinterpret_cast<const uint4*>(stg + tr * 128 + ((kk ^ (tr & 7)) << 4));
+        for (int q = 0; q < 32 / kTok; ++q) {
+          const int tr = q * kTok + lane / kCh;
+          const int kk = lane & (kCh - 1);
+          // (the slab's rows are a multiple of kFusedBN: a wider tile may reach past them)
+          if (BN > kFusedBN && row0 + tr >= a.T_pad) break;
+          const uint4 v = *reinterpret_cast<const uint4*>(stg + tr * kRow + ((kk ^ (tr & (kCh - 1))) << 4));
           store16_nt(rows + (int64_t)tr * a.ld_lslab + kk * 8, v);
         }
       }
@@ -536,8 +543,8 @@ hipError_t launch_fwd_t(const FusedArgs& a, hipStream_t stream) {
 template <class Mma, bool STORE>
 hipError_t launch_fwd_wide(const FusedArgs& a, hipStream_t stream) {
   dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt);
-  if (!STORE && a.n_rows)
-    hipLaunchKernelGGL((fused_fwd_kernel<Mma, Bf16, true, 2, false, true>), grid, dim3(Mma::NT), 0, stream, a);
+  if (a.n_rows)
+    hipLaunchKernelGGL((fused_fwd_kernel<Mma, Bf16, true, 2, STORE, true>), grid, dim3(Mma::NT), 0, stream, a);
   else if (a.tau == 1.0f)
     hipLaunchKernelGGL((fused_fwd_kernel<Mma, Bf16, true, 2, STORE>), grid, dim3(Mma::NT), 0, stream,
                        a);
@@ -578,7 +585,7 @@ int fused_tile_rows(bool f32) { return f32 ? kFusedF32 : kFusedBM; }
 int fused_tile_cols(bool f32) { return f32 ? kFusedF32 : kFusedBN; }
 
 hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
-  if (a.n_rows && (a.M != 1 || a.lslab)) return hipErrorInvalidValue;
+  if (a.n_rows && (a.M != 1 || (a.lslab && f32))) return hipErrorInvalidValue;
   if (f32) return launch_fwd_t<MmaF32, F32>(a, stream);
   // bf16: the wide core for every width. K tails (widths that are not multiples
   // of 64) have their own form, so that the loads of the others carry no masks:
@@ -587,10 +594,15 @@ hipError_t launch_fused_fwd(const FusedArgs& a, bool f32, hipStream_t stream) {
   // tile launches 394 instead of 652, and the gradient GEMMs need no transposed
   // copies (117 us).
   if (a.n_rows && a.tile_v == kRowsTile) {
-    hipLaunchKernelGGL((fused_fwd_kernel<WideRows, Bf16, true, 1, false, true>),
-                       dim3((unsigned)a.n_tt * (unsigned)a.n_vt), dim3(WideRows::NT), 0, stream, a);
+    const dim3 grid((unsigned)a.n_tt * (unsigned)a.n_vt), block(WideRows::NT);
+    if (a.lslab)
+      hipLaunchKernelGGL((fused_fwd_kernel<WideRows, Bf16, true, 1, true, true>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((fused_fwd_kernel<WideRows, Bf16, true, 1, false, true>), grid, block, 0, stream, a);
     return hipGetLastError();
   }
+  if (a.n_rows && a.lslab)
+    return a.ktail ? launch_fwd_wide<WideFusedTail, true>(a, stream) : launch_fwd_wide<WideFused, true>(a, stream);
   if (a.lslab)  // the stored-logit plan takes multiples of 64 only
     return a.ktail ? hipErrorInvalidValue : launch_fwd_wide<WideFused, true>(a, stream);
   return a.ktail ? launch_fwd_wide<WideFusedTail, false>(a, stream)

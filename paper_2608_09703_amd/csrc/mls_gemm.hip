@@ -470,6 +470,7 @@ __global__ __launch_bounds__(MmaH::NT, 1) void gemm_wide_rows_kernel(GemmArgs a)
     wide_tile<MmaH>(g, tm, tn, part, rows, g.ldc, g.rows, g.cols, g.K, smem, threadIdx.x);
   } else {
     // K: the rows, in whole K-tiles; h reads as zero past them
+    static_assert(kRowsKTile % MmaW::BK == 0, "rows of the slab that are written");
     const int64_t K = ((int64_t)rows + MmaW::BK - 1) / MmaW::BK * MmaW::BK;
     wide_tile<MmaW>(g, local / g.tiles_n, local % g.tiles_n, 0, g.ldc_rows, g.ldc, K, rows, K, smem, threadIdx.x);
   }

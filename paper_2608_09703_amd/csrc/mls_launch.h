@@ -15,6 +15,7 @@ constexpr int kMaxModels = 8;
 constexpr int kFusedBM = 128;      // general core
 constexpr int kFusedWideBM = 128;  // wide bf16 core
 constexpr int kFusedF32 = 64;      // fp32 core, rows and columns
+constexpr int kRowsKTile = 64;     // rows that its gradient products read at a time
 constexpr int kRowsTile = 256;     // core of token log-probabilities, rows and columns
 // forward partial records per (vocabulary tile, token, sub-model): one per
 // wave row of the tile, each over its own half of the tile's rows; their
@@ -205,6 +206,14 @@ struct TokenArgs {
   float* lab;             // [T] forward: their own logits
   const float* g;         // [T] backward: gradients by token
   float* g_c;             // [T] and by row
+  // logit gradients of a vocabulary chunk from the kept logits
+  const uint16_t* kept;   // [T_pad][ld_kept] fp16 distances to their record's maximum
+  int64_t ld_kept;
+  int32_t rec_rows;       // vocabulary rows of a record
+  int64_t v0;             // first column of the chunk
+  int64_t cols;           // columns of the chunk to write (a multiple of 8; zeros from V on)
+  uint16_t* slab;         // [T_pad][ld_slab]
+  int64_t ld_slab;
   // row merge of rows [t0, t0 + Tc)
   int64_t t0;
   int64_t Tc;
@@ -504,6 +513,7 @@ hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_finalize_rows(const RowArgs& a, hipStream_t stream);
 hipError_t launch_token_pack(const TokenArgs& a, hipStream_t stream);
 hipError_t launch_token_gather(const TokenArgs& a, bool f32, hipStream_t stream);
+hipError_t launch_token_grad(const TokenArgs& a, hipStream_t stream);
 hipError_t launch_token_merge(const TokenArgs& a, hipStream_t stream);
 hipError_t launch_token_scatter(const TokenArgs& a, hipStream_t stream);
 hipError_t launch_reduce_losses(const RowArgs& a, hipStream_t stream);

@@ -85,10 +85,11 @@ def _problem(**kw):
 
 def test_token_logp_refusals():
     p = _problem()
-    ws, wb = B.token_logp_workspace(p)
-    fwd = lambda q=p, s=_at(4), lp=_at(5), en=None, w=_at(6), nb=ws: B.token_logp_fwd(q, s, lp, en, w, nb, None)  # noqa: E731
-    bwd = lambda q=p, s=_at(4), g=_at(5), gh=_at(7), gW=_at(8), w=_at(6), nb=wb: B.token_logp_bwd(  # noqa: E731
-        q, s, g, gh, gW, w, nb, None)
+    ws, wb, kb = B.token_logp_workspace(p)
+    assert kb >= 384 * 5120 * 2
+    fwd = lambda q=p, s=_at(4), lp=_at(5), en=None, k=None, w=_at(6), nb=ws: B.token_logp_fwd(q, s, lp, en, k, w, nb, None)  # noqa: E731
+    bwd = lambda q=p, s=_at(4), g=_at(5), gh=_at(7), gW=_at(8), k=None, w=_at(6), nb=wb: B.token_logp_bwd(  # noqa: E731
+        q, s, k, g, gh, gW, w, nb, None)
     for call in (fwd, bwd):
         _refused(B.MLS_INVALID_ARG, lambda: call(q=_problem(M=2)), text="one sub-model")
         _refused(B.MLS_INVALID_ARG, lambda: call(q=_problem(tau=0.0)))
@@ -100,6 +101,10 @@ def test_token_logp_refusals():
         for kw in (dict(s=None), dict(w=None), dict(s=_at(4, 8)), dict(w=_at(6, 8))):
             _refused(B.MLS_INVALID_ARG, lambda: call(**kw))
         _refused(B.MLS_WORKSPACE_TOO_SMALL, lambda: call(nb=16))
+        _refused(B.MLS_INVALID_ARG, lambda: call(k=_at(9, 8)))
+        f32 = _problem(dtype=B.MLS_F32)
+        assert B.token_logp_workspace(f32)[2] == 0
+        _refused(B.MLS_UNSUPPORTED, lambda: call(q=f32, k=_at(9), nb=1 << 40), text="kept")
     for kw in (dict(lp=None), dict(lp=_at(5, 2)), dict(en=_at(9, 1))):
         _refused(B.MLS_INVALID_ARG, lambda: fwd(**kw))
     for kw in (dict(g=None), dict(g=_at(5, 2)), dict(gh=_at(7, 2)), dict(gW=_at(8, 2))):
@@ -107,10 +112,10 @@ def test_token_logp_refusals():
 
 
 def test_a_token_logp_workspace_for_the_longest_batch_serves_the_shorter_ones():
-    last = (0, 0)
+    last = (0, 0, 0)
     for T in (1, 127, 128, 129, 300, 512, 1000, 2000, 4096, 9000):
         now = B.token_logp_workspace(_problem(T=T, V=50000, d=512, grad_h_dtype=B.MLS_BF16))
-        assert now[0] >= last[0] and now[1] >= last[1]
+        assert all(a >= b for a, b in zip(now, last))
         assert now[0] < T * 50000 * 4 // 2 + (1 << 26)
         last = now
 

@@ -43,17 +43,18 @@ def test_token_logp(T, d, V, chunk, dtype):
     tokens[1::4] = -100
     g = _Guarded()
     es = h.element_size()
-    for flags in (0, B.MLS_ACCUMULATE_GRAD_H):
+    for flags, keep in ((0, False), (0, True), (B.MLS_ACCUMULATE_GRAD_H, False)):
         p = D.make_problem([h], [W], tokens, grad_h_dtype=dtype, vocab_chunk=chunk,
                            flags=flags | (B.MLS_GRAD_W_BF16 if es == 2 else 0))
-        fwd, bwd = B.token_logp_workspace(p)
+        fwd, bwd, kb = B.token_logp_workspace(p)
+        kept = g(kb, "kept").data_ptr() if keep and kb else None
         stats, logp, ent = g(B.query_sizes(p)[1], "stats"), g(4 * T, "logp"), g(4 * T, "entropy")
         gh, gW = g(T * d * es, "grad_h"), g(V * d * es, "grad_W")
         gl = torch.randn(T, device=DEV)
         s = D._stream(h.device)
         w1, w2 = g(fwd, "forward workspace"), g(bwd, "backward workspace")
-        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), ent.data_ptr(), w1.data_ptr(), fwd, s)
-        B.token_logp_bwd(p, stats.data_ptr(), gl.data_ptr(), gh.data_ptr(), gW.data_ptr(), w2.data_ptr(), bwd, s)
+        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), ent.data_ptr(), kept, w1.data_ptr(), fwd, s)
+        B.token_logp_bwd(p, stats.data_ptr(), kept, gl.data_ptr(), gh.data_ptr(), gW.data_ptr(), w2.data_ptr(), bwd, s)
         g.check(f"T={T} d={d} V={V} chunk={chunk}")
 
 

@@ -6,7 +6,11 @@ gradient bounds (the logit gradient is bf16 in between on the bf16 path), and
 element by element within what the roundings allow: with G the exact logit gradient,
 2^-8 sum |G| |W| for its rounding, as much again of the result for the output's, and
 2^-12 sum |G| |W| for the recomputed logits (a logit of fp32 sums is off by less than
-2^-13 here, and exp turns that into a relative error of G's softmax part).
+2^-13 here, and exp turns that into a relative error of G's softmax part). A kept
+logit is an fp16 distance x below a maximum, off by 2^-11 x: that times p = exp(-x) / Z
+with the maximum's own share exp(0) / Z <= 1 is at most 2^-11 x exp(-x) <= 2^-11 / e of
+the largest p of its record, less than 2^-12 of it: on the bf16 path 2^-12 sum_v g p_max
+|W| is added, and p_max taken as 1.
 """
 
 import numpy as np
@@ -55,11 +59,18 @@ def _check(h, W, tokens, gl, temperature, got, what):
         G[rows] *= np.abs(gn[rows])[:, None] / temperature
     rel = 2.0 ** -8 + 2.0 ** -12 if bf16 else 2.0 ** -12
     half = 2.0 ** -8 if bf16 else 2.0 ** -24
-    for g, r, s, name in ((gh, rh, G @ np.abs(Wn), "grad_h"), (gW, rW, G.T @ np.abs(hn), "grad_W")):
+    # kept logits: 2^-11 x exp(-x) p_max with x the distance to the row's maximum, for every entry
+    E = np.zeros_like(G)
+    if bf16 and rows.size:
+        x = z.max(1, keepdims=True) - z
+        top = 1.0 / np.exp(-x).sum(1, keepdims=True)
+        E[rows] = 2.0 ** -11 * temperature * x * np.exp(-x) * top * np.abs(gn[rows])[:, None] / temperature ** 2
+    for g, r, s, e, name in ((gh, rh, G @ np.abs(Wn), E @ np.abs(Wn), "grad_h"),
+                             (gW, rW, G.T @ np.abs(hn), E.T @ np.abs(hn), "grad_W")):
         if g is None:
             continue
         gn_ = _np(g)
-        bad = ~(np.abs(gn_ - r) <= rel * s + half * np.abs(r))
+        bad = ~(np.abs(gn_ - r) <= rel * s + e + half * np.abs(r))
         assert not bad.any(), f"{what} {name}: {bad.sum()} off, first at {np.argwhere(bad)[0]}"
         assert_grad_rows(gn_, r, f"{what} {name}")
     return rh, rW
@@ -78,10 +89,29 @@ SHAPES = [(1, 8, 2), (1, 64, 300), (2, 64, 128), (127, 64, 129), (128, 72, 1000)
 
 @pytest.mark.parametrize("T,d,V", SHAPES)
 @pytest.mark.parametrize("temperature", [1.0, 0.7])
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_shapes(T, d, V, temperature, dtype):
+@pytest.mark.parametrize("dtype,keep", [(torch.bfloat16, True), (torch.bfloat16, False), (torch.float32, False)])
+def test_shapes(T, d, V, temperature, dtype, keep):
     h, W, tokens, gl = _draw(T, d, V, dtype, T + d)
-    _check(h, W, tokens, gl, temperature, _run(h, W, tokens, gl, temperature=temperature), f"{T} {d} {V}")
+    got = _run(h, W, tokens, gl, temperature=temperature, keep_logits=keep)
+    _check(h, W, tokens, gl, temperature, got, f"{T} {d} {V}")
+
+
+@pytest.mark.parametrize("d", [64, 200, 2048])
+def test_kept_logits(d, monkeypatch):
+    """Kept by themselves up to a size; read, not written, by the backward."""
+    h, W, tokens, gl = _draw(300, d, 1500, torch.bfloat16, d)
+    h, W = h.requires_grad_(True), W.requires_grad_(True)
+
+    def grads(times=1, **kw):
+        logp, _ = D.token_logp(h, W, tokens, **kw)
+        return [logp.detach()] + [torch.autograd.grad(logp, (h, W), gl, retain_graph=True) for _ in range(times)]
+    kept, first, second = grads(2, keep_logits=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    assert all(torch.equal(a, b) for a, b in zip(first, grads()[1]))
+    again = grads(keep_logits=False)
+    assert torch.equal(kept, again[0]) and not torch.equal(first[1], again[1][1])
+    monkeypatch.setattr(D, "KEEP_LOGITS_BYTES", 1000)
+    assert all(torch.equal(a, b) for a, b in zip(again[1], grads()[1]))
 
 
 @pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 96), (torch.bfloat16, 2048), (torch.float32, 96)])
@@ -115,7 +145,7 @@ def test_tokens_out_of_range_are_ignored_and_flagged():
     logp = torch.empty(200, device=DEV)
 
     def flags():
-        B.token_logp_fwd(p, buf.stats.data_ptr(), logp.data_ptr(), None, ws.data_ptr(), ws.numel(),
+        B.token_logp_fwd(p, buf.stats.data_ptr(), logp.data_ptr(), None, None, ws.data_ptr(), ws.numel(),
                          D._stream(h.device))
         n, f = B.read_stats_header(p, buf.stats.data_ptr(), D._stream(h.device))
         assert n == int(((tokens >= 0) & (tokens < 500)).sum()) and f == B.device_error(
@@ -173,11 +203,11 @@ def test_accumulated_gradients(dtype, out):
         p = D.make_problem([h], [W], tokens, grad_h_dtype=out, flags=flags | acc)
         stats = torch.empty(B.query_sizes(p)[1], dtype=torch.uint8, device=DEV)
         logp, s = torch.empty(300, device=DEV), D._stream(h.device)
-        ws = torch.full((max(B.token_logp_workspace(p)),), 255, dtype=torch.uint8, device=DEV)
-        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), None, ws.data_ptr(), ws.numel(), s)
+        ws = torch.full((max(B.token_logp_workspace(p)[:2]),), 255, dtype=torch.uint8, device=DEV)
+        B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), None, None, ws.data_ptr(), ws.numel(), s)
         g = [x.clone() if acc else torch.full_like(x, float("nan")) for x in g0]
         ws.fill_(255)
-        B.token_logp_bwd(p, stats.data_ptr(), gl.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), ws.data_ptr(),
+        B.token_logp_bwd(p, stats.data_ptr(), None, gl.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), ws.data_ptr(),
                          ws.numel(), s)
         torch.cuda.synchronize()
         return g
