@@ -355,8 +355,9 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  * p->M = 1, temperature p->tau and the tokens in p->labels,
  *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
- * as device float32 [T]. p->alpha and p->teacher do not matter. Tokens with ignore_index cost no product: the others' hidden states are
- * packed first, and those of ignored tokens are not used, whatever they hold.
+ * as device float32 [T]. p->alpha and p->teacher do not matter. Tokens with
+ * ignore_index cost no product: the others' hidden states are packed first, and those
+ * of ignored tokens are not used, whatever they hold.
  * stats: mls_query_sizes' stats_bytes; it receives what the backward needs, the
  * number of tokens that count and the device flags (mls_read_stats_header,
  * mls_device_error): a token outside [0, V) is treated as ignored and raises

@@ -111,6 +111,32 @@ def test_step_on_another_stream_has_the_same_bits():
         assert torch.equal(a, b)
 
 
+def test_step_with_saved_tensors_on_the_host_has_the_same_bits():
+    s = _Step(torch.bfloat16)
+    ref = s.run()
+    with torch.autograd.graph.save_on_cpu():
+        got = s.run()
+    for a, b in zip(ref, got):
+        assert torch.equal(a, b)
+
+
+def test_two_steps_at_once():
+    """On two streams, each with its own tensors but the same head."""
+    steps = [_Step(torch.bfloat16, seed=k) for k in (1, 2)]
+    steps[1].W = steps[1].leaves[3] = steps[0].W
+    ref = [s.run() for s in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+    got = []
+    for s, q in zip(steps, streams):
+        with torch.cuda.stream(q):
+            got.append(s.run())
+    torch.cuda.synchronize()
+    for a, b in zip(ref, got):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_captured_step_replays(dtype):
     """Two graphs of the step replayed in turn, with eager work in between, after new inputs."""

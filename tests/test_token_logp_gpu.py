@@ -7,10 +7,9 @@ element by element within what the roundings allow: with G the exact logit gradi
 2^-8 sum |G| |W| for its rounding, as much again of the result for the output's, and
 2^-12 sum |G| |W| for the recomputed logits (a logit of fp32 sums is off by less than
 2^-13 here, and exp turns that into a relative error of G's softmax part). A kept
-logit is an fp16 distance x below a maximum, off by 2^-11 x: that times p = exp(-x) / Z
-with the maximum's own share exp(0) / Z <= 1 is at most 2^-11 x exp(-x) <= 2^-11 / e of
-the largest p of its record, less than 2^-12 of it: on the bf16 path 2^-12 sum_v g p_max
-|W| is added, and p_max taken as 1.
+logit is fp16, as its distance below the maximum of a few vocabulary rows, which is at
+most its distance x below the row's: it is off by 2^-11 x, and the softmax entry p by
+2^-11 (x / tau) p. E in the check is what that adds to G.
 """
 
 import numpy as np
@@ -59,12 +58,10 @@ def _check(h, W, tokens, gl, temperature, got, what):
         G[rows] *= np.abs(gn[rows])[:, None] / temperature
     rel = 2.0 ** -8 + 2.0 ** -12 if bf16 else 2.0 ** -12
     half = 2.0 ** -8 if bf16 else 2.0 ** -24
-    # kept logits: 2^-11 x exp(-x) p_max with x the distance to the row's maximum, for every entry
     E = np.zeros_like(G)
     if bf16 and rows.size:
-        x = z.max(1, keepdims=True) - z
-        top = 1.0 / np.exp(-x).sum(1, keepdims=True)
-        E[rows] = 2.0 ** -11 * temperature * x * np.exp(-x) * top * np.abs(gn[rows])[:, None] / temperature ** 2
+        x = z.max(1, keepdims=True) - z  # over tau
+        E[rows] = 2.0 ** -11 * x * p / p.sum(1, keepdims=True) * np.abs(gn[rows])[:, None] / temperature
     for g, r, s, e, name in ((gh, rh, G @ np.abs(Wn), E @ np.abs(Wn), "grad_h"),
                              (gW, rW, G.T @ np.abs(hn), E.T @ np.abs(hn), "grad_W")):
         if g is None:
@@ -112,6 +109,44 @@ def test_kept_logits(d, monkeypatch):
     assert torch.equal(kept, again[0]) and not torch.equal(first[1], again[1][1])
     monkeypatch.setattr(D, "KEEP_LOGITS_BYTES", 1000)
     assert all(torch.equal(a, b) for a, b in zip(again[1], grads()[1]))
+
+
+def test_kept_logits_are_freed_by_the_backward():
+    T, d, V = 2000, 64, 20000
+    h, W, tokens, gl = _draw(T, d, V, torch.bfloat16, 13)
+    W.requires_grad_(True)
+    used = torch.cuda.memory_allocated
+    before = used()
+    logp, entropy = D.token_logp(h, W, tokens)
+    assert used() - before >= 2 * T * V
+    gW = torch.autograd.grad(logp, W, gl)
+    assert used() - before < T * V and logp.requires_grad
+    del gW
+    with torch.no_grad():
+        before = used()
+        logp = D.token_logp(h, W, tokens)
+        assert used() - before < T * V
+
+
+@pytest.mark.parametrize("T,d,V,chunk", [(20001, 64, 130, 0), (3000, 64, 3001, 256), (1000, 2048, 5003, 1280)])
+def test_kept_logits_over_many_tokens_and_chunks(T, d, V, chunk):
+    h, W, tokens, gl = _draw(T, d, V, torch.bfloat16, 14, ignore=0.4)
+    got = _run(h, W, tokens, gl, temperature=1.3, vocab_chunk=chunk, keep_logits=True)
+    _check(h, W, tokens, gl, 1.3, got, f"{T} {d} {V}")
+
+
+@pytest.mark.parametrize("keep", [True, False])
+def test_far_logits(keep):
+    """Logits hundreds apart: entries that the softmax leaves nothing of, and distances past fp16."""
+    h, W, tokens, gl = _draw(130, 64, 1000, torch.bfloat16, 15)
+    h[::3] *= 30
+    h[1::3] *= 3e4
+    logp, entropy, gh, gW = _run(h, W, tokens, gl, keep_logits=keep)
+    rh, rW = P.token_logp_backward(_np(h), _np(W), tokens.cpu().numpy(), _np(gl))
+    # (a logit of size 1e5 is off by 1e-2 itself: rows near a tie are left to the others)
+    assert torch.isfinite(logp).all() and torch.isfinite(gh).all() and torch.isfinite(gW).all()
+    assert_grad_rows(_np(gh)[::3], rh[::3], "grad_h")
+    assert_grad_rows(_np(gh)[2::3], rh[2::3], "grad_h")
 
 
 @pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 96), (torch.bfloat16, 2048), (torch.float32, 96)])
