@@ -77,8 +77,9 @@ enum mls_flags {
   MLS_ACCUMULATE_GRAD_H = 2u, /* grad_h_i += instead of = */
   MLS_FWD_BWD_RECOMPUTE = 4u, /* mls_distill_fwd_bwd: recompute the logits in the backward
                                  instead of storing them per token chunk */
-  MLS_GRAD_W_BF16 = 8u        /* mls_distill_bwd: the grad_W_i are bfloat16 (rounded once
-                                 from the fp32 sums); mls_distill_fwd_bwd refuses it */
+  MLS_GRAD_W_BF16 = 8u        /* mls_distill_bwd, mls_token_logp_bwd: the grad_W_i are
+                                 bfloat16 (rounded once from the fp32 sums);
+                                 mls_distill_fwd_bwd refuses it */
 };
 
 /* Device-side error bits written into the statistics buffer by the forward. */

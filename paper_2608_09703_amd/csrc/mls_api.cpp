@@ -904,8 +904,8 @@ mls_status validate_tokens(const mls_problem* p) {
 // A head of one sub-model needs no four chunks to stay far below its [T, V]: what
 // few chunks save is launches and the part-filled last round of each. T = 4,096
 // (3,071 counted), d = 4,352, V = 49,152, us for 12,288 / 24,576 / 49,152 columns:
-// 4,756 / 4,594 / 4,686; T = 1,531, d = 1,000, V = 32,003, for 8,192 / 32,256: 590 /
-// 485; fp32, T = 256, d = 256, V = 4,096, for 1,024 / 4,096: 183 / 117.
+// 3,597 / 3,569 / 3,672 (logits computed again: 4,756 / 4,594 / 4,686); T = 1,531,
+// d = 1,000, V = 32,003, for 8,192 / 16,128 / 32,256: 485 / 415 / 393; fp32, T = 256, d = 256, V = 4,096, for 1,024 / 4,096: 183 / 117.
 constexpr int64_t kTokenSlabBytes = 256ll << 20;
 
 // Workspaces of token log-probabilities: the packed rows, then what the tile kernels

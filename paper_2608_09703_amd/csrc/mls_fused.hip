@@ -86,7 +86,8 @@ __device__ __forceinline__ int64_t live_rows(const FusedArgs& a) {
 // (max, sum exp, sum exp at tau, teacher-weighted logit sum) per token and wave
 // row. Each wave normalises to the max over its own rows, so the epilogue needs
 // no exchange between waves; the row merge rescales the records.
-// STORE (fused forward + backward): every logit also goes to the chunk's slab as
+// STORE (fused forward + backward; token log-probabilities with kept logits): every
+// logit also goes to the chunk's slab as
 // fp16 of its distance to the record's maximum (at most 0; 2^-11 relative, so
 // the entries that carry the softmax's mass, near the maximum, are the most
 // exact), token-major, for the logit gradient pass.
