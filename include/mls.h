@@ -365,9 +365,9 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  * MLS_DEVFLAG_LABEL_RANGE, a log-probability that is NaN or infinite
  * MLS_DEVFLAG_NONFINITE.
  * kept: NULL, or a device buffer of kept_bytes that receives the counted tokens'
- * logits (fp16, each as its distance to a maximum over 64 or 128 vocabulary rows) for
- * the backward, which then does not compute them again; about 2 T V bytes. kept_bytes
- * is 0 where that is not done (fp32, or operands near 4 GiB).
+ * logits (16 bits each: the distance to a maximum over 64 or 128 vocabulary rows, over
+ * tau, in 65,535ths of 32) for the backward, which then does not compute them again;
+ * about 2 T V bytes. kept_bytes is 0 where that is not done (fp32, or operands near 4 GiB).
  * workspace: fwd_bytes of mls_token_logp_workspace (contents are not kept between
  * calls). Any output of mls_token_logp_workspace may be NULL. Asynchronous on stream.
  */
@@ -384,9 +384,9 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
  * Either may be NULL. G is formed one vocabulary chunk at a time (p->vocab_chunk = 0:
  * as few chunks as keep a chunk's G within 256 MiB), from the kept logits or, with
- * kept NULL, from logits computed again, and rounded to bfloat16 (bf16 inputs) in
- * between, as in mls_distill_bwd, whose accumulation flags apply (an accumulated
- * grad_h is added to in fp32). stats and kept: as mls_token_logp_fwd left them on the
+ * kept NULL, from logits computed again. bf16 inputs: G over its token's own entry s
+ * (then 1) and, for grad_W, s h[t] are rounded to bfloat16 in between. mls_distill_bwd's
+ * accumulation flags apply (an accumulated grad_h is added to in fp32). stats and kept: as mls_token_logp_fwd left them on the
  * same inputs; neither is changed. workspace: bwd_bytes of
  * mls_token_logp_workspace. Asynchronous on stream.
  */

@@ -493,8 +493,8 @@ def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temper
     ``ignore_index``. Ignored tokens cost no product, and what their rows of ``h`` hold
     does not matter.
 
-    ``keep_logits``: whether the backward finds the logits kept (fp16, ``2 T V`` bytes
-    until it is done; bf16 inputs only) or computes them again; by itself, kept up to
+    ``keep_logits``: whether the backward finds the logits kept (16 bits each, ``2 T V``
+    bytes until it is done; bf16 inputs only) or computes them again; by itself, kept up to
     ``KEEP_LOGITS_BYTES``. It forms the logit gradients a chunk of the vocabulary at a
     time (``vocab_chunk`` columns, or as many as fit 256 MiB).
     """

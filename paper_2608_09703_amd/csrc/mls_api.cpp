@@ -580,7 +580,7 @@ bool rows_core(const mls_problem* p, const Plan& pl) {
 }
 
 // Tile kernel of the forward of tokens [t0, t0 + tc): partial records, and with
-// lslab the fp16 logits. n_rows: of token log-probabilities' rows, as many of these
+// lslab the 16-bit logits. n_rows: of token log-probabilities' rows, as many of these
 // as the device counts.
 hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc, float4* partials,
                          uint16_t* lslab, const int32_t* n_rows, hipStream_t s) {
@@ -644,8 +644,8 @@ hipError_t finish_losses(const mls_problem* p, const Plan& pl, void* stats, floa
 }
 
 // Launches of the backward: of the losses (g_ce, g_kl) or, with rows, of token
-// log-probabilities, whose problem p holds the packed rows, whose number of rows the
-// header has and whose logits rows->kept may hold.
+// log-probabilities, whose problem p holds the packed and scaled rows, whose number of
+// rows the header has and whose logits rows->kept may hold.
 mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats, const float* g_ce,
                         const float* g_kl, const TokenArgs* rows, void* const* grad_h, float* const* grad_W,
                         void* workspace, size_t workspace_bytes, void* stream) {
@@ -669,6 +669,7 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   a.g_ce = g_ce;
   a.g_kl = g_kl;
   a.g_row = g_row;
+  if (rows) a.h[0] = rows->hc;  // (p has the scaled ones, for grad_W)
   a.n_rows = g_row ? a.n_valid : nullptr;
   const bool rows_tiles = g_row && rows_core(p, pl);
   const int fbm = rows_tiles ? kRowsTile : fused_tile_rows(pl.f32);
@@ -912,10 +913,10 @@ constexpr int64_t kTokenSlabBytes = 256ll << 20;
 // and products need.
 struct TokenPlan {
   Plan pl;         // of the packed rows
-  mls_problem q;   // p with the rows' grad_h (the scatter adds to an output)
-  size_t off_hc = 0, off_tokens = 0, off_lab = 0, off_part = 0, off_gh = 0, off_work = 0;
+  mls_problem q;   // p with the rows' grad_h (fp32: the scatter scales it, and adds to an output)
+  size_t off_hc = 0, off_tokens = 0, off_lab = 0, off_scale = 0, off_hs = 0, off_part = 0, off_gh = 0, off_work = 0;
   size_t fwd_bytes = 0, bwd_bytes = 0, bwd_room = 0;  // room: see Plan
-  // kept logits (bf16 in one forward chunk): the rows' fp16 distances, then the
+  // kept logits (bf16 in one forward chunk): the rows' distances, then the
   // partial records with the maxima they are relative to
   int n_rec = 0;
   size_t kept_rec = 0, kept_bytes = 0;
@@ -923,8 +924,7 @@ struct TokenPlan {
 
 void token_plan(const mls_problem* p, TokenPlan& tp) {
   tp.q = *p;
-  // what is added to an output is added in fp32
-  if (p->flags & MLS_ACCUMULATE_GRAD_H) tp.q.grad_h_dtype = MLS_F32;
+  tp.q.grad_h_dtype = MLS_F32;
   tp.q.flags &= ~(uint32_t)MLS_ACCUMULATE_GRAD_H;
   const int64_t es = p->in_dtype == MLS_F32 ? 4 : 2, T_pad = round_up(p->T, kFusedBN);
   const int64_t whole = T_pad * round_up(p->V, 256) * es;
@@ -939,6 +939,8 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   off = align256(off + (size_t)pl.T * sizeof(int64_t));
   tp.off_lab = off;  // forward: own logits; backward: gradients
   off = align256(off + (size_t)pl.T * sizeof(float));
+  tp.off_scale = off;
+  off = align256(off + (size_t)pl.T * sizeof(float));
   tp.off_part = tp.off_gh = off;
   tp.fwd_bytes = off + pl.off_lab;  // the forward's partial records
   tp.n_rec = (rows_core(p, pl) ? (int)((pl.V + kRowsTile - 1) / kRowsTile) : pl.n_vt_fwd) * kFusedFwdParts;
@@ -946,7 +948,9 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
     tp.kept_rec = align256((size_t)pl.T_pad * kept_ld(pl) * 2);
     tp.kept_bytes = tp.kept_rec + align256((size_t)tp.n_rec * pl.T_pad * sizeof(float4));
   }
-  off = align256(off + (size_t)pl.T * p->d[0] * (tp.q.grad_h_dtype == MLS_F32 ? 4 : 2));
+  off = align256(off + (size_t)pl.T * p->d[0] * sizeof(float));
+  tp.off_hs = off;
+  off = align256(off + (size_t)pl.T_pad * p->d[0] * pl.es);
   tp.off_work = off;
   tp.bwd_bytes = off + pl.bwd_bytes;
   // (the slab alone may be smaller for more tokens, where chunks get narrower)
@@ -971,6 +975,7 @@ TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
   a.rank = reinterpret_cast<int32_t*>(sf);           // lse1
   a.lse = sf + pl.T;                                 // lset
   a.index = reinterpret_cast<int32_t*>(sf + 2 * pl.T);  // ce_row
+  a.logp_c = sf + 3 * pl.T;                          // kl_row
   a.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
   return a;
 }
@@ -1483,25 +1488,26 @@ mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const voi
     a.rec_rows = (int32_t)((rows_core(p, pl) ? kRowsTile : kFusedBM) / kFusedFwdParts);
     a.partials = reinterpret_cast<const float4*>(static_cast<const char*>(kept) + tp.kept_rec);
   }
-  a.hc = ws + tp.off_hc;
+  a.hc = kept ? nullptr : ws + tp.off_hc;
+  a.hs = ws + tp.off_hs;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
   a.g = g_logp;
   a.g_c = reinterpret_cast<float*>(ws + tp.off_lab);
+  a.scale = reinterpret_cast<float*>(ws + tp.off_scale);
   hipError_t e;
   {
     ProfScope ps("token_gather", s);
     e = launch_token_gather(a, pl.f32, s);
   }
   if (e != hipSuccess) return hip_fail(e, "token rows launch");
-  tp.q.h[0] = a.hc;
+  tp.q.h[0] = a.hs;
   tp.q.labels = a.tokens_c;
   void* const gh[1] = {grad_h ? ws + tp.off_gh : nullptr};
   float* const gW[1] = {static_cast<float*>(grad_W)};
   st = run_backward(&tp.q, pl, stats, nullptr, nullptr, &a, gh, gW, ws + tp.off_work,
                     workspace_bytes - tp.off_work, stream);
   if (st != MLS_OK || !grad_h) return st;
-  a.gh_c = gh[0];
-  a.gh_f32 = tp.q.grad_h_dtype == MLS_F32 ? 1 : 0;
+  a.gh_c = static_cast<const float*>(gh[0]);
   a.out_f32 = p->grad_h_dtype == MLS_F32 ? 1 : 0;
   a.accumulate = (p->flags & MLS_ACCUMULATE_GRAD_H) ? 1 : 0;
   a.grad_h = grad_h;

@@ -86,13 +86,13 @@ __device__ __forceinline__ int64_t live_rows(const FusedArgs& a) {
 // (max, sum exp, sum exp at tau, teacher-weighted logit sum) per token and wave
 // row. Each wave normalises to the max over its own rows, so the epilogue needs
 // no exchange between waves; the row merge rescales the records.
-// STORE (fused forward + backward; token log-probabilities with kept logits): every
-// logit also goes to the chunk's slab as
+// STORE (fused forward + backward): every logit also goes to the chunk's slab as
 // fp16 of its distance to the record's maximum (at most 0; 2^-11 relative, so
 // the entries that carry the softmax's mass, near the maximum, are the most
 // exact), token-major, for the logit gradient pass.
 // ROWS (token log-probabilities): the number of rows is read from the device;
-// with one temperature, TAU1's single sum at a.tau.
+// with one temperature, TAU1's single sum at a.tau. STORE keeps the logits, in
+// kKeptRange's form.
 template <class Mma, typename E, bool TAU1, int MINB = 1, bool STORE = false, bool ROWS = false>
 __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
@@ -121,6 +121,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   const int64_t tbase = (int64_t)tt * BN;
   const bool full = vbase + BM <= a.V;
   const float ct = kLog2e * a.inv_tau;
+  const float ks = -a.inv_tau / kKeptRange;
   // records of sub-model order[oi] and token group tbase / kFusedBN: [n_vt * WGM][kFusedBN]
   const int64_t n_rec = (int64_t)a.n_vt * WGM;
   const int64_t n_tg = (T + kFusedBN - 1) / kFusedBN;
@@ -180,8 +181,11 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
             for (int k = 0; k < 2; ++k) {
               const float x0 = mma.acc[fm][fn][rg * 4 + 2 * k] - mb;
               const float x1 = mma.acc[fm][fn][rg * 4 + 2 * k + 1] - mb;
-              w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x0) |
-                     ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x1) << 16);
+              if constexpr (ROWS)  // (the conversion takes what lies outside of [0, 1] to its ends)
+                w[k] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(x0 * ks, x1 * ks));
+              else
+                w[k] = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x0) |
+                       ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x1) << 16);
             }
             const int chunk = (fm * 4 + rg) ^ (c & (kCh - 1));  // 8 vocabulary rows per chunk
             *reinterpret_cast<uint2*>(stg + c * kRow + chunk * 16 + hi * 8) = make_uint2(w[0], w[1]);
@@ -287,9 +291,9 @@ __device__ __forceinline__ void store4<F32>(float* p, float a0, float a1, float 
 
 // Backward tile kernel of the fp32 path (one slab, token-major) and of the
 // general bf16 path (both slab layouts).
-// ROWG (one sub-model): the gradient of the rows' log-probabilities at
-// temperature tau, G = g_row / tau (onehot - softmax(l / tau)), in place of the
-// losses', over the rows that the device counts.
+// ROWG (one sub-model): the scaled gradient of the rows' log-probabilities at
+// temperature tau, g_row / tau (onehot - softmax(l / tau)), in place of the losses',
+// over the rows that the device counts.
 template <class Mma, typename E, bool TAU1, bool ROWG = false>
 __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;

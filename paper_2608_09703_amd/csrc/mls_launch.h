@@ -16,6 +16,12 @@ constexpr int kFusedBM = 128;      // general core
 constexpr int kFusedWideBM = 128;  // wide bf16 core
 constexpr int kFusedF32 = 64;      // fp32 core, rows and columns
 constexpr int kRowsKTile = 64;     // rows that its gradient products read at a time
+// Kept logits of token log-probabilities: 16 bits of the distance below a maximum,
+// over tau, in 65,535ths of this. A step of 2^-11 wherever in the range (an exponential
+// wants its argument to an absolute precision, which fp16 has near 0 only: softmax entries
+// 2^-12 off at most, for fp16 2^-9 where most of a wide softmax lies, 4 to 8 below);
+// entries further below count as this far, e^-32 of the maximum's.
+constexpr float kKeptRange = 32.f;
 constexpr int kRowsTile = 256;     // core of token log-probabilities, rows and columns
 // forward partial records per (vocabulary tile, token, sub-model): one per
 // wave row of the tile, each over its own half of the tile's rows; their
@@ -67,8 +73,8 @@ struct FusedArgs {
   const float* g_kl;
   // token log-probabilities (M = 1); null for the losses. The rows are the tokens
   // that count, *n_rows of them: this launch's are [row0, min(row0 + T, *n_rows)),
-  // and T and n_tt only bound them. g_row (backward): upstream gradient of each
-  // row's log-probability at temperature tau
+  // and T and n_tt only bound them. g_row (backward): what each row's
+  // onehot - softmax at temperature tau is multiplied with, times tau
   const int32_t* n_rows;
   int64_t row0;
   int32_t tile_v;  // kRowsTile: that core's tiles; else 0
@@ -201,13 +207,17 @@ struct TokenArgs {
   int32_t* index;         // [T] token of each row
   float* logp;            // [T]
   float* entropy;         // [T] or null
-  void* hc;               // [T_pad][d] their hidden states; zeros behind the last
+  void* hc;               // [T_pad][d] their hidden states; zeros behind the last (or null)
+  void* hs;               // backward: the same, scaled
   int64_t* tokens_c;      // [T] their ids
   float* lab;             // [T] forward: their own logits
   const float* g;         // [T] backward: gradients by token
-  float* g_c;             // [T] and by row
+  // by row, with q = 1 - exp(logp): tau / q (what the logit gradients are formed
+  // with) and g q / tau (their scale, which goes into hs and into grad_h)
+  float* g_c;             // [T]
+  float* scale;           // [T]
   // logit gradients of a vocabulary chunk from the kept logits
-  const uint16_t* kept;   // [T_pad][ld_kept] fp16 distances to their record's maximum
+  const uint16_t* kept;   // [T_pad][ld_kept] distances to their record's maximum (kKeptRange)
   int64_t ld_kept;
   int32_t rec_rows;       // vocabulary rows of a record
   int64_t v0;             // first column of the chunk
@@ -220,9 +230,9 @@ struct TokenArgs {
   int32_t n_rec;
   const float4* partials;
   float* lse;             // [T] by row
-  // grad_h by token from the rows' one
-  const void* gh_c;       // [T][d] in the type gh_f32 says
-  int32_t gh_f32;
+  float* logp_c;          // [T] by row
+  // grad_h by token from the rows' one, before the scale
+  const float* gh_c;      // [T][d]
   int32_t out_f32;
   int32_t accumulate;
   void* grad_h;           // [T][d]

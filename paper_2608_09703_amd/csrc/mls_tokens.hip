@@ -75,9 +75,18 @@ __global__ __launch_bounds__(kPackThreads) void token_pack_kernel(TokenArgs a) {
   a.header[1] = bad ? MLS_DEVFLAG_LABEL_RANGE : 0;
 }
 
+// What of 1 - p an fp32 log-probability near 0 still tells: scales are not smaller.
+constexpr float kMinRest = 0x1p-20f;
+
 // One wave per token and, for the rows behind the last one, per row: copies the
-// token's hidden state to its row and its id and gradient along, and takes its own
-// logit <h, W[y]> on the way (forward).
+// token's hidden state to its row and its id along, and takes its own logit <h, W[y]>
+// on the way (forward).
+// Backward: with q = 1 - p[y] the logit gradient is G = s E, s = g q / tau and
+// E = (onehot(y) - p) / q, and the products run on E, rounded to bfloat16, whose own
+// token's entry is 1. That entry carries most of G, and whole rows of grad_W when few
+// tokens count: rounded as g q / tau it left them up to 2^-8 off in every element at
+// once. s goes into the copied hidden states for grad_W (sum_t E s h: one rounding an
+// element, which the others average) and, in fp32, into grad_h's rows after the product.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
   using S = typename E::storage;
@@ -86,9 +95,12 @@ __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= a.T_pad) return;
   S* hc = static_cast<S*>(a.hc);
+  S* hs = static_cast<S*>(a.hs);
   if (t >= a.header[0]) {
-    for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer)
-      *reinterpret_cast<uint4*>(hc + t * a.d + k) = make_uint4(0, 0, 0, 0);
+    for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer) {
+      if (hc) *reinterpret_cast<uint4*>(hc + t * a.d + k) = make_uint4(0, 0, 0, 0);
+      if (hs) *reinterpret_cast<uint4*>(hs + t * a.d + k) = make_uint4(0, 0, 0, 0);
+    }
   }
   if (t >= a.T) return;
   const int64_t r = a.rank[t];
@@ -96,11 +108,22 @@ __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
   const int64_t y = a.tokens[t];
   const S* h = static_cast<const S*>(a.h) + t * a.d;
   const S* w = static_cast<const S*>(a.W) + y * a.d;
-  float s = 0.f;
+  float s = 0.f, scale = 0.f, rest = 0.f;
+  if (hs) {
+    rest = fmaxf(-expm1f(a.logp_c[r]), kMinRest);
+    scale = a.g[t] / a.tau * rest;
+  }
   for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer) {
     const uint4 hv = *reinterpret_cast<const uint4*>(h + k);
-    *reinterpret_cast<uint4*>(hc + r * a.d + k) = hv;
-    if (!a.lab) continue;
+    if (hc) *reinterpret_cast<uint4*>(hc + r * a.d + k) = hv;
+    if (hs) {
+      float v[kPer];
+      Chunk<E>::unpack(hv, v);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[i] *= scale;
+      *reinterpret_cast<uint4*>(hs + r * a.d + k) = Chunk<E>::pack(v);
+      continue;
+    }
     const uint4 wv = *reinterpret_cast<const uint4*>(w + k);
     const uint32_t hu[4] = {hv.x, hv.y, hv.z, hv.w};
     const uint32_t wu[4] = {wv.x, wv.y, wv.z, wv.w};
@@ -114,11 +137,15 @@ __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
       }
     }
   }
-  if (a.lab) s = wave_sum(s);
+  if (!hs) s = wave_sum(s);
   if (lane != 0) return;
   a.tokens_c[r] = y;
-  if (a.lab) a.lab[r] = s;
-  if (a.g) a.g_c[r] = a.g[t];
+  if (hs) {
+    a.g_c[r] = a.tau / rest;
+    a.scale[r] = scale;
+  } else {
+    a.lab[r] = s;
+  }
 }
 
 // Row merge (one sub-model, temperature tau):
@@ -160,21 +187,20 @@ __global__ __launch_bounds__(kThreads) void token_merge_kernel(TokenArgs a) {
   const float lse = st.m[0] * inv_tau + logf(st.st[0]);
   const float lp = fmaf(a.lab[r], inv_tau, -lse);
   a.lse[r] = lse;
+  a.logp_c[r] = lp;
   a.logp[t] = lp;
   if (a.entropy) a.entropy[t] = lse - st.xr[0] / (a.tau * st.st[0]);
   if (!isfinite(lp)) atomicOr(a.header + 1, MLS_DEVFLAG_NONFINITE);
 }
 
 // Logit gradients of a vocabulary chunk from the kept logits:
-//   G = g / tau (onehot(y) - softmax(l / tau)),  l = m + d
-// with the kept fp16 distance d to the record's maximum m. One wave per row and 512
+//   E = g_c / tau (onehot(y) - softmax(l / tau)),  l / tau = m / tau - d
+// (see the gather), with the kept distance d (kKeptRange's form) to the record's maximum m. One wave per row and 512
 // columns, 16-byte accesses; bound by the 4 bytes an element that it moves, where the
 // tile kernel computes 2 d operations an element again. T = 4,096 (3,071 counted),
-// d = 4,352, V = 49,152: 112 us (5.4 TB/s) for 1,200, and the forward's stores cost
-// it 43; T = 1,531, d = 1,000, V = 32,003: 37 for 139. fp16: d is off by 2^-11 d at
-// most, and exp(d) is small where that is much: the error of p is below 2^-12 of the
-// record's largest p, 1/16 of the rounding of G to bf16 there. Rows behind the last are
-// 0 as far as a K-tile of the products reads.
+// d = 4,352, V = 49,152: 106 us (5.7 TB/s) for 1,200, and the forward's stores cost
+// it 43; T = 1,531, d = 1,000, V = 32,003: 37 for 139. Rows
+// behind the last are 0 as far as a K-tile of the products reads.
 constexpr int kGradSpan = 512;
 __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenArgs a) {
   const int lane = threadIdx.x & 63;
@@ -192,40 +218,45 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenArgs a) {
   const uint4 w4 = load16_nt(a.kept + r * a.ld_kept + v);
   const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
   const float inv_tau = 1.0f / a.tau;
-  const float ct = kLog2e * inv_tau;
-  const float ls = a.lse[r] * kLog2e;
+  const float mt = fmaf(m, kLog2e * inv_tau, -a.lse[r] * kLog2e);
   const float c = a.g_c[r] * inv_tau;
   const int yrel = (int)(a.tokens_c[r] - v);
   float g[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float d = (float)__builtin_bit_cast(_Float16, (uint16_t)((i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu));
-    const float p = v + i < a.V ? fast_exp2(fmaf(d + m, ct, -ls)) : 0.f;
-    g[i] = c * ((i == yrel ? 1.f : 0.f) - p);
+    const uint32_t d = (i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
+    const float p = fast_exp2(fmaf((float)d, -kLog2e * kKeptRange / 65535.f, mt));
+    g[i] = v + i < a.V ? -c * p : 0.f;
+  }
+  if (yrel >= 0 && yrel < 8) {
+    const float own = -expm1f(a.logp_c[r]) * c;  // 1, up to the floor of the rest
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i == yrel) g[i] = own;
   }
   *reinterpret_cast<uint4*>(out) = Chunk<Bf16>::pack(g);
 }
 
-// grad_h by token: its row's, or zeros (with accumulate, nothing) where it does not
-// count. One wave per token, 4 elements per lane and step (both widths' granularity).
-template <typename G, typename O>
+// grad_h by token: its row's times the row's scale, or zeros (with accumulate, nothing)
+// where it does not count. One wave per token, 4 elements per lane and step (both
+// widths' granularity).
+template <typename O>
 __global__ __launch_bounds__(kThreads) void token_scatter_kernel(TokenArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= a.T) return;
   const int64_t r = a.rank[t];
   if (r < 0 && a.accumulate) return;
-  const typename Elt<G>::type* src = static_cast<const typename Elt<G>::type*>(a.gh_c) + r * a.d;
+  const float* src = a.gh_c + r * a.d;
+  const float scale = r >= 0 ? a.scale[r] : 0.f;
   typename Elt<O>::type* out = static_cast<typename Elt<O>::type*>(a.grad_h) + t * a.d;
   for (int64_t k = (int64_t)lane * 4; k < a.d; k += 64 * 4) {
     float v[4] = {0.f, 0.f, 0.f, 0.f};
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
     if (r >= 0) load4<false>(src + k, v);
-    if (a.accumulate) {
-      float o[4];
-      load4<false>(out + k, o);
+    if (a.accumulate) load4<false>(out + k, o);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] += o[i];
-    }
+    for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], scale, o[i]);
     store4<false>(out + k, v);
   }
 }
@@ -261,14 +292,10 @@ hipError_t launch_token_merge(const TokenArgs& a, hipStream_t stream) {
 
 hipError_t launch_token_scatter(const TokenArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.T + 3) / 4));
-  if (a.gh_f32 && a.out_f32)
-    hipLaunchKernelGGL((token_scatter_kernel<F32, F32>), grid, dim3(kThreads), 0, stream, a);
-  else if (a.gh_f32)
-    hipLaunchKernelGGL((token_scatter_kernel<F32, Bf16>), grid, dim3(kThreads), 0, stream, a);
-  else if (!a.out_f32)
-    hipLaunchKernelGGL((token_scatter_kernel<Bf16, Bf16>), grid, dim3(kThreads), 0, stream, a);
+  if (a.out_f32)
+    hipLaunchKernelGGL(token_scatter_kernel<F32>, grid, dim3(kThreads), 0, stream, a);
   else
-    return hipErrorInvalidValue;
+    hipLaunchKernelGGL(token_scatter_kernel<Bf16>, grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -4,12 +4,14 @@ Forward: fp32 rows, the statistics' tolerance of the fused loss (5e-5 for a
 log-sum-exp and a logit of fp32 sums). Gradients: every row within the fused loss's
 gradient bounds (the logit gradient is bf16 in between on the bf16 path), and
 element by element within what the roundings allow: with G the exact logit gradient,
-2^-8 sum |G| |W| for its rounding, as much again of the result for the output's, and
+2^-8 sum |G| |W| for its rounding (of its entries over the own token's one), for grad_W
+2^-8 sum |G| |h| more for the rounding of the scaled hidden states (and the product of
+both, 2^-16), 2^-8 of the result for the output's, and
 2^-12 sum |G| |W| for the recomputed logits (a logit of fp32 sums is off by less than
 2^-13 here, and exp turns that into a relative error of G's softmax part). A kept
-logit is fp16, as its distance below the maximum of a few vocabulary rows, which is at
-most its distance x below the row's: it is off by 2^-11 x, and the softmax entry p by
-2^-11 (x / tau) p. E in the check is what that adds to G.
+logit's distance below a maximum, over tau, is off by half a step of 32 / 65535, and so
+the softmax entry p by 2^-12 p (1.01 of it, with exp's second order); entries further than
+32 below count as e^-32 of the maximum's. E in the check is what that adds to G.
 """
 
 import numpy as np
@@ -60,14 +62,14 @@ def _check(h, W, tokens, gl, temperature, got, what):
     half = 2.0 ** -8 if bf16 else 2.0 ** -24
     E = np.zeros_like(G)
     if bf16 and rows.size:
-        x = z.max(1, keepdims=True) - z  # over tau
-        E[rows] = 2.0 ** -11 * x * p / p.sum(1, keepdims=True) * np.abs(gn[rows])[:, None] / temperature
-    for g, r, s, e, name in ((gh, rh, G @ np.abs(Wn), E @ np.abs(Wn), "grad_h"),
-                             (gW, rW, G.T @ np.abs(hn), E.T @ np.abs(hn), "grad_W")):
+        E[rows] = (1.01 * 2.0 ** -12 * p / p.sum(1, keepdims=True) + np.exp(-32.0)) * np.abs(gn[rows])[:, None] / temperature
+    rel_W = rel + 2.0 ** -8 + 2.0 ** -16 if bf16 else rel
+    for g, r, s, e, name in ((gh, rh, rel * (G @ np.abs(Wn)), E @ np.abs(Wn), "grad_h"),
+                             (gW, rW, rel_W * (G.T @ np.abs(hn)), E.T @ np.abs(hn), "grad_W")):
         if g is None:
             continue
         gn_ = _np(g)
-        bad = ~(np.abs(gn_ - r) <= rel * s + e + half * np.abs(r))
+        bad = ~(np.abs(gn_ - r) <= s + e + half * np.abs(r))
         assert not bad.any(), f"{what} {name}: {bad.sum()} off, first at {np.argwhere(bad)[0]}"
         assert_grad_rows(gn_, r, f"{what} {name}")
     return rh, rW
@@ -111,6 +113,65 @@ def test_kept_logits(d, monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(again[1], grads()[1]))
 
 
+@pytest.mark.parametrize("d,rec", [(64, 64), (2048, 128)])
+def test_what_is_kept_of_a_logit(d, rec):
+    """Rows of 16 bits: the nearest 65,535th of 32 to the distance below the record's maximum, over tau."""
+    T, V, tau = 300, 700, 0.5
+    h = torch.zeros(T, d, dtype=torch.bfloat16, device=DEV)
+    h[:, 0] = torch.linspace(0.25, 1.5, T)
+    W = torch.zeros(V, d, dtype=torch.bfloat16, device=DEV)
+    W[:, 0] = torch.randn(V, device=DEV) * 4
+    W[::90, 0] = -40.0
+    tokens = torch.zeros(T, dtype=torch.int64, device=DEV)
+    p = D.make_problem([h], [W], tokens, tau=tau)
+    fwd, _, size = B.token_logp_workspace(p)
+    kept = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(fwd, dtype=torch.uint8, device=DEV)
+    stats = torch.empty(B.query_sizes(p)[1], dtype=torch.uint8, device=DEV)
+    logp = torch.empty(T, device=DEV)
+    B.token_logp_fwd(p, stats.data_ptr(), logp.data_ptr(), None, kept.data_ptr(), ws.data_ptr(), fwd,
+                     D._stream(h.device))
+    ld = (V + 255) // 256 * 256
+    got = kept[:2 * T * ld].cpu().numpy().view(np.uint16).reshape(T, ld)[:, :V].astype(np.float64)
+    z = _np(h)[:, :1] * _np(W)[:, 0]  # exact: products of two bf16 numbers
+    for v0 in range(0, V, rec):
+        x = (z[:, v0:v0 + rec].max(1, keepdims=True) - z[:, v0:v0 + rec]) / tau / 32 * 65535
+        # half a step, and three fp32 roundings of a value up to 65535
+        assert np.abs(got[:, v0:v0 + rec] - np.minimum(x, 65535)).max() <= 0.5 + 3 * 65535 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("keep", [True, False])
+@pytest.mark.parametrize("T", [1, 5, 40])
+def test_few_tokens_keep_their_digits(T, keep):
+    """The token's own entry of the logit gradient carries grad_h and the own rows of grad_W: it is not
+    rounded, so what is left is one rounding of each element (relative rms 2^-8 / sqrt(3) at most, where
+    roundings were uniform) and 2^-12 of the softmax; a rounded entry would add up to 2^-8 to all at once."""
+    h, W, tokens, gl = _draw(T, 512, 4000, torch.bfloat16, 20 + T, ignore=0.0)
+    logp, _, gh, gW = _run(h, W, tokens, gl, keep_logits=keep)
+    rh, rW = P.token_logp_backward(_np(h), _np(W), tokens.cpu().numpy(), _np(gl))
+    for g, r, name in ((gh, rh, "grad_h"), (gW, rW, "grad_W")):
+        rows = np.unique(tokens.cpu().numpy()) if name == "grad_W" else slice(None)
+        e = np.linalg.norm(_np(g)[rows] - r[rows], axis=1) / np.linalg.norm(r[rows], axis=1)
+        assert e.max() <= 2.0 ** -8 / 3 ** 0.5 + 2.0 ** -11, (name, e)
+
+
+def test_a_token_that_is_nearly_certain():
+    """1 - p from the log-probability: gradients of confident tokens keep their size."""
+    h, W, tokens, gl = _draw(64, 256, 1000, torch.bfloat16, 30, ignore=0.0)
+    W[tokens] += (h.float() * 0.05).to(W.dtype)
+    logp, _, gh, gW = _run(h, W, tokens, gl)
+    lp = P.token_logp(_np(h), _np(W), tokens.cpu().numpy())[0]
+    assert np.median(lp) > -0.1
+    rh, rW = P.token_logp_backward(_np(h), _np(W), tokens.cpu().numpy(), _np(gl))
+    # one rounding of each element, one of each softmax entry over 1 - p (2^-8 at most, of entries that add up
+    # to 1 like the own token's), and 1 - p is off by logp's error, under 2^-18 for logits of 16: 2^-10 of 2^-8
+    z = 1 - np.exp(lp)
+    n = np.linalg.norm
+    ok = z > 2.0 ** -8
+    e = n(_np(gh) - rh, axis=1) / n(rh, axis=1)
+    assert ok.any() and e[ok].max() <= 2.0 ** -8 + 2.0 ** -10
+
+
 def test_kept_logits_are_freed_by_the_backward():
     T, d, V = 2000, 64, 20000
     h, W, tokens, gl = _draw(T, d, V, torch.bfloat16, 13)
@@ -137,7 +198,7 @@ def test_kept_logits_over_many_tokens_and_chunks(T, d, V, chunk):
 
 @pytest.mark.parametrize("keep", [True, False])
 def test_far_logits(keep):
-    """Logits hundreds apart: entries that the softmax leaves nothing of, and distances past fp16."""
+    """Logits hundreds apart: entries that the softmax leaves nothing of, and distances past what is kept."""
     h, W, tokens, gl = _draw(130, 64, 1000, torch.bfloat16, 15)
     h[::3] *= 30
     h[1::3] *= 3e4
