@@ -218,17 +218,17 @@ void grad_h_parts(const mls_problem* p, int64_t rows, int64_t vrows, size_t room
 }
 
 // K parts of grad_h's products on the fp32 path of token log-probabilities, whose one
-// chunk has a K of all of V: as many as make 512 tiles of 32 x 32 of it, 256 of K or
-// more each (T = 256, d = 256, V = 4,096: 64 tiles of 4,096 took 50 us of a launch
-// whose other 1,024 tiles need half of that). ksplit is a multiple of the K-tile.
-constexpr int64_t kF32PartK = 256;
-int64_t f32_most_parts(int64_t T, int64_t V, int64_t d) {
-  const int64_t tiles = (T + 31) / 32 * ((d + 31) / 32);
-  return std::min<int64_t>({kMaxSplits, 512 / tiles, V / kF32PartK});
-}
+// chunk has a K of all of V where grad_W's tiles have one of T: parts of about T, or of
+// 512 where T is less, so that the launch's tiles are alike and the few of grad_h are
+// not what it waits for. ksplit is a multiple of the K-tile. us of the gradient products
+// with these / with as many parts as make 512 tiles of 32 x 32 / in one: T = 256, d = 256,
+// V = 4,096: 25 / 28 / 50; T = 939, d = 240, V = 9,409: 123 / 162; T = 1,500, d = 512,
+// V = 16,000: 387 / 567. Parts of 256 or 1,024 in place of 512: up to 3 more or 4 more.
+constexpr int64_t kF32PartK = 512;
+int64_t f32_most_parts(int64_t T, int64_t V) { return std::min<int64_t>(kMaxSplits, V / std::max(T, kF32PartK)); }
 void f32_parts(const mls_problem* p, const Plan& pl, size_t room, int* splits, int64_t* ksplit) {
   const int64_t V = std::min(pl.Vc, pl.V), out = pl.T * p->d[0] * 4;
-  const int64_t n = std::min<int64_t>(f32_most_parts(pl.T, V, p->d[0]), room / out);
+  const int64_t n = std::min<int64_t>(f32_most_parts(pl.T, V), room / out);
   if (n < 2) return;
   *ksplit = ((V + n - 1) / n + 127) / 128 * 128;
   *splits = (int)((V + *ksplit - 1) / *ksplit);
@@ -510,11 +510,13 @@ void host_coeffs(int M, int s, float alpha, float tau, int mode, const float* w,
 // fill the chip. Measured per launch, 32 against 64: 22 against 37 us at 120
 // tiles of 64 x 64 (T = 256, widths 128 / 256, chunks of 1,024), 48 against 71
 // at 258, 73 against 73 at 504, 102 against 109 at 696, 161 against 125 at 1,160.
-int f32_gemm_tile(const Plan& pl, const mls_problem* p) {
+// Token log-probabilities, whose grad_h comes in parts (or has a K no longer than
+// grad_W's), gain from the larger tile earlier: 28 against 25 at 384, 191 against 162 at 504.
+int f32_gemm_tile(const Plan& pl, const mls_problem* p, int parts, bool rows) {
   int64_t tiles = 0;
   for (int i = 0; i < pl.M; ++i)
-    tiles += ((pl.T + 63) / 64 + (pl.Vc + 63) / 64) * ((p->d[i] + 63) / 64);
-  return tiles >= 900 ? 64 : 32;
+    tiles += ((pl.T + 63) / 64 * parts + (pl.Vc + 63) / 64) * ((p->d[i] + 63) / 64);
+  return tiles >= (rows ? 300 : 900) ? 64 : 32;
 }
 
 // grad_h rows [t0, t0 + rows) of every sub-model from their K parts, which lie
@@ -691,7 +693,7 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   const size_t slab_stride = (size_t)pl.T_pad * pl.Vc * pl.es;
   int tbm = gemm_tile_rows(pl.wide_bwd);
   int tbn = gemm_tile_cols(pl.wide_bwd);
-  if (pl.f32) tbm = tbn = f32_gemm_tile(pl, p);
+  if (pl.f32) tbm = tbn = f32_gemm_tile(pl, p, splits, g_row != nullptr);
   hipError_t e;
 
   // general path: h_i^T [d_i, T_pad] for the grad_W products
@@ -955,7 +957,8 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   tp.bwd_bytes = off + pl.bwd_bytes;
   // (the slab alone may be smaller for more tokens, where chunks get narrower)
   tp.bwd_room = off + std::max<size_t>(pl.bwd_room, align256((size_t)std::min(whole, kTokenSlabBytes)));
-  if (pl.f32) tp.bwd_room += align256((size_t)f32_most_parts(p->T, std::min(pl.Vc, pl.V), p->d[0]) * p->T * p->d[0] * 4);
+  // (as many parts times T, rounded up to what does not shrink for more tokens)
+  if (pl.f32) tp.bwd_room += align256((size_t)(std::min(kMaxSplits * p->T, pl.V) * p->d[0]) * 4);
 }
 
 TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
