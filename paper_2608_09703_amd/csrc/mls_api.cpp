@@ -90,6 +90,11 @@ constexpr int64_t kLogitSlabBudget = 16ll << 30;  // stored logits of one token 
 constexpr int64_t kPanelMax = (1ll << 32) - 1;    // bytes one wide-GEMM operand may span
 constexpr int64_t kCus = 256;                     // compute units of the part
 constexpr int64_t kMaxSplits = 16;                // K parts of a grad_h product
+// and of token log-probabilities', whose one chunk has a K of all of V for as little as
+// a row. us of the gradient products, at most 16 / 32 / 64 / 128 parts: T = 18, d = 504,
+// V = 105,482: 108 / 60 / 55 / 53 (and their sum 7 / 9 / 13 / 13); T = 132, d = 448,
+// V = 60,836: 68 / 42 / 41 / 41; T = 651, d = 440, V = 121,655: 232 / 199 / 197 / 193
+constexpr int64_t kRowsMaxSplits = 64;
 constexpr int64_t kPartTiles = 192;               // grad_h tiles of a launch that still takes K parts
 constexpr int64_t kPartBytes = 128ll << 20;       // fp32 outputs of all parts
 
@@ -167,9 +172,9 @@ int64_t grad_h_cols(const mls_problem* p) {
 }
 
 // The most K parts for vrows of K: 16 K-tiles or more each.
-int64_t max_parts(int64_t vrows) {
+int64_t max_parts(int64_t vrows, int64_t cap) {
   const int64_t bk = gemm_wide_k_tile();
-  return std::min(kMaxSplits, (vrows + bk - 1) / bk / 16);
+  return std::min(cap, (vrows + bk - 1) / bk / 16);
 }
 
 // K parts of the grad_h products of one launch of the wide gradient GEMM over
@@ -177,7 +182,7 @@ int64_t max_parts(int64_t vrows) {
 // bytes, and the K extent of a part. A grad_h tile runs over all of vrows, a
 // grad_W tile over the tokens only, so with few tokens the launch has few, long
 // grad_h tiles and lasts as long as one of them while most CUs are done. K is
-// cut into as many parts (at most kMaxSplits) as give the shortest launch by a
+// cut into as many parts (at most cap) as give the shortest launch by a
 // count of K-tiles per CU, a tile's prologue and output counted as 6 and the sum
 // over the parts at 5 TB/s; not for less than 4 %. Above kPartTiles tiles few CUs
 // idle and parts pay little or nothing: at 196, two parts against one take 1,321
@@ -187,7 +192,7 @@ int64_t max_parts(int64_t vrows) {
 // and with them: T = 512, widths 1,024 / 2,048 / 3,072, V = 50,304: 3,273 ->
 // 1,829 us; T = 1,024, widths 512 / 1,024, V = 32,000: 1,394 -> 483 us. With
 // 4,096 tokens of the headline shape one part remains the shortest.
-void grad_h_parts(const mls_problem* p, int64_t rows, int64_t vrows, size_t room, int* splits,
+void grad_h_parts(const mls_problem* p, int64_t rows, int64_t vrows, size_t room, int64_t cap, int* splits,
                   int64_t* ksplit) {
   constexpr int64_t kTileCost = 6;       // K-tiles
   constexpr int64_t kTileBytes = 4 << 20;  // bytes at 5 TB/s in a K-tile's 0.8 us
@@ -203,7 +208,7 @@ void grad_h_parts(const mls_problem* p, int64_t rows, int64_t vrows, size_t room
   if (n1 > kPartTiles || most < 2) return;
   int64_t best = launch_span(n1, nk + kTileCost, n2, nkw + kTileCost);
   best -= best / 25;
-  for (int64_t want = 2; want <= max_parts(vrows); ++want) {
+  for (int64_t want = 2; want <= max_parts(vrows, cap); ++want) {
     const int64_t per = (nk + want - 1) / want;
     const int64_t s = (nk + per - 1) / per;
     if (s > most) break;
@@ -289,7 +294,7 @@ int64_t chunk_rows(const mls_problem* p, const Plan& pl, int64_t T_pad) {
 // Bytes of the parts' outputs a workspace is reported with, for rows of tokens
 // and vrows of K.
 size_t parts_room(const Plan& pl, int64_t rows, int64_t vrows) {
-  const int64_t n = max_parts(vrows);
+  const int64_t n = max_parts(vrows, kMaxSplits);
   return n < 2 ? 0 : align256((size_t)std::min(kPartBytes, n * rows * pl.sumd * 4));
 }
 
@@ -655,7 +660,8 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   int splits = 1;  // K parts of the grad_h products
   int64_t ksplit = 0;
   if (pl.wide_bwd)
-    grad_h_parts(p, pl.T, std::min(pl.Vc, pl.V), workspace_bytes - pl.off_ghp, &splits, &ksplit);
+    grad_h_parts(p, pl.T, std::min(pl.Vc, pl.V), workspace_bytes - pl.off_ghp, rows ? kRowsMaxSplits : kMaxSplits,
+                 &splits, &ksplit);
   else if (pl.f32 && g_row)
     f32_parts(p, pl, workspace_bytes - pl.off_ghp, &splits, &ksplit);
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -958,6 +964,7 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   // (the slab alone may be smaller for more tokens, where chunks get narrower)
   tp.bwd_room = off + std::max<size_t>(pl.bwd_room, align256((size_t)std::min(whole, kTokenSlabBytes)));
   // (as many parts times T, rounded up to what does not shrink for more tokens)
+  if (pl.wide_bwd) tp.bwd_room += align256((size_t)std::min(kPartBytes, kRowsMaxSplits * p->T * p->d[0] * 4));
   if (pl.f32) tp.bwd_room += align256((size_t)(std::min(kMaxSplits * p->T, pl.V) * p->d[0]) * 4);
 }
 
@@ -1155,7 +1162,7 @@ mls_status mls_distill_fwd_bwd(const mls_problem* p, void* stats, float* ce, flo
   }
   int splits;  // K parts of the grad_h products
   int64_t ksplit;
-  grad_h_parts(p, pl.fb_tc, pl.V, workspace_bytes - pl.fb_off_ghp, &splits, &ksplit);
+  grad_h_parts(p, pl.fb_tc, pl.V, workspace_bytes - pl.fb_off_ghp, kMaxSplits, &splits, &ksplit);
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   float* lab = reinterpret_cast<float*>(ws + pl.fb_off_lab);
