@@ -652,9 +652,10 @@ hipError_t finish_losses(const mls_problem* p, const Plan& pl, void* stats, floa
 
 // Launches of the backward: of the losses (g_ce, g_kl) or, with rows, of token
 // log-probabilities, whose problem p holds the packed and scaled rows, whose number of
-// rows the header has and whose logits rows->kept may hold.
+// rows the header has and whose logits rows->kept may hold; rows->gh_c and gh_parts say
+// where its grad_h is then.
 mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats, const float* g_ce,
-                        const float* g_kl, const TokenArgs* rows, void* const* grad_h, float* const* grad_W,
+                        const float* g_kl, TokenArgs* rows, void* const* grad_h, float* const* grad_W,
                         void* workspace, size_t workspace_bytes, void* stream) {
   const float* g_row = rows ? rows->g_c : nullptr;
   int splits = 1;  // K parts of the grad_h products
@@ -895,7 +896,10 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
     }
     if (e != hipSuccess) return hip_fail(e, "gradient GEMM launch");
   }
-  if (splits > 1) {
+  if (rows) {
+    rows->gh_c = splits > 1 ? reinterpret_cast<const float*>(ws + pl.off_ghp) : static_cast<const float*>(grad_h[0]);
+    rows->gh_parts = splits;
+  } else if (splits > 1) {
     e = sum_parts(p, splits, pl.T, reinterpret_cast<const float*>(ws + pl.off_ghp), grad_h, 0, s);
     if (e != hipSuccess) return hip_fail(e, "grad_h sum launch");
   }
@@ -1517,7 +1521,6 @@ mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const voi
   st = run_backward(&tp.q, pl, stats, nullptr, nullptr, &a, gh, gW, ws + tp.off_work,
                     workspace_bytes - tp.off_work, stream);
   if (st != MLS_OK || !grad_h) return st;
-  a.gh_c = static_cast<const float*>(gh[0]);
   a.out_f32 = p->grad_h_dtype == MLS_F32 ? 1 : 0;
   a.accumulate = (p->flags & MLS_ACCUMULATE_GRAD_H) ? 1 : 0;
   a.grad_h = grad_h;

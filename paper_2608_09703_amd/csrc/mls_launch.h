@@ -231,8 +231,9 @@ struct TokenArgs {
   const float4* partials;
   float* lse;             // [T] by row
   float* logp_c;          // [T] by row
-  // grad_h by token from the rows' one, before the scale
-  const float* gh_c;      // [T][d]
+  // grad_h by token from the rows' one, before the scale and in gh_parts K parts
+  const float* gh_c;      // [gh_parts][T][d]
+  int32_t gh_parts;
   int32_t out_f32;
   int32_t accumulate;
   void* grad_h;           // [T][d]

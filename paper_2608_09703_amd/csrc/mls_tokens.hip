@@ -243,28 +243,37 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenArgs a) {
   *reinterpret_cast<uint4*>(out) = Chunk<Bf16>::pack(g);
 }
 
-// grad_h by token: its row's times the row's scale, or zeros (with accumulate, nothing)
-// where it does not count. One wave per token, 4 elements per lane and step (both
-// widths' granularity).
+// grad_h by token: the sum of its row's K parts, in order, times the row's scale, or
+// zeros (with accumulate, nothing) where it does not count. One wave per token and 256
+// columns, 4 elements a lane (both widths' granularity).
+constexpr int kScatterSpan = 256;
 template <typename O>
 __global__ __launch_bounds__(kThreads) void token_scatter_kernel(TokenArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= a.T) return;
+  const int64_t k = (int64_t)blockIdx.y * kScatterSpan + (int64_t)lane * 4;
+  if (t >= a.T || k >= a.d) return;
   const int64_t r = a.rank[t];
   if (r < 0 && a.accumulate) return;
-  const float* src = a.gh_c + r * a.d;
-  const float scale = r >= 0 ? a.scale[r] : 0.f;
-  typename Elt<O>::type* out = static_cast<typename Elt<O>::type*>(a.grad_h) + t * a.d;
-  for (int64_t k = (int64_t)lane * 4; k < a.d; k += 64 * 4) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
+  typename Elt<O>::type* out = static_cast<typename Elt<O>::type*>(a.grad_h) + t * a.d + k;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (r >= 0) {
+    const float* src = a.gh_c + r * a.d + k;
+    load4<false>(src, v);
+#pragma unroll 8
+    for (int s = 1; s < a.gh_parts; ++s) {
+      float p[4];
+      load4<false>(src + s * a.T * a.d, p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += p[i];
+    }
+    const float scale = a.scale[r];
     float o[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r >= 0) load4<false>(src + k, v);
-    if (a.accumulate) load4<false>(out + k, o);
+    if (a.accumulate) load4<false>(out, o);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = fmaf(v[i], scale, o[i]);
-    store4<false>(out + k, v);
   }
+  store4<false>(out, v);
 }
 
 }  // namespace
@@ -300,7 +309,7 @@ hipError_t launch_token_merge(const TokenArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_token_scatter(const TokenArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.T + 3) / 4));
+  const dim3 grid((unsigned)((a.T + 3) / 4), (unsigned)((a.d + kScatterSpan - 1) / kScatterSpan));
   if (a.out_f32)
     hipLaunchKernelGGL(token_scatter_kernel<F32>, grid, dim3(kThreads), 0, stream, a);
   else
