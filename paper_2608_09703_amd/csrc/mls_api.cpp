@@ -949,7 +949,7 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   size_t off = align256((size_t)pl.T_pad * p->d[0] * pl.es);
   tp.off_tokens = off;
   off = align256(off + (size_t)pl.T * sizeof(int64_t));
-  tp.off_lab = off;  // forward: own logits; backward: gradients
+  tp.off_lab = off;  // forward: own logits; backward: g_c
   off = align256(off + (size_t)pl.T * sizeof(float));
   tp.off_scale = off;
   off = align256(off + (size_t)pl.T * sizeof(float));

@@ -115,7 +115,7 @@ struct GemmGroup {
   // of A/B for these layouts (see WideMma::run).
   int32_t kind;
   int64_t ldc_rows;  // grad_W (kind 1): rows of C to write (the chunk's vocabulary rows)
-  // wide path, kind 0: K in `splits` parts of ksplit elements (the last may be
+  // wide path (and fp32 with n_rows), kind 0: K in `splits` parts of ksplit elements (the last may be
   // shorter); part s goes to the fp32 matrix C + s * csplit
   int32_t splits;
   int64_t ksplit;
