@@ -358,7 +358,9 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
  * as device float32 [T]. p->alpha and p->teacher do not matter. Tokens with
  * ignore_index cost no product: the others' hidden states are packed first, and those
- * of ignored tokens are not used, whatever they hold.
+ * of ignored tokens are not used, whatever they hold. logp is never above 0, and
+ * near it as exact relative to itself as the logits allow (1 - exp(logp) is formed from
+ * sums of positive terms).
  * stats: mls_query_sizes' stats_bytes; it receives what the backward needs, the
  * number of tokens that count and the device flags (mls_read_stats_header,
  * mls_device_error): a token outside [0, V) is treated as ignored and raises

@@ -588,9 +588,9 @@ bool rows_core(const mls_problem* p, const Plan& pl) {
 
 // Tile kernel of the forward of tokens [t0, t0 + tc): partial records, and with
 // lslab the 16-bit logits. n_rows: of token log-probabilities' rows, as many of these
-// as the device counts.
+// as the device counts; own [T] receives the rows' own logits.
 hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc, float4* partials,
-                         uint16_t* lslab, const int32_t* n_rows, hipStream_t s) {
+                         uint16_t* lslab, const int32_t* n_rows, float* own, hipStream_t s) {
   FusedArgs a;
   fill_common(p, pl, a);
   for (int i = 0; i < pl.M; ++i)
@@ -610,6 +610,10 @@ hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64
   a.ld_lslab = n_rows ? kept_ld(pl) : pl.fb_ld;
   a.n_rows = n_rows;
   a.row0 = t0;
+  if (n_rows) {
+    a.labels += t0;
+    a.own = own + t0;
+  }
   if (n_rows && rows_core(p, pl)) {
     a.tile_v = kRowsTile;
     a.n_vt = (int)((pl.V + kRowsTile - 1) / kRowsTile);
@@ -623,7 +627,7 @@ hipError_t forward_tiles(const mls_problem* p, const Plan& pl, int64_t t0, int64
 hipError_t forward_chunk(const mls_problem* p, const Plan& pl, int64_t t0, int64_t tc,
                          float4* partials, const float* lab, uint16_t* lslab, void* stats,
                          hipStream_t s) {
-  hipError_t e = forward_tiles(p, pl, t0, tc, partials, lslab, nullptr, s);
+  hipError_t e = forward_tiles(p, pl, t0, tc, partials, lslab, nullptr, nullptr, s);
   if (e != hipSuccess) return e;
   RowArgs r;
   fill_rows(p, pl, r);
@@ -678,7 +682,10 @@ mls_status run_backward(const mls_problem* p, const Plan& pl, const void* stats,
   a.g_ce = g_ce;
   a.g_kl = g_kl;
   a.g_row = g_row;
-  if (rows) a.h[0] = rows->hc;  // (p has the scaled ones, for grad_W)
+  if (rows) {
+    a.h[0] = rows->hc;  // (p has the scaled ones, for grad_W)
+    a.q_row = rows->q;
+  }
   a.n_rows = g_row ? a.n_valid : nullptr;
   const bool rows_tiles = g_row && rows_core(p, pl);
   const int fbm = rows_tiles ? kRowsTile : fused_tile_rows(pl.f32);
@@ -926,7 +933,7 @@ constexpr int64_t kTokenSlabBytes = 256ll << 20;
 struct TokenPlan {
   Plan pl;         // of the packed rows
   mls_problem q;   // p with the rows' grad_h (fp32: the scatter scales it, and adds to an output)
-  size_t off_hc = 0, off_tokens = 0, off_lab = 0, off_scale = 0, off_hs = 0, off_part = 0, off_gh = 0, off_work = 0;
+  size_t off_hc = 0, off_tokens = 0, off_own = 0, off_scale = 0, off_hs = 0, off_part = 0, off_gh = 0, off_work = 0;
   size_t fwd_bytes = 0, bwd_bytes = 0, bwd_room = 0;  // room: see Plan
   // kept logits (bf16 in one forward chunk): the rows' distances, then the
   // partial records with the maxima they are relative to
@@ -949,7 +956,7 @@ void token_plan(const mls_problem* p, TokenPlan& tp) {
   size_t off = align256((size_t)pl.T_pad * p->d[0] * pl.es);
   tp.off_tokens = off;
   off = align256(off + (size_t)pl.T * sizeof(int64_t));
-  tp.off_lab = off;  // forward: own logits; backward: g_c
+  tp.off_own = off;  // forward: own logits; backward: g_c
   off = align256(off + (size_t)pl.T * sizeof(float));
   tp.off_scale = off;
   off = align256(off + (size_t)pl.T * sizeof(float));
@@ -989,7 +996,7 @@ TokenArgs token_args(const mls_problem* p, const Plan& pl, void* stats) {
   a.rank = reinterpret_cast<int32_t*>(sf);           // lse1
   a.lse = sf + pl.T;                                 // lset
   a.index = reinterpret_cast<int32_t*>(sf + 2 * pl.T);  // ce_row
-  a.logp_c = sf + 3 * pl.T;                          // kl_row
+  a.q = sf + 3 * pl.T;                               // kl_row
   a.header = reinterpret_cast<int32_t*>(static_cast<char*>(stats) + pl.header_off);
   return a;
 }
@@ -1444,7 +1451,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   a.entropy = entropy;
   a.hc = ws + tp.off_hc;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
-  a.lab = reinterpret_cast<float*>(ws + tp.off_lab);
+  a.own = reinterpret_cast<float*>(ws + tp.off_own);
   a.n_rec = tp.n_rec;
   uint16_t* const lslab = static_cast<uint16_t*>(kept);
   a.partials = reinterpret_cast<const float4*>(kept ? static_cast<char*>(kept) + tp.kept_rec : ws + tp.off_part);
@@ -1464,7 +1471,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
   for (int c = 0; c < pl.fwd_nc; ++c) {
     a.t0 = (int64_t)c * pl.fwd_tc;
     a.Tc = std::min(pl.fwd_tc, pl.T - a.t0);
-    e = forward_tiles(&tp.q, pl, a.t0, a.Tc, const_cast<float4*>(a.partials), lslab, a.header, s);
+    e = forward_tiles(&tp.q, pl, a.t0, a.Tc, const_cast<float4*>(a.partials), lslab, a.header, a.own, s);
     if (e != hipSuccess) return hip_fail(e, "forward launch");
     ProfScope ps("token_merge", s);
     e = launch_token_merge(a, s);
@@ -1506,7 +1513,7 @@ mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const voi
   a.hs = ws + tp.off_hs;
   a.tokens_c = reinterpret_cast<int64_t*>(ws + tp.off_tokens);
   a.g = g_logp;
-  a.g_c = reinterpret_cast<float*>(ws + tp.off_lab);
+  a.g_c = reinterpret_cast<float*>(ws + tp.off_own);
   a.scale = reinterpret_cast<float*>(ws + tp.off_scale);
   hipError_t e;
   {

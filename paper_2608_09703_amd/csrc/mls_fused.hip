@@ -17,6 +17,7 @@
 //   G_i = ( g_ce,i (softmax(l_i) - onehot(y)) + g_kl,i / tau (softmax(l_i / tau) - q) ) / N
 // (eq. (2) with stop_grad on q, eq. (3) through the coefficients) is written
 // to the chunk slab in two layouts for the two backward GEMMs.
+#include <float.h>
 #include <math.h>
 
 #include "mls_core.h"
@@ -75,6 +76,13 @@ struct TeacherTile<FM, FN, true> {
   }
 };
 
+// x, but another value for the compiler: exponentials of differences to it are not kept
+// in 64 registers a lane in between (T = 2,048, d = 2,304, V = 49,152: 377 us for 384).
+__device__ __forceinline__ float another(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Rows of a launch over the tokens that count (see FusedArgs::n_rows).
 __device__ __forceinline__ int64_t live_rows(const FusedArgs& a) {
   const int64_t n = *a.n_rows - a.row0;
@@ -92,7 +100,11 @@ __device__ __forceinline__ int64_t live_rows(const FusedArgs& a) {
 // exact), token-major, for the logit gradient pass.
 // ROWS (token log-probabilities): the number of rows is read from the device;
 // with one temperature, TAU1's single sum at a.tau. STORE keeps the logits, in
-// kKeptRange's form.
+// kKeptRange's form. Each row's own logit leaves by itself and is left out of the
+// sums, so that 1 - p is a quotient of sums of positive terms and log p never
+// above 0; a second product of the same operands, summed in another order, would
+// be off by a few 1e-6 of 1 - p. A wave looks for it only where one of its 32
+// tokens has its own logit in the wave's rows.
 template <class Mma, typename E, bool TAU1, int MINB = 1, bool STORE = false, bool ROWS = false>
 __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
@@ -126,6 +138,17 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
   const int64_t n_rec = (int64_t)a.n_vt * WGM;
   const int64_t n_tg = (T + kFusedBN - 1) / kFusedBN;
   const int64_t rec = (int64_t)vt * WGM + wm;
+
+  // the columns' tokens (below 2^30: the low word; past the last one any), not used
+  // before the product, so that nothing waits for these loads
+  int token[FN];
+  if constexpr (ROWS) {
+#pragma unroll
+    for (int fn = 0; fn < FN; ++fn) {
+      const int64_t t = tbase + Mma::col_of(wn, fn, lane);
+      token[fn] = reinterpret_cast<const int32_t*>(a.labels)[2 * (t < T ? t : T - 1)];
+    }
+  }
 
   // teacher weights exp((l_s - max_s) / tau); 0 outside V
   TeacherTile<FM, FN, false> e_t;
@@ -259,6 +282,35 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_fwd_kernel(FusedArgs a) {
           }
         if (TAU1) st = s1;
       }
+      if constexpr (ROWS) {
+        // own logits among these rows leave, and the sums are taken without them
+        // (rows counted from the lane's first one: constants below)
+        const int row0 = (int)vbase + Mma::row_of(wm, 0, 0, lane);
+        const int rel = token[fn] - row0, left = (int)(a.V - row0);
+        if (__builtin_expect(__any(rel >= 0 && rel < Mma::WTM), 0)) {
+          float mine = 0.f;
+          bool here = false;
+          st = xr = 0.f;
+          // (where the logits are kept their differences to mb are at hand)
+          const float m = STORE ? mb : another(mb);
+#pragma unroll
+          for (int fm = 0; fm < FM; ++fm)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int row = Mma::row_of(0, fm, r, 0);
+              const bool it = row == rel;
+              const float l = mma.acc[fm][fn][r];
+              const float e = row < left && !it ? fast_exp2((l - m) * ct) : 0.f;
+              mine = it ? l : mine;
+              here |= it;
+              st += e;
+              xr = fmaf(e, l, xr);
+            }
+          s1 = st;
+          const int64_t t = tbase + Mma::col_of(wn, fn, lane);
+          if (here && t < T) a.own[t] = mine;
+        }
+      }
       s1 += shfl_xor32(s1);
       st += shfl_xor32(st);
       xr += shfl_xor32(xr);
@@ -293,7 +345,7 @@ __device__ __forceinline__ void store4<F32>(float* p, float a0, float a1, float 
 // general bf16 path (both slab layouts).
 // ROWG (one sub-model): the scaled gradient of the rows' log-probabilities at
 // temperature tau, g_row / tau (onehot - softmax(l / tau)), in place of the losses',
-// over the rows that the device counts.
+// over the rows that the device counts; 1 - p of the own token is the forward's.
 template <class Mma, typename E, bool TAU1, bool ROWG = false>
 __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
   constexpr int BM = Mma::kBM;
@@ -359,6 +411,7 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
       const float l1 = !ROWG && rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
       const float lt = rv[fn] ? a.lset[(int64_t)i * a.T + t] : INFINITY;
       const float cg = !rv[fn] ? 0.f : ROWG ? -a.g_row[t] * a.inv_tau : gce * invN;
+      const float ow = ROWG && ylab[fn] >= 0 ? -cg * a.q_row[t] : 0.f;
       const float ck = (!ROWG && rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
       const float l1s = l1 * kLog2e;
       const float lts = lt * kLog2e;
@@ -376,7 +429,7 @@ __global__ __launch_bounds__(Mma::NT, 1) void fused_bwd_kernel(FusedArgs a) {
             const float l = mma.acc[fm][fn][r];
             const float oh = row == ylab[fn] ? 1.f : 0.f;
             if (ROWG) {
-              g[rr] = cg * ((ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f) - oh);
+              g[rr] = row == ylab[fn] ? ow : cg * (ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f);
             } else if (oi == 0) {
               const float q = ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f;
               q_t.set(fm, fn, r, q);
@@ -473,6 +526,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
       const float l1 = !ROWG && rv[fn] ? a.lse1[(int64_t)i * a.T + t] : INFINITY;
       const float lt = rv[fn] ? a.lset[(int64_t)i * a.T + t] : INFINITY;
       const float cg = !rv[fn] ? 0.f : ROWG ? -a.g_row[t] * a.inv_tau : gce * invN;
+      const float ow = ROWG && ylab[fn] >= 0 ? -cg * a.q_row[t] : 0.f;
       const float ck = (!ROWG && rv[fn] && oi != 0) ? gkl * invN * a.inv_tau : 0.f;
       const float l1s = l1 * kLog2e;
       const float lts = lt * kLog2e;
@@ -490,7 +544,7 @@ __global__ __launch_bounds__(Mma::NT, MINB) void fused_bwd_wide_kernel(FusedArgs
             const float l = mma.acc[fm][fn][r];
             const float oh = row == ylab[fn] ? 1.f : 0.f;
             if (ROWG) {
-              g[rr] = cg * ((ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f) - oh);
+              g[rr] = row == ylab[fn] ? ow : cg * (ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f);
             } else if (oi == 0) {
               const float q = ok ? fast_exp2(fmaf(l, ct, -lts)) : 0.f;
               q_t.set(fm, fn, r, q);

@@ -79,6 +79,8 @@ struct FusedArgs {
   int64_t row0;
   int32_t tile_v;  // kRowsTile: that core's tiles; else 0
   const float* g_row;  // [T]
+  const float* q_row;  // [T] backward: 1 - p of each row's own token
+  float* own;          // [T] forward: receives each row's own logit
   float host_gce[kMaxModels];
   float host_gkl[kMaxModels];
   void* slab;   // [M][T_pad][Vc]  dJ/dlogits, token-major
@@ -210,9 +212,9 @@ struct TokenArgs {
   void* hc;               // [T_pad][d] their hidden states; zeros behind the last (or null)
   void* hs;               // backward: the same, scaled
   int64_t* tokens_c;      // [T] their ids
-  float* lab;             // [T] forward: their own logits
+  float* own;             // [T] by row, forward: their own logits (from the tile kernel)
   const float* g;         // [T] backward: gradients by token
-  // by row, with q = 1 - exp(logp): tau / q (what the logit gradients are formed
+  // by row, with q = 1 - p: tau / q (what the logit gradients are formed
   // with) and g q / tau (their scale, which goes into hs and into grad_h)
   float* g_c;             // [T]
   float* scale;           // [T]
@@ -230,7 +232,7 @@ struct TokenArgs {
   int32_t n_rec;
   const float4* partials;
   float* lse;             // [T] by row
-  float* logp_c;          // [T] by row
+  float* q;               // [T] by row, 1 - p
   // grad_h by token from the rows' one, before the scale and in gh_parts K parts
   const float* gh_c;      // [gh_parts][T][d]
   int32_t gh_parts;

@@ -75,12 +75,13 @@ __global__ __launch_bounds__(kPackThreads) void token_pack_kernel(TokenArgs a) {
   a.header[1] = bad ? MLS_DEVFLAG_LABEL_RANGE : 0;
 }
 
-// What of 1 - p an fp32 log-probability near 0 still tells: scales are not smaller.
-constexpr float kMinRest = 0x1p-20f;
+// Scales of rows are not smaller than with this as 1 - p: far above what kept logits
+// may add to each other entry (e^-32, see kKeptRange; below it they would count for
+// more than those entries themselves).
+constexpr float kMinRest = 0x1p-40f;
 
 // One wave per token and, for the rows behind the last one, per row: copies the
-// token's hidden state to its row and its id along, and takes its own logit <h, W[y]>
-// on the way (forward).
+// token's hidden state to its row and its id along.
 // Backward: with q = 1 - p[y] the logit gradient is G = s E, s = g q / tau and
 // E = (onehot(y) - p) / q, and the products run on E, rounded to bfloat16, whose own
 // token's entry is 1. That entry carries most of G, and whole rows of grad_W when few
@@ -107,10 +108,9 @@ __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
   if (r < 0) return;
   const int64_t y = a.tokens[t];
   const S* h = static_cast<const S*>(a.h) + t * a.d;
-  const S* w = static_cast<const S*>(a.W) + y * a.d;
-  float s = 0.f, scale = 0.f, rest = 0.f;
+  float scale = 0.f, rest = 0.f;
   if (hs) {
-    rest = fmaxf(-expm1f(a.logp_c[r]), kMinRest);
+    rest = fmaxf(a.q[r], kMinRest);
     scale = a.g[t] / a.tau * rest;
   }
   for (int64_t k = (int64_t)lane * kPer; k < a.d; k += 64 * kPer) {
@@ -122,34 +122,20 @@ __global__ __launch_bounds__(kThreads) void token_gather_kernel(TokenArgs a) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) v[i] *= scale;
       *reinterpret_cast<uint4*>(hs + r * a.d + k) = Chunk<E>::pack(v);
-      continue;
-    }
-    const uint4 wv = *reinterpret_cast<const uint4*>(w + k);
-    const uint32_t hu[4] = {hv.x, hv.y, hv.z, hv.w};
-    const uint32_t wu[4] = {wv.x, wv.y, wv.z, wv.w};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (E::kBytes == 2) {
-        s = fmaf(__uint_as_float(hu[q] << 16), __uint_as_float(wu[q] << 16), s);
-        s = fmaf(__uint_as_float(hu[q] & 0xffff0000u), __uint_as_float(wu[q] & 0xffff0000u), s);
-      } else {
-        s = fmaf(__uint_as_float(hu[q]), __uint_as_float(wu[q]), s);
-      }
     }
   }
-  if (!hs) s = wave_sum(s);
   if (lane != 0) return;
   a.tokens_c[r] = y;
   if (hs) {
     a.g_c[r] = a.tau / rest;
     a.scale[r] = scale;
-  } else {
-    a.lab[r] = s;
   }
 }
 
-// Row merge (one sub-model, temperature tau):
-//   logp = l_y / tau - logsumexp(l / tau),  entropy = logsumexp(l / tau) - mean_p(l) / tau
+// Row merge (one sub-model, temperature tau). With m the maximum of all logits, S the
+// records' sum of exp((l - m) / tau) over the other entries and e that of the token's own,
+//   q = 1 - p = S / (S + e),  logp = log(1 - q) where q is small, else (l_y - m) / tau - log(S + e),
+//   entropy = logsumexp(l / tau) - mean_p(l) / tau.
 // TOK tokens a block, a thread a token and TOK / 256 of its records (added pairwise, in
 // a fixed tree): one up to 256 tokens, else the losses' four, in us for TOK 4 / 1: T = 96,
 // V = 97,683 24 / 12; T = 18, V = 105,482 17 / 10; T = 651, V = 121,655 21 / 25.
@@ -190,12 +176,16 @@ __global__ __launch_bounds__(kThreads) void token_merge_kernel(TokenArgs a) {
   if (grp != 0 || tc >= Tc) return;
   const int64_t r = a.t0 + tc;
   const int64_t t = a.index[r];
-  const float lse = st.m[0] * inv_tau + logf(st.st[0]);
-  const float lp = fmaf(a.lab[r], inv_tau, -lse);
+  const float own = a.own[r];
+  const float e = fast_exp2((own - st.m[0]) * ct);
+  const float sum = st.st[0] + e;
+  const float q = st.st[0] / sum;
+  const float lse = st.m[0] * inv_tau + logf(sum);
+  const float lp = q < 0.5f ? log1pf(-q) : (own - st.m[0]) * inv_tau - logf(sum);
   a.lse[r] = lse;
-  a.logp_c[r] = lp;
+  a.q[r] = q;
   a.logp[t] = lp;
-  if (a.entropy) a.entropy[t] = lse - st.xr[0] / (a.tau * st.st[0]);
+  if (a.entropy) a.entropy[t] = lse - fmaf(e, own, st.xr[0]) / (a.tau * sum);
   if (!isfinite(lp)) atomicOr(a.header + 1, MLS_DEVFLAG_NONFINITE);
 }
 
@@ -235,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void token_grad_kernel(TokenArgs a) {
     g[i] = v + i < a.V ? -c * p : 0.f;
   }
   if (yrel >= 0 && yrel < 8) {
-    const float own = -expm1f(a.logp_c[r]) * c;  // 1, up to the floor of the rest
+    const float own = a.q[r] * c;  // 1, up to the floor of the rest
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i == yrel) g[i] = own;
