@@ -21,6 +21,7 @@ import functools
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -95,10 +96,23 @@ def _on(dev: torch.device):
     return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
-def _once(ctx_name: str):
+def _primal(name: str, *xs: Optional[torch.Tensor]):
+    """Refuses tensors that carry a tangent: addresses do not, so that the result would be
+    without one, which later operations take for a derivative of zero."""
+    # (outside of dual levels no tensor does: a tenth of the three questions' 1 us, which
+    # the smallest calls would show; a torch without this number is asked them always)
+    if getattr(forward_ad, "_current_level", 0) < 0:
+        return
+    for x in xs:
+        if x is not None and forward_ad.unpack_dual(x).tangent is not None:
+            raise NotImplementedError(f"{name}: forward-mode derivatives are not available")
+
+
+def _once(name: str, g: Optional[torch.Tensor]):
     """Backward passes run with gradients enabled only where their own are asked for."""
     if torch.is_grad_enabled():
-        raise RuntimeError(f"{ctx_name}: gradients of gradients are not available")
+        raise RuntimeError(f"{name}: gradients of gradients are not available")
+    _primal(name, g)
 
 
 # Backward passes below run on the engine's thread, where every step costs about twice
@@ -385,7 +399,7 @@ class _LayerNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, g_y):
-        _once("layer_norm")
+        _once("layer_norm", g_y)
         x, weight, stats = ctx.saved_tensors
         if not g_y.is_contiguous():
             g_y = g_y.contiguous()
@@ -417,6 +431,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     sub-model's channels). ``weight`` and ``bias [d]`` are bf16 or float32, whatever
     ``x`` is; their gradients are summed in float32 and rounded once.
     """
+    _primal("layer_norm", x, weight, bias)
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
                                     (bias is not None and bias.requires_grad)):
         return _LayerNorm.apply(x, weight, bias, eps)
@@ -458,7 +473,7 @@ class _TokenLogp(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, g_logp, g_entropy):
-        _once("token_logp")
+        _once("token_logp", g_logp)
         if g_logp is None:
             return None, None, None, None, None
         # the saved tensors' addresses are taken anew, as in the loss's backward
@@ -499,6 +514,7 @@ def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temper
     time (``vocab_chunk`` columns, or as many as fit 256 MiB).
     """
     opts = dict(tau=temperature, ignore_index=ignore_index, vocab_chunk=vocab_chunk)
+    _primal("token_logp", h, W)
     if torch.is_grad_enabled() and (h.requires_grad or W.requires_grad):
         return _TokenLogp.apply(tokens, opts, keep_logits, h, W)
     return _token_logp_forward(h, W, tokens, opts, False)[:2]
@@ -536,7 +552,7 @@ class _PolicyLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, g_loss, g_kl, g_clipped):
-        _once("policy_loss")
+        _once("policy_loss", g_loss)
         if g_loss is None:
             return None, None
         grad, = ctx.saved_tensors
@@ -599,6 +615,7 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Te
                          ("[S]" if per_sequence else "logp's shape"))
     desc = B.make_policy(N, S, clip_low, clip_high, kl_coef, flags)
     args = (old_logp, advantages, ref_logp, mask, cu_seqlens, desc)
+    _primal("policy_loss", logp)
     if torch.is_grad_enabled() and logp.requires_grad:
         return _PolicyLoss.apply(logp, args)
     return _policy_forward(logp, args, False)[:3]
