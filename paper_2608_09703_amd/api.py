@@ -655,6 +655,8 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
     with _on(dev):
         B.clip_grad_norm(len(data), tensors, max_norm, norm.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
+    if max_norm:  # written through addresses: graphs that saved these tensors are told
+        torch.autograd.graph.increment_version(grads if out is None else out)
     return norm
 
 

@@ -1,0 +1,44 @@
+"""Gradient clipping: what autograd sees of it.
+Tolerances as in test_clip_grad_norm_gpu.py."""
+
+import pytest
+import torch
+
+from paper_2608_09703_amd import api as D
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def test_a_graph_that_saved_a_gradient_sees_it_change():
+    """As with torch's own in-place operations."""
+    w = torch.randn(300, device=DEV, requires_grad=True)
+    g, = torch.autograd.grad((w ** 3).sum(), w, create_graph=True)
+    penalty = (g * g).sum()
+    D.clip_grad_norm([g], 1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        penalty.backward()
+
+
+@pytest.mark.parametrize("max_norm", [1e-3, 1e6])
+def test_versions_of_what_is_written(max_norm):
+    grads = [torch.randn(100, device=DEV), None, torch.randn(7, device=DEV).bfloat16()]
+    some = [g for g in grads if g is not None]
+    out = [torch.empty_like(g) for g in some]
+    versions = lambda ts: [t._version for t in ts]  # noqa: E731
+    before = versions(some), versions(out)
+    D.grad_norm(grads)
+    assert (versions(some), versions(out)) == before
+    D.clip_grad_norm(some, max_norm, out=out)
+    assert versions(some) == before[0] and all(a > b for a, b in zip(versions(out), before[1]))
+    D.clip_grad_norm(grads, max_norm)
+    assert all(a > b for a, b in zip(versions(some), before[0]))
+
+
+def test_gradients_made_under_inference_mode():
+    with torch.inference_mode():
+        g = [torch.full((100,), 3.0, device=DEV), torch.full((8,), 3.0, device=DEV).bfloat16()]
+        want = 3.0 * 108 ** 0.5
+        assert abs(float(D.clip_grad_norm(g, want / 2)) - want) < 1e-4 * want
+        assert all(abs(float(x[0]) - 1.5) < 0.01 for x in g)
