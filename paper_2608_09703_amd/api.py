@@ -628,9 +628,14 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
     # (one pass over the list for each property: hundreds of tensors, whose properties
     # cost more than the launches when asked for one by one)
     T = torch.Tensor
-    grads = [g for g in grads if g is not None] if out is None else list(grads)
+    if out is not None:
+        grads, out = list(grads), list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must hold one entry for each entry of grads")
+        out = [o for g, o in zip(grads, out) if g is not None]
+    grads = [g for g in grads if g is not None]
     if not grads:
-        raise ValueError("no gradients given")
+        raise ValueError("no gradients given: the norm would be on no device")
     dev = grads[0].device
     if dev.type != "cuda":
         raise RuntimeError("gradient norms run on the GPU only; got tensors on " + str(dev))
@@ -644,9 +649,8 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
     sizes, data = [*map(T.numel, grads)], [*map(T.data_ptr, grads)]
     to = data
     if out is not None:
-        out = list(out)
-        if [*map(T.numel, out)] != sizes or [o.dtype for o in out] != dtypes or {*map(T.get_device, out)} != on or \
-                not all(map(T.is_contiguous, out)):
+        if any(o is None for o in out) or [*map(T.numel, out)] != sizes or [o.dtype for o in out] != dtypes or \
+                {*map(T.get_device, out)} != on or not all(map(T.is_contiguous, out)):
             raise ValueError("out must hold for each gradient one contiguous tensor of its size, dtype and device")
         to = [*map(T.data_ptr, out)]
     tensors = B.make_grad_tensors(data, to, sizes, codes)
@@ -662,19 +666,21 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
 
 @torch.no_grad()
 def grad_norm(grads: Sequence[Optional[torch.Tensor]]) -> torch.Tensor:
-    """The global L2 norm (float32, on the device) of a list of bf16 or float32 gradients."""
+    """The global L2 norm (float32, on the device, not differentiated) of a list of bf16 or
+    float32 gradients; entries that are None are left out."""
     return _clip(grads, 0.0, None)
 
 
 @torch.no_grad()
 def clip_grad_norm(grads: Sequence[Optional[torch.Tensor]], max_norm: float, *,
-                   out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+                   out: Optional[Sequence[Optional[torch.Tensor]]] = None) -> torch.Tensor:
     """Scales gradients by ``min(1, max_norm / norm)`` and returns their global L2 norm before.
 
     The norm is a float32 scalar on the device: nothing waits for it. The gradients
-    (bf16 and float32 mixed; entries that are None are left out) are scaled in place,
-    or into the tensors ``out`` of the same sizes and dtypes. A norm that is NaN or
-    infinite scales nothing.
+    (bf16 and float32 mixed) are scaled in place, or into the tensors ``out`` of the
+    same sizes and dtypes. Entries that are None are left out, and with them their
+    entries of ``out``; one gradient there has to be. A norm that is NaN or infinite
+    scales nothing.
     """
     if not max_norm > 0:
         raise ValueError(f"max_norm must be > 0, got {max_norm}")

@@ -1,4 +1,4 @@
-"""Gradient clipping: what autograd sees of it.
+"""Gradient clipping: what autograd sees of it, entries without a gradient.
 Tolerances as in test_clip_grad_norm_gpu.py."""
 
 import pytest
@@ -42,3 +42,25 @@ def test_gradients_made_under_inference_mode():
         want = 3.0 * 108 ** 0.5
         assert abs(float(D.clip_grad_norm(g, want / 2)) - want) < 1e-4 * want
         assert all(abs(float(x[0]) - 1.5) < 0.01 for x in g)
+
+
+def test_entries_without_a_gradient_and_their_outputs():
+    a, b = torch.randn(50, device=DEV), torch.randn(9, device=DEV).bfloat16()
+    keep = torch.randn(4, device=DEV)
+    spare = keep.clone()
+    want = [torch.empty_like(a), torch.empty_like(b)]
+    norm = D.clip_grad_norm([a, b], 0.5, out=want)
+    for grads, out in (([None, a, b], [spare, torch.empty_like(a), torch.empty_like(b)]),
+                       ([a, None, b], [torch.empty_like(a), None, torch.empty_like(b)])):
+        got = D.clip_grad_norm(grads, 0.5, out=out)
+        pairs = [o for g, o in zip(grads, out) if g is not None]
+        assert torch.equal(got, norm) and all(torch.equal(x, y) for x, y in zip(pairs, want))
+    assert torch.equal(spare, keep)
+    for grads, out in (([a, None], [torch.empty_like(a)]), ([a], [torch.empty_like(a), spare]), ([a], [None])):
+        with pytest.raises(ValueError):
+            D.clip_grad_norm(grads, 0.5, out=out)
+    for nothing in ([], [None, None]):
+        with pytest.raises(ValueError):
+            D.clip_grad_norm(nothing, 0.5)
+        with pytest.raises(ValueError):
+            D.grad_norm(nothing)
