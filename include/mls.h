@@ -455,8 +455,9 @@ mls_status mls_policy_loss_bwd(int64_t N, const float* grad, const float* g_loss
  * Global L2 norm of a list of gradient tensors, and their clipping (the paper's
  * recipe, section 3, clips at 1.0):
  *   norm = sqrt(sum over all tensors and elements of x^2),  out = x * min(1, max_norm / norm).
- * Squares are added in 64 bits, in a fixed order. A norm that is NaN or infinite
- * scales nothing (the caller sees it in norm and skips the step).
+ * Squares are added in 64 bits, in a fixed order. A norm that is NaN or infinite as
+ * the float32 it is returned in scales nothing (the caller sees it there and skips the
+ * step).
  */
 typedef struct mls_grad_tensor {
   const void* data;  /* device, n elements */

@@ -118,9 +118,10 @@ __global__ __launch_bounds__(kClipFinThreads) void grad_norm_finish_kernel(const
   s = 0.0;
   for (int w = 0; w < kClipFinThreads / 64; ++w) s += red[w];
   const double x = sqrt(s);
-  *norm = (float)x;
-  // a norm that is NaN or infinite scales nothing
-  if (coef) *coef = x > max_norm && isfinite(x) ? (float)(max_norm / x) : 1.f;
+  const float f = (float)x;
+  *norm = f;
+  // a norm that is NaN or infinite, as the caller sees it in fp32, scales nothing
+  if (coef) *coef = x > max_norm && isfinite(f) ? (float)(max_norm / x) : 1.f;
 }
 
 template <typename E>

@@ -1,4 +1,4 @@
-"""Gradient clipping: what autograd sees of it, entries without a gradient.
+"""Gradient clipping: what autograd sees of it, norms past float32, entries without a gradient.
 Tolerances as in test_clip_grad_norm_gpu.py."""
 
 import pytest
@@ -42,6 +42,24 @@ def test_gradients_made_under_inference_mode():
         want = 3.0 * 108 ** 0.5
         assert abs(float(D.clip_grad_norm(g, want / 2)) - want) < 1e-4 * want
         assert all(abs(float(x[0]) - 1.5) < 0.01 for x in g)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("given", [False, True])
+def test_a_norm_past_float32_scales_nothing(dtype, given):
+    """Finite elements whose norm is finite in 64 bits and infinite in the float32 that is returned."""
+    g = [torch.full((4000,), 1e38, device=DEV).to(dtype), torch.ones(5, device=DEV)]
+    before = [x.clone() for x in g]
+    out = [torch.empty_like(x) for x in g] if given else None
+    norm = D.clip_grad_norm(g, 1.0, out=out)
+    assert torch.isinf(norm) and torch.isinf(D.grad_norm(g))
+    assert all(torch.equal(a, b) for a, b in zip(before, out if given else g))
+    # the largest norm that float32 holds still scales
+    g = [torch.full((1,), 3.3e38, device=DEV).to(dtype)]
+    x = g[0].double()
+    norm = D.clip_grad_norm(g, 2.0)
+    assert torch.isfinite(norm) and float(norm) == float(x)
+    assert abs(float(g[0]) - 2.0) <= 2.0 * ((2.0 ** -8 if dtype == torch.bfloat16 else 0) + 3 * 2.0 ** -22)
 
 
 def test_entries_without_a_gradient_and_their_outputs():
