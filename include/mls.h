@@ -436,7 +436,7 @@ mls_status mls_policy_loss_workspace(const mls_policy* p, size_t* bytes);
  *         tokens, each with the weights w above; 0 when nothing counts (kl and
  *         clipped may be NULL)
  *   grad  float32 [N + 1] (may be NULL): what the backward reads, the tokens' dL/dlogp
- *         and 1 / (tokens or sequences counted)
+ *         up to a factor, and that factor
  * Asynchronous on stream.
  */
 mls_status mls_policy_loss_fwd(const mls_policy* p, const float* logp, const float* old_logp,

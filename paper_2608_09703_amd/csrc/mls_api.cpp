@@ -1843,6 +1843,8 @@ mls_status mls_policy_loss_fwd(const mls_policy* p, const float* logp, const flo
   a.lo = 1.0 - p->clip_low;
   a.hi = 1.0 + p->clip_high;
   a.beta = p->kl_coef;
+  // the largest power of two up to 1 / N or 1 / S
+  a.grad_scale = exp2(-ceil(log2((double)(a.by_seq ? p->S : p->N))));
   a.loss = loss;
   a.kl = kl;
   a.clipped = clipped;

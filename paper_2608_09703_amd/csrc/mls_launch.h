@@ -371,9 +371,10 @@ struct PolicyArgs {
   float* loss;
   float* kl;              // or null
   float* clipped;         // or null
-  // null, or [N + 1]: dL/dlogp before the division by the number of tokens or
-  // sequences, then 1 / that number
+  // null, or [N + 1]: dL/dlogp with grad_scale in place of the division by the number
+  // of tokens or sequences, then what that division is over grad_scale
   float* grad;
+  double grad_scale;      // a power of two
   double* part;           // [blocks][4]
   int32_t* counts;        // [S], with by_seq and a mask
 };

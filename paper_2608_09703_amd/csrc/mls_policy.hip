@@ -12,8 +12,9 @@
 // inputs, so that whether a ratio is clipped does not depend on a rounding (the
 // two exponentials of a million tokens take the chip a few microseconds). The
 // gradient is written by the forward, without the 1 / N or 1 / S that is known
-// only once every token has been counted; the backward multiplies that and the
-// upstream gradient in. Sums leave the blocks as 64-bit parts that one block adds
+// only once every token has been counted, but with a power of two near it (of all
+// tokens or sequences), so that what fp32 holds of the mean it holds in between;
+// the backward multiplies the rest and the upstream gradient in. Sums leave the blocks as 64-bit parts that one block adds
 // in block order: results are bitwise reproducible.
 #include <math.h>
 
@@ -106,7 +107,7 @@ __device__ __forceinline__ void write_losses(const PolicyArgs& a, const double* 
   *a.loss = (float)(s[0] * inv);
   if (a.kl) *a.kl = (float)(s[1] * inv);
   if (a.clipped) *a.clipped = (float)(s[2] * inv);
-  if (a.grad) a.grad[a.N] = (float)inv;
+  if (a.grad) a.grad[a.N] = (float)(inv / a.grad_scale);
 }
 
 // Sum over the block of each of kPolSums values; valid in thread 0. red: one row per wave.
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(NT) void policy_fwd_kernel(PolicyArgs a) {
     sum[1] += seq_w * k;
     sum[2] += take ? 0.0 : seq_w;
     sum[3] += 1.0;
-    g[i] = (float)(seq_w * dl);
+    g[i] = (float)(seq_w * dl * a.grad_scale);
   }
   if (a.grad) store_four(a.grad, t0, a.N, g);
   if (a.by_seq) sum[3] = gridDim.x == 1 ? live_sequences<NT>(a) : 0.0;
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(kPolFinThreads) void policy_finish_kernel(PolicyArg
   if (threadIdx.x == 0) write_losses(a, sum);
 }
 
-// g_logp = grad * upstream / (tokens or sequences counted)
+// g_logp = grad * upstream * (what is left of 1 / (tokens or sequences counted))
 // (a token without a gradient keeps its exact zero, whatever the upstream one is)
 __global__ __launch_bounds__(kPolThreads) void policy_bwd_kernel(int64_t N, const float* grad, const float* g_loss,
                                                                  float* g_logp) {

@@ -1,0 +1,44 @@
+"""The clipped policy loss at the ends of its ranges, against the float64 oracle."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import post as P
+from paper_2608_09703_amd import api as D
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def _np(x):
+    return x.detach().double().cpu().numpy()
+
+
+@pytest.mark.parametrize("N", [1500, 5000, 70000])
+@pytest.mark.parametrize("reduction", ["token", "sequence"])
+@pytest.mark.parametrize("kl_coef", [0.0, 0.1])
+def test_gradients_that_are_finite_after_the_mean_only(N, reduction, kl_coef):
+    """r A and kl_coef exp(ref - logp) past float32 at some tokens, their share of the mean below it. Five
+    roundings of the gradient as elsewhere (the powers of two in between are exact)."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    old = -torch.rand(N, generator=g, device=DEV)
+    logp = old + 0.1 * torch.randn(N, generator=g, device=DEV)
+    ref = logp + 0.1 * torch.randn(N, generator=g, device=DEV)
+    adv = torch.randn(N, generator=g, device=DEV)
+    logp[::7] = old[::7] + 93.0
+    adv[::7] = -1.0
+    ref[3::7] = logp[3::7] + 95.0
+    S = N // 2
+    cu = torch.arange(0, N + 1, 2, dtype=torch.int32, device=DEV) if reduction == "sequence" else None
+    leaf = logp.detach().requires_grad_(True)
+    loss, _, _ = D.policy_loss(leaf, old, adv, ref_logp=ref if kl_coef else None, cu_seqlens=cu, kl_coef=kl_coef,
+                               reduction=reduction)
+    loss.backward()
+    want = P.policy(_np(logp), _np(old), _np(adv), ref=_np(ref) if kl_coef else None,
+                    cu=None if cu is None else cu.cpu().numpy(), reduction=reduction, kl_coef=kl_coef)
+    assert abs(want[3]).max() * (S if cu is not None else N) > 3.4e38 > abs(want[3]).max()
+    got = _np(leaf.grad)
+    assert np.all(np.abs(got - want[3]) <= 5 * U * np.abs(want[3]) + 1e-45)
