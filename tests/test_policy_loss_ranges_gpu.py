@@ -42,3 +42,19 @@ def test_gradients_that_are_finite_after_the_mean_only(N, reduction, kl_coef):
     assert abs(want[3]).max() * (S if cu is not None else N) > 3.4e38 > abs(want[3]).max()
     got = _np(leaf.grad)
     assert np.all(np.abs(got - want[3]) <= 5 * U * np.abs(want[3]) + 1e-45)
+
+
+@pytest.mark.parametrize("N", [1, 1000, 9000])
+@pytest.mark.parametrize("step", [2.0 ** -22, 2.0 ** -14])
+def test_a_policy_next_to_its_reference_keeps_the_digits_of_k(N, step):
+    """k = exp(x) - x - 1 for x of a few steps: x^2 / 2 + x^3 / 6 + x^4 / 24 (the rest is below 2^-39 of it)
+    to a rounding of the mean and, in 64 bits, an ulp of x in k: 2^-52 / (x / 2) < 2^-29 of k."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    logp = -1.0 - torch.randint(0, 2 ** 20, (N,), generator=g, device=DEV).float() * 2.0 ** -21
+    ref = logp + torch.randint(1, 8, (N,), generator=g, device=DEV).float() * step
+    x = _np(ref) - _np(logp)
+    want = (x ** 2 / 2 + x ** 3 / 6 + x ** 4 / 24).mean()
+    _, kl, _ = D.policy_loss(logp, logp, torch.zeros_like(logp), ref_logp=ref, kl_coef=0.5)
+    assert abs(float(kl) - want) <= (U + 2.0 ** -29) * want
+    loss, _, _ = D.policy_loss(logp, logp, torch.zeros_like(logp), ref_logp=ref, kl_coef=0.5)
+    assert abs(float(loss) - 0.5 * want) <= (U + 2.0 ** -29) * 0.5 * want
