@@ -37,6 +37,7 @@ constexpr int kPolTile = kPolThreads * kPolTok;   // tokens per block
 constexpr int kPolSums = 4;                       // loss, KL, clipped, counted (tokens or sequences)
 constexpr int kPolFinThreads = 1024;
 constexpr int kPolOneBlock = 1024 * kPolTok;
+constexpr int64_t kPolCountBlocks = 1 << 20;
 
 __device__ __forceinline__ double wave_total(double v) {
 #pragma unroll
@@ -65,8 +66,9 @@ __device__ __forceinline__ int64_t seq_of(const PolicyArgs& a, int64_t t) {
   return lo;
 }
 
-// Counted tokens of every sequence under a mask, one block a sequence: 16 mask bytes
-// a thread and step, four steps in flight. NT threads: 1,024 for sequences of 64k
+// Counted tokens of every sequence under a mask, one block a sequence (and, past
+// kPolCountBlocks of them, one more after it: a launch has at most 2^32 threads): 16
+// mask bytes a thread and step, four steps in flight. NT threads: 1,024 for sequences of 64k
 // tokens and more on average (2 of 500,000: 435 us byte by byte with 256 threads, 17
 // with these), else 256, of which a short one needs few.
 typedef unsigned int u32x4_byte_t __attribute__((ext_vector_type(4), aligned(1)));
@@ -77,24 +79,29 @@ __device__ __forceinline__ int nonzero_bytes(uint32_t w) {
 template <int NT>
 __global__ __launch_bounds__(NT) void policy_count_kernel(PolicyArgs a) {
   __shared__ int part[NT / 64];
-  const int64_t b = seq_begin(a, blockIdx.x), e = seq_begin(a, (int64_t)blockIdx.x + 1);
-  int n = 0;
+  for (int64_t s = blockIdx.x;;) {
+    const int64_t b = seq_begin(a, s), e = seq_begin(a, s + 1);
+    int n = 0;
 #pragma unroll 4
-  for (int64_t t = b + (int64_t)threadIdx.x * 16; t < e; t += NT * 16) {
-    if (t + 16 <= e) {
-      const u32x4_byte_t m = *reinterpret_cast<const u32x4_byte_t*>(a.mask + t);
-      n += nonzero_bytes(m.x) + nonzero_bytes(m.y) + nonzero_bytes(m.z) + nonzero_bytes(m.w);
-    } else {
-      for (int64_t k = t; k < e; ++k) n += a.mask[k] ? 1 : 0;
+    for (int64_t t = b + (int64_t)threadIdx.x * 16; t < e; t += NT * 16) {
+      if (t + 16 <= e) {
+        const u32x4_byte_t m = *reinterpret_cast<const u32x4_byte_t*>(a.mask + t);
+        n += nonzero_bytes(m.x) + nonzero_bytes(m.y) + nonzero_bytes(m.z) + nonzero_bytes(m.w);
+      } else {
+        for (int64_t k = t; k < e; ++k) n += a.mask[k] ? 1 : 0;
+      }
     }
-  }
-  n = wave_sum(n);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    n = 0;
-    for (int k = 0; k < NT / 64; ++k) n += part[k];
-    a.counts[blockIdx.x] = n;
+    n = wave_sum(n);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      n = 0;
+      for (int k = 0; k < NT / 64; ++k) n += part[k];
+      a.counts[s] = n;
+    }
+    s += gridDim.x;
+    if (s >= a.S) break;
+    __syncthreads();  // part is written again
   }
 }
 
@@ -263,7 +270,7 @@ int64_t tiles_of(int64_t N) { return (N + kPolTile - 1) / kPolTile; }
 size_t policy_part_bytes(int64_t N) { return (size_t)tiles_of(N) * kPolSums * sizeof(double); }
 
 hipError_t launch_policy_count(const PolicyArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.S);
+  const dim3 grid((unsigned)std::min<int64_t>(a.S, kPolCountBlocks));
   if (a.N / a.S >= 65536)
     hipLaunchKernelGGL(policy_count_kernel<1024>, grid, dim3(1024), 0, stream, a);
   else

@@ -58,3 +58,31 @@ def test_a_policy_next_to_its_reference_keeps_the_digits_of_k(N, step):
     assert abs(float(kl) - want) <= (U + 2.0 ** -29) * want
     loss, _, _ = D.policy_loss(logp, logp, torch.zeros_like(logp), ref_logp=ref, kl_coef=0.5)
     assert abs(float(loss) - 0.5 * want) <= (U + 2.0 ** -29) * 0.5 * want
+
+
+def test_more_sequences_than_a_launch_has_blocks():
+    """2^24 and some sequences of 0 to 3 tokens under a mask, their mean of means in 64-bit torch."""
+    S = (1 << 24) + 77
+    g = torch.Generator(device=DEV).manual_seed(1)
+    cu = torch.zeros(S + 1, dtype=torch.int32, device=DEV)
+    lens = torch.randint(0, 4, (S,), generator=g, device=DEV)
+    cu[1:] = torch.cumsum(lens, 0)
+    N = int(cu[-1])
+    old = -torch.rand(N, generator=g, device=DEV)
+    logp = (old + 0.1 * torch.randn(N, generator=g, device=DEV)).requires_grad_(True)
+    adv = torch.randn(N, generator=g, device=DEV)
+    mask = torch.rand(N, generator=g, device=DEV) < 0.6
+    loss, _, clipped = D.policy_loss(logp, old, adv, mask=mask, cu_seqlens=cu, reduction="sequence")
+    got, = torch.autograd.grad(loss, logp)
+    owner = torch.repeat_interleave(torch.arange(S, device=DEV), lens)
+    count = torch.zeros(S, dtype=torch.float64, device=DEV).index_add_(0, owner, mask.double())
+    w = mask.double() / (count[owner].clamp(min=1) * (count > 0).sum())
+    r, a = torch.exp(logp.detach().double() - old.double()), adv.double()
+    free, bound = r * a, r.clamp(0.8, 1.2) * a
+    take = free <= bound
+    want = -(w * torch.minimum(free, bound)).sum()
+    # 64-bit sums on both sides, terms of size 1
+    assert abs(float(loss.detach()) - float(want)) <= U * abs(float(want)) + 1e-9
+    assert abs(float(clipped) - float((w * ~take).sum())) <= U + 1e-9
+    grad = torch.where(take, -w * free, 0.0)
+    assert bool(((got.double() - grad).abs() <= 5 * U * grad.abs() + 1e-45).all())
