@@ -353,7 +353,7 @@ mls_status mls_layer_norm_bwd(const mls_layer_norm* n, const void* x, const void
 
 /*
  * Log-probabilities of given tokens under one head, for post-training: with
- * p->M = 1, temperature p->tau and the tokens in p->labels,
+ * p->M = 1, T <= 2^26 - 128, temperature p->tau and the tokens in p->labels,
  *   logp[t] = log softmax(W h[t] / tau)[tokens[t]]      (0 where the token is ignore_index)
  *   entropy[t] = entropy of softmax(W h[t] / tau)       (likewise; may be NULL)
  * as device float32 [T]. p->alpha and p->teacher do not matter. Tokens with
@@ -384,7 +384,7 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
  * 0 on ignored tokens (whose g_logp is not used):
  *   grad_h = G W  [T, d] of p->grad_h_dtype (0 on ignored tokens),
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
- * Either may be NULL. G is formed one vocabulary chunk at a time (p->vocab_chunk = 0:
+ * Either may be NULL; grad_h is aligned to four of its elements. G is formed one vocabulary chunk at a time (p->vocab_chunk = 0:
  * as few chunks as keep a chunk's G within 256 MiB), from the kept logits or, with
  * kept NULL, from logits computed again. bf16 inputs: G over its token's own entry s
  * (then 1) and, for grad_W, s h[t] are rounded to bfloat16 in between. mls_distill_bwd's

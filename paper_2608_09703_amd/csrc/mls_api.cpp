@@ -917,6 +917,9 @@ mls_status validate_tokens(const mls_problem* p) {
   mls_status st = validate(p);
   if (st != MLS_OK) return st;
   if (p->M != 1) return fail(MLS_INVALID_ARG, "token log-probabilities are of one sub-model, got M=%d", p->M);
+  // a wave a token, and 2^32 threads a launch at most
+  if (round_up(p->T, kFusedBN) * 64 >= 1ll << 32)
+    return fail(MLS_UNSUPPORTED, "T=%lld: at most 2^26 - 128 tokens a call", (long long)p->T);
   return MLS_OK;
 }
 
