@@ -37,12 +37,6 @@ constexpr int kClipTileBytes = kClipThreads * kClipUnroll * 16;
 constexpr int kClipBlocks = 2048;                              // blocks (and parts) of a launch
 constexpr int kClipFinThreads = 1024;
 
-__device__ __forceinline__ double wave_total(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 // Tensor that tile `tile` lies in.
 template <class Args>
 __device__ __forceinline__ int tensor_of(const Args& a, int tile) {
@@ -100,7 +94,7 @@ __global__ __launch_bounds__(kClipThreads) void grad_norm_kernel(GradNormArgs a)
     s += (a.n[i] & kClipF32) ? tile_squares<F32>(a.data[i], t * (kClipTileBytes / 4), n)
                              : tile_squares<Bf16>(a.data[i], t * (kClipTileBytes / 2), n);
   }
-  s = wave_total(s);
+  s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) a.part[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
@@ -111,7 +105,7 @@ __global__ __launch_bounds__(kClipFinThreads) void grad_norm_finish_kernel(const
   __shared__ double red[kClipFinThreads / 64];
   double s = 0.0;
   for (int k = threadIdx.x; k < n; k += kClipFinThreads) s += part[k];
-  s = wave_total(s);
+  s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x != 0) return;

@@ -39,12 +39,6 @@ constexpr int kPolFinThreads = 1024;
 constexpr int kPolOneBlock = 1024 * kPolTok;
 constexpr int64_t kPolCountBlocks = 1 << 20;
 
-__device__ __forceinline__ double wave_total(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 // Start of sequence s inside [0, N]: offsets out of range are clamped, so that a
 // bad one reads no memory outside the arrays.
 __device__ __forceinline__ int64_t seq_begin(const PolicyArgs& a, int64_t s) {
@@ -124,7 +118,7 @@ __device__ __forceinline__ void write_losses(const PolicyArgs& a, const double* 
 template <int NT>
 __device__ __forceinline__ void block_totals(double* v, double (*red)[kPolSums]) {
 #pragma unroll
-  for (int q = 0; q < kPolSums; ++q) v[q] = wave_total(v[q]);
+  for (int q = 0; q < kPolSums; ++q) v[q] = wave_sum(v[q]);
   if ((threadIdx.x & 63) == 0)
 #pragma unroll
     for (int q = 0; q < kPolSums; ++q) red[threadIdx.x >> 6][q] = v[q];

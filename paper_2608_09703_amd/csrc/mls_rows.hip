@@ -10,6 +10,7 @@
 #include "mls_device.h"
 #include "mls_launch.h"
 #include "mls_merge.h"
+#include "mls_wave.h"
 
 namespace mls {
 
@@ -127,12 +128,6 @@ __global__ __launch_bounds__(kThreads) void finalize_rows_kernel(RowArgs a) {
     kl_row[i * T + t] = (valid && k != 0) ? (xr_s - st.xr[k]) / den - lset_s + lt : 0.f;
   }
   h_row[t] = valid ? lset_s - xr_s / den : 0.f;
-}
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
 }
 
 constexpr int kRedThreads = 1024;

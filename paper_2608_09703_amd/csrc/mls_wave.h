@@ -71,6 +71,13 @@ __device__ __forceinline__ int wave_sum(int v) {
   return (lane_read(v, 0) + lane_read(v, 16)) + (lane_read(v, 32) + lane_read(v, 48));
 }
 
+// (64 bits, once or a few times a block: through the LDS crossbar)
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
 __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, dpp_move<dppc::kXor1>(v, -INFINITY));
   v = fmaxf(v, dpp_move<dppc::kXor2>(v, -INFINITY));
