@@ -628,12 +628,14 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
     # (one pass over the list for each property: hundreds of tensors, whose properties
     # cost more than the launches when asked for one by one)
     T = torch.Tensor
+    entries = list(grads)
+    grads = [g for g in entries if g is not None]
     if out is not None:
-        grads, out = list(grads), list(out)
-        if len(out) != len(grads):
+        out = list(out)
+        if len(out) != len(entries):
             raise ValueError("out must hold one entry for each entry of grads")
-        out = [o for g, o in zip(grads, out) if g is not None]
-    grads = [g for g in grads if g is not None]
+        if len(grads) != len(entries):
+            out = [o for g, o in zip(entries, out) if g is not None]
     if not grads:
         raise ValueError("no gradients given: the norm would be on no device")
     dev = grads[0].device
@@ -649,7 +651,7 @@ def _clip(grads, max_norm: float, out) -> torch.Tensor:
     sizes, data = [*map(T.numel, grads)], [*map(T.data_ptr, grads)]
     to = data
     if out is not None:
-        if any(o is None for o in out) or [*map(T.numel, out)] != sizes or [o.dtype for o in out] != dtypes or \
+        if type(None) in map(type, out) or [*map(T.numel, out)] != sizes or [o.dtype for o in out] != dtypes or \
                 {*map(T.get_device, out)} != on or not all(map(T.is_contiguous, out)):
             raise ValueError("out must hold for each gradient one contiguous tensor of its size, dtype and device")
         to = [*map(T.data_ptr, out)]
