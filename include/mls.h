@@ -384,13 +384,14 @@ mls_status mls_token_logp_fwd(const mls_problem* p, void* stats, float* logp, fl
  * 0 on ignored tokens (whose g_logp is not used):
  *   grad_h = G W  [T, d] of p->grad_h_dtype (0 on ignored tokens),
  *   grad_W = G^T h [V, d], float32 or with MLS_GRAD_W_BF16 bfloat16.
- * Either may be NULL; grad_h is aligned to four of its elements. G is formed one vocabulary chunk at a time (p->vocab_chunk = 0:
- * as few chunks as keep a chunk's G within 256 MiB), from the kept logits or, with
+ * Either may be NULL; grad_h is aligned to four of its elements. G is formed one
+ * vocabulary chunk at a time (p->vocab_chunk = 0: as few chunks as keep a chunk's G
+ * within 256 MiB), from the kept logits or, with
  * kept NULL, from logits computed again. bf16 inputs: G over its token's own entry s
  * (then 1) and, for grad_W, s h[t] are rounded to bfloat16 in between. mls_distill_bwd's
- * accumulation flags apply (an accumulated grad_h is added to in fp32). stats and kept: as mls_token_logp_fwd left them on the
- * same inputs; neither is changed. workspace: bwd_bytes of
- * mls_token_logp_workspace. Asynchronous on stream.
+ * accumulation flags apply (an accumulated grad_h is added to in fp32). stats and
+ * kept: as mls_token_logp_fwd left them on the same inputs; neither is changed.
+ * workspace: bwd_bytes of mls_token_logp_workspace. Asynchronous on stream.
  */
 mls_status mls_token_logp_bwd(const mls_problem* p, const void* stats, const void* kept,
                               const float* g_logp, void* grad_h, void* grad_W, void* workspace,

@@ -508,9 +508,14 @@ def token_logp(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, *, temper
     ``ignore_index``. Ignored tokens cost no product, and what their rows of ``h`` hold
     does not matter.
 
-    ``keep_logits``: whether the backward finds the logits kept (16 bits each, ``2 T V``
-    bytes until it is done; bf16 inputs only) or computes them again; by itself, kept up to
-    ``KEEP_LOGITS_BYTES``. It forms the logit gradients a chunk of the vocabulary at a
+    bf16 gradients are sums of bf16 products: each softmax entry over 1 - p (the token's
+    own one is exact), for ``W`` each entry of ``h`` times its token's factor, and the
+    results are rounded to bf16 once (the whole of it is 0.0022 of a gradient's norm in
+    large batches, of which the results' own rounding is 0.0017). float32 has none of these.
+
+    ``keep_logits``: whether the backward finds the logits kept (16 bits each, which is up
+    to 2^-12 of a softmax entry; ``2 T V`` bytes until it is done; bf16 inputs only) or
+    computes them again; by itself, kept up to ``KEEP_LOGITS_BYTES``. It forms the logit gradients a chunk of the vocabulary at a
     time (``vocab_chunk`` columns, or as many as fit 256 MiB).
     """
     opts = dict(tau=temperature, ignore_index=ignore_index, vocab_chunk=vocab_chunk)
