@@ -585,6 +585,136 @@ mls_status mls_spec_verify_noalloc(const mls_sampling* s, int64_t batch, int64_t
                                    int32_t* n_accepted, int32_t* next_token, void* stream);
 
 /*
+ * Pages of cached keys and values, for decoding (paper section 2, paragraph "Speculative
+ * Decoding": draft and verifier share a cache). Entry t of sequence b is row
+ * t % page_size of page page_table[b * ld_table + t / page_size], for every layer and
+ * key head. Pages, table and lengths are the caller's; sequences may name the same page
+ * (a common prefix) as long as neither writes to it. A page number outside [0, pages) or
+ * an entry past the table's row is not there: it is not read or written, and attention
+ * leaves it out. Strides are in elements, and multiples of 16 bytes; k and v have the same.
+ */
+typedef struct mls_kv_cache {
+  int32_t dtype;              /* mls_dtype of k and v */
+  int32_t page_size;          /* entries of a page: a power of two in [16, 65536] */
+  int32_t kv_heads;           /* key heads, 1..65536 */
+  int32_t head_dim;           /* elements of an entry's head: a multiple of 16 bytes, up to 1024 */
+  int64_t layers;             /* layers of the pool (mls_cache_compact); the others take 1 */
+  int64_t pages;              /* pages of a layer, 1..2^31 - 1 */
+  int64_t batch;              /* sequences, 1..65535 */
+  int64_t table_pages;        /* pages a row of the table holds, >= 1; with page_size below 2^31 entries */
+  int64_t ld_layer;
+  int64_t ld_page;
+  int64_t ld_head;
+  int64_t ld_entry;           /* 16 entries span less than 2 GiB */
+  int64_t ld_table;           /* int32 elements between rows of the table, >= table_pages */
+  void* k;                    /* device */
+  void* v;                    /* device */
+  const int32_t* page_table;  /* device [batch] rows of table_pages */
+  const int32_t* lengths;     /* device [batch]: entries a sequence has; below 0: it takes no part */
+} mls_kv_cache;
+
+/*
+ * Writes n new entries of each sequence behind those it has: entry lengths[b] + i takes
+ * k[b][i] and v[b][i], for i < counts[b] (device int32 [batch]; NULL: all n). k and v are
+ * device arrays [batch][n][kv_heads][head_dim] of the cache's dtype, 16-byte aligned, with
+ * the given strides (elements, multiples of 16 bytes; the heads' elements are neighbours),
+ * and must not overlap the pages. Nothing else is written; lengths stay as they are.
+ * Asynchronous on stream.
+ */
+mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, const void* v, int64_t ld_batch,
+                           int64_t ld_node, int64_t ld_head, const int32_t* counts, void* stream);
+
+/*
+ * Moves the entries of an accepted path together, in all layers: entry lengths[b] + j takes
+ * what entry lengths[b] + path[b][j] held, for j = 0..n_accepted[b]. path (device int32
+ * [batch][n]) and n_accepted (device int32 [batch], below 0: the sequence takes no part) are
+ * mls_tree_verify's; n_accepted is taken as at most n - 1, and a path[b][j] outside [j, n)
+ * leaves its entry as it is. new_lengths (device int32 [batch], apart from lengths) receives
+ * lengths[b] + n_accepted[b] + 1, or lengths[b] where the sequence takes no part.
+ * Asynchronous on stream.
+ */
+mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* path, const int32_t* n_accepted,
+                             int32_t* new_lengths, void* stream);
+
+/*
+ * Attention from the n nodes of each sequence's tree of drafted tokens. The nodes' entries
+ * are in the cache behind the sequence's lengths[b] entries (mls_cache_write). Node i of
+ * head h attends to all lengths[b] entries and to the nodes on its way to the root, itself
+ * among them:
+ *   out[b][i][h] = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale q[b][i][h] . k_t),
+ * with the key head h / (heads / kv_heads). parents (device int32 [batch][n]; NULL: a chain)
+ * holds each node's parent: -1 for one behind the context, else an earlier node. A node
+ * with any other parent, or below such a node, is not there: its rows are zeros, and no
+ * node attends to it. One that has nothing to attend to gives zeros too. Keys and values
+ * that a row does not attend to do not matter to it, whatever they hold.
+ * q [batch][n][heads][head_dim] has strides like mls_cache_write's k; out is contiguous, of
+ * the cache's dtype, 16-byte aligned. n in 1..64, heads a multiple of kv_heads, head_dim
+ * 32, 64, 96, 128, 192 or 256. Sums are fp32; bf16 weights are rounded to bfloat16 for the
+ * product with the values. Results depend on the table's width (entries are taken in parts),
+ * and are the same bits on every call. Asynchronous on stream.
+ */
+mls_status mls_tree_attention_workspace(const mls_kv_cache* c, int64_t n, int64_t heads, size_t* bytes);
+mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, const void* q, int64_t ld_batch,
+                              int64_t ld_node, int64_t ld_head, const int32_t* parents, float scale, void* out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of `batch` trees of n nodes (1..64), node 0 the last decided token. Device
+ * arrays:
+ *   target_logits [batch][n][V]  the verifier's logits at each node
+ *   tokens        [batch][n]     int32, node i's drafted token (node 0's is not used)
+ *   parents       [batch][n]     int32, an earlier node; a node with any other parent is not
+ *                                reached. NULL: a chain
+ *   u_accept      [batch][n]     uniforms of the acceptance tests (node 0's is not used)
+ *   u_sample      [batch]        uniform of the final draw
+ *   draft_logits  [batch][n][V]  the draft's logits at each node, from which its children were
+ *                                drawn, each by itself; NULL: children without probabilities
+ * The walk starts at node 0. At node c with p = the verifier's sampling distribution (as
+ * mls_sample has it) and q the draft's, child x of c, in node order, is taken when u_accept
+ * q(x) < p(x); otherwise p becomes max(0, p - q) over its sum (p itself where that is 0), and
+ * the next child is tried. Without draft_logits q(x) is 1 and p loses x. Where no child is
+ * taken, next_token is drawn from p with u_sample, as mls_sample draws. Greedy mode takes
+ * the first child that is the verifier's argmax and ends with the argmax (the uniforms,
+ * draft_logits and the workspace may be NULL). A chain gives mls_spec_verify's results.
+ * Probabilities are formed in 64 bits; which tokens top_p keeps is mls_sample's choice.
+ * draft_params (may be NULL): [batch][n] records of MLS_ROW_PARAMS_BYTES from mls_sample on
+ * the draft's rows with the same settings; records of nodes without children are not used.
+ * Outputs: n_accepted int32 [batch], the drafted tokens taken; path int32 [batch][n], the
+ * taken nodes from node 0 on, then -1; next_token int32 [batch], -1 where the verifier's row
+ * keeps no token. Asynchronous on stream.
+ */
+mls_status mls_tree_verify_workspace(int64_t batch, int64_t n, size_t* bytes);
+mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, const float* target_logits,
+                           const float* draft_logits, const int32_t* tokens, const int32_t* parents,
+                           const float* u_accept, const float* u_sample, const void* draft_params,
+                           int32_t* n_accepted, int32_t* path, int32_t* next_token, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * Rows as 8-bit integers, one scale each: for a row x of d entries, scale = the float32
+ * number next to max |x| / 127, q = the integer next to x / scale (ties to even), in
+ * [-127, 127]; a row of zeros has scale 0. A row with an infinity or NaN has scale NaN and
+ * zeros. x has rows ld_x elements apart; q int8 [T][d] and scale float32 [T] are contiguous,
+ * and q must not overlap x. T in 1..2^31 - 1, d in 1..2^17. Pointers need their element's
+ * alignment only. Asynchronous on stream.
+ */
+mls_status mls_quantize_rows(int64_t T, int64_t d, int64_t ld_x, int32_t dtype, const void* x, int8_t* q,
+                             float* scale, void* stream);
+
+/*
+ * mls_head_logits with the head's weights as 8-bit integers (mls_quantize_rows of W [V][d],
+ * once, when a server loads them): the rows of o are made 8-bit integers q, scale alike, and
+ *   logits[t][v] = scale[t] W_scale[v] sum_k q[t][k] W[v][k],
+ * the sum in 32-bit integers, exact. o [T][d] of dtype, W int8 [V][d], logits float32
+ * [T][V], all contiguous and 16-byte aligned; W_scale float32 [V]. d is a multiple of 16, at
+ * most 2^17. A row of o with an infinity or NaN gives NaN. Asynchronous on stream.
+ */
+mls_status mls_head_logits_quantized_workspace(int64_t T, int64_t d, size_t* bytes);
+mls_status mls_head_logits_quantized(int64_t T, int64_t V, int64_t d, int32_t dtype, const void* o, const int8_t* W,
+                                const float* W_scale, float* logits, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
  * Host helper: loss coefficients of the objective (host arrays of length M).
  *   mode MLS_MODE_PAPER (eq. (3) summed over sub-models):
  *     student g_ce = w (1 - alpha), g_kl = w alpha tau^2; teacher g_ce = w, g_kl = 0

@@ -772,6 +772,239 @@ def spec_verify(draft_logits: Optional[torch.Tensor], target_logits: torch.Tenso
     return n_acc, nxt
 
 
+# ---------------------------------------------------------------------------
+# decoding with a tree of drafted tokens: cache entries, attention, verification, and
+# the head in 8-bit integers
+# ---------------------------------------------------------------------------
+
+def _no_grad(name: str, *xs: Optional[torch.Tensor]):
+    """Refuses tensors that a gradient is wanted for: the result would be without one."""
+    if torch.is_grad_enabled():
+        for x in xs:
+            if x is not None and x.requires_grad:
+                raise RuntimeError(f"{name}: gradients are not available; call it under torch.no_grad()")
+    _primal(name, *xs)
+
+
+def _written(*xs: torch.Tensor):
+    """Tells autograd of tensors that were written through their addresses."""
+    torch.autograd.graph.increment_version([x for x in xs if not x.is_inference()])
+
+
+def _kv_cache(name: str, k_pages, v_pages, page_table, lengths, all_layers: bool = False) -> B.KVCache:
+    if not k_pages.is_cuda:
+        raise RuntimeError(f"{name} runs on the GPU only; got tensors on {k_pages.device}")
+    dev = k_pages.device
+    dims = k_pages.dim()
+    if v_pages.device != dev or v_pages.dtype != k_pages.dtype or v_pages.shape != k_pages.shape or \
+            v_pages.stride() != k_pages.stride() or not (dims == 4 or (all_layers and dims == 5)):
+        raise ValueError(f"{name}: k_pages and v_pages are [pages, kv_heads, page_size, head_dim] tensors" +
+                         (", or such of several layers," if all_layers else "") + " of one layout, dtype and device")
+    shape, stride = k_pages.shape, k_pages.stride()
+    if dims == 4:
+        layers, ld_layer = 1, 0
+    else:
+        layers, ld_layer, shape, stride = shape[0], stride[0], shape[1:], stride[1:]
+    if stride[3] != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: the elements of an entry must be neighbours")
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != dev or \
+            (page_table.size(1) > 1 and page_table.stride(1) != 1):
+        raise ValueError(f"{name}: page_table must be an int32 [B, pages of a sequence] tensor on the pages' device")
+    Bt, width = page_table.shape
+    if lengths.dtype != torch.int32 or lengths.shape != (Bt,) or lengths.device != dev or not lengths.is_contiguous():
+        raise ValueError(f"{name}: lengths must be a contiguous int32 [B] tensor on the pages' device")
+    return B.KVCache(_dtype_code(k_pages.dtype), shape[2], shape[1], shape[3], layers, shape[0], Bt, width, ld_layer,
+                     stride[0], stride[1], stride[2], page_table.stride(0) if Bt > 1 else width, k_pages.data_ptr(),
+                     v_pages.data_ptr(), page_table.data_ptr(), lengths.data_ptr())
+
+
+def _step_rows(name: str, x: torch.Tensor, what: str, c: B.KVCache, like: torch.Tensor, heads: Optional[int] = None):
+    """Checks ``x [B, n, heads, head_dim]`` and returns its strides."""
+    if x.device != like.device or x.dtype != like.dtype or x.dim() != 4 or x.size(0) != c.batch or \
+            x.size(3) != c.head_dim or x.size(1) == 0 or (heads is not None and x.size(2) != heads) or \
+            (x.stride(3) != 1 and x.size(3) > 1):
+        raise ValueError(f"{name}: {what} must be a [B, n, heads, head_dim] tensor of the pages' dtype and device")
+    s = x.stride()
+    return (s[0] if x.size(0) > 1 else 0, s[1] if x.size(1) > 1 else 0, s[2] if x.size(2) > 1 else 0)
+
+
+def _ints(name: str, what: str, x: Optional[torch.Tensor], shape, dev):
+    if x is not None and (x.dtype != torch.int32 or x.shape != shape or x.device != dev or not x.is_contiguous()):
+        raise ValueError(f"{name}: {what} must be a contiguous int32 {list(shape)} tensor on the same device")
+
+
+def cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                page_table: torch.Tensor, lengths: torch.Tensor, *, counts: Optional[torch.Tensor] = None) -> None:
+    """Writes new entries ``k``, ``v [B, n, kv_heads, head_dim]`` behind the ``lengths [B]`` that each sequence has.
+
+    ``k_pages`` and ``v_pages`` are ``[pages, kv_heads, page_size, head_dim]`` (bf16 or float32, any strides of whole
+    16 bytes), ``page_table`` (int32 ``[B, pages of a sequence]``; columns of a wider table will do) names the pages
+    of each sequence: entry ``t`` is row ``t % page_size`` of page ``page_table[b, t // page_size]``. ``counts``
+    (int32 ``[B]``): how many of the ``n`` a sequence has (a padded batch of prompts or trees). A sequence of length
+    below 0 takes no part, and pages outside the pool are not written. ``lengths`` stay as they are.
+    """
+    _no_grad("cache_write", k, v, k_pages, v_pages)
+    c = _kv_cache("cache_write", k_pages, v_pages, page_table, lengths)
+    ld = _step_rows("cache_write", k, "k", c, k_pages, c.kv_heads)
+    if v.shape != k.shape:
+        raise ValueError("cache_write: k and v must be of one shape")
+    if _step_rows("cache_write", v, "v", c, k_pages, c.kv_heads) != ld:
+        v = v.contiguous()
+        k = k.contiguous()
+        ld = _step_rows("cache_write", k, "k", c, k_pages, c.kv_heads)
+    _ints("cache_write", "counts", counts, (c.batch,), k.device)
+    with _on(k.device):
+        B.cache_write(c, k.size(1), k.data_ptr(), v.data_ptr(), ld, counts.data_ptr() if counts is not None else None,
+                      _stream(k.device))
+    _written(k_pages, v_pages)
+
+
+def cache_compact(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                  path: torch.Tensor, n_accepted: torch.Tensor) -> torch.Tensor:
+    """Moves the entries of an accepted path together and returns the sequences' new lengths (int32 ``[B]``).
+
+    ``path [B, n]`` and ``n_accepted [B]`` are those of :func:`tree_verify` for a tree whose entries
+    :func:`cache_write` put behind ``lengths``: entry ``lengths + j`` takes what entry ``lengths + path[:, j]`` held,
+    for ``j`` up to ``n_accepted``. The pages may be those of all layers, ``[layers, pages, kv_heads, page_size,
+    head_dim]``, for one call. Where ``lengths`` or ``n_accepted`` is below 0, nothing moves.
+    """
+    _no_grad("cache_compact", k_pages, v_pages)
+    c = _kv_cache("cache_compact", k_pages, v_pages, page_table, lengths, all_layers=True)
+    dev = k_pages.device
+    if path.dim() != 2:
+        raise ValueError("cache_compact: path must be an int32 [B, n] tensor")
+    _ints("cache_compact", "path", path, (c.batch, path.size(1)), dev)
+    _ints("cache_compact", "n_accepted", n_accepted, (c.batch,), dev)
+    new = torch.empty(c.batch, dtype=torch.int32, device=dev)
+    with _on(dev):
+        B.cache_compact(c, path.size(1), path.data_ptr(), n_accepted.data_ptr(), new.data_ptr(), _stream(dev))
+    _written(k_pages, v_pages)
+    return new
+
+
+def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                   lengths: torch.Tensor, parents: Optional[torch.Tensor] = None, *,
+                   scale: Optional[float] = None) -> torch.Tensor:
+    """Attention from the nodes of each sequence's tree of drafted tokens, ``q [B, n, heads, head_dim]``.
+
+    Pages, ``page_table`` and ``lengths`` as in :func:`cache_write`, which has put the ``n`` nodes' entries behind the
+    ``lengths`` of the context. Node ``i`` attends to the whole context, to its ancestors and to itself. ``parents``
+    (int32 ``[B, n]``): -1 for a node behind the context, else an earlier node; any other number marks a node that
+    the tree does not have (nor any below it), whose rows are zeros. Without ``parents`` the nodes are a chain, and
+    ``n = 1`` is a decoding step without a draft. Up to 64 nodes; ``heads`` is a multiple of the pages' ``kv_heads``
+    (consecutive heads share one); ``head_dim`` 32, 64, 96, 128, 192 or 256; ``scale`` is ``head_dim ** -0.5`` by
+    itself. bf16 or float32, sums in float32; the weights of bf16 values are rounded to bf16. The entries are taken
+    in parts as the table's width has it, so pass the columns that are in use.
+    """
+    _no_grad("tree_attention", q, k_pages, v_pages)
+    c = _kv_cache("tree_attention", k_pages, v_pages, page_table, lengths)
+    ld = _step_rows("tree_attention", q, "q", c, k_pages)
+    dev, n, heads = q.device, q.size(1), q.size(2)
+    _ints("tree_attention", "parents", parents, (c.batch, n), dev)
+    ws_bytes = B.tree_attention_workspace(c, n, heads)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    with _on(dev):
+        B.tree_attention(c, n, heads, q.data_ptr(), ld, parents.data_ptr() if parents is not None else None,
+                         c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                         ws.data_ptr() if ws is not None else None, ws_bytes, _stream(dev))
+    return out
+
+
+def tree_verify(target_logits: torch.Tensor, tokens: torch.Tensor, parents: Optional[torch.Tensor],
+                u_accept: Optional[torch.Tensor], u_sample: Optional[torch.Tensor], *,
+                draft_logits: Optional[torch.Tensor] = None, draft_params: Optional[torch.Tensor] = None,
+                temperature: float = 1.0, top_p: float = 1.0, greedy: bool = False):
+    """``(n_accepted [B], path [B, n], next_token [B])`` (int32): speculative verification of drafted trees.
+
+    Node 0 of each tree is the last decided token. ``target_logits [B, n, V]`` (fp32) are the verifier's at every
+    node, ``tokens [B, n]`` (int32) the drafted ones and ``parents [B, n]`` (int32) the tree: an earlier node, or any
+    other number for a node that is not there; None is a chain. ``draft_logits [B, n, V]``: the draft's at every
+    node, from which its children were drawn, each by itself (rows of nodes without children are not used); without
+    them the children are taken as proposals without probabilities, such as the draft's most likely tokens. Children
+    are tried in node order with ``u_accept [B, n]``; where none is taken the next token is drawn with ``u_sample
+    [B]`` from what is left of the verifier's distribution, which the tokens follow in either case.
+    ``path`` holds the taken nodes from node 0 on, then -1 (:func:`cache_compact` takes it). ``draft_params``: optional
+    uint8 records ``[B, n]`` from ``sample(params=)`` on the draft's rows with the same settings.
+    """
+    _no_grad("tree_verify", target_logits, draft_logits)
+    if not target_logits.is_cuda:
+        raise RuntimeError("tree_verify runs on the GPU only; got tensors on " + str(target_logits.device))
+    if target_logits.dim() != 3:
+        raise ValueError("tree_verify: target_logits must be a [B, n, V] tensor")
+    Bt, n, V = target_logits.shape
+    dev = target_logits.device
+    for what, x, shape in (("target_logits", target_logits, (Bt, n, V)), ("draft_logits", draft_logits, (Bt, n, V)),
+                           ("u_accept", u_accept, (Bt, n)), ("u_sample", u_sample, (Bt,))):
+        if x is not None and (x.dtype != torch.float32 or x.shape != shape or x.device != dev or
+                              not x.is_contiguous()):
+            raise ValueError(f"tree_verify: {what} must be a contiguous float32 {list(shape)} tensor on one device")
+    _ints("tree_verify", "tokens", tokens, (Bt, n), dev)
+    _ints("tree_verify", "parents", parents, (Bt, n), dev)
+    if draft_params is not None and (draft_params.dtype != torch.uint8 or not draft_params.is_contiguous() or
+                                     draft_params.device != dev or
+                                     draft_params.numel() < Bt * n * B.ROW_PARAMS_BYTES):
+        raise ValueError("tree_verify: draft_params must be contiguous uint8 of B * n records")
+    ptr = (lambda x: x.data_ptr() if x is not None else None)
+    s = _sampling(V, temperature, top_p, greedy)
+    out = torch.empty(Bt * (n + 2), dtype=torch.int32, device=dev)
+    n_acc, path, nxt = out[:Bt], out[Bt:Bt * (n + 1)].view(Bt, n), out[Bt * (n + 1):]
+    ws_bytes = 0 if greedy else B.tree_verify_workspace(Bt, n)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    with _on(dev):
+        B.tree_verify(s, Bt, n, target_logits.data_ptr(), ptr(draft_logits), tokens.data_ptr(), ptr(parents),
+                      ptr(u_accept), ptr(u_sample), n_acc.data_ptr(), path.data_ptr(), nxt.data_ptr(), ptr(ws), ws_bytes,
+                      _stream(dev), draft_params=ptr(draft_params))
+    return n_acc, path, nxt
+
+
+def quantize_rows(x: torch.Tensor):
+    """``(q int8 [T, d], scale float32 [T])`` of the rows of ``x [T, d]`` (bf16 or float32; rows may lie apart).
+
+    ``scale = max |x| / 127`` of a row (float32) and ``q`` the integers next to ``x / scale``: the form in which
+    :func:`head_logits_int8` takes a head's weights.
+    """
+    _no_grad("quantize_rows", x)
+    if not x.is_cuda:
+        raise RuntimeError("quantize_rows runs on the GPU only; got a tensor on " + str(x.device))
+    if x.dim() != 2:
+        raise ValueError("quantize_rows: x must be a [T, d] tensor")
+    rows, ld = _norm_rows(x)
+    T, d = rows.shape
+    q = torch.empty(T, d, dtype=torch.int8, device=x.device)
+    scale = torch.empty(T, dtype=torch.float32, device=x.device)
+    with _on(x.device):
+        B.quantize_rows(T, d, ld, _dtype_code(x.dtype), rows.data_ptr(), q.data_ptr(), scale.data_ptr(),
+                        _stream(x.device))
+    return q, scale
+
+
+def head_logits_int8(o: torch.Tensor, W: torch.Tensor, W_scale: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """:func:`head_logits` with the head's weights as 8-bit integers, ``W int8 [V, d]`` and ``W_scale [V]`` of
+    :func:`quantize_rows`: half the bytes of bf16. The rows of ``o [T, d]`` (bf16 or float32) are made 8-bit integers
+    in the same way, and the products are summed exactly. ``d`` is a multiple of 16.
+    """
+    _no_grad("head_logits_int8", o, W_scale)
+    if not o.is_cuda or W.device != o.device or W_scale.device != o.device:
+        raise RuntimeError("head_logits_int8 runs on the GPU only, on tensors of one device")
+    if W.dtype != torch.int8 or W_scale.dtype != torch.float32:
+        raise TypeError("head_logits_int8: W must be int8 and W_scale float32")
+    if o.dim() != 2 or W.dim() != 2 or o.shape[1] != W.shape[1] or W_scale.shape != (W.shape[0],) or \
+            not (o.is_contiguous() and W.is_contiguous() and W_scale.is_contiguous()):
+        raise ValueError("o [T, d], W [V, d] and W_scale [V] must be contiguous with a shared d")
+    dev, (T, d), V = o.device, o.shape, W.shape[0]
+    if out is None:
+        out = torch.empty(T, V, dtype=torch.float32, device=dev)
+    elif out.dtype != torch.float32 or out.shape != (T, V) or out.device != dev or not out.is_contiguous():
+        raise ValueError("out must be a contiguous float32 [T, V] tensor")
+    ws_bytes = B.head_logits_int8_workspace(T, d)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        B.head_logits_int8(T, V, d, _dtype_code(o.dtype), o.data_ptr(), W.data_ptr(), W_scale.data_ptr(),
+                           out.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
+    return out
+
+
 def coefficients(M: int, *, alpha: float, tau: float = 1.0, teacher: int = -1,
                  mode: str = "paper", weights: Optional[Sequence[float]] = None):
     """``(g_ce, g_kl)`` lists of eq. (3) (``mode="paper"``) or the additive form."""

@@ -73,6 +73,15 @@ EXPORTED = (
     "mls_spec_verify_workspace",
     "mls_spec_verify",
     "mls_spec_verify_noalloc",
+    "mls_cache_write",
+    "mls_cache_compact",
+    "mls_tree_attention_workspace",
+    "mls_tree_attention",
+    "mls_tree_verify_workspace",
+    "mls_tree_verify",
+    "mls_quantize_rows",
+    "mls_head_logits_quantized_workspace",
+    "mls_head_logits_quantized",
     "mls_coeffs",
     "mls_read_stats_header",
     "mls_device_error",
@@ -173,6 +182,28 @@ class GradTensor(ctypes.Structure):
     ]
 
 
+class KVCache(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("layers", ctypes.c_int64),
+        ("pages", ctypes.c_int64),
+        ("batch", ctypes.c_int64),
+        ("table_pages", ctypes.c_int64),
+        ("ld_layer", ctypes.c_int64),
+        ("ld_page", ctypes.c_int64),
+        ("ld_head", ctypes.c_int64),
+        ("ld_entry", ctypes.c_int64),
+        ("ld_table", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -223,6 +254,18 @@ def lib():
                                       vp, vp, ctypes.c_size_t, vp]
         L.mls_spec_verify_noalloc.argtypes = [S, ctypes.c_int64, ctypes.c_int64, vp, vp, vp, vp,
                                               vp, vp, vp, vp, vp]
+        K = ctypes.POINTER(KVCache)
+        i64 = ctypes.c_int64
+        L.mls_cache_write.argtypes = [K, i64, vp, vp, i64, i64, i64, vp, vp]
+        L.mls_cache_compact.argtypes = [K, i64, vp, vp, vp, vp]
+        L.mls_tree_attention_workspace.argtypes = [K, i64, i64, sz]
+        L.mls_tree_attention.argtypes = [K, i64, i64, vp, i64, i64, i64, vp, ctypes.c_float, vp, vp, ctypes.c_size_t,
+                                         vp]
+        L.mls_tree_verify_workspace.argtypes = [i64, i64, sz]
+        L.mls_tree_verify.argtypes = [S, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.mls_quantize_rows.argtypes = [i64, i64, i64, ctypes.c_int32, vp, vp, vp, vp]
+        L.mls_head_logits_quantized_workspace.argtypes = [i64, i64, sz]
+        L.mls_head_logits_quantized.argtypes = [i64, i64, i64, ctypes.c_int32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.mls_coeffs.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_float,
                                  ctypes.c_int32, fp, fp, fp]
         L.mls_read_stats_header.argtypes = [P, vp, vp, ctypes.POINTER(ctypes.c_int32),
@@ -475,6 +518,59 @@ def spec_verify_noalloc(s: Sampling, batch: int, gamma: int, draft_logits: Optio
                                         draft_tokens, u_accept, u_sample, draft_params,
                                         n_accepted, next_token, stream),
           "mls_spec_verify_noalloc")
+
+
+def cache_write(c: KVCache, n: int, k: int, v: int, ld: Sequence[int], counts: Optional[int], stream: int):
+    """``ld``: elements between batch entries, nodes and heads of ``k`` and ``v``."""
+    check(lib().mls_cache_write(ctypes.byref(c), n, k, v, ld[0], ld[1], ld[2], counts, stream), "mls_cache_write")
+
+
+def cache_compact(c: KVCache, n: int, path: int, n_accepted: int, new_lengths: int, stream: int):
+    check(lib().mls_cache_compact(ctypes.byref(c), n, path, n_accepted, new_lengths, stream), "mls_cache_compact")
+
+
+def tree_attention_workspace(c: KVCache, n: int, heads: int) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_tree_attention_workspace(ctypes.byref(c), n, heads, ctypes.byref(b)),
+          "mls_tree_attention_workspace")
+    return b.value
+
+
+def tree_attention(c: KVCache, n: int, heads: int, q: int, ld: Sequence[int], parents: Optional[int], scale: float,
+                   out: int, ws: Optional[int], ws_bytes: int, stream: int):
+    check(lib().mls_tree_attention(ctypes.byref(c), n, heads, q, ld[0], ld[1], ld[2], parents, scale, out, ws,
+                                   ws_bytes, stream), "mls_tree_attention")
+
+
+def tree_verify_workspace(batch: int, n: int) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_tree_verify_workspace(batch, n, ctypes.byref(b)), "mls_tree_verify_workspace")
+    return b.value
+
+
+def tree_verify(s: Sampling, batch: int, n: int, target_logits: int, draft_logits: Optional[int],
+                tokens: Optional[int], parents: Optional[int], u_accept: Optional[int], u_sample: Optional[int],
+                n_accepted: int, path: int, next_token: int, ws: Optional[int], ws_bytes: int, stream: int,
+                draft_params: Optional[int] = None):
+    check(lib().mls_tree_verify(ctypes.byref(s), batch, n, target_logits, draft_logits, tokens, parents, u_accept,
+                                u_sample, draft_params, n_accepted, path, next_token, ws, ws_bytes, stream),
+          "mls_tree_verify")
+
+
+def quantize_rows(T: int, d: int, ld_x: int, dtype: int, x: int, q: int, scale: int, stream: int):
+    check(lib().mls_quantize_rows(T, d, ld_x, dtype, x, q, scale, stream), "mls_quantize_rows")
+
+
+def head_logits_int8_workspace(T: int, d: int) -> int:
+    b = ctypes.c_size_t(0)
+    check(lib().mls_head_logits_quantized_workspace(T, d, ctypes.byref(b)), "mls_head_logits_quantized_workspace")
+    return b.value
+
+
+def head_logits_int8(T: int, V: int, d: int, dtype: int, o: int, W: int, W_scale: int, logits: int, ws: int,
+                     ws_bytes: int, stream: int):
+    check(lib().mls_head_logits_quantized(T, V, d, dtype, o, W, W_scale, logits, ws, ws_bytes, stream),
+          "mls_head_logits_quantized")
 
 
 def coeffs(M: int, teacher: int = -1, alpha: float = 0.0, tau: float = 1.0,

@@ -20,7 +20,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmls.so")
 
 SOURCES = ["mls_api.cpp", "mls_fused.hip", "mls_gemm.hip", "mls_rows.hip", "mls_diag.hip", "mls_junction.hip", "mls_decode.hip", "mls_static.hip",
-           "mls_probe.hip", "mls_norm.hip", "mls_policy.hip", "mls_clip.hip", "mls_tokens.hip"]
+           "mls_probe.hip", "mls_norm.hip", "mls_policy.hip", "mls_clip.hip", "mls_tokens.hip",
+           "mls_attn.hip", "mls_cache.hip", "mls_tree.hip", "mls_quant.hip"]
 ARCH = "gfx950"
 
 

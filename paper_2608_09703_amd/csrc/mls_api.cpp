@@ -89,6 +89,7 @@ constexpr int64_t kRecordBudget = 1ll << 30;      // forward partial records of 
 constexpr int64_t kLogitSlabBudget = 16ll << 30;  // stored logits of one token chunk (all sub-models)
 constexpr int64_t kPanelMax = (1ll << 32) - 1;    // bytes one wide-GEMM operand may span
 constexpr int64_t kCus = 256;                     // compute units of the part
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxSplits = 16;                // K parts of a grad_h product
 // and of token log-probabilities', whose one chunk has a K of all of V for as little as
 // a row. us of the gradient products, at most 16 / 32 / 64 / 128 parts: T = 18, d = 504,
@@ -2213,6 +2214,437 @@ mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
     e = launch_verify(a, ept, hs);
   }
   if (e != hipSuccess) return hip_fail(e, "verification launch");
+  return MLS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxNodes = 64;  // nodes of a tree
+
+mls_status validate_cache(const mls_kv_cache* c, int64_t layers_max) {
+  if (!c) return fail(MLS_INVALID_ARG, "cache descriptor is NULL");
+  if (c->dtype != MLS_BF16 && c->dtype != MLS_F32) return fail(MLS_UNSUPPORTED, "dtype=%d unsupported", c->dtype);
+  const int64_t es = c->dtype == MLS_BF16 ? 2 : 4;
+  if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return fail(MLS_UNSUPPORTED, "page_size=%d is not a power of two in [16, 65536]", c->page_size);
+  if (c->kv_heads < 1 || c->kv_heads > 65536) return fail(MLS_INVALID_ARG, "kv_heads=%d out of range", c->kv_heads);
+  if (c->head_dim < 1 || c->head_dim > 1024 || c->head_dim * es % 16)
+    return fail(MLS_UNSUPPORTED, "head_dim=%d: heads are multiples of 16 bytes, up to 1024 elements", c->head_dim);
+  if (c->layers < 1 || c->layers > layers_max)
+    return fail(MLS_INVALID_ARG, "layers=%lld out of [1, %lld]", (long long)c->layers, (long long)layers_max);
+  if (c->pages < 1 || c->pages > 0x7fffffff) return fail(MLS_INVALID_ARG, "pages=%lld out of range", (long long)c->pages);
+  if (c->batch < 1 || c->batch > 65535) return fail(MLS_INVALID_ARG, "batch=%lld out of range", (long long)c->batch);
+  if (c->table_pages < 1 || c->table_pages > 0x7fffffff / c->page_size)
+    return fail(MLS_INVALID_ARG, "table_pages=%lld out of range", (long long)c->table_pages);
+  if (c->ld_table < c->table_pages) return fail(MLS_INVALID_ARG, "the table's rows overlap");
+  const int64_t lds[4] = {c->ld_layer, c->ld_page, c->ld_head, c->ld_entry};
+  const int64_t counts[4] = {c->layers, c->pages, c->kv_heads, c->page_size};
+  for (int i = 0; i < 4; ++i) {
+    if (lds[i] < 0 || lds[i] > (1ll << 48) || lds[i] * es % 16)
+      return fail(MLS_INVALID_ARG, "strides must be multiples of 16 bytes");
+    if (counts[i] > 1 && lds[i] < c->head_dim) return fail(MLS_INVALID_ARG, "entries overlap");
+  }
+  if (16 * c->ld_entry * es >= (1ll << 31)) return fail(MLS_UNSUPPORTED, "16 entries span 2 GiB or more");
+  if (!c->k || !c->v || !c->page_table || !c->lengths)
+    return fail(MLS_INVALID_ARG, "pages, table and lengths must be non-NULL");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(MLS_INVALID_ARG, "pages must be 16-byte aligned");
+  if (!aligned(c->page_table, 4) || !aligned(c->lengths, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  return MLS_OK;
+}
+
+CacheArgs cache_args(const mls_kv_cache* c) {
+  CacheArgs a;
+  memset(&a, 0, sizeof(a));
+  const int64_t per = 16 / (c->dtype == MLS_BF16 ? 2 : 4);  // elements of a chunk
+  a.k = static_cast<char*>(c->k);
+  a.v = static_cast<char*>(c->v);
+  a.table = c->page_table;
+  a.lengths = c->lengths;
+  a.batch = c->batch;
+  a.pages = c->pages;
+  a.table_pages = c->table_pages;
+  a.table_ld = c->ld_table;
+  a.s_layer = c->ld_layer / per;
+  a.s_page = c->ld_page / per;
+  a.s_head = c->ld_head / per;
+  a.s_entry = c->ld_entry / per;
+  a.layers = (int32_t)c->layers;
+  a.kv_heads = c->kv_heads;
+  a.page_log2 = __builtin_ctz((unsigned)c->page_size);
+  a.chunks = (int32_t)(c->head_dim / per);
+  return a;
+}
+
+// Strides of a step's rows [batch][n][heads][head_dim].
+mls_status validate_rows(const char* what, const void* p, int64_t es, int64_t ld_batch, int64_t ld_node,
+                         int64_t ld_head) {
+  if (!p) return fail(MLS_INVALID_ARG, "%s is NULL", what);
+  if (!aligned(p, 16)) return fail(MLS_INVALID_ARG, "%s must be 16-byte aligned", what);
+  for (int64_t ld : {ld_batch, ld_node, ld_head})
+    if (ld < 0 || ld > (1ll << 48) || ld * es % 16)
+      return fail(MLS_INVALID_ARG, "%s's strides must be multiples of 16 bytes", what);
+  return MLS_OK;
+}
+
+// Parts of the entries: enough blocks for the chip where a batch has few sequences and
+// heads, and parts of kPartMost entries at most, so that one long sequence among short
+// ones does not run alone at the end.
+constexpr int64_t kAttnBlocks = 1024;
+constexpr int64_t kPartLeast = 256;
+constexpr int64_t kPartMost = 4096;
+
+struct AttnPlan {
+  int64_t rows, tile, n_rt, part, splits, records;
+  size_t acc_bytes, bytes;
+};
+
+mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnPlan& pl) {
+  mls_status st = validate_cache(c, 1);
+  if (st != MLS_OK) return st;
+  if (n < 1 || n > kMaxNodes) return fail(MLS_UNSUPPORTED, "n=%lld nodes outside [1, 64]", (long long)n);
+  if (heads < 1 || heads > 65536 || heads % c->kv_heads)
+    return fail(MLS_INVALID_ARG, "heads=%lld is not a multiple of kv_heads=%d", (long long)heads, c->kv_heads);
+  const int32_t D = c->head_dim;
+  if (D != 32 && D != 64 && D != 96 && D != 128 && D != 192 && D != 256)
+    return fail(MLS_UNSUPPORTED, "head_dim=%d: attention takes 32, 64, 96, 128, 192 or 256", D);
+  pl.rows = n * (heads / c->kv_heads);
+  pl.tile = attn_tile_rows((int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
+  pl.n_rt = (pl.rows + pl.tile - 1) / pl.tile;
+  const int64_t base = c->batch * c->kv_heads * pl.n_rt;
+  const int64_t cap = c->table_pages * c->page_size;
+  const int64_t want = (kAttnBlocks + base - 1) / base;
+  pl.part = std::min(std::max(round_up((cap + want - 1) / want, 128), kPartLeast), kPartMost);
+  pl.splits = (cap + pl.part - 1) / pl.part;
+  if (base * pl.splits > 0x7fffffff || c->batch * n * heads * (D / 4) > (1ll << 38))
+    return fail(MLS_UNSUPPORTED, "%lld parts of the cache are more than one launch takes", (long long)(base * pl.splits));
+  pl.records = pl.splits > 1 ? base * pl.splits * pl.tile : 0;
+  pl.acc_bytes = align256((size_t)pl.records * D * 4);
+  pl.bytes = pl.acc_bytes + align256((size_t)pl.records * 8);
+  return MLS_OK;
+}
+
+size_t tree_ws_bytes(int64_t batch, int64_t n) { return align256((size_t)(2 * batch * n) * sizeof(RowDist)); }
+
+mls_status validate_tree(int64_t batch, int64_t n) {
+  if (batch < 1 || batch > (1 << 24) || n < 1 || n > kMaxNodes)
+    return fail(MLS_INVALID_ARG, "batch=%lld n=%lld out of range", (long long)batch, (long long)n);
+  return MLS_OK;
+}
+
+mls_status validate_quant(int64_t T, int64_t d, int32_t dtype) {
+  if (T < 1 || T > 0x7fffffff || d < 1 || d > (1 << 17))
+    return fail(MLS_INVALID_ARG, "T=%lld d=%lld out of range", (long long)T, (long long)d);
+  if (dtype != MLS_BF16 && dtype != MLS_F32) return fail(MLS_UNSUPPORTED, "dtype=%d unsupported", dtype);
+  return MLS_OK;
+}
+
+size_t int8_ws_bytes(int64_t T, int64_t d) { return align256((size_t)T * d) + align256((size_t)T * 4); }
+
+}  // namespace
+
+extern "C" {
+
+mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, const void* v, int64_t ld_batch,
+                           int64_t ld_node, int64_t ld_head, const int32_t* counts, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_cache(c, 1);
+  if (st != MLS_OK) return st;
+  const int64_t es = c->dtype == MLS_BF16 ? 2 : 4;
+  CacheWriteArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache_args(c);
+  if (n < 1 || n > (1ll << 30) || n * a.c.kv_heads > (1ll << 40) ||
+      n * a.c.kv_heads * a.c.chunks > 0x7fffffff - (1 << 20))
+    return fail(MLS_INVALID_ARG, "n=%lld out of range", (long long)n);
+  if ((st = validate_rows("k", k, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
+  if ((st = validate_rows("v", v, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
+  if (!aligned(counts, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  const int64_t per = 16 / es;
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.s_batch = ld_batch / per;
+  a.s_node = ld_node / per;
+  a.s_head = ld_head / per;
+  a.counts = counts;
+  a.n = (int32_t)n;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope ps("cache_write", hs);
+    e = launch_cache_write(a, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "cache write launch");
+  return MLS_OK;
+}
+
+mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* path, const int32_t* n_accepted,
+                             int32_t* new_lengths, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_cache(c, 65536);
+  if (st != MLS_OK) return st;
+  if (n < 1 || n > kMaxNodes) return fail(MLS_UNSUPPORTED, "n=%lld nodes outside [1, 64]", (long long)n);
+  if (!path || !n_accepted || !new_lengths)
+    return fail(MLS_INVALID_ARG, "path, n_accepted and new_lengths must be non-NULL");
+  if (!aligned(path, 4) || !aligned(n_accepted, 4) || !aligned(new_lengths, 4))
+    return fail(MLS_INVALID_ARG, "misaligned pointer");
+  const size_t nb = (size_t)c->batch * 4;
+  if (!disjoint(new_lengths, nb, c->lengths, nb) || !disjoint(new_lengths, nb, n_accepted, nb) ||
+      !disjoint(new_lengths, nb, path, nb * n))
+    return fail(MLS_INVALID_ARG, "new_lengths overlaps an input");
+  CacheCompactArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache_args(c);
+  if (c->layers * a.c.kv_heads * a.c.chunks > 0x7fffffff - (1 << 20))
+    return fail(MLS_UNSUPPORTED, "an entry's heads in all layers are more than one launch takes");
+  a.path = path;
+  a.n_accepted = n_accepted;
+  a.new_lengths = new_lengths;
+  a.n = (int32_t)n;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope ps("cache_compact", hs);
+    e = launch_cache_compact(a, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "cache compaction launch");
+  return MLS_OK;
+}
+
+mls_status mls_tree_attention_workspace(const mls_kv_cache* c, int64_t n, int64_t heads, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  AttnPlan pl;
+  mls_status st = plan_attention(c, n, heads, pl);
+  if (st != MLS_OK) return st;
+  *bytes = pl.bytes;
+  return MLS_OK;
+}
+
+mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, const void* q, int64_t ld_batch,
+                              int64_t ld_node, int64_t ld_head, const int32_t* parents, float scale, void* out,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  AttnPlan pl;
+  mls_status st = plan_attention(c, n, heads, pl);
+  if (st != MLS_OK) return st;
+  const int64_t es = c->dtype == MLS_BF16 ? 2 : 4;
+  if ((st = validate_rows("q", q, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
+  if (!out || !aligned(out, 16)) return fail(MLS_INVALID_ARG, "out must be non-NULL and 16-byte aligned");
+  if (!aligned(parents, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  if (!isfinite(scale)) return fail(MLS_INVALID_ARG, "scale must be finite");
+  if (pl.bytes && (!workspace || workspace_bytes < pl.bytes))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "attention needs %zu workspace bytes, got %zu", pl.bytes,
+                workspace ? workspace_bytes : 0);
+  if (!aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned workspace");
+  const int64_t per = 16 / es;
+  AttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = cache_args(c);
+  a.q = static_cast<const char*>(q);
+  a.q_batch = ld_batch / per;
+  a.q_node = ld_node / per;
+  a.q_head = ld_head / per;
+  a.out = out;
+  a.parents = parents;
+  a.scale = scale * kLog2e;
+  a.n = (int32_t)n;
+  a.heads = (int32_t)heads;
+  a.group = (int32_t)(heads / c->kv_heads);
+  a.rows = (int32_t)pl.rows;
+  a.n_rt = (int32_t)pl.n_rt;
+  a.splits = (int32_t)pl.splits;
+  a.part = (int32_t)pl.part;
+  a.acc = static_cast<float*>(workspace);
+  a.ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.acc_bytes);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope ps("tree_attention", hs);
+    e = launch_tree_attention(a, c->head_dim, c->dtype == MLS_F32, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "tree attention launch");
+  return MLS_OK;
+}
+
+mls_status mls_tree_verify_workspace(int64_t batch, int64_t n, size_t* bytes) {
+  g_last_error.clear();
+  mls_status st = validate_tree(batch, n);
+  if (st != MLS_OK) return st;
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  *bytes = tree_ws_bytes(batch, n);
+  return MLS_OK;
+}
+
+mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, const float* target_logits,
+                           const float* draft_logits, const int32_t* tokens, const int32_t* parents,
+                           const float* u_accept, const float* u_sample, const void* draft_params,
+                           int32_t* n_accepted, int32_t* path, int32_t* next_token, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_sampling(s);
+  if (st != MLS_OK) return st;
+  if ((st = validate_tree(batch, n)) != MLS_OK) return st;
+  if (!target_logits || !n_accepted || !path || !next_token || (n > 1 && !tokens))
+    return fail(MLS_INVALID_ARG, "target_logits, tokens and outputs must be non-NULL");
+  if (!s->greedy && (!u_sample || (n > 1 && !u_accept)))
+    return fail(MLS_INVALID_ARG, "sampling needs u_accept and u_sample");
+  if (draft_params && !draft_logits) return fail(MLS_INVALID_ARG, "draft_params go with draft_logits");
+  if (!s->greedy && (!workspace || workspace_bytes < tree_ws_bytes(batch, n)))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "verification needs %zu workspace bytes, got %zu", tree_ws_bytes(batch, n),
+                workspace ? workspace_bytes : 0);
+  if (!aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned workspace");
+  for (const void* p : {(const void*)target_logits, (const void*)draft_logits, (const void*)tokens,
+                        (const void*)parents, (const void*)u_accept, (const void*)u_sample, draft_params,
+                        (const void*)n_accepted, (const void*)path, (const void*)next_token})
+    if (!aligned(p, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  RowDist* params = static_cast<RowDist*>(workspace);
+  const float inv_temp = s->greedy ? 1.f : 1.f / s->temperature;
+  const bool draft = !s->greedy && draft_logits && n > 1;
+  if (!s->greedy) {
+    // workspace: the draft rows' records [batch][n], then the verifier's
+    RowParamArgs r;
+    memset(&r, 0, sizeof(r));
+    r.rows0 = draft && !draft_params ? batch * n : 0;
+    r.rows1 = batch * n;
+    r.V = s->V;
+    r.inv_temp = inv_temp;
+    r.top_p = s->top_p;
+    r.logits0 = draft_logits;
+    r.logits1 = target_logits;
+    r.params = params + (batch * n - r.rows0);
+    {
+      ProfScope ps("row_params", hs);
+      e = launch_row_params(r, row_elems_per_thread(s->V), hs);
+    }
+    if (e != hipSuccess) return hip_fail(e, "row parameter launch");
+  }
+  TreeVerifyArgs a;
+  memset(&a, 0, sizeof(a));
+  a.target = target_logits;
+  a.draft = draft ? draft_logits : nullptr;
+  a.tparams = params + batch * n;
+  a.dparams = draft_params ? static_cast<const RowDist*>(draft_params) : params;
+  a.tokens = tokens;
+  a.parents = parents;
+  a.u_accept = u_accept;
+  a.u_sample = u_sample;
+  a.n_accepted = n_accepted;
+  a.path = path;
+  a.next_token = next_token;
+  a.batch = batch;
+  a.V = (int32_t)s->V;
+  a.n = (int32_t)n;
+  a.greedy = s->greedy ? 1 : 0;
+  a.temperature = s->temperature;
+  a.inv_temp = inv_temp;
+  a.top_p = s->top_p;
+  {
+    ProfScope ps("tree_verify", hs);
+    e = launch_tree_verify(a, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "tree verification launch");
+  return MLS_OK;
+}
+
+mls_status mls_quantize_rows(int64_t T, int64_t d, int64_t ld_x, int32_t dtype, const void* x, int8_t* q,
+                             float* scale, void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_quant(T, d, dtype);
+  if (st != MLS_OK) return st;
+  const size_t es = dtype == MLS_BF16 ? 2 : 4;
+  if (ld_x < d || ld_x > (1ll << 40)) return fail(MLS_INVALID_ARG, "ld_x=%lld below d=%lld", (long long)ld_x, (long long)d);
+  if (!x || !q || !scale) return fail(MLS_INVALID_ARG, "x, q and scale must be non-NULL");
+  if (!aligned(x, es) || !aligned(scale, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  const size_t nx = ((size_t)(T - 1) * ld_x + d) * es;
+  if (!disjoint(q, (size_t)T * d, x, nx) || !disjoint(scale, (size_t)T * 4, x, nx) ||
+      !disjoint(scale, (size_t)T * 4, q, (size_t)T * d))
+    return fail(MLS_INVALID_ARG, "outputs overlap x or each other");
+  QuantArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.q = q;
+  a.scale = scale;
+  a.T = T;
+  a.ld = ld_x;
+  a.d = (int32_t)d;
+  a.f32 = dtype == MLS_F32;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope ps("quantize_rows", hs);
+    e = launch_quantize_rows(a, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "quantization launch");
+  return MLS_OK;
+}
+
+mls_status mls_head_logits_quantized_workspace(int64_t T, int64_t d, size_t* bytes) {
+  g_last_error.clear();
+  mls_status st = validate_quant(T, d, MLS_BF16);
+  if (st != MLS_OK) return st;
+  if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
+  *bytes = int8_ws_bytes(T, d);
+  return MLS_OK;
+}
+
+mls_status mls_head_logits_quantized(int64_t T, int64_t V, int64_t d, int32_t dtype, const void* o, const int8_t* W,
+                                const float* W_scale, float* logits, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  g_last_error.clear();
+  mls_status st = validate_quant(T, d, dtype);
+  if (st != MLS_OK) return st;
+  if (T > (1ll << 30) || V < 1 || V > (1ll << 30)) return fail(MLS_INVALID_ARG, "T=%lld V=%lld out of range", (long long)T, (long long)V);
+  if (d % 16) return fail(MLS_UNSUPPORTED, "d=%lld is not a multiple of 16", (long long)d);
+  if (!o || !W || !W_scale || !logits) return fail(MLS_INVALID_ARG, "o, W, W_scale and logits must be non-NULL");
+  if (!aligned(o, 16) || !aligned(W, 16) || !aligned(logits, 16) || !aligned(W_scale, 4))
+    return fail(MLS_INVALID_ARG, "o, W and logits must be 16-byte aligned");
+  if (!workspace || workspace_bytes < int8_ws_bytes(T, d))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "the 8-bit head needs %zu workspace bytes, got %zu", int8_ws_bytes(T, d),
+                workspace ? workspace_bytes : 0);
+  if (!aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned workspace");
+  int8_t* q = static_cast<int8_t*>(workspace);
+  float* scale = reinterpret_cast<float*>(q + align256((size_t)T * d));
+  HeadArgs a;
+  memset(&a, 0, sizeof(a));
+  a.T = T;
+  a.V = V;
+  a.d = d;
+  a.o = q;
+  a.W = W;
+  a.logits = logits;
+  a.o_scale = scale;
+  a.W_scale = W_scale;
+  int rows, cols;
+  head_i8_tile(T, V, &rows, &cols);
+  a.n_tt = (int)((T + cols - 1) / cols);
+  a.n_vt = (int)((V + rows - 1) / rows);
+  if ((int64_t)a.n_tt * a.n_vt > 0x7fffffff) return fail(MLS_INVALID_ARG, "T=%lld V=%lld out of range", (long long)T, (long long)V);
+  a.group_v = rows == 192 ? 4 : 8;
+  QuantArgs z;
+  memset(&z, 0, sizeof(z));
+  z.x = o;
+  z.q = q;
+  z.scale = scale;
+  z.T = T;
+  z.ld = d;
+  z.d = (int32_t)d;
+  z.f32 = dtype == MLS_F32;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  {
+    ProfScope ps("quantize_rows", hs);
+    e = launch_quantize_rows(z, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "quantization launch");
+  {
+    ProfScope ps("head_logits_int8", hs);
+    e = launch_head_logits_i8(a, hs);
+  }
+  if (e != hipSuccess) return hip_fail(e, "8-bit head launch");
   return MLS_OK;
 }
 

@@ -1,0 +1,623 @@
+// Attention of a tree of drafted tokens over a paged cache (paper section 2, paragraph
+// "Speculative Decoding": the verifier scores all drafted tokens in one pass over the
+// cache it shares with the draft).
+//
+// For node i of sequence b with context length L, head h and key head h / group,
+//   o = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale q . k_t),
+// over t < L and over the entries L + j of the nodes j on i's way to the root (i among
+// them). A row keeps a running maximum m and sum; w is taken relative to m, in base 2.
+//
+// A block takes up to 64 rows (nodes x heads of one key head) and one part of the
+// entries; its four waves take the part's tiles in turn, each for itself, and join their
+// sums at the end. Nothing goes through LDS on the way there, and no wave waits for
+// another: the two products are laid out so that each one's operands are what loads and
+// the other product leave in a lane's registers.
+//   S^T = K Q^T   v_mfma 16x16x32: lane (g = lane / 16, r = lane % 16) brings 16 bytes of
+//                 entry r's head and 16 bytes of row r; it receives row r's scores with
+//                 entries 4 g .. 4 g + 3 of each 16.
+//   O^T = V^T P^T the contraction runs over entries in any order that both operands
+//                 share: lane (g, r) brings as K values just those entries, for row r its
+//                 own weights; of V it has loaded these entries' elements DE r .. DE r +
+//                 DE - 1 (DE = D / 16), and product m takes element m of each, entry pairs
+//                 joined by one byte permute. A lane's results are row r's elements
+//                 4 DE g .. 4 DE g + 4 DE - 1.
+// float32 is laid out the same way on v_mfma 16x16x4 (no permutes: one value a register).
+//
+// Entries 16 s .. 16 s + 15 of a sequence lie in one page, so page numbers and page
+// addresses are scalar.
+#include <math.h>
+
+#include "mls_core.h"
+#include "mls_device.h"
+#include "mls_launch.h"
+#include "mls_wave.h"
+
+namespace mls {
+
+namespace {
+
+constexpr int kAttnWaves = 4;
+constexpr int kAttnThreads = 64 * kAttnWaves;
+// A row's weights are relative to a maximum that is brought up to date only where a score
+// passes it by this much (base 2): the weights stay below 2^8, which costs the sums nothing.
+constexpr float kMaxSlack = 8.f;
+
+template <typename E>
+struct AttnTile;
+template <>
+struct AttnTile<Bf16> {
+  static constexpr int kSubs = 2;  // runs of 16 entries of a tile
+};
+template <>
+struct AttnTile<F32> {
+  static constexpr int kSubs = 1;
+};
+
+// The nodes on the way from each node to the root (bit j: node j), 0 for a node that the
+// tree does not have. One thread per node.
+__device__ __forceinline__ unsigned long long ancestors(const int32_t* parents, int i, int n) {
+  unsigned long long m = 0;
+  for (;;) {  // i falls with every step
+    m |= 1ull << i;
+    const int p = parents[i];
+    if (p == -1) return m;
+    if (p < 0 || p >= i) return 0;
+    i = p;
+  }
+}
+
+// Loads of NB bytes, a multiple of 4, at lane offset `voff` and scalar offset `soff` of a
+// buffer.
+template <int NB>
+__device__ __forceinline__ void load_bytes(__amdgpu_buffer_rsrc_t rs, int voff, int soff, uint32_t* r) {
+  typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t words3 __attribute__((ext_vector_type(3)));
+  typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+  if constexpr (NB >= 16) {
+    const words4 v = __builtin_bit_cast(words4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff, soff, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = v[i];
+    if constexpr (NB > 16) load_bytes<NB - 16>(rs, voff + 16, soff, r + 4);
+  } else if constexpr (NB == 12) {
+    const words3 v = __builtin_bit_cast(words3, __builtin_amdgcn_raw_buffer_load_b96(rs, voff, soff, 0));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r[i] = v[i];
+  } else if constexpr (NB == 8) {
+    const words2 v = __builtin_bit_cast(words2, __builtin_amdgcn_raw_buffer_load_b64(rs, voff, soff, 0));
+    r[0] = v[0];
+    r[1] = v[1];
+  } else {
+    static_assert(NB == 4, "whole words");
+    r[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff, soff, 0);
+  }
+}
+
+// A word of values with infinities and NaN taken out.
+template <typename E>
+__device__ __forceinline__ uint32_t finite_word(uint32_t x);
+template <>
+__device__ __forceinline__ uint32_t finite_word<F32>(uint32_t x) {
+  return (x & 0x7f800000u) == 0x7f800000u ? 0u : x;
+}
+template <>
+__device__ __forceinline__ uint32_t finite_word<Bf16>(uint32_t x) {
+  x = (x & 0x7f800000u) == 0x7f800000u ? x & 0xffffu : x;
+  return (x & 0x7f80u) == 0x7f80u ? x & 0xffff0000u : x;
+}
+
+template <typename E, int D, int RT>
+struct Attn {
+  static constexpr int DE = D / 16;                     // elements of a lane's piece of an entry of V
+  static constexpr int SUBS = AttnTile<E>::kSubs;
+  static constexpr int KT = 16 * SUBS;                  // entries of a tile
+  static constexpr int VB = DE * E::kBytes;             // bytes of such a piece
+  static constexpr int VW = VB / 4;
+  static constexpr int KC = D * E::kBytes / 64;         // 16-byte pieces of a lane's share of an entry of K
+  static constexpr int ROWS = 16 * RT;
+  static constexpr int LD = D + 4;                      // floats of a row in LDS
+
+  uint4 qf[RT][KC];
+  uint32_t kf[SUBS][KC][4];
+  uint32_t vf[SUBS * 4][VW];
+  f32x4_t acc[RT][DE];
+  float m[RT];
+  float l[RT];
+
+  // The 16 entries from t0 on (head hk) in one pool: a scalar base, so that a lane's part
+  // of any address is one 32-bit offset. (The host has checked that 16 entries span less
+  // than 2 GiB.)
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t run_rsrc(const char* pool, const AttnArgs& a, int32_t page,
+                                                                    int hk, int t0) {
+    const int64_t off = (int64_t)page * a.c.s_page + (int64_t)hk * a.c.s_head +
+                        (int64_t)(t0 & ((1 << a.c.page_log2) - 1)) * a.c.s_entry;
+    return uniform_rsrc(pool + off * 16, (int)(15 * a.c.s_entry * 16) + D * E::kBytes);
+  }
+  __device__ __forceinline__ void load_k(const AttnArgs& a, const int32_t* page, int hk, int t0, int lane) {
+    const int voff = ((lane & 15) * (int)a.c.s_entry + (lane >> 4)) * 16;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const __amdgpu_buffer_rsrc_t rs = run_rsrc(a.c.k, a, page[s], hk, t0 + 16 * s);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) load_bytes<16>(rs, voff + 64 * c, 0, kf[s][c]);
+    }
+  }
+  __device__ __forceinline__ void load_v(const AttnArgs& a, const int32_t* page, int hk, int t0, int lane) {
+    const int voff = 4 * (lane >> 4) * (int)a.c.s_entry * 16 + (lane & 15) * VB;
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const __amdgpu_buffer_rsrc_t rs = run_rsrc(a.c.v, a, page[s], hk, t0 + 16 * s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_bytes<VB>(rs, voff, i * (int)a.c.s_entry * 16, vf[4 * s + i]);
+    }
+  }
+
+  // scores of the tile, s[t][sub]
+  __device__ __forceinline__ void scores(f32x4_t (&s)[RT][SUBS]) const {
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) {
+        s[t][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const uint4 k = make_uint4(kf[u][c][0], kf[u][c][1], kf[u][c][2], kf[u][c][3]);
+          if constexpr (E::kBytes == 2) {
+            s[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k),
+                                                              __builtin_bit_cast(bf16x8_t, qf[t][c]), s[t][u], 0, 0, 0);
+          } else {
+            const uint32_t kw[4] = {k.x, k.y, k.z, k.w};
+            const uint32_t qw[4] = {qf[t][c].x, qf[t][c].y, qf[t][c].z, qf[t][c].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              s[t][u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[j]), __uint_as_float(qw[j]), s[t][u], 0,
+                                                             0, 0);
+          }
+        }
+      }
+  }
+
+  // Product m's operand from pieces of V (w[entry][word])
+  __device__ __forceinline__ static uint4 v_pairs(const uint32_t (&w)[SUBS * 4][VW], int mm) {
+    uint32_t x[4];
+    const uint32_t sel = (mm & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) x[p] = __builtin_amdgcn_perm(w[2 * p + 1][mm >> 1], w[2 * p][mm >> 1], sel);
+    return make_uint4(x[0], x[1], x[2], x[3]);
+  }
+  // acc + sum over the tile's entries of w's element m times the weights p
+  __device__ __forceinline__ static f32x4_t v_product(const uint32_t (&w)[SUBS * 4][VW], int mm,
+                                                      const f32x4_t (&p)[SUBS], uint4 pb, f32x4_t c) {
+    if constexpr (E::kBytes == 2) {
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v_pairs(w, mm)),
+                                                     __builtin_bit_cast(bf16x8_t, pb), c, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i][mm]), p[0][i], c, 0, 0, 0);
+      return c;
+    }
+  }
+  __device__ __forceinline__ static uint4 pack_weights(const f32x4_t (&p)[SUBS]) {
+    if constexpr (E::kBytes == 2) {
+      bf16x8_t b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        b[i] = static_cast<__bf16>(p[0][i]);
+        b[4 + i] = static_cast<__bf16>(p[SUBS - 1][i]);
+      }
+      return __builtin_bit_cast(uint4, b);
+    } else {
+      return make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+
+  // Tiles in which not every row sees every entry: `see[t]` has the nodes that the lane's
+  // row sees, `first` the node of the tile's entry 0 (below 0: context, which every row
+  // sees); runs without a page and entries past the last node are seen by none.
+  __device__ __forceinline__ void mask(f32x4_t (&s)[RT][SUBS], const unsigned long long (&see)[RT], int first, int n,
+                                       const bool (&page)[SUBS], int lane) {
+    const int g4 = 4 * (lane >> 4);
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int node = first + 16 * u + g4 + i;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const bool in = page[u] && node < n && (node < 0 || ((see[t] >> (node & 63)) & 1));
+          s[t][u][i] = in ? s[t][u][i] : -INFINITY;
+        }
+        // what no row sees is not used, whatever it holds
+        if (!page[u] || node >= n) {
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vf[4 * u + i][w] = 0;
+        }
+      }
+  }
+
+  // Infinities and NaN among the values of nodes: a row that does not see the node must
+  // not take part in them, which 0 x inf would. They are taken out here (true where there
+  // were any), and added to the rows that see them when the block's sums are joined.
+  __device__ __forceinline__ bool take_out_odd(int first, int lane) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < SUBS * 4; ++e) {
+      const bool node = first + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3) >= 0;  // (all rows see the context)
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+        const uint32_t x = node ? finite_word<E>(vf[e][w]) : vf[e][w];
+        odd = odd || x != vf[e][w];
+        vf[e][w] = x;
+      }
+    }
+    return odd;
+  }
+};
+
+template <typename E>
+__device__ __forceinline__ void store_out(void* out, int64_t i, float4 v) {
+  if constexpr (E::kBytes == 2) {
+    uint2 r;
+    r.x = (uint32_t)to_storage<Bf16>(v.x) | ((uint32_t)to_storage<Bf16>(v.y) << 16);
+    r.y = (uint32_t)to_storage<Bf16>(v.z) | ((uint32_t)to_storage<Bf16>(v.w) << 16);
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i) = r;
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + i) = v;
+  }
+}
+
+// Entries that sequence b has in all: context and nodes; 0 for one that takes no part.
+__device__ __forceinline__ int entries(const AttnArgs& a, int64_t b) {
+  const int32_t len = a.c.lengths[b];
+  return len < 0 || len > 0x7fffffff - a.n ? 0 : len + a.n;
+}
+
+// Adds the infinities and NaN among elements d .. d + 3 of the values of the nodes `see`
+// whose entries lie in [t_begin, t_end).
+template <typename E>
+__device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d, unsigned long long see, int t_begin,
+                                     int t_end, int ctx, float4& v) {
+  for (int j = 0; j < a.n; ++j) {
+    const int t = ctx + j;
+    const int64_t pg = t >> a.c.page_log2;
+    if (!((see >> j) & 1) || t < t_begin || t >= t_end || pg >= a.c.table_pages) continue;
+    const int32_t id = a.c.table[(int64_t)b * a.c.table_ld + pg];
+    if (id < 0 || id >= a.c.pages) continue;
+    const char* p = a.c.v + ((int64_t)id * a.c.s_page + (int64_t)hk * a.c.s_head +
+                             (int64_t)(t & ((1 << a.c.page_log2) - 1)) * a.c.s_entry) * 16;
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const typename E::storage e = reinterpret_cast<const typename E::storage*>(p)[d + i];
+      uint32_t bits;
+      if constexpr (E::kBytes == 2)
+        bits = (uint32_t)e << 16;
+      else
+        bits = __float_as_uint(e);
+      x[i] = (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.f;
+    }
+    v.x += x[0];
+    v.y += x[1];
+    v.z += x[2];
+    v.w += x[3];
+  }
+}
+
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(kAttnThreads) void tree_attention_kernel(AttnArgs a) {
+  using A = Attn<E, D, RT>;
+  constexpr int SUBS = A::SUBS;
+  constexpr int ROWS = A::ROWS;
+  __shared__ __attribute__((aligned(16))) float o_sh[kAttnWaves][16][A::LD];
+  __shared__ float m_sh[kAttnWaves][ROWS];
+  __shared__ float l_sh[kAttnWaves][ROWS];
+  __shared__ unsigned long long see_sh[64];
+  __shared__ int32_t parent_sh[64];
+  __shared__ int odd_sh;  // some node's values were infinite or NaN
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int x = xcd_remap(blockIdx.x, gridDim.x);
+  const int rt = x % a.n_rt;
+  x /= a.n_rt;
+  const int sp = x % a.splits;
+  x /= a.splits;
+  const int hk = x % a.c.kv_heads;
+  const int b = x / a.c.kv_heads;
+
+  const int total = entries(a, b);
+  const int ctx = total - a.n;
+  const int t_begin = (int)((int64_t)sp * a.part < total ? sp * a.part : total);
+  const int t_end = total - t_begin > a.part ? t_begin + a.part : total;
+  if (sp > 0 && t_begin >= total) return;
+  const bool alone = total <= a.part;  // the sequence has one part
+
+  if (tid == 0) odd_sh = 0;
+  if (tid < a.n) parent_sh[tid] = a.parents ? a.parents[(int64_t)b * a.n + tid] : tid - 1;
+  __syncthreads();
+  if (tid < a.n) see_sh[tid] = ancestors(parent_sh, tid, a.n);
+  __syncthreads();
+
+  A w;
+  unsigned long long see[RT];
+  const int row0 = rt * ROWS;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = row0 + 16 * t + (lane & 15);
+    const bool in = r < a.rows && total > 0;
+    const int node = in ? r / a.group : 0;
+    const int h = hk * a.group + (in ? r - node * a.group : 0);
+    see[t] = in ? see_sh[node] : 0;
+    const char* q = a.q + ((int64_t)b * a.q_batch + (int64_t)node * a.q_node + (int64_t)h * a.q_head) * 16;
+#pragma unroll
+    for (int c = 0; c < A::KC; ++c) {
+      w.qf[t][c] = make_uint4(0u, 0u, 0u, 0u);
+      if (in) w.qf[t][c] = *reinterpret_cast<const uint4*>(q + 64 * c + 16 * (lane >> 4));
+    }
+    w.m[t] = -INFINITY;
+    w.l[t] = 0.f;
+#pragma unroll
+    for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // pages of a tile's runs of 16 entries; without one, page 0's bytes are read and not used
+  const int32_t* table = a.c.table + (int64_t)b * a.c.table_ld;
+  auto pages_of = [&](int t0, int32_t (&id)[SUBS], bool (&ok)[SUBS]) {
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const int64_t pg = (t0 + 16 * s) >> a.c.page_log2;
+      ok[s] = t0 + 16 * s < total && pg < a.c.table_pages;
+      const int32_t p = __builtin_amdgcn_readfirstlane(ok[s] ? table[pg] : -1);
+      ok[s] = p >= 0 && p < a.c.pages;
+      id[s] = ok[s] ? p : 0;
+    }
+  };
+
+  int t0 = t_begin + wave * A::KT;
+  int32_t id[SUBS];
+  bool ok[SUBS];
+  if (t0 < t_end) {
+    pages_of(t0, id, ok);
+    w.load_k(a, id, hk, t0, lane);
+    w.load_v(a, id, hk, t0, lane);
+  }
+  for (; t0 < t_end; t0 += kAttnWaves * A::KT) {
+    const int tn = t0 + kAttnWaves * A::KT;
+    int32_t id_n[SUBS];
+    bool ok_n[SUBS];
+    if (tn < t_end) pages_of(tn, id_n, ok_n);
+    f32x4_t s[RT][SUBS];
+    w.scores(s);
+    if (tn < t_end) w.load_k(a, id_n, hk, tn, lane);
+    bool whole = t0 + A::KT <= ctx;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) whole = whole && ok[u];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) s[t][u] *= a.scale;
+    if (!whole) {
+      w.mask(s, see, t0 - ctx, a.n, ok, lane);
+      if (w.take_out_odd(t0 - ctx, lane)) odd_sh = 1;
+    }
+    // (a NaN score passes neither test and makes its row NaN)
+    float top[RT];
+    bool grow = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      top[t] = s[t][0][0];
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][u][i]);
+      grow = grow || top[t] > w.m[t] + kMaxSlack;
+    }
+    if (__ballot(grow) != 0) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(w.m[t], mx);
+        const float f = w.m[t] == mn ? 1.f : fast_exp2(w.m[t] - mn);
+        w.m[t] = mn;
+        w.l[t] *= f;
+#pragma unroll
+        for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] *= f;
+      }
+    }
+    uint4 pb[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float ref = w.m[t] == -INFINITY ? 0.f : w.m[t];
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[t][u][i] = fast_exp2(s[t][u][i] - ref);
+          w.l[t] += s[t][u][i];
+        }
+      // bf16 weights, as the values are: up to 2^-8 of each, in both directions
+      pb[t] = A::pack_weights(s[t]);
+    }
+#pragma unroll
+    for (int mm = 0; mm < A::DE; ++mm)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) w.acc[t][mm] = A::v_product(w.vf, mm, s[t], pb[t], w.acc[t][mm]);
+    if (tn < t_end) w.load_v(a, id_n, hk, tn, lane);
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+      id[u] = id_n[u];
+      ok[u] = ok_n[u];
+    }
+  }
+
+  // the four waves' sums, relative to the largest of their maxima
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float l = w.l[t];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (lane < 16) {
+      m_sh[wave][16 * t + lane] = w.m[t];
+      l_sh[wave][16 * t + lane] = l;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = 16 * t + (lane & 15);
+    float m = m_sh[0][r];
+#pragma unroll
+    for (int i = 1; i < kAttnWaves; ++i) m = fmaxf(m, m_sh[i][r]);
+    const float f = w.m[t] == m ? 1.f : fast_exp2(w.m[t] - m);
+    if (t > 0) __syncthreads();  // the last tile's rows have been read
+    float* o = &o_sh[wave][lane & 15][4 * A::DE * (lane >> 4)];
+#pragma unroll
+    for (int j = 0; j < 4 * A::DE; j += 4)
+      *reinterpret_cast<float4*>(o + j) =
+          make_float4(w.acc[t][j % A::DE][j / A::DE] * f, w.acc[t][(j + 1) % A::DE][(j + 1) / A::DE] * f,
+                      w.acc[t][(j + 2) % A::DE][(j + 2) / A::DE] * f, w.acc[t][(j + 3) % A::DE][(j + 3) / A::DE] * f);
+    __syncthreads();
+    for (int i = tid; i < 16 * (D / 4); i += kAttnThreads) {
+      const int rl = i / (D / 4);
+      const int d = 4 * (i % (D / 4));
+      const int r2 = 16 * t + rl;
+      if (row0 + r2 >= a.rows) continue;
+      float mm = m_sh[0][r2];
+#pragma unroll
+      for (int k = 1; k < kAttnWaves; ++k) mm = fmaxf(mm, m_sh[k][r2]);
+      float l = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAttnWaves; ++k) {
+        l += l_sh[k][r2] * (m_sh[k][r2] == mm ? 1.f : fast_exp2(m_sh[k][r2] - mm));
+        const float4 p = *reinterpret_cast<const float4*>(&o_sh[k][rl][d]);
+        v.x += p.x;
+        v.y += p.y;
+        v.z += p.z;
+        v.w += p.w;
+      }
+      const int node = (row0 + r2) / a.group;
+      if (odd_sh) add_odd<E>(a, b, hk, d, see_sh[node], t_begin, t_end, ctx, v);
+      if (alone) {
+        const bool none = total == 0 || see_sh[node] == 0 || l == 0.f;
+        const float inv = none ? 0.f : 1.f / l;
+        const int h = hk * a.group + (row0 + r2) - node * a.group;
+        const float4 o4 = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        store_out<E>(a.out, (((int64_t)b * a.n + node) * a.heads + h) * D + d, o4);
+      } else {
+        const int64_t rec = ((((int64_t)b * a.c.kv_heads + hk) * a.n_rt + rt) * a.splits + sp) * ROWS + r2;
+        *reinterpret_cast<float4*>(a.acc + rec * D + d) = v;
+        if (d == 0) {
+          // (a node that is not there: no weight in any part)
+          *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mm, see_sh[node] == 0 ? 0.f : l);
+        }
+      }
+    }
+  }
+}
+
+// Joins the parts of a sequence that has several: a thread per four elements of a row.
+template <typename E>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D, int tile_rows) {
+  const int64_t per = (int64_t)a.n * a.heads * (D / 4);
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t b = i / per;
+  if (b >= a.c.batch) return;
+  const int total = entries(a, b);
+  if (total <= a.part) return;
+  const int in = (int)(i - b * per);
+  const int d = 4 * (in % (D / 4));
+  const int nh = in / (D / 4);
+  const int node = nh / a.heads;
+  const int h = nh - node * a.heads;
+  const int hk = h / a.group;
+  const int r = node * a.group + (h - hk * a.group);
+  // (entries past the table's row are in no part)
+  const int all = (int)(((int64_t)total + a.part - 1) / a.part);
+  const int parts = all < a.splits ? all : a.splits;
+  const int64_t rec = (((b * a.c.kv_heads + hk) * a.n_rt + r / tile_rows) * a.splits) * tile_rows + r % tile_rows;
+  float m = -INFINITY;
+  for (int s = 0; s < parts; ++s) {
+    const float2 ml = *reinterpret_cast<const float2*>(a.ml + (rec + (int64_t)s * tile_rows) * 2);
+    m = fmaxf(m, ml.x);
+  }
+  float l = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < parts; ++s) {
+    const int64_t x = rec + (int64_t)s * tile_rows;
+    const float2 ml = *reinterpret_cast<const float2*>(a.ml + x * 2);
+    const float f = ml.x == m ? 1.f : fast_exp2(ml.x - m);
+    const float4 p = *reinterpret_cast<const float4*>(a.acc + x * D + d);
+    l += ml.y * f;
+    v.x += p.x * f;
+    v.y += p.y * f;
+    v.z += p.z * f;
+    v.w += p.w * f;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store_out<E>(a.out, ((b * a.n + node) * a.heads + h) * (int64_t)D + d,
+               l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+}
+
+constexpr int kWideRow = 256;    // bytes of a head up to which a tile has 64 rows
+constexpr int kMiddleRow = 768;  // and 32
+
+template <typename E, int D>
+hipError_t launch_attn_d(const AttnArgs& a, int64_t blocks, hipStream_t stream) {
+  const dim3 grid((unsigned)blocks);
+  switch (attn_tile_rows(a.rows, D * E::kBytes)) {
+    case 16: hipLaunchKernelGGL((tree_attention_kernel<E, D, 1>), grid, dim3(kAttnThreads), 0, stream, a); break;
+    case 32:
+      if constexpr (D * E::kBytes <= kMiddleRow) {
+        hipLaunchKernelGGL((tree_attention_kernel<E, D, 2>), grid, dim3(kAttnThreads), 0, stream, a);
+        break;
+      }
+    case 64:
+      if constexpr (D * E::kBytes <= kWideRow) {
+        hipLaunchKernelGGL((tree_attention_kernel<E, D, 4>), grid, dim3(kAttnThreads), 0, stream, a);
+        break;
+      }
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_attn(const AttnArgs& a, int D, int64_t blocks, hipStream_t stream) {
+  switch (D) {
+    case 32: return launch_attn_d<E, 32>(a, blocks, stream);
+    case 64: return launch_attn_d<E, 64>(a, blocks, stream);
+    case 96: return launch_attn_d<E, 96>(a, blocks, stream);
+    case 128: return launch_attn_d<E, 128>(a, blocks, stream);
+    case 192: return launch_attn_d<E, 192>(a, blocks, stream);
+    case 256: return launch_attn_d<E, 256>(a, blocks, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+// Rows of a tile. Its queries and sums lie in registers, 512 of a lane, beside the
+// entries in flight.
+int attn_tile_rows(int32_t rows, int32_t head_bytes) {
+  const int most = head_bytes <= kWideRow ? 64 : head_bytes <= kMiddleRow ? 32 : 16;
+  return rows <= 16 ? 16 : rows <= 32 && most > 32 ? 32 : most;
+}
+
+hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream) {
+  const int64_t blocks = a.c.batch * a.c.kv_heads * a.n_rt * a.splits;
+  hipError_t e = f32 ? launch_attn<F32>(a, D, blocks, stream) : launch_attn<Bf16>(a, D, blocks, stream);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t threads = a.c.batch * a.n * a.heads * (D / 4);
+  const dim3 grid((unsigned)((threads + 255) / 256));
+  const int tile = attn_tile_rows(a.rows, D * (f32 ? 4 : 2));
+  if (f32)
+    hipLaunchKernelGGL(attn_join_kernel<F32>, grid, dim3(256), 0, stream, a, (int)D, tile);
+  else
+    hipLaunchKernelGGL(attn_join_kernel<Bf16>, grid, dim3(256), 0, stream, a, (int)D, tile);
+  return hipGetLastError();
+}
+
+}  // namespace mls

@@ -1,0 +1,131 @@
+// Entries of a paged key-value cache: writing a step's drafted tokens or a prompt, and
+// moving an accepted path's entries together (paper section 2, paragraph "Speculative
+// Decoding": the verifier reuses the draft's cache, and drafted entries that are not
+// accepted leave it).
+//
+// Both only move bytes, 16 at a time: an entry's head is 64 to 512 contiguous bytes on
+// either side, so every access covers whole lines. Page numbers and positions from the
+// device are checked against the pool before they become addresses.
+#include "mls_device.h"
+#include "mls_launch.h"
+
+namespace mls {
+
+namespace {
+
+constexpr int kCacheThreads = 256;
+constexpr int kWriteUnroll = 4;  // chunks of a thread, of the keys and of the values each
+constexpr int kMoveBatch = 8;    // entries loaded before the first of them is stored
+
+// Chunk offset of entry `t` (head 0, layer 0) of sequence b in the pool; -1 where the
+// table has no such page.
+__device__ __forceinline__ int64_t entry_at(const CacheArgs& c, int64_t b, int64_t t) {
+  const int64_t pg = t >> c.page_log2;
+  if (t < 0 || pg >= c.table_pages) return -1;
+  const int32_t id = c.table[b * c.table_ld + pg];
+  if (id < 0 || id >= c.pages) return -1;
+  return id * c.s_page + (t & ((1 << c.page_log2) - 1)) * c.s_entry;
+}
+
+// Bound by its bytes: one read and one write of each. Thread order is (entry, head,
+// chunk), so that a wave reads 1 KB of contiguous rows and writes whole heads.
+__global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheWriteArgs a) {
+  const int64_t b = blockIdx.y;
+  const int32_t len = a.c.lengths[b];
+  int32_t n = a.counts ? a.counts[b] : a.n;
+  n = n < a.n ? n : a.n;
+  if (len < 0 || n <= 0) return;
+  const uint32_t per = (uint32_t)a.c.kv_heads * (uint32_t)a.c.chunks;
+  const uint32_t total = (uint32_t)n * per;
+  const uint32_t first = blockIdx.x * (uint32_t)(kCacheThreads * kWriteUnroll) + threadIdx.x;
+  uint4 rk[kWriteUnroll], rv[kWriteUnroll];
+  int64_t to[kWriteUnroll];
+#pragma unroll
+  for (int u = 0; u < kWriteUnroll; ++u) {
+    const uint32_t x = first + u * kCacheThreads;
+    to[u] = -1;
+    if (x >= total) continue;
+    const uint32_t i = x / per;
+    const uint32_t hc = x - i * per;
+    const uint32_t h = hc / (uint32_t)a.c.chunks;
+    const uint32_t ch = hc - h * a.c.chunks;
+    const int64_t e = entry_at(a.c, b, (int64_t)len + i);
+    if (e < 0) continue;
+    to[u] = (e + h * a.c.s_head + ch) * 16;
+    const int64_t from = (b * a.s_batch + i * a.s_node + h * a.s_head + ch) * 16;
+    rk[u] = *reinterpret_cast<const uint4*>(a.k + from);
+    rv[u] = *reinterpret_cast<const uint4*>(a.v + from);
+  }
+#pragma unroll
+  for (int u = 0; u < kWriteUnroll; ++u) {
+    if (to[u] < 0) continue;
+    *reinterpret_cast<uint4*>(a.c.k + to[u]) = rk[u];
+    *reinterpret_cast<uint4*>(a.c.v + to[u]) = rv[u];
+  }
+}
+
+// Entry len + j takes what entry len + path[j] held, for j = 0 .. n_accepted. A thread
+// owns one chunk of one head for all j and goes through them in order, a batch of loads
+// before its stores: with path[j] >= j (nodes come after their ancestors) no entry is
+// overwritten before it has been read, and nothing needs a second buffer or a barrier.
+__global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompactArgs a) {
+  const int64_t b = blockIdx.y;
+  const int32_t len = a.c.lengths[b];
+  int32_t acc = a.n_accepted[b];
+  acc = acc < a.n ? acc : a.n - 1;
+  const bool idle = len < 0 || acc < 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.new_lengths[b] = idle ? len : len + acc + 1;
+  if (idle) return;
+  const uint32_t per = (uint32_t)a.c.kv_heads * (uint32_t)a.c.chunks;
+  const uint32_t x = blockIdx.x * (uint32_t)kCacheThreads + threadIdx.x;
+  const uint32_t layer = x / per;
+  if (layer >= (uint32_t)a.c.layers) return;
+  const uint32_t hc = x - layer * per;
+  const uint32_t h = hc / (uint32_t)a.c.chunks;
+  const int64_t off = layer * a.c.s_layer + h * a.c.s_head + (hc - h * a.c.chunks);
+  const int32_t* path = a.path + b * a.n;
+  for (int j0 = 0; j0 <= acc; j0 += kMoveBatch) {
+    uint4 rk[kMoveBatch], rv[kMoveBatch];
+    int64_t to[kMoveBatch];
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      const int j = j0 + u;
+      to[u] = -1;
+      if (j > acc) continue;
+      const int32_t node = path[j];
+      if (node <= j || node >= a.n) continue;  // in place already, or no node of the tree
+      const int64_t src = entry_at(a.c, b, (int64_t)len + node);
+      const int64_t dst = entry_at(a.c, b, (int64_t)len + j);
+      if (src < 0 || dst < 0) continue;
+      to[u] = (dst + off) * 16;
+      rk[u] = *reinterpret_cast<const uint4*>(a.c.k + (src + off) * 16);
+      rv[u] = *reinterpret_cast<const uint4*>(a.c.v + (src + off) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      if (to[u] < 0) continue;
+      *reinterpret_cast<uint4*>(a.c.k + to[u]) = rk[u];
+      *reinterpret_cast<uint4*>(a.c.v + to[u]) = rv[u];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream) {
+  const int64_t total = (int64_t)a.n * a.c.kv_heads * a.c.chunks;
+  const int64_t per_block = kCacheThreads * kWriteUnroll;
+  hipLaunchKernelGGL(cache_write_kernel, dim3((unsigned)((total + per_block - 1) / per_block), (unsigned)a.c.batch),
+                     dim3(kCacheThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream) {
+  const int64_t total = (int64_t)a.c.layers * a.c.kv_heads * a.c.chunks;
+  hipLaunchKernelGGL(cache_compact_kernel,
+                     dim3((unsigned)((total + kCacheThreads - 1) / kCacheThreads), (unsigned)a.c.batch),
+                     dim3(kCacheThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace mls

@@ -140,7 +140,7 @@ __device__ __forceinline__ uint2 lds_read_tr8(const char* p) {
 }
 
 template <int BM, int BN, int WGM, int WGN, int STAGES, int RB = 128, int ALAY = kLayoutKC,
-          int BLAY = kLayoutKC, bool KTAIL = false>
+          int BLAY = kLayoutKC, bool KTAIL = false, typename ET = Bf16>
 struct WideMma {
   static constexpr int kBM = BM;
   static constexpr int kBN = BN;
@@ -153,8 +153,8 @@ struct WideMma {
   static constexpr int FM = WTM / 32;
   static constexpr int FN = WTN / 32;
   static constexpr int CPR = RB / 16;     // 16-byte chunks per LDS row (KC layout)
-  static constexpr int KSTEPS = RB / 32;  // MFMA K-steps (16 bf16) per K-tile
-  static constexpr int BK = RB / 2;       // K values per K-tile
+  static constexpr int KSTEPS = RB / 32;  // MFMA K-steps (16 bf16, 32 int8) per K-tile
+  static constexpr int BK = RB / ET::kBytes;  // K values per K-tile
   static constexpr int kStageBytes = (BM + BN) * RB;
   static constexpr int kSmemBytes = STAGES * kStageBytes;
   static constexpr int LA = BM * CPR / NT;  // load instructions per thread per K-tile, A
@@ -166,8 +166,10 @@ struct WideMma {
   static_assert(kLoadsPerTile * (STAGES - 1) < 64, "vmcnt range");
   static_assert(!KTAIL || (RB == 128 && ALAY == kLayoutKC && BLAY == kLayoutKC),
                 "K tails: K-contiguous operands");
+  static_assert(ET::kBytes == 2 || (ALAY == kLayoutKC && BLAY == kLayoutKC), "MC fragments are of 16-bit values");
+  typedef typename AccOf<ET>::type acc_t;
 
-  f32x16_t acc[FM][FN];
+  acc_t acc[FM][FN];
 
   __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -175,7 +177,7 @@ struct WideMma {
 #pragma unroll
       for (int fn = 0; fn < FN; ++fn)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[fm][fn][r] = 0.0f;
+        for (int r = 0; r < 16; ++r) acc[fm][fn][r] = 0;
   }
 
   // Per-lane byte offsets (inside the operand panel) of the L chunks this lane
@@ -315,7 +317,7 @@ struct WideMma {
 #pragma unroll
       for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
-        for (int fn = 0; fn < FN; ++fn) mma_step<Bf16>(acc[fm][fn], a[kk & 1][fm], b[kk & 1][fn]);
+        for (int fn = 0; fn < FN; ++fn) mma_step<ET>(acc[fm][fn], a[kk & 1][fm], b[kk & 1][fn]);
       if (kk < KSTEPS - 1) {
 #pragma unroll
         for (int q = 0; q < kReads; ++q) {
@@ -327,7 +329,7 @@ struct WideMma {
     }
   }
 
-  // acc = A[a_row0 : +BM, :K] * B[b_row0 : +BN, :K]^T with K = kbytes / 2, both
+  // acc = A[a_row0 : +BM, :K] * B[b_row0 : +BN, :K]^T with K the kbytes bytes' values, both
   // operands K-contiguous; a_rows / b_rows: rows of the stored operand matrix
   // (rows beyond it read as zero).
   // On return every wave has passed a barrier after its last LDS read, so the
@@ -412,7 +414,7 @@ struct WideMma {
     static_assert(kMfma >= kFrags && kMfma >= kLoadsPerTile, "a slot for every read and load");
 #pragma unroll
     for (int m = 0; m < kMfma; ++m) {
-      mma_step<Bf16>(acc[m / FN][m % FN], a[m / FN], b[m % FN]);
+      mma_step<ET>(acc[m / FN][m % FN], a[m / FN], b[m % FN]);
       if (m < kFrags) rd(m < FN ? FM + m : m - FN);  // B's first: the next K-step's first MFMAs need all of them
       if (m >= kMfma - kLoadsPerTile) ld(m - (kMfma - kLoadsPerTile));
       __builtin_amdgcn_sched_barrier(0);

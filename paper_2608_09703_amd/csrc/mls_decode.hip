@@ -89,8 +89,8 @@ __global__ __launch_bounds__(Mma::NT, Mma::kBM == 64 ? 1 : 2) void head_logits_k
 #pragma unroll
           for (int rg = 0; rg < 4; ++rg) {
             const int v0 = Mma::row_of(wm, fm, rg * 4, lane);  // multiple of 4
-            const float4 w = make_float4(mma.acc[fm][fn][rg * 4], mma.acc[fm][fn][rg * 4 + 1],
-                                         mma.acc[fm][fn][rg * 4 + 2], mma.acc[fm][fn][rg * 4 + 3]);
+            const float4 w = make_float4((float)mma.acc[fm][fn][rg * 4], (float)mma.acc[fm][fn][rg * 4 + 1],
+                                         (float)mma.acc[fm][fn][rg * 4 + 2], (float)mma.acc[fm][fn][rg * 4 + 3]);
             *reinterpret_cast<float4*>(st + t * BM + (((v0 >> 2) ^ (t & (kSw - 1))) << 2)) = w;
           }
       }
@@ -102,7 +102,14 @@ __global__ __launch_bounds__(Mma::NT, Mma::kBM == 64 ? 1 : 2) void head_logits_k
       const int64_t tg = tbase + ps * kTok + t;
       const int64_t v = vbase + 4 * c;
       if (tg >= a.T || v >= a.V) continue;
-      const float4 w = *reinterpret_cast<const float4*>(st + t * BM + ((c ^ (t & (kSw - 1))) << 2));
+      float4 w = *reinterpret_cast<const float4*>(st + t * BM + ((c ^ (t & (kSw - 1))) << 2));
+      if constexpr (E::kBytes == 1) {
+        const float so = a.o_scale[tg];
+        w.x = w.x * so * a.W_scale[v];
+        w.y = w.y * so * a.W_scale[v + 1 < a.V ? v + 1 : v];
+        w.z = w.z * so * a.W_scale[v + 2 < a.V ? v + 2 : v];
+        w.w = w.w * so * a.W_scale[v + 3 < a.V ? v + 3 : v];
+      }
       float* out = a.logits + tg * a.V + v;
       if (vec) {
         // whole lines, non-temporal (decode step 0.74 -> 0.72 ms: draft heads
@@ -1110,6 +1117,9 @@ using HeadSomeTail = WideMma<64, 64, 2, 2, 3, 128, kLayoutKC, kLayoutKC, true>;
 using HeadWideTail = WideMma<128, 128, 2, 2, 2, 128, kLayoutKC, kLayoutKC, true>;
 using HeadWide192Tail = WideMma<192, 128, 2, 2, 2, 128, kLayoutKC, kLayoutKC, true>;
 using HeadGenF32 = TileMma<F32, 128, 128, 2, 2>;
+// 8-bit operands: the same tiles, with twice the K values in a K-tile
+template <int BM, int BN, int WGM, int WGN, int STAGES, bool KTAIL>
+using HeadI8 = WideMma<BM, BN, WGM, WGN, STAGES, 128, kLayoutKC, kLayoutKC, KTAIL, I8>;
 
 }  // namespace
 
@@ -1160,6 +1170,27 @@ hipError_t launch_head_logits(const HeadArgs& a, bool f32, hipStream_t stream) {
     tail ? launch_head_t<HeadWide192Tail, Bf16>(a, stream) : launch_head_t<HeadWide192, Bf16>(a, stream);
   else
     tail ? launch_head_t<HeadWideTail, Bf16>(a, stream) : launch_head_t<HeadWide, Bf16>(a, stream);
+  return hipGetLastError();
+}
+
+void head_i8_tile(int64_t T, int64_t V, int* rows, int* cols) { head_tile(true, T, V, rows, cols); }
+
+hipError_t launch_head_logits_i8(const HeadArgs& a, hipStream_t stream) {
+  int rows, cols;
+  head_i8_tile(a.T, a.V, &rows, &cols);
+  if (a.n_vt != (int)((a.V + rows - 1) / rows) || a.n_tt != (int)((a.T + cols - 1) / cols))
+    return hipErrorInvalidValue;
+  const bool tail = a.d % 128 != 0;
+  if (cols == 32)
+    tail ? launch_head_t<HeadI8<64, 32, 2, 1, 4, true>, I8>(a, stream) : launch_head_t<HeadI8<64, 32, 2, 1, 4, false>, I8>(a, stream);
+  else if (cols == 64)
+    tail ? launch_head_t<HeadI8<64, 64, 2, 2, 3, true>, I8>(a, stream) : launch_head_t<HeadI8<64, 64, 2, 2, 3, false>, I8>(a, stream);
+  else if (rows == 64)
+    tail ? launch_head_t<HeadI8<64, 128, 2, 2, 3, true>, I8>(a, stream) : launch_head_t<HeadI8<64, 128, 2, 2, 3, false>, I8>(a, stream);
+  else if (rows == 192)
+    tail ? launch_head_t<HeadI8<192, 128, 2, 2, 2, true>, I8>(a, stream) : launch_head_t<HeadI8<192, 128, 2, 2, 2, false>, I8>(a, stream);
+  else
+    tail ? launch_head_t<HeadI8<128, 128, 2, 2, 2, true>, I8>(a, stream) : launch_head_t<HeadI8<128, 128, 2, 2, 2, false>, I8>(a, stream);
   return hipGetLastError();
 }
 

@@ -30,6 +30,8 @@ namespace mls {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;   // 4 waves of 64
 constexpr int kRowBytes = 128;  // bytes of K per LDS tile row
@@ -44,8 +46,24 @@ struct F32 {
   static constexpr int kBytes = 4;
 };
 
+// 8-bit integers, summed in 32 bits (v_mfma_i32_32x32x32_i8: twice the K values of
+// bf16 in the same bytes, operands and results laid out alike)
+struct I8 {
+  typedef int8_t storage;
+  static constexpr int kBytes = 1;
+};
+
 template <typename E>
-__device__ __forceinline__ void mma_step(f32x16_t& acc, uint4 a, uint4 b);
+struct AccOf {
+  typedef f32x16_t type;
+};
+template <>
+struct AccOf<I8> {
+  typedef i32x16_t type;
+};
+
+template <typename E>
+__device__ __forceinline__ void mma_step(typename AccOf<E>::type& acc, uint4 a, uint4 b);
 
 template <>
 __device__ __forceinline__ void mma_step<Bf16>(f32x16_t& acc, uint4 a, uint4 b) {
@@ -59,6 +77,12 @@ __device__ __forceinline__ void mma_step<F32>(f32x16_t& acc, uint4 a, uint4 b) {
   acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
   acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
   acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+}
+
+template <>
+__device__ __forceinline__ void mma_step<I8>(i32x16_t& acc, uint4 a, uint4 b) {
+  acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), acc, 0,
+                                              0, 0);
 }
 
 // Position of 16-byte chunk c of LDS tile row `row`. Rows r..r+7 get distinct

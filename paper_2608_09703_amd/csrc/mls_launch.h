@@ -415,6 +415,9 @@ struct HeadArgs {
   int32_t n_tt;
   int32_t n_vt;
   int32_t group_v;
+  // 8-bit operands: what a row of o and a row of W stand for times these
+  const float* o_scale;  // [T]
+  const float* W_scale;  // [V]
 };
 // Parameters of one row's sampling distribution.
 struct RowDist {
@@ -461,6 +464,96 @@ struct VerifyArgs {
   const float* u_sample;       // [batch]
   int32_t* n_accepted;         // [batch]
   int32_t* next_token;         // [batch]
+};
+
+// Pages of cached keys and values: entry t of sequence b lies in page
+// table[b * table_ld + t / page], at position t % page; k and v are laid out alike, with
+// strides in 16-byte chunks.
+struct CacheArgs {
+  char* k;
+  char* v;
+  const int32_t* table;
+  const int32_t* lengths;  // [batch]; below 0: the sequence takes no part
+  int64_t batch;
+  int64_t pages;
+  int64_t table_pages;  // pages a row of the table names
+  int64_t table_ld;
+  int64_t s_layer;
+  int64_t s_page;
+  int64_t s_head;
+  int64_t s_entry;
+  int32_t layers;
+  int32_t kv_heads;
+  int32_t page_log2;
+  int32_t chunks;  // 16-byte chunks of an entry's head
+};
+struct CacheWriteArgs {
+  CacheArgs c;
+  const char* k;  // [batch][n][kv_heads][D], strides in 16-byte chunks
+  const char* v;
+  int64_t s_batch;
+  int64_t s_node;
+  int64_t s_head;
+  const int32_t* counts;  // [batch] or null: all n
+  int32_t n;
+};
+struct CacheCompactArgs {
+  CacheArgs c;
+  const int32_t* path;        // [batch][n]
+  const int32_t* n_accepted;  // [batch]
+  int32_t* new_lengths;       // [batch]
+  int32_t n;
+};
+// Attention from the nodes of a tree to cached entries.
+struct AttnArgs {
+  CacheArgs c;
+  const char* q;  // [batch][n][heads][D], strides in 16-byte chunks
+  int64_t q_batch;
+  int64_t q_node;
+  int64_t q_head;
+  void* out;               // [batch][n][heads][D]
+  const int32_t* parents;  // [batch][n] or null: a chain
+  float scale;             // of the scores, times log2 e
+  int32_t n;
+  int32_t heads;
+  int32_t group;   // query heads of a key head
+  int32_t rows;    // n * group: rows that read one key head
+  int32_t n_rt;    // row tiles
+  int32_t splits;  // parts of the entries
+  int32_t part;    // entries of a part
+  float* acc;      // [batch][kv_heads][n_rt][splits][tile rows][D] partial sums, if splits > 1
+  float* ml;       // and [..][tile rows][2]: their maximum and sum of weights
+};
+// Verification of a tree of drafted tokens.
+struct TreeVerifyArgs {
+  const float* target;      // [batch][n][V]
+  const float* draft;       // [batch][n][V] or null
+  const RowDist* tparams;   // [batch][n]
+  const RowDist* dparams;   // [batch][n] or null
+  const int32_t* tokens;    // [batch][n]
+  const int32_t* parents;   // [batch][n] or null: a chain
+  const float* u_accept;    // [batch][n]
+  const float* u_sample;    // [batch]
+  int32_t* n_accepted;      // [batch]
+  int32_t* path;            // [batch][n]
+  int32_t* next_token;      // [batch]
+  int64_t batch;
+  int32_t V;
+  int32_t n;
+  int32_t greedy;
+  float temperature;
+  float inv_temp;
+  float top_p;
+};
+// Rows as 8-bit integers.
+struct QuantArgs {
+  const void* x;  // [T] rows of d, ld apart
+  int8_t* q;      // [T][d]
+  float* scale;   // [T]
+  int64_t T;
+  int64_t ld;
+  int32_t d;
+  int32_t f32;
 };
 
 // MFMA ceiling probe (measurement aid).
@@ -523,6 +616,16 @@ hipError_t launch_head_logits(const HeadArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_sample(const SampleArgs& a, int ept, hipStream_t stream);
 hipError_t launch_row_params(const RowParamArgs& a, int ept, hipStream_t stream);
 hipError_t launch_verify(const VerifyArgs& a, int ept, hipStream_t stream);
+// 8-bit integers: d a multiple of 16
+void head_i8_tile(int64_t T, int64_t V, int* rows, int* cols);
+hipError_t launch_head_logits_i8(const HeadArgs& a, hipStream_t stream);
+hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t stream);
+hipError_t launch_tree_verify(const TreeVerifyArgs& a, hipStream_t stream);
+hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
+hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
+// rows of a tile of tree attention, which read an entry's head once
+int attn_tile_rows(int32_t rows, int32_t head_bytes);
+hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_finalize_rows(const RowArgs& a, hipStream_t stream);
 hipError_t launch_token_pack(const TokenArgs& a, hipStream_t stream);
