@@ -2325,7 +2325,7 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   return MLS_OK;
 }
 
-size_t tree_ws_bytes(int64_t batch, int64_t n) { return align256((size_t)(2 * batch * n) * sizeof(RowDist)); }
+size_t tree_ws_bytes(int64_t batch, int64_t n) { return align256(tree_ready_bytes(batch, n)); }
 
 mls_status validate_tree(int64_t batch, int64_t n) {
   if (batch < 1 || batch > (1 << 24) || n < 1 || n > kMaxNodes)
@@ -2491,7 +2491,7 @@ mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, cons
   if (!s->greedy && (!u_sample || (n > 1 && !u_accept)))
     return fail(MLS_INVALID_ARG, "sampling needs u_accept and u_sample");
   if (draft_params && !draft_logits) return fail(MLS_INVALID_ARG, "draft_params go with draft_logits");
-  if (!s->greedy && (!workspace || workspace_bytes < tree_ws_bytes(batch, n)))
+  if (!s->greedy && tree_ws_bytes(batch, n) && (!workspace || workspace_bytes < tree_ws_bytes(batch, n)))
     return fail(MLS_WORKSPACE_TOO_SMALL, "verification needs %zu workspace bytes, got %zu", tree_ws_bytes(batch, n),
                 workspace ? workspace_bytes : 0);
   if (!aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned workspace");
@@ -2501,33 +2501,12 @@ mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, cons
     if (!aligned(p, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
   hipStream_t hs = static_cast<hipStream_t>(stream);
   hipError_t e;
-  RowDist* params = static_cast<RowDist*>(workspace);
-  const float inv_temp = s->greedy ? 1.f : 1.f / s->temperature;
   const bool draft = !s->greedy && draft_logits && n > 1;
-  if (!s->greedy) {
-    // workspace: the draft rows' records [batch][n], then the verifier's
-    RowParamArgs r;
-    memset(&r, 0, sizeof(r));
-    r.rows0 = draft && !draft_params ? batch * n : 0;
-    r.rows1 = batch * n;
-    r.V = s->V;
-    r.inv_temp = inv_temp;
-    r.top_p = s->top_p;
-    r.logits0 = draft_logits;
-    r.logits1 = target_logits;
-    r.params = params + (batch * n - r.rows0);
-    {
-      ProfScope ps("row_params", hs);
-      e = launch_row_params(r, row_elems_per_thread(s->V), hs);
-    }
-    if (e != hipSuccess) return hip_fail(e, "row parameter launch");
-  }
   TreeVerifyArgs a;
   memset(&a, 0, sizeof(a));
   a.target = target_logits;
   a.draft = draft ? draft_logits : nullptr;
-  a.tparams = params + batch * n;
-  a.dparams = draft_params ? static_cast<const RowDist*>(draft_params) : params;
+  a.dparams = static_cast<const RowDist*>(draft_params);
   a.tokens = tokens;
   a.parents = parents;
   a.u_accept = u_accept;
@@ -2540,11 +2519,15 @@ mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, cons
   a.n = (int32_t)n;
   a.greedy = s->greedy ? 1 : 0;
   a.temperature = s->temperature;
-  a.inv_temp = inv_temp;
+  a.inv_temp = s->greedy ? 1.f : 1.f / s->temperature;
   a.top_p = s->top_p;
+  if (!s->greedy) {
+    a.ready = tree_ready_nodes(batch, n);
+    tree_ready_layout(a, workspace);
+  }
   {
     ProfScope ps("tree_verify", hs);
-    e = launch_tree_verify(a, hs);
+    e = launch_tree_verify(a, row_elems_per_thread(s->V), hs);
   }
   if (e != hipSuccess) return hip_fail(e, "tree verification launch");
   return MLS_OK;

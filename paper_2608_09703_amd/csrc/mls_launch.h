@@ -528,8 +528,7 @@ struct AttnArgs {
 struct TreeVerifyArgs {
   const float* target;      // [batch][n][V]
   const float* draft;       // [batch][n][V] or null
-  const RowDist* tparams;   // [batch][n]
-  const RowDist* dparams;   // [batch][n] or null
+  const RowDist* dparams;   // [batch][n] records of the draft's rows, or null
   const int32_t* tokens;    // [batch][n]
   const int32_t* parents;   // [batch][n] or null: a chain
   const float* u_accept;    // [batch][n]
@@ -544,6 +543,12 @@ struct TreeVerifyArgs {
   float temperature;
   float inv_temp;
   float top_p;
+  // rows of each tree's first `ready` nodes, opened before the walk: [2][batch][ready]
+  // (the verifier's, the draft's), and their lists
+  int32_t ready;
+  void* ready_rows;
+  double* list_p;
+  int32_t* list_idx;
 };
 // Rows as 8-bit integers.
 struct QuantArgs {
@@ -620,7 +625,10 @@ hipError_t launch_verify(const VerifyArgs& a, int ept, hipStream_t stream);
 void head_i8_tile(int64_t T, int64_t V, int* rows, int* cols);
 hipError_t launch_head_logits_i8(const HeadArgs& a, hipStream_t stream);
 hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t stream);
-hipError_t launch_tree_verify(const TreeVerifyArgs& a, hipStream_t stream);
+int tree_ready_nodes(int64_t batch, int64_t n);
+size_t tree_ready_bytes(int64_t batch, int64_t n);
+void tree_ready_layout(TreeVerifyArgs& a, void* workspace);
+hipError_t launch_tree_verify(const TreeVerifyArgs& a, int ept, hipStream_t stream);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
 // rows of a tile of tree attention, which read an entry's head once

@@ -16,126 +16,187 @@
 // Which tokens a distribution keeps (top_p) is in its row's record, in float32; the
 // probabilities of kept tokens, their differences and the draws are in 64 bits, so that a
 // token is decided by the numbers given and not by roundings along the way.
+//
+// A distribution that keeps up to kMaxCand tokens is opened once into a list, one token
+// to a thread, in index order: what becomes of p at that node, children turned down and
+// the draw, then takes place in registers and a few barriers, and reads q at the listed
+// tokens only. Opening a row is nearly all the time (its load, its threshold, a few
+// dependent steps on one CU), so the rows of each tree's first nodes are opened
+// beforehand, side by side, and left in the workspace (tree_rows_kernel); rows that the
+// walk reaches beyond them it opens itself. Larger distributions (top_p = 1, flat rows) are
+// walked over the whole row, from the logits.
 #include <math.h>
 
 #include "mls_device.h"
 #include "mls_launch.h"
+#include "mls_rowdist.h"
 #include "mls_wave.h"
 
 namespace mls {
 
 namespace {
 
-constexpr int kTreeThreads = 1024;
+constexpr int kTreeThreads = kRowThreads;
 constexpr int kTreeWaves = kTreeThreads / 64;
 constexpr int kMaxNodes = 64;
 constexpr int kMaxSlabs = 64;  // of kTreeThreads tokens: rows of up to 65,536
+static_assert(kMaxCand <= kTreeThreads, "a thread owns at most one token of a list");
+
+// An opened row in the workspace; its list is idx[kMaxCand], p[kMaxCand].
+struct TreeRow {
+  RowDist d;
+  int32_t n;    // tokens of its list; -1: none, the row keeps more
+  double norm;  // 1 / (sum of kept weights); 0: the row keeps no token
+};
+
+struct Row {
+  const float* logits;
+  RowDist d;
+  double norm;
+};
 
 struct TreeShared {
-  double red[kTreeWaves];
+  Row row[2];  // the present node's: the verifier's, the draft's
+  double red[2][kTreeWaves];
   double seg[kMaxSlabs * kTreeWaves];
-  float fval[kTreeWaves];
-  int ival[kTreeWaves];
+  double scale[kMaxNodes];
+  int32_t gone[kMaxNodes];
+  RowDist d;
   int pick;
   double before;
+  double at;
   int32_t token[kMaxNodes];
   int32_t parent[kMaxNodes];
   float u[kMaxNodes];
 };
 
-__device__ __forceinline__ double block_sum(double v, TreeShared& sh) {
+// (two buffers in turn: the next sum's writes do not meet this one's reads)
+__device__ __forceinline__ double block_sum(double v, TreeShared& ts, int& turn) {
   v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = v;
+  double* red = ts.red[turn];
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = 0.0;
 #pragma unroll
-  for (int i = 0; i < kTreeWaves; ++i) s += sh.red[i];
-  __syncthreads();
+  for (int i = 0; i < kTreeWaves; ++i) s += red[i];
   return s;
 }
 
-// One row's sampling distribution.
-struct Row {
-  const float* logits;
-  RowDist d;
-  double norm;  // 1 / (sum of kept weights); 0: the row keeps no token
-};
-
-// Whether the record keeps token v: by the float32 weight, formed as the record's was.
-__device__ __forceinline__ bool kept(const Row& r, float logit, int v, float inv_temp) {
-#pragma clang fp contract(off)
-  const float scaled = logit * inv_temp;
-  const float e = fast_exp2((scaled - r.d.m) * kLog2e);
-  return e > r.d.theta || (e == r.d.theta && e > 0.f && v <= r.d.tie_cut);
-}
-__device__ __forceinline__ double weight(const Row& r, float logit, double temperature) {
-  return exp((double)logit / temperature - (double)r.d.m);
+__device__ __forceinline__ double weight(const RowDist& d, float logit, double temperature) {
+  return exp((double)logit / temperature - (double)d.m);
 }
 __device__ __forceinline__ double prob(const Row& r, int v, const TreeVerifyArgs& a) {
   if (r.norm == 0.0) return 0.0;
   const float l = r.logits[v];
-  return kept(r, l, v, a.inv_temp) ? weight(r, l, (double)a.temperature) * r.norm : 0.0;
+  return kept_w(exp_weight(l, a.inv_temp, r.d), v, r.d) ? weight(r.d, l, (double)a.temperature) * r.norm : 0.0;
 }
 
-__device__ __forceinline__ Row open_row(const float* logits, const RowDist* d, const TreeVerifyArgs& a,
-                                        TreeShared& sh) {
-  Row r;
+// Opens a row (its record given, or found): its distribution, and where it keeps few
+// enough tokens thread i < the returned number owns list entry i (idx, p normalised; p is
+// 0 for an entry that is not kept). Returns -1 for larger ones. All threads call it.
+template <int EPT>
+__device__ __forceinline__ int open_row(const float* logits, const RowDist* rec, const TreeVerifyArgs& a,
+                                        RowShared& sh, TreeShared& ts, int& turn, Row& r, int& idx, double& p) {
+  __syncthreads();  // the list of the last row has been read
   r.logits = logits;
-  r.d = *d;
+  int n;
+  if (rec) {
+    r.d = *rec;
+    n = compact_kept<EPT>(logits, a.V, a.inv_temp, r.d, sh);
+  } else {
+    float e[EPT];
+    uint32_t lo = 0, hi = 0;
+    float P = 0.f;
+    n = row_dist<EPT>(logits, a.V, a.inv_temp, a.top_p, e, sh, r.d, lo, hi, P);
+    if (n >= 0) {
+      if (threadIdx.x < 64) {
+        list_finish(sh, n, lo, hi, P, a.V, -1.f, r.d);
+        if (threadIdx.x == 0) ts.d = r.d;
+      }
+      __syncthreads();
+      r.d = ts.d;
+    } else {
+      n = kMaxCand + 1;
+    }
+  }
+  idx = -1;
+  p = 0.0;
   double s = 0.0;
-  for (int v = threadIdx.x; v < a.V; v += kTreeThreads) {
-    const float l = logits[v];
-    if (kept(r, l, v, a.inv_temp)) s += weight(r, l, (double)a.temperature);
+  if (n <= kMaxCand) {
+    if ((int)threadIdx.x < n) {
+      idx = sh.ci[cand_slot(threadIdx.x)];
+      if (kept_w(sh.cw[cand_slot(threadIdx.x)], idx, r.d)) p = weight(r.d, logits[idx], (double)a.temperature);
+    }
+    s = p;
+  } else {
+    n = -1;
+    for (int v = threadIdx.x; v < a.V; v += kTreeThreads) {
+      const float l = logits[v];
+      if (kept_w(exp_weight(l, a.inv_temp, r.d), v, r.d)) s += weight(r.d, l, (double)a.temperature);
+    }
   }
-  s = block_sum(s, sh);
+  s = block_sum(s, ts, turn);
   r.norm = s > 0.0 && s < INFINITY ? 1.0 / s : 0.0;
-  return r;
+  p *= r.norm;
+  return n;
 }
 
-// Argmax with the lowest index on ties; -1 without a logit above -inf.
-__device__ __forceinline__ int row_argmax(const float* logits, int V, TreeShared& sh) {
-  float best = -INFINITY;
-  int at = 0x7fffffff;
-  for (int v = threadIdx.x; v < V; v += kTreeThreads) {
-    const float l = logits[v];
-    if (l > best) {
-      best = l;
-      at = v;
-    }
+// Opens row `which` (0: the verifier's, 1: the draft's) of node blockIdx / batch-major in
+// the workspace, where the walk may want it: every node that the tree has, of the draft
+// those with a child.
+template <int EPT>
+__global__ __launch_bounds__(kTreeThreads) void tree_rows_kernel(TreeVerifyArgs a) {
+  __shared__ RowShared sh;
+  __shared__ TreeShared ts;
+  const int64_t row = blockIdx.x;  // [which][batch][ready]
+  const int64_t half = a.batch * a.ready;
+  const bool draft = row >= half;
+  const int64_t in = draft ? row - half : row;
+  const int64_t b = in / a.ready;
+  const int i = (int)(in - b * a.ready);
+  const int lane = threadIdx.x & 63;
+  // (every wave asks for itself)
+  const int parent = lane < a.n ? (a.parents ? a.parents[b * a.n + lane] : lane - 1) : -1;
+  if (draft && __ballot(lane < a.n && lane > i && parent == i) == 0) return;
+  const int up = __builtin_amdgcn_readlane(parent, i);
+  if (i > 0 && (up < 0 || up >= i)) return;
+  const int64_t at = b * a.n + i;
+  int turn = 0;
+  Row r;
+  int idx;
+  double p;
+  const RowDist* rec = draft && a.dparams ? a.dparams + at : nullptr;
+  const int n = open_row<EPT>((draft ? a.draft : a.target) + at * a.V, rec, a, sh, ts, turn, r, idx, p);
+  if ((int)threadIdx.x < n) {
+    a.list_idx[row * kMaxCand + threadIdx.x] = idx;
+    a.list_p[row * kMaxCand + threadIdx.x] = p;
   }
-  wave_argmax(best, at);
-  const int w = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) {
-    sh.fval[w] = best;
-    sh.ival[w] = at;
+  if (threadIdx.x == 0) {
+    TreeRow t;
+    t.d = r.d;
+    t.n = n;
+    t.norm = r.norm;
+    static_cast<TreeRow*>(a.ready_rows)[row] = t;
   }
-  __syncthreads();
-  best = sh.fval[0];
-  at = sh.ival[0];
-  for (int i = 1; i < kTreeWaves; ++i)
-    if (argmax_better(sh.fval[i], sh.ival[i], best, at)) {
-      best = sh.fval[i];
-      at = sh.ival[i];
-    }
-  __syncthreads();
-  return at == 0x7fffffff ? -1 : at;
 }
 
-// Smallest index whose cumulative weight in index order exceeds `target`; the last index
-// of positive weight where rounding leaves the target at the sum; -1 without any.
+// Smallest index whose cumulative weight in index order exceeds u times the sum; the last
+// index of positive weight where rounding leaves the target at the sum; -1 without any.
 template <class Wt>
-__device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& sh) {
+__device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& ts) {
   const int wave = threadIdx.x >> 6;
   const int lane = threadIdx.x & 63;
   const int slabs = (V + kTreeThreads - 1) / kTreeThreads;
+  __syncthreads();
   for (int s = 0; s < slabs; ++s) {
     const int v = s * kTreeThreads + (int)threadIdx.x;
     const double w = v < V ? wt(v) : 0.0;
     double t = 0.0;
     if (__ballot(w > 0.0) != 0) t = wave_sum(w);
-    if (lane == 0) sh.seg[s * kTreeWaves + wave] = t;
+    if (lane == 0) ts.seg[s * kTreeWaves + wave] = t;
   }
-  if (threadIdx.x == 0) sh.pick = -1;
+  if (threadIdx.x == 0) ts.pick = -1;
   __syncthreads();
   if (wave == 0) {
     // each lane owns a run of segments, in index order
@@ -143,7 +204,7 @@ __device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& sh
     const int per = (n + 63) / 64;
     double run = 0.0;
     for (int k = 0; k < per; ++k)
-      if (lane * per + k < n) run += sh.seg[lane * per + k];
+      if (lane * per + k < n) run += ts.seg[lane * per + k];
     const double incl = wave_incl_scan(run);
     const double target = u * lane_read(incl, 63);
     double before = incl - run;
@@ -152,7 +213,7 @@ __device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& sh
     double found_before = 0.0, last_before = 0.0;
     for (int k = 0; k < per; ++k) {
       const int i = lane * per + k;
-      const double s = i < n ? sh.seg[i] : 0.0;
+      const double s = i < n ? ts.seg[i] : 0.0;
       if (s > 0.0) {
         last = i;
         last_before = before;
@@ -167,19 +228,19 @@ __device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& sh
     const unsigned long long some = __ballot(last >= 0);
     if (hit) {
       if (lane == __builtin_ctzll(hit)) {
-        sh.pick = found;
-        sh.before = found_before - target;
+        ts.pick = found;
+        ts.before = found_before - target;
       }
     } else if (some) {
       if (lane == 63 - __builtin_clzll(some)) {
-        sh.pick = last;
-        sh.before = last_before - target;
+        ts.pick = last;
+        ts.before = last_before - target;
       }
     }
   }
   __syncthreads();
-  const int seg = sh.pick;
-  const double ahead = sh.before;  // what comes before the segment, less the target
+  const int seg = ts.pick;
+  const double ahead = ts.before;  // what comes before the segment, less the target
   __syncthreads();
   if (seg < 0) return -1;
   if (wave == seg % kTreeWaves) {
@@ -189,96 +250,175 @@ __device__ __forceinline__ int draw_index(Wt wt, int V, double u, TreeShared& sh
     const unsigned long long m = __ballot(w > 0.0 && ahead + incl > 0.0);
     const unsigned long long pos = __ballot(w > 0.0);
     const int l = m ? __builtin_ctzll(m) : 63 - __builtin_clzll(pos);
-    if (lane == 0) sh.pick = (seg / kTreeWaves) * kTreeThreads + wave * 64 + l;
+    if (lane == 0) ts.pick = (seg / kTreeWaves) * kTreeThreads + wave * 64 + l;
   }
   __syncthreads();
-  const int v = sh.pick;
-  __syncthreads();
-  return v;
+  return ts.pick;
 }
 
-template <bool GREEDY>
+// The same over a list, thread i its entry i.
+__device__ __forceinline__ int draw_list(int idx, double w, double u, TreeShared& ts) {
+  const int wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const double incl = wave_incl_scan(w);
+  __syncthreads();
+  if (lane == 63) ts.seg[wave] = incl;
+  if (threadIdx.x == 0) ts.pick = -1;
+  __syncthreads();
+  double before = 0.0, total = 0.0;
+#pragma unroll
+  for (int i = 0; i < kTreeWaves; ++i) {
+    if (i == wave) before = total;
+    total += ts.seg[i];
+  }
+  const double target = u * total;
+  const unsigned long long hit = __ballot(w > 0.0 && before + incl > target);
+  const unsigned long long some = __ballot(w > 0.0);
+  // each wave's first entry past the target, or its last one of all
+  if (lane == 0) {
+    ts.gone[wave] = hit ? wave * 64 + __builtin_ctzll(hit) : -1;
+    ts.gone[kTreeWaves + wave] = some ? wave * 64 + 63 - __builtin_clzll(some) : -1;
+  }
+  __syncthreads();
+  int pick = -1;
+  for (int i = kTreeWaves - 1; i >= 0; --i) pick = ts.gone[i] >= 0 ? ts.gone[i] : pick;
+  if (pick < 0)
+    for (int i = 0; i < kTreeWaves; ++i) pick = ts.gone[kTreeWaves + i] >= 0 ? ts.gone[kTreeWaves + i] : pick;
+  if (pick >= 0 && (int)threadIdx.x == pick) ts.pick = idx;
+  __syncthreads();
+  return ts.pick;
+}
+
+template <int EPT, bool GREEDY>
 __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArgs a) {
-  __shared__ TreeShared sh;
-  __shared__ double scale[kMaxNodes];
-  __shared__ int32_t gone[kMaxNodes];
+  __shared__ RowShared sh;
+  __shared__ TreeShared ts;
   const int64_t b = blockIdx.x;
   const int64_t row0 = b * a.n;
   if ((int)threadIdx.x < a.n) {
     const int64_t i = row0 + threadIdx.x;
-    sh.token[threadIdx.x] = threadIdx.x > 0 ? a.tokens[i] : -1;
-    sh.parent[threadIdx.x] = a.parents ? a.parents[i] : (int)threadIdx.x - 1;
-    sh.u[threadIdx.x] = GREEDY || threadIdx.x == 0 ? 0.f : a.u_accept[i];
+    ts.token[threadIdx.x] = threadIdx.x > 0 ? a.tokens[i] : -1;
+    ts.parent[threadIdx.x] = a.parents ? a.parents[i] : (int)threadIdx.x - 1;
+    ts.u[threadIdx.x] = GREEDY || threadIdx.x == 0 ? 0.f : a.u_accept[i];
     a.path[i] = threadIdx.x == 0 ? 0 : -1;
   }
   __syncthreads();
+  int turn = 0;
   int cur = 0;
   int depth = 0;
   int rejected = 0;
-  Row p, q;
-  q.norm = 0.0;
   int best = -1;
-  auto open = [&]() {
-    const float* t = a.target + (row0 + cur) * a.V;
-    rejected = 0;
-    if (GREEDY) {
-      best = row_argmax(t, a.V, sh);
-    } else {
-      p = open_row(t, a.tparams + row0 + cur, a, sh);
-      q.norm = -1.0;  // opened when a child asks for it
-    }
-  };
-  // p after the children turned down so far, at token v
+  // the present node: with a list (n >= 0) the thread's token of it, what
+  // has become of its probability, and q there
+  const Row& p = ts.row[0];
+  const Row& q = ts.row[1];
+  bool q_open = false;
+  int n = 0;
+  int idx = -1;
+  double r = 0.0, qi = 0.0;
+  // Without a list: what the children turned down so far have left of p at token v.
   auto left = [&](int v) {
-    double r = prob(p, v, a);
-    if (r == 0.0) return 0.0;
+    double x = prob(p, v, a);
+    if (x == 0.0 || rejected == 0) return x;
     if (a.draft) {
-      if (rejected == 0) return r;
       const double qv = prob(q, v, a);
       for (int j = 0; j < rejected; ++j)
-        if (scale[j] != 0.0) r = fmax(r - qv, 0.0) * scale[j];
-      return r;
+        if (ts.scale[j] != 0.0) x = fmax(x - qv, 0.0) * ts.scale[j];
+      return x;
     }
     for (int j = 0; j < rejected; ++j)
-      if (gone[j] == v) return 0.0;
-    return rejected == 0 ? r : r * scale[rejected - 1];
+      if (ts.gone[j] == v) return 0.0;
+    return x * ts.scale[rejected - 1];
   };
-  open();
-#pragma nounroll
-  for (int i = 1; i < a.n; ++i) {
-    if (sh.parent[i] != cur) continue;
-    const int x = sh.token[i];
-    const bool in = x >= 0 && x < a.V;
-    bool take;
+  bool want_q = false;  // the row to open next: the draft's at this node, or the verifier's at a new one
+  int i = 1;
+  for (;;) {
+    const float* logits = (want_q ? a.draft : a.target) + (row0 + cur) * a.V;
     if (GREEDY) {
-      take = in && x == best;
+      best = row_argmax<EPT>(logits, a.V, sh);
     } else {
-      if (a.draft && q.norm < 0.0) q = open_row(a.draft + (row0 + cur) * a.V, a.dparams + row0 + cur, a, sh);
-      const double px = in ? left(x) : 0.0;
+      Row x;
+      int xn, xi;
+      double xp;
+      if (cur < a.ready) {
+        const int64_t at = (want_q ? a.batch * a.ready : 0) + b * a.ready + cur;
+        const TreeRow t = static_cast<const TreeRow*>(a.ready_rows)[at];
+        x.logits = logits;
+        x.d = t.d;
+        x.norm = t.norm;
+        xn = t.n;
+        const bool in = !want_q && (int)threadIdx.x < xn;
+        xi = in ? a.list_idx[at * kMaxCand + threadIdx.x] : -1;
+        xp = in ? a.list_p[at * kMaxCand + threadIdx.x] : 0.0;
+      } else {
+        xn = open_row<EPT>(logits, want_q && a.dparams ? a.dparams + row0 + cur : nullptr, a, sh, ts, turn, x, xi, xp);
+      }
+      __syncthreads();  // nothing reads the row that leaves
+      if (threadIdx.x == 0) ts.row[want_q ? 1 : 0] = x;
+      __syncthreads();
+      if (want_q) {
+        q_open = true;
+        qi = idx >= 0 ? prob(q, idx, a) : 0.0;
+      } else {
+        n = xn;
+        idx = xi;
+        r = xp;
+        q_open = false;
+        rejected = 0;
+      }
+    }
+    want_q = false;
+    bool take = false;
+#pragma nounroll
+    for (; i < a.n; ++i) {
+      if (ts.parent[i] != cur) continue;
+      const int x = ts.token[i];
+      const bool in = x >= 0 && x < a.V;
+      if (GREEDY) {
+        take = in && x == best;
+        if (take) break;
+        continue;
+      }
+      if (a.draft && !q_open) {
+        want_q = true;
+        break;
+      }
+      double px;
+      if (n >= 0) {
+        __syncthreads();
+        if (threadIdx.x == 0) ts.at = 0.0;
+        __syncthreads();
+        if (idx == x && in) ts.at = r;
+        __syncthreads();
+        px = ts.at;
+      } else {
+        px = in ? left(x) : 0.0;
+      }
       const double qx = !a.draft ? 1.0 : in ? prob(q, x, a) : 0.0;
-      take = (double)sh.u[i] * qx < px;
-      if (!take) {
-        // the mass that is left, and 1 over it
-        double s = 0.0;
-        if (a.draft) {
-          for (int v = threadIdx.x; v < a.V; v += kTreeThreads) {
-            const double r = left(v);
-            if (r > 0.0) s += fmax(r - prob(q, v, a), 0.0);
+      take = (double)ts.u[i] * qx < px;
+      if (take) break;
+      // what is left of p, over its mass (no mass left: p stays as it was)
+      double s = 0.0;
+      if (n >= 0) {
+        const double w = a.draft ? fmax(r - qi, 0.0) : idx == x ? 0.0 : r;
+        s = block_sum(w, ts, turn);
+        if (s > 0.0) r = w * (1.0 / s);
+      } else {
+        for (int v = threadIdx.x; v < a.V; v += kTreeThreads) {
+          if (a.draft) {
+            const double w = left(v);
+            if (w > 0.0) s += fmax(w - prob(q, v, a), 0.0);
+          } else if (v != x) {
+            bool was = false;
+            for (int j = 0; j < rejected; ++j) was = was || ts.gone[j] == v;
+            if (!was) s += prob(p, v, a);
           }
-        } else {
-          for (int v = threadIdx.x; v < a.V; v += kTreeThreads)
-            if (v != x) {
-              bool was = false;
-              for (int j = 0; j < rejected; ++j) was = was || gone[j] == v;
-              if (!was) s += prob(p, v, a);
-            }
         }
-        s = block_sum(s, sh);
-        // (no mass left: p stays as it was)
+        s = block_sum(s, ts, turn);
         if (a.draft || s > 0.0) {
           if (threadIdx.x == 0) {
-            scale[rejected] = s > 0.0 ? 1.0 / s : 0.0;
-            gone[rejected] = x;
+            ts.scale[rejected] = s > 0.0 ? 1.0 / s : 0.0;
+            ts.gone[rejected] = x;
           }
           ++rejected;
         }
@@ -288,30 +428,68 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
     if (take) {
       cur = i;
       ++depth;
-      if (threadIdx.x == 0) a.path[row0 + depth] = i;
-      open();
+      ++i;
+      if (threadIdx.x == 0) a.path[row0 + depth] = cur;
+    } else if (!want_q) {
+      break;
     }
   }
   int next;
   if (GREEDY)
     next = best;
+  else if (n >= 0)
+    next = draw_list(idx, r, (double)a.u_sample[b], ts);
   else
-    next = draw_index(left, a.V, (double)a.u_sample[b], sh);
+    next = draw_index(left, a.V, (double)a.u_sample[b], ts);
   if (threadIdx.x == 0) {
     a.n_accepted[b] = depth;
     a.next_token[b] = next;
   }
 }
 
+template <int EPT>
+hipError_t launch_tree_ept(const TreeVerifyArgs& a, hipStream_t stream) {
+  const dim3 block(kTreeThreads);
+  if (a.greedy) {
+    hipLaunchKernelGGL((tree_verify_kernel<EPT, true>), dim3((unsigned)a.batch), block, 0, stream, a);
+    return hipGetLastError();
+  }
+  if (a.ready > 0) {
+    const int64_t rows = a.batch * a.ready * (a.draft ? 2 : 1);
+    hipLaunchKernelGGL(tree_rows_kernel<EPT>, dim3((unsigned)rows), block, 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((tree_verify_kernel<EPT, false>), dim3((unsigned)a.batch), block, 0, stream, a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
-hipError_t launch_tree_verify(const TreeVerifyArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.batch);
-  if (a.greedy)
-    hipLaunchKernelGGL(tree_verify_kernel<true>, grid, dim3(kTreeThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(tree_verify_kernel<false>, grid, dim3(kTreeThreads), 0, stream, a);
-  return hipGetLastError();
+constexpr int64_t kReadyRows = 1024;
+int tree_ready_nodes(int64_t batch, int64_t n) {
+  const int64_t k = kReadyRows / (2 * batch);
+  return (int)(k < n ? k : n);
+}
+size_t tree_ready_bytes(int64_t batch, int64_t n) {
+  return (size_t)(2 * batch * tree_ready_nodes(batch, n)) * (sizeof(TreeRow) + kMaxCand * 12);
+}
+void tree_ready_layout(TreeVerifyArgs& a, void* workspace) {
+  const int64_t rows = 2 * a.batch * a.ready;
+  char* p = static_cast<char*>(workspace);
+  a.ready_rows = p;
+  a.list_p = reinterpret_cast<double*>(p + rows * sizeof(TreeRow));
+  a.list_idx = reinterpret_cast<int32_t*>(p + rows * (sizeof(TreeRow) + kMaxCand * 8));
+}
+
+hipError_t launch_tree_verify(const TreeVerifyArgs& a, int ept, hipStream_t stream) {
+  switch (ept) {
+    case 16: return launch_tree_ept<16>(a, stream);
+    case 32: return launch_tree_ept<32>(a, stream);
+    case 48: return launch_tree_ept<48>(a, stream);
+    case 64: return launch_tree_ept<64>(a, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace mls
