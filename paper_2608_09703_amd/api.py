@@ -788,49 +788,98 @@ def _no_grad(name: str, *xs: Optional[torch.Tensor]):
 
 def _written(*xs: torch.Tensor):
     """Tells autograd of tensors that were written through their addresses."""
-    torch.autograd.graph.increment_version([x for x in xs if not x.is_inference()])
+    if not xs[0].is_inference():
+        torch.autograd.graph.increment_version(xs)
+
+
+# What a call checks and works out from the tensors' types, shapes and strides alone is
+# kept per set of these (bounded, as the descriptors above): 8 of a call's 18 us.
+
+def _meta(x: Optional[torch.Tensor]):
+    return None if x is None else (x.dtype, x.get_device(), x.shape, x.stride())
 
 
 def _kv_cache(name: str, k_pages, v_pages, page_table, lengths, all_layers: bool = False) -> B.KVCache:
-    if not k_pages.is_cuda:
-        raise RuntimeError(f"{name} runs on the GPU only; got tensors on {k_pages.device}")
-    dev = k_pages.device
-    dims = k_pages.dim()
-    if v_pages.device != dev or v_pages.dtype != k_pages.dtype or v_pages.shape != k_pages.shape or \
-            v_pages.stride() != k_pages.stride() or not (dims == 4 or (all_layers and dims == 5)):
+    """The descriptor without addresses; the tensors as their :func:`_meta`."""
+    dtype, dev, shape, stride = k_pages
+    if dev < 0:
+        raise RuntimeError(f"{name} runs on the GPU only")
+    dims = len(shape)
+    if v_pages != k_pages or not (dims == 4 or (all_layers and dims == 5)):
         raise ValueError(f"{name}: k_pages and v_pages are [pages, kv_heads, page_size, head_dim] tensors" +
                          (", or such of several layers," if all_layers else "") + " of one layout, dtype and device")
-    shape, stride = k_pages.shape, k_pages.stride()
     if dims == 4:
         layers, ld_layer = 1, 0
     else:
         layers, ld_layer, shape, stride = shape[0], stride[0], shape[1:], stride[1:]
     if stride[3] != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the elements of an entry must be neighbours")
-    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != dev or \
-            (page_table.size(1) > 1 and page_table.stride(1) != 1):
+    t_dtype, t_dev, t_shape, t_stride = page_table
+    if t_dtype != torch.int32 or len(t_shape) != 2 or t_dev != dev or (t_shape[1] > 1 and t_stride[1] != 1):
         raise ValueError(f"{name}: page_table must be an int32 [B, pages of a sequence] tensor on the pages' device")
-    Bt, width = page_table.shape
-    if lengths.dtype != torch.int32 or lengths.shape != (Bt,) or lengths.device != dev or not lengths.is_contiguous():
-        raise ValueError(f"{name}: lengths must be a contiguous int32 [B] tensor on the pages' device")
-    return B.KVCache(_dtype_code(k_pages.dtype), shape[2], shape[1], shape[3], layers, shape[0], Bt, width, ld_layer,
-                     stride[0], stride[1], stride[2], page_table.stride(0) if Bt > 1 else width, k_pages.data_ptr(),
-                     v_pages.data_ptr(), page_table.data_ptr(), lengths.data_ptr())
+    Bt, width = t_shape
+    _ints(name, "lengths", lengths, (Bt,), dev)
+    return B.KVCache(_dtype_code(dtype), shape[2], shape[1], shape[3], layers, shape[0], Bt, width, ld_layer,
+                     stride[0], stride[1], stride[2], t_stride[0] if Bt > 1 else width)
 
 
-def _step_rows(name: str, x: torch.Tensor, what: str, c: B.KVCache, like: torch.Tensor, heads: Optional[int] = None):
+def _step_rows(name: str, x, what: str, c: B.KVCache, like, heads: Optional[int] = None):
     """Checks ``x [B, n, heads, head_dim]`` and returns its strides."""
-    if x.device != like.device or x.dtype != like.dtype or x.dim() != 4 or x.size(0) != c.batch or \
-            x.size(3) != c.head_dim or x.size(1) == 0 or (heads is not None and x.size(2) != heads) or \
-            (x.stride(3) != 1 and x.size(3) > 1):
+    dtype, dev, shape, stride = x
+    if dev != like[1] or dtype != like[0] or len(shape) != 4 or shape[0] != c.batch or shape[3] != c.head_dim or \
+            shape[1] == 0 or (heads is not None and shape[2] != heads) or (stride[3] != 1 and shape[3] > 1):
         raise ValueError(f"{name}: {what} must be a [B, n, heads, head_dim] tensor of the pages' dtype and device")
-    s = x.stride()
-    return (s[0] if x.size(0) > 1 else 0, s[1] if x.size(1) > 1 else 0, s[2] if x.size(2) > 1 else 0)
+    return tuple(stride[i] if shape[i] > 1 else 0 for i in range(3))
 
 
-def _ints(name: str, what: str, x: Optional[torch.Tensor], shape, dev):
-    if x is not None and (x.dtype != torch.int32 or x.shape != shape or x.device != dev or not x.is_contiguous()):
+def _ints(name: str, what: str, x, shape, dev):
+    if x is not None and (x[0] != torch.int32 or x[2] != shape or x[1] != dev or not _packed(x[2], x[3])):
         raise ValueError(f"{name}: {what} must be a contiguous int32 {list(shape)} tensor on the same device")
+
+
+def _packed(shape, stride) -> bool:
+    want = 1
+    for n, s in zip(reversed(shape), reversed(stride)):
+        if n != 1 and s != want:
+            return False
+        want *= n
+    return True
+
+
+def _with_addresses(c: B.KVCache, k_pages, v_pages, page_table, lengths) -> B.KVCache:
+    c = B.KVCache.from_buffer_copy(c)
+    c.k, c.v, c.page_table, c.lengths = k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), lengths.data_ptr()
+    return c
+
+
+@functools.lru_cache(maxsize=256)
+def _write_plan(k, v, k_pages, v_pages, page_table, lengths, counts):
+    c = _kv_cache("cache_write", k_pages, v_pages, page_table, lengths)
+    ld = _step_rows("cache_write", k, "k", c, k_pages, c.kv_heads)
+    if v[2] != k[2]:
+        raise ValueError("cache_write: k and v must be of one shape")
+    same = _step_rows("cache_write", v, "v", c, k_pages, c.kv_heads) == ld
+    _ints("cache_write", "counts", counts, (c.batch,), k[1])
+    return c, k[2][1], ld, same
+
+
+@functools.lru_cache(maxsize=256)
+def _compact_plan(k_pages, v_pages, page_table, lengths, path, n_accepted):
+    c = _kv_cache("cache_compact", k_pages, v_pages, page_table, lengths, all_layers=True)
+    if len(path[2]) != 2:
+        raise ValueError("cache_compact: path must be an int32 [B, n] tensor")
+    _ints("cache_compact", "path", path, (c.batch, path[2][1]), k_pages[1])
+    _ints("cache_compact", "n_accepted", n_accepted, (c.batch,), k_pages[1])
+    return c, path[2][1]
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_plan(q, k_pages, v_pages, page_table, lengths, parents):
+    c = _kv_cache("tree_attention", k_pages, v_pages, page_table, lengths)
+    ld = _step_rows("tree_attention", q, "q", c, k_pages)
+    n, heads = q[2][1], q[2][2]
+    _ints("tree_attention", "parents", parents, (c.batch, n), q[1])
+    return c, n, heads, ld, c.head_dim ** -0.5
 
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -844,18 +893,15 @@ def cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages
     below 0 takes no part, and pages outside the pool are not written. ``lengths`` stay as they are.
     """
     _no_grad("cache_write", k, v, k_pages, v_pages)
-    c = _kv_cache("cache_write", k_pages, v_pages, page_table, lengths)
-    ld = _step_rows("cache_write", k, "k", c, k_pages, c.kv_heads)
-    if v.shape != k.shape:
-        raise ValueError("cache_write: k and v must be of one shape")
-    if _step_rows("cache_write", v, "v", c, k_pages, c.kv_heads) != ld:
-        v = v.contiguous()
-        k = k.contiguous()
-        ld = _step_rows("cache_write", k, "k", c, k_pages, c.kv_heads)
-    _ints("cache_write", "counts", counts, (c.batch,), k.device)
-    with _on(k.device):
-        B.cache_write(c, k.size(1), k.data_ptr(), v.data_ptr(), ld, counts.data_ptr() if counts is not None else None,
-                      _stream(k.device))
+    c, n, ld, same = _write_plan(_meta(k), _meta(v), _meta(k_pages), _meta(v_pages), _meta(page_table),
+                                 _meta(lengths), _meta(counts))
+    if not same:  # one set of strides for both
+        return cache_write(k.contiguous(), v.contiguous(), k_pages, v_pages, page_table, lengths, counts=counts)
+    c = _with_addresses(c, k_pages, v_pages, page_table, lengths)
+    dev = k.device
+    with _on(dev):
+        B.cache_write(c, n, k.data_ptr(), v.data_ptr(), ld, counts.data_ptr() if counts is not None else None,
+                      _stream(dev))
     _written(k_pages, v_pages)
 
 
@@ -869,15 +915,13 @@ def cache_compact(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torc
     head_dim]``, for one call. Where ``lengths`` or ``n_accepted`` is below 0, nothing moves.
     """
     _no_grad("cache_compact", k_pages, v_pages)
-    c = _kv_cache("cache_compact", k_pages, v_pages, page_table, lengths, all_layers=True)
+    c, n = _compact_plan(_meta(k_pages), _meta(v_pages), _meta(page_table), _meta(lengths), _meta(path),
+                         _meta(n_accepted))
+    c = _with_addresses(c, k_pages, v_pages, page_table, lengths)
     dev = k_pages.device
-    if path.dim() != 2:
-        raise ValueError("cache_compact: path must be an int32 [B, n] tensor")
-    _ints("cache_compact", "path", path, (c.batch, path.size(1)), dev)
-    _ints("cache_compact", "n_accepted", n_accepted, (c.batch,), dev)
     new = torch.empty(c.batch, dtype=torch.int32, device=dev)
     with _on(dev):
-        B.cache_compact(c, path.size(1), path.data_ptr(), n_accepted.data_ptr(), new.data_ptr(), _stream(dev))
+        B.cache_compact(c, n, path.data_ptr(), n_accepted.data_ptr(), new.data_ptr(), _stream(dev))
     _written(k_pages, v_pages)
     return new
 
@@ -897,16 +941,16 @@ def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
     in parts as the table's width has it, so pass the columns that are in use.
     """
     _no_grad("tree_attention", q, k_pages, v_pages)
-    c = _kv_cache("tree_attention", k_pages, v_pages, page_table, lengths)
-    ld = _step_rows("tree_attention", q, "q", c, k_pages)
-    dev, n, heads = q.device, q.size(1), q.size(2)
-    _ints("tree_attention", "parents", parents, (c.batch, n), dev)
+    c, n, heads, ld, default = _attention_plan(_meta(q), _meta(k_pages), _meta(v_pages), _meta(page_table),
+                                               _meta(lengths), _meta(parents))
+    c = _with_addresses(c, k_pages, v_pages, page_table, lengths)
+    dev = q.device
     ws_bytes = B.tree_attention_workspace(c, n, heads)
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
     out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     with _on(dev):
         B.tree_attention(c, n, heads, q.data_ptr(), ld, parents.data_ptr() if parents is not None else None,
-                         c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                         default if scale is None else scale, out.data_ptr(),
                          ws.data_ptr() if ws is not None else None, ws_bytes, _stream(dev))
     return out
 
@@ -939,8 +983,8 @@ def tree_verify(target_logits: torch.Tensor, tokens: torch.Tensor, parents: Opti
         if x is not None and (x.dtype != torch.float32 or x.shape != shape or x.device != dev or
                               not x.is_contiguous()):
             raise ValueError(f"tree_verify: {what} must be a contiguous float32 {list(shape)} tensor on one device")
-    _ints("tree_verify", "tokens", tokens, (Bt, n), dev)
-    _ints("tree_verify", "parents", parents, (Bt, n), dev)
+    _ints("tree_verify", "tokens", _meta(tokens), (Bt, n), target_logits.get_device())
+    _ints("tree_verify", "parents", _meta(parents), (Bt, n), target_logits.get_device())
     if draft_params is not None and (draft_params.dtype != torch.uint8 or not draft_params.is_contiguous() or
                                      draft_params.device != dev or
                                      draft_params.numel() < Bt * n * B.ROW_PARAMS_BYTES):

@@ -2317,7 +2317,7 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   const int64_t want = (kAttnBlocks + base - 1) / base;
   pl.part = std::min(std::max(round_up((cap + want - 1) / want, 128), kPartLeast), kPartMost);
   pl.splits = (cap + pl.part - 1) / pl.part;
-  if (base * pl.splits > 0x7fffffff || c->batch * n * heads * (D / 4) > (1ll << 38))
+  if (base * pl.splits > 0x7fffff00 - 8 * pl.n_rt || c->batch * n * heads * (D / 4) > (1ll << 38))
     return fail(MLS_UNSUPPORTED, "%lld parts of the cache are more than one launch takes", (long long)(base * pl.splits));
   pl.records = pl.splits > 1 ? base * pl.splits * pl.tile : 0;
   pl.acc_bytes = align256((size_t)pl.records * D * 4);

@@ -115,6 +115,12 @@ struct Attn {
   static constexpr int KC = D * E::kBytes / 64;         // 16-byte pieces of a lane's share of an entry of K
   static constexpr int ROWS = 16 * RT;
   static constexpr int LD = D + 4;                      // floats of a row in LDS
+  // Registers of a lane that hold sums, queries, keys and values. Two waves a SIMD have
+  // 256 each: below 192 everything else fits beside them (bf16, heads of 128, 32 rows: 160,
+  // 215 in all). Asked for, the compiler also keeps the sums out of the accumulation
+  // registers, which it otherwise copies them to and from.
+  static constexpr int kHeld = RT * DE * 4 + (RT + SUBS) * KC * 4 + SUBS * 4 * VW;
+  static constexpr int kWaves = kHeld < 192 ? 2 : 1;
 
   uint4 qf[RT][KC];
   uint32_t kf[SUBS][KC][4];
@@ -304,7 +310,7 @@ __device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d,
 }
 
 template <typename E, int D, int RT>
-__global__ __launch_bounds__(kAttnThreads) void tree_attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_attention_kernel(AttnArgs a) {
   using A = Attn<E, D, RT>;
   constexpr int SUBS = A::SUBS;
   constexpr int ROWS = A::ROWS;
@@ -318,9 +324,14 @@ __global__ __launch_bounds__(kAttnThreads) void tree_attention_kernel(AttnArgs a
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int x = xcd_remap(blockIdx.x, gridDim.x);
-  const int rt = x % a.n_rt;
-  x /= a.n_rt;
+  // Blocks go to the 8 XCDs in turn. The row tiles of one part, which read the same
+  // entries, follow each other on one XCD; parts of one sequence go to all of them (in one
+  // range of blocks an XCD, the longest sequence's XCD was the last: 4 sequences of 44,000
+  // to 65,536 entries 805 us).
+  const int turn = blockIdx.x / 8;
+  const int rt = turn % a.n_rt;
+  int x = (turn / a.n_rt) * 8 + blockIdx.x % 8;
+  if (x >= (int)a.c.batch * a.c.kv_heads * a.splits) return;
   const int sp = x % a.splits;
   x /= a.splits;
   const int hk = x % a.c.kv_heads;
@@ -607,7 +618,7 @@ int attn_tile_rows(int32_t rows, int32_t head_bytes) {
 }
 
 hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream) {
-  const int64_t blocks = a.c.batch * a.c.kv_heads * a.n_rt * a.splits;
+  const int64_t blocks = (a.c.batch * a.c.kv_heads * a.splits + 7) / 8 * 8 * a.n_rt;
   hipError_t e = f32 ? launch_attn<F32>(a, D, blocks, stream) : launch_attn<Bf16>(a, D, blocks, stream);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t threads = a.c.batch * a.n * a.heads * (D / 4);
