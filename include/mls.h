@@ -649,7 +649,7 @@ mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* pa
  * that a row does not attend to do not matter to it, whatever they hold.
  * q [batch][n][heads][head_dim] has strides like mls_cache_write's k; out is contiguous, of
  * the cache's dtype, 16-byte aligned. n in 1..64, heads a multiple of kv_heads, head_dim
- * 32, 64, 96, 128, 192 or 256. Sums are fp32; bf16 weights are rounded to bfloat16 for the
+ * 32, 64, 96, 128, 192 or 256, scale finite and > 0. Sums are fp32; bf16 weights are rounded to bfloat16 for the
  * product with the values. Results depend on the table's width (entries are taken in parts),
  * and are the same bits on every call. Asynchronous on stream.
  */

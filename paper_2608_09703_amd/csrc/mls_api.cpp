@@ -2295,8 +2295,13 @@ constexpr int64_t kAttnBlocks = 1024;
 constexpr int64_t kPartLeast = 256;
 constexpr int64_t kPartMost = 4096;
 
+// The memory side's cache: a larger cache of entries has left it before it is read again.
+constexpr int64_t kMemorySideBytes = 256ll << 20;
+
 struct AttnPlan {
   int64_t rows, tile, n_rt, part, splits, records;
+  bool shorts;  // one part, more waves to a block
+  bool once;
   size_t acc_bytes, bytes;
 };
 
@@ -2316,9 +2321,12 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   const int64_t cap = c->table_pages * c->page_size;
   const int64_t want = (kAttnBlocks + base - 1) / base;
   pl.part = std::min(std::max(round_up((cap + want - 1) / want, 128), kPartLeast), kPartMost);
+  pl.shorts = attn_short(base, cap, (int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
+  if (pl.shorts) pl.part = round_up(cap, 128);
   pl.splits = (cap + pl.part - 1) / pl.part;
   if (base * pl.splits > 0x7fffff00 - 8 * pl.n_rt || c->batch * n * heads * (D / 4) > (1ll << 38))
     return fail(MLS_UNSUPPORTED, "%lld parts of the cache are more than one launch takes", (long long)(base * pl.splits));
+  pl.once = pl.n_rt == 1 && c->batch * cap * c->kv_heads * D * (c->dtype == MLS_BF16 ? 4 : 8) > kMemorySideBytes;
   pl.records = pl.splits > 1 ? base * pl.splits * pl.tile : 0;
   pl.acc_bytes = align256((size_t)pl.records * D * 4);
   pl.bytes = pl.acc_bytes + align256((size_t)pl.records * 8);
@@ -2355,8 +2363,7 @@ mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, cons
   CacheWriteArgs a;
   memset(&a, 0, sizeof(a));
   a.c = cache_args(c);
-  if (n < 1 || n > (1ll << 30) || n * a.c.kv_heads > (1ll << 40) ||
-      n * a.c.kv_heads * a.c.chunks > 0x7fffffff - (1 << 20))
+  if (n < 1 || n > (1ll << 30) || cache_write_blocks(n, a.c.kv_heads) > 0x7fffffff)
     return fail(MLS_INVALID_ARG, "n=%lld out of range", (long long)n);
   if ((st = validate_rows("k", k, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if ((st = validate_rows("v", v, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
@@ -2433,7 +2440,7 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   if ((st = validate_rows("q", q, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if (!out || !aligned(out, 16)) return fail(MLS_INVALID_ARG, "out must be non-NULL and 16-byte aligned");
   if (!aligned(parents, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
-  if (!isfinite(scale)) return fail(MLS_INVALID_ARG, "scale must be finite");
+  if (!isfinite(scale) || !(scale > 0.f)) return fail(MLS_INVALID_ARG, "scale must be finite and > 0");
   if (pl.bytes && (!workspace || workspace_bytes < pl.bytes))
     return fail(MLS_WORKSPACE_TOO_SMALL, "attention needs %zu workspace bytes, got %zu", pl.bytes,
                 workspace ? workspace_bytes : 0);
@@ -2456,6 +2463,8 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   a.n_rt = (int32_t)pl.n_rt;
   a.splits = (int32_t)pl.splits;
   a.part = (int32_t)pl.part;
+  a.shorts = pl.shorts;
+  a.once = pl.once;
   a.acc = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.acc_bytes);
   hipStream_t hs = static_cast<hipStream_t>(stream);

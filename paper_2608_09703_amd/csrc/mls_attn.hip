@@ -8,7 +8,7 @@
 // them). A row keeps a running maximum m and sum; w is taken relative to m, in base 2.
 //
 // A block takes up to 64 rows (nodes x heads of one key head) and one part of the
-// entries; its four waves take the part's tiles in turn, each for itself, and join their
+// entries; its waves take the part's tiles in turn, each for itself, and join their
 // sums at the end. Nothing goes through LDS on the way there, and no wave waits for
 // another: the two products are laid out so that each one's operands are what loads and
 // the other product leave in a lane's registers.
@@ -37,10 +37,15 @@ namespace mls {
 namespace {
 
 constexpr int kAttnWaves = 4;
-constexpr int kAttnThreads = 64 * kAttnWaves;
+// Few blocks with short sequences: more waves to a block, and no parts to join. One
+// sequence of 700 entries, 16 heads of 64: two launches of 7.4 and 3.6 us before.
+constexpr int kShortWaves = 8;
 // A row's weights are relative to a maximum that is brought up to date only where a score
 // passes it by this much (base 2): the weights stay below 2^8, which costs the sums nothing.
 constexpr float kMaxSlack = 8.f;
+// ... and a row's before its first entry: finite, so that a row that has none (every
+// score -inf) adds weights of 0 and no NaN.
+constexpr float kNoMax = -3e38f;
 
 template <typename E>
 struct AttnTile;
@@ -66,29 +71,37 @@ __device__ __forceinline__ unsigned long long ancestors(const int32_t* parents, 
   }
 }
 
+// Cache policy of the entries' loads. Where one block alone reads an entry and the cache is
+// larger than the memory side's 256 MB, non-temporal: 4 sequences of 65,536 entries, 34
+// heads of 128, one row: 783 -> 698 us (6.5 TB/s), 32 rows 838 -> 797; 102 of 1,280
+// entries, 16 rows 421 -> 387. Not where row tiles share them (16 sequences, 320 rows of
+// one key head: 164 -> 171), nor where the memory side may still hold them (197 MB: 59 -> 71).
+constexpr int kLoadKeep = 0;
+constexpr int kLoadOnce = 2;
+
 // Loads of NB bytes, a multiple of 4, at lane offset `voff` and scalar offset `soff` of a
 // buffer.
-template <int NB>
+template <int NB, int AUX>
 __device__ __forceinline__ void load_bytes(__amdgpu_buffer_rsrc_t rs, int voff, int soff, uint32_t* r) {
   typedef uint32_t words4 __attribute__((ext_vector_type(4)));
   typedef uint32_t words3 __attribute__((ext_vector_type(3)));
   typedef uint32_t words2 __attribute__((ext_vector_type(2)));
   if constexpr (NB >= 16) {
-    const words4 v = __builtin_bit_cast(words4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff, soff, 0));
+    const words4 v = __builtin_bit_cast(words4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff, soff, AUX));
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = v[i];
-    if constexpr (NB > 16) load_bytes<NB - 16>(rs, voff + 16, soff, r + 4);
+    if constexpr (NB > 16) load_bytes<NB - 16, AUX>(rs, voff + 16, soff, r + 4);
   } else if constexpr (NB == 12) {
-    const words3 v = __builtin_bit_cast(words3, __builtin_amdgcn_raw_buffer_load_b96(rs, voff, soff, 0));
+    const words3 v = __builtin_bit_cast(words3, __builtin_amdgcn_raw_buffer_load_b96(rs, voff, soff, AUX));
 #pragma unroll
     for (int i = 0; i < 3; ++i) r[i] = v[i];
   } else if constexpr (NB == 8) {
-    const words2 v = __builtin_bit_cast(words2, __builtin_amdgcn_raw_buffer_load_b64(rs, voff, soff, 0));
+    const words2 v = __builtin_bit_cast(words2, __builtin_amdgcn_raw_buffer_load_b64(rs, voff, soff, AUX));
     r[0] = v[0];
     r[1] = v[1];
   } else {
     static_assert(NB == 4, "whole words");
-    r[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff, soff, 0);
+    r[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff, soff, AUX);
   }
 }
 
@@ -105,7 +118,7 @@ __device__ __forceinline__ uint32_t finite_word<Bf16>(uint32_t x) {
   return (x & 0x7f80u) == 0x7f80u ? x & 0xffff0000u : x;
 }
 
-template <typename E, int D, int RT>
+template <typename E, int D, int RT, int AUX>
 struct Attn {
   static constexpr int DE = D / 16;                     // elements of a lane's piece of an entry of V
   static constexpr int SUBS = AttnTile<E>::kSubs;
@@ -144,7 +157,7 @@ struct Attn {
     for (int s = 0; s < SUBS; ++s) {
       const __amdgpu_buffer_rsrc_t rs = run_rsrc(a.c.k, a, page[s], hk, t0 + 16 * s);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) load_bytes<16>(rs, voff + 64 * c, 0, kf[s][c]);
+      for (int c = 0; c < KC; ++c) load_bytes<16, AUX>(rs, voff + 64 * c, 0, kf[s][c]);
     }
   }
   __device__ __forceinline__ void load_v(const AttnArgs& a, const int32_t* page, int hk, int t0, int lane) {
@@ -153,7 +166,7 @@ struct Attn {
     for (int s = 0; s < SUBS; ++s) {
       const __amdgpu_buffer_rsrc_t rs = run_rsrc(a.c.v, a, page[s], hk, t0 + 16 * s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_bytes<VB>(rs, voff, i * (int)a.c.s_entry * 16, vf[4 * s + i]);
+      for (int i = 0; i < 4; ++i) load_bytes<VB, AUX>(rs, voff, i * (int)a.c.s_entry * 16, vf[4 * s + i]);
     }
   }
 
@@ -309,14 +322,16 @@ __device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d,
   }
 }
 
-template <typename E, int D, int RT>
-__global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_attention_kernel(AttnArgs a) {
-  using A = Attn<E, D, RT>;
+template <typename E, int D, int RT, int WAVES, int AUX>
+__global__ __launch_bounds__(64 * WAVES, (WAVES > kAttnWaves ? WAVES / 4 : Attn<E, D, RT, AUX>::kWaves))
+void tree_attention_kernel(AttnArgs a) {
+  using A = Attn<E, D, RT, AUX>;
+  constexpr int kThreadsOf = 64 * WAVES;
   constexpr int SUBS = A::SUBS;
   constexpr int ROWS = A::ROWS;
-  __shared__ __attribute__((aligned(16))) float o_sh[kAttnWaves][16][A::LD];
-  __shared__ float m_sh[kAttnWaves][ROWS];
-  __shared__ float l_sh[kAttnWaves][ROWS];
+  __shared__ __attribute__((aligned(16))) float o_sh[WAVES][16][A::LD];
+  __shared__ float m_sh[WAVES][ROWS];
+  __shared__ float l_sh[WAVES][ROWS];
   __shared__ unsigned long long see_sh[64];
   __shared__ int32_t parent_sh[64];
   __shared__ int odd_sh;  // some node's values were infinite or NaN
@@ -366,7 +381,7 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
       w.qf[t][c] = make_uint4(0u, 0u, 0u, 0u);
       if (in) w.qf[t][c] = *reinterpret_cast<const uint4*>(q + 64 * c + 16 * (lane >> 4));
     }
-    w.m[t] = -INFINITY;
+    w.m[t] = kNoMax;
     w.l[t] = 0.f;
 #pragma unroll
     for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -393,8 +408,8 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
     w.load_k(a, id, hk, t0, lane);
     w.load_v(a, id, hk, t0, lane);
   }
-  for (; t0 < t_end; t0 += kAttnWaves * A::KT) {
-    const int tn = t0 + kAttnWaves * A::KT;
+  for (; t0 < t_end; t0 += WAVES * A::KT) {
+    const int tn = t0 + WAVES * A::KT;
     int32_t id_n[SUBS];
     bool ok_n[SUBS];
     if (tn < t_end) pages_of(tn, id_n, ok_n);
@@ -404,10 +419,6 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
     bool whole = t0 + A::KT <= ctx;
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) whole = whole && ok[u];
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u) s[t][u] *= a.scale;
     if (!whole) {
       w.mask(s, see, t0 - ctx, a.n, ok, lane);
       if (w.take_out_odd(t0 - ctx, lane)) odd_sh = 1;
@@ -422,6 +433,7 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
       for (int u = 0; u < SUBS; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][u][i]);
+      top[t] *= a.scale;  // (above 0)
       grow = grow || top[t] > w.m[t] + kMaxSlack;
     }
     if (__ballot(grow) != 0) {
@@ -440,12 +452,11 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
     uint4 pb[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const float ref = w.m[t] == -INFINITY ? 0.f : w.m[t];
 #pragma unroll
       for (int u = 0; u < SUBS; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[t][u][i] = fast_exp2(s[t][u][i] - ref);
+          s[t][u][i] = fast_exp2(fmaf(s[t][u][i], a.scale, -w.m[t]));
           w.l[t] += s[t][u][i];
         }
       // bf16 weights, as the values are: up to 2^-8 of each, in both directions
@@ -463,7 +474,7 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
     }
   }
 
-  // the four waves' sums, relative to the largest of their maxima
+  // the waves' sums, relative to the largest of their maxima
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     float l = w.l[t];
@@ -480,7 +491,7 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
     const int r = 16 * t + (lane & 15);
     float m = m_sh[0][r];
 #pragma unroll
-    for (int i = 1; i < kAttnWaves; ++i) m = fmaxf(m, m_sh[i][r]);
+    for (int i = 1; i < WAVES; ++i) m = fmaxf(m, m_sh[i][r]);
     const float f = w.m[t] == m ? 1.f : fast_exp2(w.m[t] - m);
     if (t > 0) __syncthreads();  // the last tile's rows have been read
     float* o = &o_sh[wave][lane & 15][4 * A::DE * (lane >> 4)];
@@ -490,18 +501,18 @@ __global__ __launch_bounds__(kAttnThreads, (Attn<E, D, RT>::kWaves)) void tree_a
           make_float4(w.acc[t][j % A::DE][j / A::DE] * f, w.acc[t][(j + 1) % A::DE][(j + 1) / A::DE] * f,
                       w.acc[t][(j + 2) % A::DE][(j + 2) / A::DE] * f, w.acc[t][(j + 3) % A::DE][(j + 3) / A::DE] * f);
     __syncthreads();
-    for (int i = tid; i < 16 * (D / 4); i += kAttnThreads) {
+    for (int i = tid; i < 16 * (D / 4); i += kThreadsOf) {
       const int rl = i / (D / 4);
       const int d = 4 * (i % (D / 4));
       const int r2 = 16 * t + rl;
       if (row0 + r2 >= a.rows) continue;
       float mm = m_sh[0][r2];
 #pragma unroll
-      for (int k = 1; k < kAttnWaves; ++k) mm = fmaxf(mm, m_sh[k][r2]);
+      for (int k = 1; k < WAVES; ++k) mm = fmaxf(mm, m_sh[k][r2]);
       float l = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < kAttnWaves; ++k) {
+      for (int k = 0; k < WAVES; ++k) {
         l += l_sh[k][r2] * (m_sh[k][r2] == mm ? 1.f : fast_exp2(m_sh[k][r2] - mm));
         const float4 p = *reinterpret_cast<const float4*>(&o_sh[k][rl][d]);
         v.x += p.x;
@@ -574,25 +585,37 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D, int t
 
 constexpr int kWideRow = 256;    // bytes of a head up to which a tile has 64 rows
 constexpr int kMiddleRow = 768;  // and 32
+constexpr int kShortRow = 384;   // and up to which kShortWaves waves of 16 rows have registers
+
+template <typename E, int D, int RT, int WAVES, int AUX>
+hipError_t launch_attn_k(const AttnArgs& a, int64_t blocks, hipStream_t stream) {
+  hipLaunchKernelGGL((tree_attention_kernel<E, D, RT, WAVES, AUX>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, stream,
+                     a);
+  return hipGetLastError();
+}
 
 template <typename E, int D>
 hipError_t launch_attn_d(const AttnArgs& a, int64_t blocks, hipStream_t stream) {
-  const dim3 grid((unsigned)blocks);
-  switch (attn_tile_rows(a.rows, D * E::kBytes)) {
-    case 16: hipLaunchKernelGGL((tree_attention_kernel<E, D, 1>), grid, dim3(kAttnThreads), 0, stream, a); break;
+  constexpr int kHeadBytes = D * E::kBytes;
+  constexpr int kMost = kHeadBytes <= kWideRow ? 4 : kHeadBytes <= kMiddleRow ? 2 : 1;  // 16 rows each
+  switch (attn_tile_rows(a.rows, kHeadBytes)) {
+    case 16:
+      if constexpr (kHeadBytes <= kShortRow)
+        if (a.shorts) return launch_attn_k<E, D, 1, kShortWaves, kLoadKeep>(a, blocks, stream);
+      return a.once ? launch_attn_k<E, D, 1, kAttnWaves, kLoadOnce>(a, blocks, stream)
+                    : launch_attn_k<E, D, 1, kAttnWaves, kLoadKeep>(a, blocks, stream);
     case 32:
-      if constexpr (D * E::kBytes <= kMiddleRow) {
-        hipLaunchKernelGGL((tree_attention_kernel<E, D, 2>), grid, dim3(kAttnThreads), 0, stream, a);
-        break;
-      }
+      if constexpr (kMost >= 2)
+        return a.once ? launch_attn_k<E, D, 2, kAttnWaves, kLoadOnce>(a, blocks, stream)
+                      : launch_attn_k<E, D, 2, kAttnWaves, kLoadKeep>(a, blocks, stream);
+      break;
     case 64:
-      if constexpr (D * E::kBytes <= kWideRow) {
-        hipLaunchKernelGGL((tree_attention_kernel<E, D, 4>), grid, dim3(kAttnThreads), 0, stream, a);
-        break;
-      }
-    default: return hipErrorInvalidValue;
+      if constexpr (kMost >= 4)
+        return a.once ? launch_attn_k<E, D, 4, kAttnWaves, kLoadOnce>(a, blocks, stream)
+                      : launch_attn_k<E, D, 4, kAttnWaves, kLoadKeep>(a, blocks, stream);
+      break;
   }
-  return hipGetLastError();
+  return hipErrorInvalidValue;
 }
 
 template <typename E>
@@ -615,6 +638,11 @@ hipError_t launch_attn(const AttnArgs& a, int D, int64_t blocks, hipStream_t str
 int attn_tile_rows(int32_t rows, int32_t head_bytes) {
   const int most = head_bytes <= kWideRow ? 64 : head_bytes <= kMiddleRow ? 32 : 16;
   return rows <= 16 ? 16 : rows <= 32 && most > 32 ? 32 : most;
+}
+
+// blocks: of one part each; entries: that a table's row has room for
+bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes) {
+  return blocks <= 256 && entries <= 1536 && rows <= 16 && head_bytes <= kShortRow;
 }
 
 hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream) {

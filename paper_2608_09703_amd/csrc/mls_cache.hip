@@ -14,7 +14,8 @@ namespace mls {
 namespace {
 
 constexpr int kCacheThreads = 256;
-constexpr int kWriteUnroll = 4;  // chunks of a thread, of the keys and of the values each
+constexpr int kWriteUnroll = 4;  // chunks of a thread in flight, of the keys and of the values each
+constexpr int kTileHeads = 8;    // heads of a block's tile
 constexpr int kMoveBatch = 8;    // entries loaded before the first of them is stored
 
 // Chunk offset of entry `t` (head 0, layer 0) of sequence b in the pool; -1 where the
@@ -27,40 +28,53 @@ __device__ __forceinline__ int64_t entry_at(const CacheArgs& c, int64_t b, int64
   return id * c.s_page + (t & ((1 << c.page_log2) - 1)) * c.s_entry;
 }
 
-// Bound by its bytes: one read and one write of each. Thread order is (entry, head,
-// chunk), so that a wave reads 1 KB of contiguous rows and writes whole heads.
+// Bound by its bytes: one read and one write of each. A block takes 8 heads of the 16
+// entries of one run of a page, so that both sides move pieces of 2 KB and more (the
+// step's entries lie head behind head, a page's entry behind entry): entry after entry with
+// all heads, every write of a wave began at one place of a head's 4 KB, and five layers of
+// 102 trees took 27 us each.
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheWriteArgs a) {
   const int64_t b = blockIdx.y;
   const int32_t len = a.c.lengths[b];
   int32_t n = a.counts ? a.counts[b] : a.n;
   n = n < a.n ? n : a.n;
+  const int head_tiles = (a.c.kv_heads + kTileHeads - 1) / kTileHeads;
+  const int run = blockIdx.x / head_tiles;
+  const int h0 = (blockIdx.x - run * head_tiles) * kTileHeads;
   if (len < 0 || n <= 0) return;
-  const uint32_t per = (uint32_t)a.c.kv_heads * (uint32_t)a.c.chunks;
-  const uint32_t total = (uint32_t)n * per;
-  const uint32_t first = blockIdx.x * (uint32_t)(kCacheThreads * kWriteUnroll) + threadIdx.x;
-  uint4 rk[kWriteUnroll], rv[kWriteUnroll];
-  int64_t to[kWriteUnroll];
+  const int64_t t0 = (((int64_t)len >> 4) + run) << 4;  // the run's first entry
+  const int i0 = (int)(t0 - len);                       // ... and new entry: below 0 in front of them
+  if (i0 >= n) return;
+  const int64_t at = entry_at(a.c, b, t0);
+  if (at < 0) return;
+  const uint32_t chunks = (uint32_t)a.c.chunks;
+  const uint32_t total = 16u * kTileHeads * chunks;
+#pragma nounroll
+  for (uint32_t x0 = threadIdx.x; x0 < total; x0 += kCacheThreads * kWriteUnroll) {
+    u32x4_t rk[kWriteUnroll] = {}, rv[kWriteUnroll] = {};
+    int64_t to[kWriteUnroll];
 #pragma unroll
-  for (int u = 0; u < kWriteUnroll; ++u) {
-    const uint32_t x = first + u * kCacheThreads;
-    to[u] = -1;
-    if (x >= total) continue;
-    const uint32_t i = x / per;
-    const uint32_t hc = x - i * per;
-    const uint32_t h = hc / (uint32_t)a.c.chunks;
-    const uint32_t ch = hc - h * a.c.chunks;
-    const int64_t e = entry_at(a.c, b, (int64_t)len + i);
-    if (e < 0) continue;
-    to[u] = (e + h * a.c.s_head + ch) * 16;
-    const int64_t from = (b * a.s_batch + i * a.s_node + h * a.s_head + ch) * 16;
-    rk[u] = *reinterpret_cast<const uint4*>(a.k + from);
-    rv[u] = *reinterpret_cast<const uint4*>(a.v + from);
-  }
+    for (int u = 0; u < kWriteUnroll; ++u) {
+      const uint32_t x = x0 + u * kCacheThreads;
+      const uint32_t eh = x / chunks;
+      const uint32_t ch = x - eh * chunks;
+      const int h = h0 + (int)(eh % kTileHeads);
+      const int e = (int)(eh / kTileHeads);
+      const int i = i0 + e;
+      const bool in = x < total && i >= 0 && i < n && h < a.c.kv_heads;
+      to[u] = in ? (at + e * a.c.s_entry + h * a.c.s_head + ch) * 16 : -1;
+      // (a piece that is not there: the first one is read, and not used)
+      const int64_t from = in ? (b * a.s_batch + i * a.s_node + h * a.s_head + ch) * 16 : 0;
+      rk[u] = *reinterpret_cast<const u32x4_t*>(a.k + from);
+      rv[u] = *reinterpret_cast<const u32x4_t*>(a.v + from);
+    }
 #pragma unroll
-  for (int u = 0; u < kWriteUnroll; ++u) {
-    if (to[u] < 0) continue;
-    *reinterpret_cast<uint4*>(a.c.k + to[u]) = rk[u];
-    *reinterpret_cast<uint4*>(a.c.v + to[u]) = rv[u];
+    for (int u = 0; u < kWriteUnroll; ++u) {
+      if (to[u] >= 0) {
+        *reinterpret_cast<u32x4_t*>(a.c.k + to[u]) = rk[u];
+        *reinterpret_cast<u32x4_t*>(a.c.v + to[u]) = rv[u];
+      }
+    }
   }
 }
 
@@ -84,39 +98,42 @@ __global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompa
   const uint32_t h = hc / (uint32_t)a.c.chunks;
   const int64_t off = layer * a.c.s_layer + h * a.c.s_head + (hc - h * a.c.chunks);
   const int32_t* path = a.path + b * a.n;
+#pragma nounroll
   for (int j0 = 0; j0 <= acc; j0 += kMoveBatch) {
-    uint4 rk[kMoveBatch], rv[kMoveBatch];
+    u32x4_t rk[kMoveBatch] = {}, rv[kMoveBatch] = {};
     int64_t to[kMoveBatch];
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
       const int j = j0 + u;
-      to[u] = -1;
-      if (j > acc) continue;
-      const int32_t node = path[j];
-      if (node <= j || node >= a.n) continue;  // in place already, or no node of the tree
-      const int64_t src = entry_at(a.c, b, (int64_t)len + node);
+      const int32_t node = path[j <= acc ? j : 0];
+      const bool move = j <= acc && node > j && node < a.n;  // (else in place, or no node of the tree)
+      int64_t src = entry_at(a.c, b, (int64_t)len + (move ? node : 0));
       const int64_t dst = entry_at(a.c, b, (int64_t)len + j);
-      if (src < 0 || dst < 0) continue;
-      to[u] = (dst + off) * 16;
-      rk[u] = *reinterpret_cast<const uint4*>(a.c.k + (src + off) * 16);
-      rv[u] = *reinterpret_cast<const uint4*>(a.c.v + (src + off) * 16);
+      to[u] = move && src >= 0 && dst >= 0 ? (dst + off) * 16 : -1;
+      // (nothing to move: some entry that is there is read, and not used)
+      src = ((src >= 0 ? src : 0) + off) * 16;
+      rk[u] = *reinterpret_cast<const u32x4_t*>(a.c.k + src);
+      rv[u] = *reinterpret_cast<const u32x4_t*>(a.c.v + src);
     }
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
-      if (to[u] < 0) continue;
-      *reinterpret_cast<uint4*>(a.c.k + to[u]) = rk[u];
-      *reinterpret_cast<uint4*>(a.c.v + to[u]) = rv[u];
+      if (to[u] >= 0) {
+        *reinterpret_cast<u32x4_t*>(a.c.k + to[u]) = rk[u];
+        *reinterpret_cast<u32x4_t*>(a.c.v + to[u]) = rv[u];
+      }
     }
   }
 }
 
 }  // namespace
 
+int64_t cache_write_blocks(int64_t n, int64_t kv_heads) {
+  return ((n + 15) / 16 + 1) * ((kv_heads + kTileHeads - 1) / kTileHeads);
+}
+
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream) {
-  const int64_t total = (int64_t)a.n * a.c.kv_heads * a.c.chunks;
-  const int64_t per_block = kCacheThreads * kWriteUnroll;
-  hipLaunchKernelGGL(cache_write_kernel, dim3((unsigned)((total + per_block - 1) / per_block), (unsigned)a.c.batch),
-                     dim3(kCacheThreads), 0, stream, a);
+  const int64_t blocks = cache_write_blocks(a.n, a.c.kv_heads);
+  hipLaunchKernelGGL(cache_write_kernel, dim3((unsigned)blocks, (unsigned)a.c.batch), dim3(kCacheThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -521,6 +521,8 @@ struct AttnArgs {
   int32_t n_rt;    // row tiles
   int32_t splits;  // parts of the entries
   int32_t part;    // entries of a part
+  int32_t shorts;  // attn_short: one part, more waves to a block
+  int32_t once;    // entries are read once, and then not for long
   float* acc;      // [batch][kv_heads][n_rt][splits][tile rows][D] partial sums, if splits > 1
   float* ml;       // and [..][tile rows][2]: their maximum and sum of weights
 };
@@ -629,10 +631,12 @@ int tree_ready_nodes(int64_t batch, int64_t n);
 size_t tree_ready_bytes(int64_t batch, int64_t n);
 void tree_ready_layout(TreeVerifyArgs& a, void* workspace);
 hipError_t launch_tree_verify(const TreeVerifyArgs& a, int ept, hipStream_t stream);
+int64_t cache_write_blocks(int64_t n, int64_t kv_heads);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
 // rows of a tile of tree attention, which read an entry's head once
 int attn_tile_rows(int32_t rows, int32_t head_bytes);
+bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes);
 hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
 hipError_t launch_finalize_rows(const RowArgs& a, hipStream_t stream);
