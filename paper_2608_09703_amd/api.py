@@ -879,7 +879,8 @@ def _attention_plan(q, k_pages, v_pages, page_table, lengths, parents):
     ld = _step_rows("tree_attention", q, "q", c, k_pages)
     n, heads = q[2][1], q[2][2]
     _ints("tree_attention", "parents", parents, (c.batch, n), q[1])
-    return c, n, heads, ld, c.head_dim ** -0.5
+    c.k = c.v = c.page_table = c.lengths = 16  # (no address is looked at for the size)
+    return c, n, heads, ld, c.head_dim ** -0.5, B.tree_attention_workspace(c, n, heads)
 
 
 def cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -941,11 +942,10 @@ def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
     in parts as the table's width has it, so pass the columns that are in use.
     """
     _no_grad("tree_attention", q, k_pages, v_pages)
-    c, n, heads, ld, default = _attention_plan(_meta(q), _meta(k_pages), _meta(v_pages), _meta(page_table),
-                                               _meta(lengths), _meta(parents))
+    c, n, heads, ld, default, ws_bytes = _attention_plan(_meta(q), _meta(k_pages), _meta(v_pages),
+                                                         _meta(page_table), _meta(lengths), _meta(parents))
     c = _with_addresses(c, k_pages, v_pages, page_table, lengths)
     dev = q.device
-    ws_bytes = B.tree_attention_workspace(c, n, heads)
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
     out = torch.empty(q.shape, dtype=q.dtype, device=dev)
     with _on(dev):

@@ -2315,10 +2315,11 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   if (D != 32 && D != 64 && D != 96 && D != 128 && D != 192 && D != 256)
     return fail(MLS_UNSUPPORTED, "head_dim=%d: attention takes 32, 64, 96, 128, 192 or 256", D);
   pl.rows = n * (heads / c->kv_heads);
-  pl.tile = attn_tile_rows((int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
+  const int64_t cap = c->table_pages * c->page_size;
+  pl.tile = attn_tile_rows((int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4),
+                           c->batch * c->kv_heads * ((cap + kPartLeast - 1) / kPartLeast));
   pl.n_rt = (pl.rows + pl.tile - 1) / pl.tile;
   const int64_t base = c->batch * c->kv_heads * pl.n_rt;
-  const int64_t cap = c->table_pages * c->page_size;
   const int64_t want = (kAttnBlocks + base - 1) / base;
   pl.part = std::min(std::max(round_up((cap + want - 1) / want, 128), kPartLeast), kPartMost);
   pl.shorts = attn_short(base, cap, (int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
@@ -2460,6 +2461,7 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   a.heads = (int32_t)heads;
   a.group = (int32_t)(heads / c->kv_heads);
   a.rows = (int32_t)pl.rows;
+  a.tile = (int32_t)pl.tile;
   a.n_rt = (int32_t)pl.n_rt;
   a.splits = (int32_t)pl.splits;
   a.part = (int32_t)pl.part;

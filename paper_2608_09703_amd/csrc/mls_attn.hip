@@ -542,7 +542,8 @@ void tree_attention_kernel(AttnArgs a) {
 
 // Joins the parts of a sequence that has several: a thread per four elements of a row.
 template <typename E>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D, int tile_rows) {
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D) {
+  const int tile_rows = a.tile;
   const int64_t per = (int64_t)a.n * a.heads * (D / 4);
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t b = i / per;
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D, int t
                l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
 }
 
-constexpr int kWideRow = 256;    // bytes of a head up to which a tile has 64 rows
+constexpr int kWideRow = 128;    // bytes of a head up to which a tile has 64 rows
 constexpr int kMiddleRow = 768;  // and 32
 constexpr int kShortRow = 384;   // and up to which kShortWaves waves of 16 rows have registers
 
@@ -598,7 +599,7 @@ template <typename E, int D>
 hipError_t launch_attn_d(const AttnArgs& a, int64_t blocks, hipStream_t stream) {
   constexpr int kHeadBytes = D * E::kBytes;
   constexpr int kMost = kHeadBytes <= kWideRow ? 4 : kHeadBytes <= kMiddleRow ? 2 : 1;  // 16 rows each
-  switch (attn_tile_rows(a.rows, kHeadBytes)) {
+  switch (a.tile) {
     case 16:
       if constexpr (kHeadBytes <= kShortRow)
         if (a.shorts) return launch_attn_k<E, D, 1, kShortWaves, kLoadKeep>(a, blocks, stream);
@@ -633,13 +634,18 @@ hipError_t launch_attn(const AttnArgs& a, int D, int64_t blocks, hipStream_t str
 
 }  // namespace
 
-// Rows of a tile. Its queries and sums lie in registers, 512 of a lane, beside the
-// entries in flight.
-int attn_tile_rows(int32_t rows, int32_t head_bytes) {
-  const int most = head_bytes <= kWideRow ? 64 : head_bytes <= kMiddleRow ? 32 : 16;
-  return rows <= 16 ? 16 : rows <= 32 && most > 32 ? 32 : most;
+// Rows of a tile. Its queries and sums lie in registers beside the entries in flight; more
+// rows share each entry's load, but one wave a SIMD (heads of 128 and 64 rows) waits for
+// most of it: 16 sequences of 8,000 entries, 320 rows of each of two heads of 128 in tiles
+// of 64 / 32 / 16: 162 / 130 / 195 us; 64 rows of each of 16 heads of 64: 126 / 144 / 204.
+// `ways`: the tiles of one row tile that run side by side, in the shortest parts. Where they
+// would leave the chip idle, smaller tiles are shorter: 7 sequences of 900 entries, 36 rows
+// of 3 float32 heads of 64: 21 -> 16 us.
+int attn_tile_rows(int32_t rows, int32_t head_bytes, int64_t ways) {
+  int tile = head_bytes <= kWideRow ? 64 : head_bytes <= kMiddleRow ? 32 : 16;
+  while (tile > 16 && (rows <= tile / 2 || ways * ((rows + tile - 1) / tile) < 512)) tile /= 2;
+  return tile;
 }
-
 // blocks: of one part each; entries: that a table's row has room for
 bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes) {
   return blocks <= 256 && entries <= 1536 && rows <= 16 && head_bytes <= kShortRow;
@@ -651,11 +657,10 @@ hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStre
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t threads = a.c.batch * a.n * a.heads * (D / 4);
   const dim3 grid((unsigned)((threads + 255) / 256));
-  const int tile = attn_tile_rows(a.rows, D * (f32 ? 4 : 2));
   if (f32)
-    hipLaunchKernelGGL(attn_join_kernel<F32>, grid, dim3(256), 0, stream, a, (int)D, tile);
+    hipLaunchKernelGGL(attn_join_kernel<F32>, grid, dim3(256), 0, stream, a, (int)D);
   else
-    hipLaunchKernelGGL(attn_join_kernel<Bf16>, grid, dim3(256), 0, stream, a, (int)D, tile);
+    hipLaunchKernelGGL(attn_join_kernel<Bf16>, grid, dim3(256), 0, stream, a, (int)D);
   return hipGetLastError();
 }
 

@@ -518,6 +518,7 @@ struct AttnArgs {
   int32_t heads;
   int32_t group;   // query heads of a key head
   int32_t rows;    // n * group: rows that read one key head
+  int32_t tile;    // rows of a tile
   int32_t n_rt;    // row tiles
   int32_t splits;  // parts of the entries
   int32_t part;    // entries of a part
@@ -635,7 +636,7 @@ int64_t cache_write_blocks(int64_t n, int64_t kv_heads);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
 // rows of a tile of tree attention, which read an entry's head once
-int attn_tile_rows(int32_t rows, int32_t head_bytes);
+int attn_tile_rows(int32_t rows, int32_t head_bytes, int64_t ways);
 bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes);
 hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);
