@@ -683,7 +683,7 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
  * taken nodes from node 0 on, then -1; next_token int32 [batch], -1 where the verifier's row
  * keeps no token. Asynchronous on stream.
  */
-mls_status mls_tree_verify_workspace(int64_t batch, int64_t n, size_t* bytes);
+mls_status mls_tree_verify_workspace(const mls_sampling* s, int64_t batch, int64_t n, size_t* bytes);
 mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, const float* target_logits,
                            const float* draft_logits, const int32_t* tokens, const int32_t* parents,
                            const float* u_accept, const float* u_sample, const void* draft_params,

@@ -883,6 +883,63 @@ def _attention_plan(q, k_pages, v_pages, page_table, lengths, parents):
     return c, n, heads, ld, c.head_dim ** -0.5, B.tree_attention_workspace(c, n, heads)
 
 
+@functools.lru_cache(maxsize=256)
+def _verify_plan(target, tokens, parents, u_accept, u_sample, draft, draft_params, temperature, top_p, greedy):
+    _, dev, shape, _ = target
+    if dev < 0:
+        raise RuntimeError("tree_verify runs on the GPU only")
+    if len(shape) != 3:
+        raise ValueError("tree_verify: target_logits must be a [B, n, V] tensor")
+    Bt, n, V = shape
+    for what, x, want in (("target_logits", target, (Bt, n, V)), ("draft_logits", draft, (Bt, n, V)),
+                          ("u_accept", u_accept, (Bt, n)), ("u_sample", u_sample, (Bt,))):
+        if x is not None and (x[0] != torch.float32 or x[2] != want or x[1] != dev or not _packed(x[2], x[3])):
+            raise ValueError(f"tree_verify: {what} must be a contiguous float32 {list(want)} tensor on one device")
+    if tokens is None:
+        raise ValueError("tree_verify: tokens are required")
+    _ints("tree_verify", "tokens", tokens, (Bt, n), dev)
+    _ints("tree_verify", "parents", parents, (Bt, n), dev)
+    if draft_params is not None:
+        count = 1
+        for k in draft_params[2]:
+            count *= k
+        if draft_params[0] != torch.uint8 or draft_params[1] != dev or not _packed(draft_params[2], draft_params[3]) or \
+                count < Bt * n * B.ROW_PARAMS_BYTES:
+            raise ValueError("tree_verify: draft_params must be contiguous uint8 of B * n records")
+    s = B.make_sampling(V, temperature, top_p, greedy)
+    return Bt, n, s, B.tree_verify_workspace(s, Bt, n)
+
+
+@functools.lru_cache(maxsize=256)
+def _quant_plan(x):
+    dtype, dev, shape, stride = x
+    if dev < 0:
+        raise RuntimeError("quantize_rows runs on the GPU only")
+    if len(shape) != 2 or 0 in shape or (shape[1] > 1 and stride[1] != 1):
+        raise ValueError("quantize_rows: x must be a non-empty [T, d] tensor with neighbouring elements in a row")
+    T, d = shape
+    ld = stride[0] if T > 1 else d
+    if ld < d:
+        raise ValueError("quantize_rows: the rows of x must not overlap (an expanded x: call .contiguous())")
+    return T, d, ld, _dtype_code(dtype)
+
+
+@functools.lru_cache(maxsize=256)
+def _int8_plan(o, W, W_scale, out):
+    if o[1] < 0 or W[1] != o[1] or W_scale[1] != o[1]:
+        raise RuntimeError("head_logits_int8 runs on the GPU only, on tensors of one device")
+    if W[0] != torch.int8 or W_scale[0] != torch.float32:
+        raise TypeError("head_logits_int8: W must be int8 and W_scale float32")
+    if len(o[2]) != 2 or len(W[2]) != 2 or o[2][1] != W[2][1] or W_scale[2] != (W[2][0],) or \
+            not all(_packed(x[2], x[3]) for x in (o, W, W_scale)):
+        raise ValueError("o [T, d], W [V, d] and W_scale [V] must be contiguous with a shared d")
+    (T, d), V = o[2], W[2][0]
+    if out is not None and (out[0] != torch.float32 or out[2] != (T, V) or out[1] != o[1] or
+                            not _packed(out[2], out[3])):
+        raise ValueError("out must be a contiguous float32 [T, V] tensor")
+    return T, d, V, _dtype_code(o[0]), B.head_logits_int8_workspace(T, d)
+
+
 def cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
                 page_table: torch.Tensor, lengths: torch.Tensor, *, counts: Optional[torch.Tensor] = None) -> None:
     """Writes new entries ``k``, ``v [B, n, kv_heads, head_dim]`` behind the ``lengths [B]`` that each sequence has.
@@ -972,32 +1029,18 @@ def tree_verify(target_logits: torch.Tensor, tokens: torch.Tensor, parents: Opti
     uint8 records ``[B, n]`` from ``sample(params=)`` on the draft's rows with the same settings.
     """
     _no_grad("tree_verify", target_logits, draft_logits)
-    if not target_logits.is_cuda:
-        raise RuntimeError("tree_verify runs on the GPU only; got tensors on " + str(target_logits.device))
-    if target_logits.dim() != 3:
-        raise ValueError("tree_verify: target_logits must be a [B, n, V] tensor")
-    Bt, n, V = target_logits.shape
+    Bt, n, s, ws_bytes = _verify_plan(_meta(target_logits), _meta(tokens), _meta(parents), _meta(u_accept),
+                                      _meta(u_sample), _meta(draft_logits), _meta(draft_params),
+                                      ctypes.c_float(temperature).value, ctypes.c_float(top_p).value, bool(greedy))
     dev = target_logits.device
-    for what, x, shape in (("target_logits", target_logits, (Bt, n, V)), ("draft_logits", draft_logits, (Bt, n, V)),
-                           ("u_accept", u_accept, (Bt, n)), ("u_sample", u_sample, (Bt,))):
-        if x is not None and (x.dtype != torch.float32 or x.shape != shape or x.device != dev or
-                              not x.is_contiguous()):
-            raise ValueError(f"tree_verify: {what} must be a contiguous float32 {list(shape)} tensor on one device")
-    _ints("tree_verify", "tokens", _meta(tokens), (Bt, n), target_logits.get_device())
-    _ints("tree_verify", "parents", _meta(parents), (Bt, n), target_logits.get_device())
-    if draft_params is not None and (draft_params.dtype != torch.uint8 or not draft_params.is_contiguous() or
-                                     draft_params.device != dev or
-                                     draft_params.numel() < Bt * n * B.ROW_PARAMS_BYTES):
-        raise ValueError("tree_verify: draft_params must be contiguous uint8 of B * n records")
     ptr = (lambda x: x.data_ptr() if x is not None else None)
-    s = _sampling(V, temperature, top_p, greedy)
     out = torch.empty(Bt * (n + 2), dtype=torch.int32, device=dev)
     n_acc, path, nxt = out[:Bt], out[Bt:Bt * (n + 1)].view(Bt, n), out[Bt * (n + 1):]
-    ws_bytes = 0 if greedy else B.tree_verify_workspace(Bt, n)
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    to = out.data_ptr()
     with _on(dev):
         B.tree_verify(s, Bt, n, target_logits.data_ptr(), ptr(draft_logits), tokens.data_ptr(), ptr(parents),
-                      ptr(u_accept), ptr(u_sample), n_acc.data_ptr(), path.data_ptr(), nxt.data_ptr(), ptr(ws), ws_bytes,
+                      ptr(u_accept), ptr(u_sample), to, to + 4 * Bt, to + 4 * Bt * (n + 1), ptr(ws), ws_bytes,
                       _stream(dev), draft_params=ptr(draft_params))
     return n_acc, path, nxt
 
@@ -1009,17 +1052,12 @@ def quantize_rows(x: torch.Tensor):
     :func:`head_logits_int8` takes a head's weights.
     """
     _no_grad("quantize_rows", x)
-    if not x.is_cuda:
-        raise RuntimeError("quantize_rows runs on the GPU only; got a tensor on " + str(x.device))
-    if x.dim() != 2:
-        raise ValueError("quantize_rows: x must be a [T, d] tensor")
-    rows, ld = _norm_rows(x)
-    T, d = rows.shape
-    q = torch.empty(T, d, dtype=torch.int8, device=x.device)
-    scale = torch.empty(T, dtype=torch.float32, device=x.device)
-    with _on(x.device):
-        B.quantize_rows(T, d, ld, _dtype_code(x.dtype), rows.data_ptr(), q.data_ptr(), scale.data_ptr(),
-                        _stream(x.device))
+    T, d, ld, code = _quant_plan(_meta(x))
+    dev = x.device
+    q = torch.empty(T, d, dtype=torch.int8, device=dev)
+    scale = torch.empty(T, dtype=torch.float32, device=dev)
+    with _on(dev):
+        B.quantize_rows(T, d, ld, code, x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(dev))
     return q, scale
 
 
@@ -1028,24 +1066,18 @@ def head_logits_int8(o: torch.Tensor, W: torch.Tensor, W_scale: torch.Tensor, ou
     :func:`quantize_rows`: half the bytes of bf16. The rows of ``o [T, d]`` (bf16 or float32) are made 8-bit integers
     in the same way, and the products are summed exactly. ``d`` is a multiple of 16.
     """
-    _no_grad("head_logits_int8", o, W_scale)
-    if not o.is_cuda or W.device != o.device or W_scale.device != o.device:
-        raise RuntimeError("head_logits_int8 runs on the GPU only, on tensors of one device")
-    if W.dtype != torch.int8 or W_scale.dtype != torch.float32:
-        raise TypeError("head_logits_int8: W must be int8 and W_scale float32")
-    if o.dim() != 2 or W.dim() != 2 or o.shape[1] != W.shape[1] or W_scale.shape != (W.shape[0],) or \
-            not (o.is_contiguous() and W.is_contiguous() and W_scale.is_contiguous()):
-        raise ValueError("o [T, d], W [V, d] and W_scale [V] must be contiguous with a shared d")
-    dev, (T, d), V = o.device, o.shape, W.shape[0]
-    if out is None:
+    _no_grad("head_logits_int8", o, W_scale, out)
+    T, d, V, code, ws_bytes = _int8_plan(_meta(o), _meta(W), _meta(W_scale), _meta(out))
+    dev = o.device
+    given = out is not None
+    if not given:
         out = torch.empty(T, V, dtype=torch.float32, device=dev)
-    elif out.dtype != torch.float32 or out.shape != (T, V) or out.device != dev or not out.is_contiguous():
-        raise ValueError("out must be a contiguous float32 [T, V] tensor")
-    ws_bytes = B.head_logits_int8_workspace(T, d)
     ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
     with _on(dev):
-        B.head_logits_int8(T, V, d, _dtype_code(o.dtype), o.data_ptr(), W.data_ptr(), W_scale.data_ptr(),
-                           out.data_ptr(), ws.data_ptr(), ws_bytes, _stream(dev))
+        B.head_logits_int8(T, V, d, code, o.data_ptr(), W.data_ptr(), W_scale.data_ptr(), out.data_ptr(),
+                           ws.data_ptr(), ws_bytes, _stream(dev))
+    if given:
+        _written(out)
     return out
 
 

@@ -261,7 +261,7 @@ def lib():
         L.mls_tree_attention_workspace.argtypes = [K, i64, i64, sz]
         L.mls_tree_attention.argtypes = [K, i64, i64, vp, i64, i64, i64, vp, ctypes.c_float, vp, vp, ctypes.c_size_t,
                                          vp]
-        L.mls_tree_verify_workspace.argtypes = [i64, i64, sz]
+        L.mls_tree_verify_workspace.argtypes = [S, i64, i64, sz]
         L.mls_tree_verify.argtypes = [S, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.mls_quantize_rows.argtypes = [i64, i64, i64, ctypes.c_int32, vp, vp, vp, vp]
         L.mls_head_logits_quantized_workspace.argtypes = [i64, i64, sz]
@@ -542,9 +542,9 @@ def tree_attention(c: KVCache, n: int, heads: int, q: int, ld: Sequence[int], pa
                                    ws_bytes, stream), "mls_tree_attention")
 
 
-def tree_verify_workspace(batch: int, n: int) -> int:
+def tree_verify_workspace(s: Sampling, batch: int, n: int) -> int:
     b = ctypes.c_size_t(0)
-    check(lib().mls_tree_verify_workspace(batch, n, ctypes.byref(b)), "mls_tree_verify_workspace")
+    check(lib().mls_tree_verify_workspace(ctypes.byref(s), batch, n, ctypes.byref(b)), "mls_tree_verify_workspace")
     return b.value
 
 

@@ -2334,7 +2334,15 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   return MLS_OK;
 }
 
-size_t tree_ws_bytes(int64_t batch, int64_t n) { return align256(tree_ready_bytes(batch, n)); }
+size_t tree_ws_bytes(const mls_sampling* s, int64_t batch, int64_t n) {
+  if (s->greedy) return 0;
+  TreeVerifyArgs a;
+  memset(&a, 0, sizeof(a));
+  a.batch = batch;
+  a.n = (int32_t)n;
+  a.V = (int32_t)s->V;
+  return align256(tree_workspace(a, nullptr));
+}
 
 mls_status validate_tree(int64_t batch, int64_t n) {
   if (batch < 1 || batch > (1 << 24) || n < 1 || n > kMaxNodes)
@@ -2479,12 +2487,13 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   return MLS_OK;
 }
 
-mls_status mls_tree_verify_workspace(int64_t batch, int64_t n, size_t* bytes) {
+mls_status mls_tree_verify_workspace(const mls_sampling* s, int64_t batch, int64_t n, size_t* bytes) {
   g_last_error.clear();
-  mls_status st = validate_tree(batch, n);
+  mls_status st = validate_sampling(s);
   if (st != MLS_OK) return st;
+  if ((st = validate_tree(batch, n)) != MLS_OK) return st;
   if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
-  *bytes = tree_ws_bytes(batch, n);
+  *bytes = tree_ws_bytes(s, batch, n);
   return MLS_OK;
 }
 
@@ -2502,8 +2511,9 @@ mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, cons
   if (!s->greedy && (!u_sample || (n > 1 && !u_accept)))
     return fail(MLS_INVALID_ARG, "sampling needs u_accept and u_sample");
   if (draft_params && !draft_logits) return fail(MLS_INVALID_ARG, "draft_params go with draft_logits");
-  if (!s->greedy && tree_ws_bytes(batch, n) && (!workspace || workspace_bytes < tree_ws_bytes(batch, n)))
-    return fail(MLS_WORKSPACE_TOO_SMALL, "verification needs %zu workspace bytes, got %zu", tree_ws_bytes(batch, n),
+  const size_t need = tree_ws_bytes(s, batch, n);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(MLS_WORKSPACE_TOO_SMALL, "verification needs %zu workspace bytes, got %zu", need,
                 workspace ? workspace_bytes : 0);
   if (!aligned(workspace, 16)) return fail(MLS_INVALID_ARG, "misaligned workspace");
   for (const void* p : {(const void*)target_logits, (const void*)draft_logits, (const void*)tokens,
@@ -2532,10 +2542,7 @@ mls_status mls_tree_verify(const mls_sampling* s, int64_t batch, int64_t n, cons
   a.temperature = s->temperature;
   a.inv_temp = s->greedy ? 1.f : 1.f / s->temperature;
   a.top_p = s->top_p;
-  if (!s->greedy) {
-    a.ready = tree_ready_nodes(batch, n);
-    tree_ready_layout(a, workspace);
-  }
+  if (!s->greedy) tree_workspace(a, workspace);
   {
     ProfScope ps("tree_verify", hs);
     e = launch_tree_verify(a, row_elems_per_thread(s->V), hs);

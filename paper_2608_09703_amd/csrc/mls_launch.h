@@ -552,6 +552,11 @@ struct TreeVerifyArgs {
   void* ready_rows;
   double* list_p;
   int32_t* list_idx;
+  // lists of large distributions at the walk's present node, [batch][V]
+  double* large_p;
+  double* large_p2;
+  double* large_q;
+  int32_t* large_idx;
 };
 // Rows as 8-bit integers.
 struct QuantArgs {
@@ -628,10 +633,9 @@ hipError_t launch_verify(const VerifyArgs& a, int ept, hipStream_t stream);
 void head_i8_tile(int64_t T, int64_t V, int* rows, int* cols);
 hipError_t launch_head_logits_i8(const HeadArgs& a, hipStream_t stream);
 hipError_t launch_quantize_rows(const QuantArgs& a, hipStream_t stream);
-int tree_ready_nodes(int64_t batch, int64_t n);
-size_t tree_ready_bytes(int64_t batch, int64_t n);
-void tree_ready_layout(TreeVerifyArgs& a, void* workspace);
-hipError_t launch_tree_verify(const TreeVerifyArgs& a, int ept, hipStream_t stream);
+// Lays the workspace out (batch, n and V are set) and returns its bytes.
+size_t tree_workspace(TreeVerifyArgs& a, void* workspace);
+hipError_t launch_tree_verify(TreeVerifyArgs a, int ept, hipStream_t stream);
 int64_t cache_write_blocks(int64_t n, int64_t kv_heads);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
