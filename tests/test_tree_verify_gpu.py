@@ -74,6 +74,16 @@ def test_greedy(Bt, n, V):
     assert taken > 0
 
 
+@pytest.mark.parametrize("V,top_p,sampled", [(300, 0.9, True), (1500, 1.0, True), (1500, 1.0, False)])
+def test_more_trees_than_rows_are_opened_beforehand(V, top_p, sampled):
+    rng = np.random.default_rng(V)
+    Bt, n = 530, 4
+    parents, target, draft, tokens, ua, us = _inputs(rng, Bt, n, V, 0.7, sampled)
+    got = _run(parents, target, draft if sampled else None, tokens, ua, us, temperature=0.7, top_p=top_p)
+    _same(got, O.verify(target, tokens, parents, ua, us, float(np.float32(0.7)), float(np.float32(top_p)),
+                        draft if sampled else None))
+
+
 def test_a_chain_gives_what_chain_verification_gives():
     rng = np.random.default_rng(5)
     Bt, G, V = 40, 5, 1200
