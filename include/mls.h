@@ -601,7 +601,7 @@ typedef struct mls_kv_cache {
   int64_t layers;             /* layers of the pool (mls_cache_compact); the others take 1 */
   int64_t pages;              /* pages of a layer, 1..2^31 - 1 */
   int64_t batch;              /* sequences, 1..65535 */
-  int64_t table_pages;        /* pages a row of the table holds, >= 1; with page_size below 2^31 entries */
+  int64_t table_pages;        /* pages a row of the table holds, >= 1; at most 2^31 - 65537 entries */
   int64_t ld_layer;
   int64_t ld_page;
   int64_t ld_head;

@@ -2236,7 +2236,7 @@ mls_status validate_cache(const mls_kv_cache* c, int64_t layers_max) {
     return fail(MLS_INVALID_ARG, "layers=%lld out of [1, %lld]", (long long)c->layers, (long long)layers_max);
   if (c->pages < 1 || c->pages > 0x7fffffff) return fail(MLS_INVALID_ARG, "pages=%lld out of range", (long long)c->pages);
   if (c->batch < 1 || c->batch > 65535) return fail(MLS_INVALID_ARG, "batch=%lld out of range", (long long)c->batch);
-  if (c->table_pages < 1 || c->table_pages > 0x7fffffff / c->page_size)
+  if (c->table_pages < 1 || c->table_pages > (0x7fffffff - 65536) / c->page_size)
     return fail(MLS_INVALID_ARG, "table_pages=%lld out of range", (long long)c->table_pages);
   if (c->ld_table < c->table_pages) return fail(MLS_INVALID_ARG, "the table's rows overlap");
   const int64_t lds[4] = {c->ld_layer, c->ld_page, c->ld_head, c->ld_entry};

@@ -359,13 +359,35 @@ void tree_attention_kernel(AttnArgs a) {
   if (sp > 0 && t_begin >= total) return;
   const bool alone = total <= a.part;  // the sequence has one part
 
+  A w;
+  // pages of a tile's runs of 16 entries; without one, page 0's bytes are read and not used
+  const int32_t* table = a.c.table + (int64_t)b * a.c.table_ld;
+  auto pages_of = [&](int t0, int32_t (&id)[SUBS], bool (&ok)[SUBS]) {
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      const int64_t pg = (t0 + 16 * s) >> a.c.page_log2;
+      ok[s] = t0 + 16 * s < total && pg < a.c.table_pages;
+      const int32_t p = __builtin_amdgcn_readfirstlane(ok[s] ? table[pg] : -1);
+      ok[s] = p >= 0 && p < a.c.pages;
+      id[s] = ok[s] ? p : 0;
+    }
+  };
+
+  int t0 = t_begin + wave * A::KT;
+  int32_t id[SUBS];
+  bool ok[SUBS];
+  if (t0 < t_end) {  // (under way while the tree is looked at)
+    pages_of(t0, id, ok);
+    w.load_k(a, id, hk, t0, lane);
+    w.load_v(a, id, hk, t0, lane);
+  }
+
   if (tid == 0) odd_sh = 0;
   if (tid < a.n) parent_sh[tid] = a.parents ? a.parents[(int64_t)b * a.n + tid] : tid - 1;
   __syncthreads();
   if (tid < a.n) see_sh[tid] = ancestors(parent_sh, tid, a.n);
   __syncthreads();
 
-  A w;
   unsigned long long see[RT];
   const int row0 = rt * ROWS;
 #pragma unroll
@@ -387,27 +409,6 @@ void tree_attention_kernel(AttnArgs a) {
     for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  // pages of a tile's runs of 16 entries; without one, page 0's bytes are read and not used
-  const int32_t* table = a.c.table + (int64_t)b * a.c.table_ld;
-  auto pages_of = [&](int t0, int32_t (&id)[SUBS], bool (&ok)[SUBS]) {
-#pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      const int64_t pg = (t0 + 16 * s) >> a.c.page_log2;
-      ok[s] = t0 + 16 * s < total && pg < a.c.table_pages;
-      const int32_t p = __builtin_amdgcn_readfirstlane(ok[s] ? table[pg] : -1);
-      ok[s] = p >= 0 && p < a.c.pages;
-      id[s] = ok[s] ? p : 0;
-    }
-  };
-
-  int t0 = t_begin + wave * A::KT;
-  int32_t id[SUBS];
-  bool ok[SUBS];
-  if (t0 < t_end) {
-    pages_of(t0, id, ok);
-    w.load_k(a, id, hk, t0, lane);
-    w.load_v(a, id, hk, t0, lane);
-  }
   for (; t0 < t_end; t0 += WAVES * A::KT) {
     const int tn = t0 + WAVES * A::KT;
     int32_t id_n[SUBS];

@@ -16,7 +16,7 @@ namespace {
 constexpr int kCacheThreads = 256;
 constexpr int kWriteUnroll = 4;  // chunks of a thread in flight, of the keys and of the values each
 constexpr int kTileHeads = 8;    // heads of a block's tile
-constexpr int kMoveBatch = 8;    // entries loaded before the first of them is stored
+constexpr int kMoveBatch = 4;    // entries loaded before the first of them is stored
 
 // Chunk offset of entry `t` (head 0, layer 0) of sequence b in the pool; -1 where the
 // table has no such page.
@@ -78,11 +78,17 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheWriteAr
   }
 }
 
-// Entry len + j takes what entry len + path[j] held, for j = 0 .. n_accepted. A thread
-// owns one chunk of one head for all j and goes through them in order, a batch of loads
-// before its stores: with path[j] >= j (nodes come after their ancestors) no entry is
-// overwritten before it has been read, and nothing needs a second buffer or a barrier.
+// Entry len + j takes what entry len + path[j] held, for j = 0 .. n_accepted. One wave
+// lists the moves that there are (many an accepted node is in place already). A thread
+// then owns one chunk of one head for all of them and goes through them in order, a batch
+// of loads before its stores: with path[j] > j (nodes come after their ancestors) no entry
+// is overwritten before it has been read, and nothing needs a second buffer or a barrier.
+// Bound by its chain of loads (length, path, table, entry): 102 sequences, five layers of 34
+// heads, two nodes accepted on average: 7 us.
 __global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompactArgs a) {
+  __shared__ int64_t from_sh[64];
+  __shared__ int64_t to_sh[64];
+  __shared__ int moves_sh;
   const int64_t b = blockIdx.y;
   const int32_t len = a.c.lengths[b];
   int32_t acc = a.n_accepted[b];
@@ -90,6 +96,23 @@ __global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompa
   const bool idle = len < 0 || acc < 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.new_lengths[b] = idle ? len : len + acc + 1;
   if (idle) return;
+  if (threadIdx.x < 64) {
+    const int j = threadIdx.x;
+    const int32_t node = j <= acc ? a.path[b * a.n + j] : -1;
+    const bool later = node > j && node < a.n;  // (else in place, or no node of the tree)
+    const int64_t from = later ? entry_at(a.c, b, (int64_t)len + node) : -1;
+    const int64_t to = later ? entry_at(a.c, b, (int64_t)len + j) : -1;
+    const bool move = from >= 0 && to >= 0;
+    const unsigned long long m = __ballot(move);
+    if (move) {
+      const int at = __builtin_popcountll(m & ((1ull << j) - 1));
+      from_sh[at] = from;
+      to_sh[at] = to;
+    }
+    if (j == 0) moves_sh = __builtin_popcountll(m);
+  }
+  __syncthreads();
+  const int moves = moves_sh;
   const uint32_t per = (uint32_t)a.c.kv_heads * (uint32_t)a.c.chunks;
   const uint32_t x = blockIdx.x * (uint32_t)kCacheThreads + threadIdx.x;
   const uint32_t layer = x / per;
@@ -97,30 +120,21 @@ __global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompa
   const uint32_t hc = x - layer * per;
   const uint32_t h = hc / (uint32_t)a.c.chunks;
   const int64_t off = layer * a.c.s_layer + h * a.c.s_head + (hc - h * a.c.chunks);
-  const int32_t* path = a.path + b * a.n;
 #pragma nounroll
-  for (int j0 = 0; j0 <= acc; j0 += kMoveBatch) {
-    u32x4_t rk[kMoveBatch] = {}, rv[kMoveBatch] = {};
-    int64_t to[kMoveBatch];
+  for (int m0 = 0; m0 < moves; m0 += kMoveBatch) {
+    u32x4_t rk[kMoveBatch], rv[kMoveBatch];
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
-      const int j = j0 + u;
-      const int32_t node = path[j <= acc ? j : 0];
-      const bool move = j <= acc && node > j && node < a.n;  // (else in place, or no node of the tree)
-      int64_t src = entry_at(a.c, b, (int64_t)len + (move ? node : 0));
-      const int64_t dst = entry_at(a.c, b, (int64_t)len + j);
-      to[u] = move && src >= 0 && dst >= 0 ? (dst + off) * 16 : -1;
-      // (nothing to move: some entry that is there is read, and not used)
-      src = ((src >= 0 ? src : 0) + off) * 16;
-      rk[u] = *reinterpret_cast<const u32x4_t*>(a.c.k + src);
-      rv[u] = *reinterpret_cast<const u32x4_t*>(a.c.v + src);
+      const int64_t from = (from_sh[m0 + u < moves ? m0 + u : m0] + off) * 16;
+      rk[u] = *reinterpret_cast<const u32x4_t*>(a.c.k + from);
+      rv[u] = *reinterpret_cast<const u32x4_t*>(a.c.v + from);
     }
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
-      if (to[u] >= 0) {
-        *reinterpret_cast<u32x4_t*>(a.c.k + to[u]) = rk[u];
-        *reinterpret_cast<u32x4_t*>(a.c.v + to[u]) = rv[u];
-      }
+      if (m0 + u >= moves) break;
+      const int64_t to = (to_sh[m0 + u] + off) * 16;
+      *reinterpret_cast<u32x4_t*>(a.c.k + to) = rk[u];
+      *reinterpret_cast<u32x4_t*>(a.c.v + to) = rv[u];
     }
   }
 }
