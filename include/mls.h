@@ -645,8 +645,9 @@ mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* pa
  * with the key head h / (heads / kv_heads). parents (device int32 [batch][n]; NULL: a chain)
  * holds each node's parent: -1 for one behind the context, else an earlier node. A node
  * with any other parent, or below such a node, is not there: its rows are zeros, and no
- * node attends to it. One that has nothing to attend to gives zeros too. Keys and values
- * that a row does not attend to do not matter to it, whatever they hold.
+ * node attends to it. One that has nothing to attend to, or whose scores are all -inf, gives
+ * zeros too. Keys and values that a row does not attend to do not matter to it, whatever they
+ * hold.
  * q [batch][n][heads][head_dim] has strides like mls_cache_write's k; out is contiguous, of
  * the cache's dtype, 16-byte aligned. n in 1..64, heads a multiple of kv_heads, head_dim
  * 32, 64, 96, 128, 192 or 256, scale finite and > 0. Sums are fp32; bf16 weights are rounded to bfloat16 for the

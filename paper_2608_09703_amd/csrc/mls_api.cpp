@@ -2449,7 +2449,7 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   if ((st = validate_rows("q", q, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if (!out || !aligned(out, 16)) return fail(MLS_INVALID_ARG, "out must be non-NULL and 16-byte aligned");
   if (!aligned(parents, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
-  if (!isfinite(scale) || !(scale > 0.f)) return fail(MLS_INVALID_ARG, "scale must be finite and > 0");
+  if (!isfinite(scale * kLog2e) || !(scale > 0.f)) return fail(MLS_INVALID_ARG, "scale must be finite and > 0");
   if (pl.bytes && (!workspace || workspace_bytes < pl.bytes))
     return fail(MLS_WORKSPACE_TOO_SMALL, "attention needs %zu workspace bytes, got %zu", pl.bytes,
                 workspace ? workspace_bytes : 0);

@@ -285,10 +285,18 @@ __device__ __forceinline__ void store_out(void* out, int64_t i, float4 v) {
   }
 }
 
-// Entries that sequence b has in all: context and nodes; 0 for one that takes no part.
-__device__ __forceinline__ int entries(const AttnArgs& a, int64_t b) {
+// What sequence b attends to: `ctx` entries of context, and with its nodes' `total`, as far as
+// the table's row reaches (the parts cover no more); 0 for one that takes no part.
+struct Span {
+  int ctx;
+  int total;
+};
+__device__ __forceinline__ Span span_of(const AttnArgs& a, int64_t b) {
   const int32_t len = a.c.lengths[b];
-  return len < 0 || len > 0x7fffffff - a.n ? 0 : len + a.n;
+  if (len < 0) return {0, 0};
+  const int64_t room = a.c.table_pages << a.c.page_log2;
+  const int64_t all = (int64_t)len + a.n;
+  return {len, (int)(all < room ? all : room)};
 }
 
 // Adds the infinities and NaN among elements d .. d + 3 of the values of the nodes `see`
@@ -297,7 +305,7 @@ template <typename E>
 __device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d, unsigned long long see, int t_begin,
                                      int t_end, int ctx, float4& v) {
   for (int j = 0; j < a.n; ++j) {
-    const int t = ctx + j;
+    const int64_t t = (int64_t)ctx + j;
     const int64_t pg = t >> a.c.page_log2;
     if (!((see >> j) & 1) || t < t_begin || t >= t_end || pg >= a.c.table_pages) continue;
     const int32_t id = a.c.table[(int64_t)b * a.c.table_ld + pg];
@@ -352,8 +360,9 @@ void tree_attention_kernel(AttnArgs a) {
   const int hk = x % a.c.kv_heads;
   const int b = x / a.c.kv_heads;
 
-  const int total = entries(a, b);
-  const int ctx = total - a.n;
+  const Span span = span_of(a, b);
+  const int total = span.total;
+  const int ctx = span.ctx;
   const int t_begin = (int)((int64_t)sp * a.part < total ? sp * a.part : total);
   const int t_end = total - t_begin > a.part ? t_begin + a.part : total;
   if (sp > 0 && t_begin >= total) return;
@@ -549,7 +558,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t b = i / per;
   if (b >= a.c.batch) return;
-  const int total = entries(a, b);
+  const int total = span_of(a, b).total;
   if (total <= a.part) return;
   const int in = (int)(i - b * per);
   const int d = 4 * (in % (D / 4));
@@ -558,9 +567,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D) {
   const int h = nh - node * a.heads;
   const int hk = h / a.group;
   const int r = node * a.group + (h - hk * a.group);
-  // (entries past the table's row are in no part)
-  const int all = (int)(((int64_t)total + a.part - 1) / a.part);
-  const int parts = all < a.splits ? all : a.splits;
+  const int parts = (total + a.part - 1) / a.part;
   const int64_t rec = (((b * a.c.kv_heads + hk) * a.n_rt + r / tile_rows) * a.splits) * tile_rows + r % tile_rows;
   float m = -INFINITY;
   for (int s = 0; s < parts; ++s) {

@@ -23,7 +23,9 @@ namespace mls {
 namespace {
 
 constexpr int kQuantThreads = 256;
-constexpr int kFewRows = 4096;  // rows up to which a block takes one at a time
+// Rows up to which a block takes one at a time. d = 4,352, bf16, a block / a wave to a row: 8,192
+// rows 28.8 / 32.5 us, 16,384 53.5 / 49.7, 49,152 145 / 128 (5.0 TB/s).
+constexpr int kFewRows = 8192;
 
 // The integer next to x / s.
 __device__ __forceinline__ int quantize(float x, float s) {

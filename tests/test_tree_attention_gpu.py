@@ -61,8 +61,8 @@ def _check(got, want, bound):
     assert np.array_equal(np.isnan(got), np.isnan(want)), "NaN"
     inf = np.isinf(want)
     assert np.array_equal(got[inf], want[inf])
-    rest = ~inf & ~np.isnan(want)
-    err = np.abs(got - want)[rest]
+    rest = np.isfinite(want)
+    err = np.abs(got[rest] - want[rest])
     assert (err <= bound[rest] + 1e-30).all(), float((err - bound[rest]).max())
 
 
@@ -177,7 +177,7 @@ def test_scores_of_very_different_sizes():
     np.testing.assert_allclose(got.cpu().numpy(), want, rtol=0, atol=3 * 2.0 ** -23 * 4)
 
 
-def test_pages_that_are_not_there_and_lengths_past_the_table():
+def test_pages_that_are_not_there():
     rng = np.random.default_rng(12)
     n = 3
     c = Cache(rng, [70, 40, 60, 50], n, 1, 32, 16, torch.float32)
@@ -192,15 +192,31 @@ def test_pages_that_are_not_there_and_lengths_past_the_table():
     for t in range(16):
         k[1][t] = None
     k[2] = [None] * len(k[2])
-    lengths = c.lengths.copy()
-    lengths[3] = 2 ** 31 - 1       # behind any page: the table's entries alone would be context, the nodes are not there
     q = values(rng, (4, n, 2, 32), torch.float32)
     got = D.tree_attention(torch.tensor(q, device=DEV).float(), c.k[0], c.v[0], torch.tensor(table, device=DEV),
-                           torch.tensor(lengths, device=DEV), torch.tensor(parents, device=DEV))
-    want = O.attention(q[:3], k[:3], v[:3], [70, 40, 60], parents[:3])
-    bound = _bound(q[:3], k[:3], v[:3], [70, 40, 60], parents[:3], torch.float32, want)
-    _check(got[:3], want, bound)
-    assert (got[2] == 0).all() and (got[3] == 0).all()
+                           c.t_lengths, torch.tensor(parents, device=DEV))
+    want = O.attention(q, k, v, [70, 40, 60, 50], parents)
+    _check(got, want, _bound(q, k, v, [70, 40, 60, 50], parents, torch.float32, want))
+    assert (got[2] == 0).all()
+
+
+@pytest.mark.parametrize("pages", [2, 40])  # in one part, and in several
+@pytest.mark.parametrize("past", [0, 1, 500, 2 ** 31 - 1])
+def test_lengths_past_the_table(pages, past):
+    """A context that fills the table's row or goes beyond it: what the row names is the context, the nodes are not
+    there."""
+    rng = np.random.default_rng(pages)
+    n, room = 5, 16 * pages
+    c = Cache(rng, [room - n], n, 1, 32, 16, torch.float32)
+    assert c.per == pages
+    chain = np.array([np.arange(-1, n - 1)], np.int32)
+    k, v = _fill(rng, c, torch.float32, chain)
+    lengths = torch.tensor([min(room + past, 2 ** 31 - 1)], dtype=torch.int32, device=DEV)
+    q = values(rng, (1, n, 2, 32), torch.float32)
+    got = D.tree_attention(torch.tensor(q, device=DEV).float(), c.k[0], c.v[0], c.t_table, lengths)
+    k, v = ([x[0] + [None] * n] for x in (k, v))
+    want = O.attention(q, k, v, [room], chain)
+    _check(got, want, _bound(q, k, v, [room], chain, torch.float32, want))
 
 
 def test_streams_graphs_and_repeats():
