@@ -2292,6 +2292,7 @@ mls_status validate_rows(const char* what, const void* p, int64_t es, int64_t ld
 // heads, and parts of kPartMost entries at most, so that one long sequence among short
 // ones does not run alone at the end.
 constexpr int64_t kAttnBlocks = 1024;
+constexpr int64_t kManyBlocks = 512;
 constexpr int64_t kPartLeast = 256;
 constexpr int64_t kPartMost = 4096;
 
@@ -2299,7 +2300,8 @@ constexpr int64_t kPartMost = 4096;
 constexpr int64_t kMemorySideBytes = 256ll << 20;
 
 struct AttnPlan {
-  int64_t rows, tile, n_rt, part, splits, records;
+  int64_t rows, tile, n_rt, n_tiles, part, splits, records;
+  bool many;
   bool shorts;  // one part, more waves to a block
   bool once;
   size_t acc_bytes, bytes;
@@ -2316,11 +2318,15 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
     return fail(MLS_UNSUPPORTED, "head_dim=%d: attention takes 32, 64, 96, 128, 192 or 256", D);
   pl.rows = n * (heads / c->kv_heads);
   const int64_t cap = c->table_pages * c->page_size;
-  pl.tile = attn_tile_rows((int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4),
-                           c->batch * c->kv_heads * ((cap + kPartLeast - 1) / kPartLeast));
-  pl.n_rt = (pl.rows + pl.tile - 1) / pl.tile;
+  const int64_t ways = c->batch * c->kv_heads * ((cap + kPartLeast - 1) / kPartLeast);
+  pl.tile = attn_tile_rows((int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4), ways);
+  pl.many = attn_many((int32_t)pl.rows, D, c->dtype == MLS_F32, ways);
+  if (pl.many) pl.tile = attn_many_tile();
+  const int64_t per = pl.many ? attn_many_tiles() : 1;  // tiles of a block
+  pl.n_rt = (pl.rows + pl.tile * per - 1) / (pl.tile * per);
+  pl.n_tiles = pl.n_rt * per;
   const int64_t base = c->batch * c->kv_heads * pl.n_rt;
-  const int64_t want = (kAttnBlocks + base - 1) / base;
+  const int64_t want = pl.many ? std::max<int64_t>(kManyBlocks / base, 1) : (kAttnBlocks + base - 1) / base;
   pl.part = std::min(std::max(round_up((cap + want - 1) / want, 128), kPartLeast), kPartMost);
   pl.shorts = attn_short(base, cap, (int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
   if (pl.shorts) pl.part = round_up(cap, 128);
@@ -2328,7 +2334,7 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   if (base * pl.splits > 0x7fffff00 - 8 * pl.n_rt || c->batch * n * heads * (D / 4) > (1ll << 38))
     return fail(MLS_UNSUPPORTED, "%lld parts of the cache are more than one launch takes", (long long)(base * pl.splits));
   pl.once = pl.n_rt == 1 && c->batch * cap * c->kv_heads * D * (c->dtype == MLS_BF16 ? 4 : 8) > kMemorySideBytes;
-  pl.records = pl.splits > 1 ? base * pl.splits * pl.tile : 0;
+  pl.records = pl.splits > 1 ? c->batch * c->kv_heads * pl.n_tiles * pl.splits * pl.tile : 0;
   pl.acc_bytes = align256((size_t)pl.records * D * 4);
   pl.bytes = pl.acc_bytes + align256((size_t)pl.records * 8);
   return MLS_OK;
@@ -2471,6 +2477,8 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
   a.rows = (int32_t)pl.rows;
   a.tile = (int32_t)pl.tile;
   a.n_rt = (int32_t)pl.n_rt;
+  a.n_tiles = (int32_t)pl.n_tiles;
+  a.many = pl.many;
   a.splits = (int32_t)pl.splits;
   a.part = (int32_t)pl.part;
   a.shorts = pl.shorts;

@@ -271,6 +271,100 @@ struct Attn {
     }
     return odd;
   }
+
+  // Queries of the rows from row0 on, and the nodes they see.
+  __device__ __forceinline__ void take_rows(const AttnArgs& a, int b, int hk, int row0, bool any,
+                                            const unsigned long long* nodes, unsigned long long (&see)[RT], int lane) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int r = row0 + 16 * t + (lane & 15);
+      const bool in = r < a.rows && any;
+      const int node = in ? r / a.group : 0;
+      const int h = hk * a.group + (in ? r - node * a.group : 0);
+      see[t] = in ? nodes[node] : 0;
+      const char* q = a.q + ((int64_t)b * a.q_batch + (int64_t)node * a.q_node + (int64_t)h * a.q_head) * 16;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        qf[t][c] = make_uint4(0u, 0u, 0u, 0u);
+        if (in) qf[t][c] = *reinterpret_cast<const uint4*>(q + 64 * c + 16 * (lane >> 4));
+      }
+      m[t] = kNoMax;
+      l[t] = 0.f;
+#pragma unroll
+      for (int mm = 0; mm < DE; ++mm) acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // The scores of the tile at entry t0 become weights (for bf16 products in pb), maxima and
+  // sums of weights follow; true where nodes' values were infinite or NaN.
+  __device__ __forceinline__ bool weigh(f32x4_t (&s)[RT][SUBS], uint4 (&pb)[RT], const AttnArgs& a,
+                                        const unsigned long long (&see)[RT], int t0, int ctx, const bool (&ok)[SUBS],
+                                        int lane) {
+    bool odd = false;
+    bool whole = t0 + KT <= ctx;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) whole = whole && ok[u];
+    if (!whole) {
+      mask(s, see, t0 - ctx, a.n, ok, lane);
+      odd = take_out_odd(t0 - ctx, lane);
+    }
+    // (a NaN score passes neither test and makes its row NaN)
+    float top[RT];
+    bool grow = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      top[t] = s[t][0][0];
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][u][i]);
+      top[t] *= a.scale;  // (above 0)
+      grow = grow || top[t] > m[t] + kMaxSlack;
+    }
+    if (__ballot(grow) != 0) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(m[t], mx);
+        const float f = m[t] == mn ? 1.f : fast_exp2(m[t] - mn);
+        m[t] = mn;
+        l[t] *= f;
+#pragma unroll
+        for (int mm = 0; mm < DE; ++mm) acc[t][mm] *= f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[t][u][i] = fast_exp2(fmaf(s[t][u][i], a.scale, -m[t]));
+          l[t] += s[t][u][i];
+        }
+      // bf16 weights, as the values are: up to 2^-8 of each, in both directions
+      pb[t] = pack_weights(s[t]);
+    }
+    return odd;
+  }
+
+  __device__ __forceinline__ void add_values(const f32x4_t (&s)[RT][SUBS], const uint4 (&pb)[RT]) {
+#pragma unroll
+    for (int mm = 0; mm < DE; ++mm)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) acc[t][mm] = v_product(vf, mm, s[t], pb[t], acc[t][mm]);
+  }
+
+  // Row tile t's sums times f to LDS, row after row.
+  __device__ __forceinline__ void put_sums(float (*o)[LD], int t, float f, int lane) const {
+    float* p = &o[lane & 15][4 * DE * (lane >> 4)];
+#pragma unroll
+    for (int j = 0; j < 4 * DE; j += 4)
+      *reinterpret_cast<float4*>(p + j) =
+          make_float4(acc[t][j % DE][j / DE] * f, acc[t][(j + 1) % DE][(j + 1) / DE] * f,
+                      acc[t][(j + 2) % DE][(j + 2) / DE] * f, acc[t][(j + 3) % DE][(j + 3) / DE] * f);
+  }
 };
 
 template <typename E>
@@ -330,6 +424,70 @@ __device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d,
   }
 }
 
+// What a block works on.
+struct Block {
+  int b, hk, sp;
+  int tile;            // row tile
+  int t_begin, t_end;  // entries
+  int ctx;
+  bool alone;  // the sequence has one part
+};
+
+// Four elements of a row whose sums are complete in the block: the result, or a part's sums
+// (v; l the sum of weights, relative to mm).
+template <typename E, int D>
+__device__ __forceinline__ void end_row(const AttnArgs& a, const Block& at, int tile_rows, int row,
+                                        const unsigned long long* nodes, bool odd, int d, float mm, float l, float4 v) {
+  const int node = row / a.group;
+  const unsigned long long see = nodes[node];
+  if (odd) add_odd<E>(a, at.b, at.hk, d, see, at.t_begin, at.t_end, at.ctx, v);
+  if (at.alone) {
+    const bool none = at.t_end == 0 || see == 0 || l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    const int h = at.hk * a.group + row - node * a.group;
+    store_out<E>(a.out, (((int64_t)at.b * a.n + node) * a.heads + h) * D + d,
+                 none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+    return;
+  }
+  const int64_t tile = ((int64_t)at.b * a.c.kv_heads + at.hk) * a.n_tiles + at.tile;
+  const int64_t rec = (tile * a.splits + at.sp) * tile_rows + row % tile_rows;
+  *reinterpret_cast<float4*>(a.acc + rec * D + d) = v;
+  // (a node that is not there: no weight in any part)
+  if (d == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mm, see == 0 ? 0.f : l);
+}
+
+// The block's place, nodes and ancestors; false where it has nothing to do.
+__device__ __forceinline__ bool find_block(const AttnArgs& a, Block& at, int& total) {
+  // Blocks go to the 8 XCDs in turn. The row tiles of one part, which read the same
+  // entries, follow each other on one XCD; parts of one sequence go to all of them (in one
+  // range of blocks an XCD, the longest sequence's XCD was the last: 4 sequences of 44,000
+  // to 65,536 entries 805 us).
+  const int turn = blockIdx.x / 8;
+  at.tile = turn % a.n_rt;
+  int x = (turn / a.n_rt) * 8 + blockIdx.x % 8;
+  if (x >= (int)a.c.batch * a.c.kv_heads * a.splits) return false;
+  at.sp = x % a.splits;
+  x /= a.splits;
+  at.hk = x % a.c.kv_heads;
+  at.b = x / a.c.kv_heads;
+  const Span span = span_of(a, at.b);
+  total = span.total;
+  at.ctx = span.ctx;
+  at.t_begin = (int)((int64_t)at.sp * a.part < total ? at.sp * a.part : total);
+  at.t_end = total - at.t_begin > a.part ? at.t_begin + a.part : total;
+  at.alone = total <= a.part;
+  return at.sp == 0 || at.t_begin < total;
+}
+
+// Page of a run of 16 entries; without one, page 0's bytes are read and not used.
+__device__ __forceinline__ int32_t page_of(const AttnArgs& a, const int32_t* table, int t, int total, bool& ok) {
+  const int64_t pg = t >> a.c.page_log2;
+  ok = t < total && pg < a.c.table_pages;
+  const int32_t p = __builtin_amdgcn_readfirstlane(ok ? table[pg] : -1);
+  ok = p >= 0 && p < a.c.pages;
+  return ok ? p : 0;
+}
+
 template <typename E, int D, int RT, int WAVES, int AUX>
 __global__ __launch_bounds__(64 * WAVES, (WAVES > kAttnWaves ? WAVES / 4 : Attn<E, D, RT, AUX>::kWaves))
 void tree_attention_kernel(AttnArgs a) {
@@ -347,39 +505,16 @@ void tree_attention_kernel(AttnArgs a) {
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Blocks go to the 8 XCDs in turn. The row tiles of one part, which read the same
-  // entries, follow each other on one XCD; parts of one sequence go to all of them (in one
-  // range of blocks an XCD, the longest sequence's XCD was the last: 4 sequences of 44,000
-  // to 65,536 entries 805 us).
-  const int turn = blockIdx.x / 8;
-  const int rt = turn % a.n_rt;
-  int x = (turn / a.n_rt) * 8 + blockIdx.x % 8;
-  if (x >= (int)a.c.batch * a.c.kv_heads * a.splits) return;
-  const int sp = x % a.splits;
-  x /= a.splits;
-  const int hk = x % a.c.kv_heads;
-  const int b = x / a.c.kv_heads;
-
-  const Span span = span_of(a, b);
-  const int total = span.total;
-  const int ctx = span.ctx;
-  const int t_begin = (int)((int64_t)sp * a.part < total ? sp * a.part : total);
-  const int t_end = total - t_begin > a.part ? t_begin + a.part : total;
-  if (sp > 0 && t_begin >= total) return;
-  const bool alone = total <= a.part;  // the sequence has one part
+  Block at;
+  int total;
+  if (!find_block(a, at, total)) return;
+  const int b = at.b, hk = at.hk, t_begin = at.t_begin, t_end = at.t_end, ctx = at.ctx;
 
   A w;
-  // pages of a tile's runs of 16 entries; without one, page 0's bytes are read and not used
   const int32_t* table = a.c.table + (int64_t)b * a.c.table_ld;
   auto pages_of = [&](int t0, int32_t (&id)[SUBS], bool (&ok)[SUBS]) {
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      const int64_t pg = (t0 + 16 * s) >> a.c.page_log2;
-      ok[s] = t0 + 16 * s < total && pg < a.c.table_pages;
-      const int32_t p = __builtin_amdgcn_readfirstlane(ok[s] ? table[pg] : -1);
-      ok[s] = p >= 0 && p < a.c.pages;
-      id[s] = ok[s] ? p : 0;
-    }
+    for (int s = 0; s < SUBS; ++s) id[s] = page_of(a, table, t0 + 16 * s, total, ok[s]);
   };
 
   int t0 = t_begin + wave * A::KT;
@@ -398,25 +533,8 @@ void tree_attention_kernel(AttnArgs a) {
   __syncthreads();
 
   unsigned long long see[RT];
-  const int row0 = rt * ROWS;
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int r = row0 + 16 * t + (lane & 15);
-    const bool in = r < a.rows && total > 0;
-    const int node = in ? r / a.group : 0;
-    const int h = hk * a.group + (in ? r - node * a.group : 0);
-    see[t] = in ? see_sh[node] : 0;
-    const char* q = a.q + ((int64_t)b * a.q_batch + (int64_t)node * a.q_node + (int64_t)h * a.q_head) * 16;
-#pragma unroll
-    for (int c = 0; c < A::KC; ++c) {
-      w.qf[t][c] = make_uint4(0u, 0u, 0u, 0u);
-      if (in) w.qf[t][c] = *reinterpret_cast<const uint4*>(q + 64 * c + 16 * (lane >> 4));
-    }
-    w.m[t] = kNoMax;
-    w.l[t] = 0.f;
-#pragma unroll
-    for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  const int row0 = at.tile * ROWS;
+  w.take_rows(a, b, hk, row0, total > 0, see_sh, see, lane);
 
   for (; t0 < t_end; t0 += WAVES * A::KT) {
     const int tn = t0 + WAVES * A::KT;
@@ -426,56 +544,9 @@ void tree_attention_kernel(AttnArgs a) {
     f32x4_t s[RT][SUBS];
     w.scores(s);
     if (tn < t_end) w.load_k(a, id_n, hk, tn, lane);
-    bool whole = t0 + A::KT <= ctx;
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u) whole = whole && ok[u];
-    if (!whole) {
-      w.mask(s, see, t0 - ctx, a.n, ok, lane);
-      if (w.take_out_odd(t0 - ctx, lane)) odd_sh = 1;
-    }
-    // (a NaN score passes neither test and makes its row NaN)
-    float top[RT];
-    bool grow = false;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      top[t] = s[t][0][0];
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][u][i]);
-      top[t] *= a.scale;  // (above 0)
-      grow = grow || top[t] > w.m[t] + kMaxSlack;
-    }
-    if (__ballot(grow) != 0) {
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = fmaxf(w.m[t], mx);
-        const float f = w.m[t] == mn ? 1.f : fast_exp2(w.m[t] - mn);
-        w.m[t] = mn;
-        w.l[t] *= f;
-#pragma unroll
-        for (int mm = 0; mm < A::DE; ++mm) w.acc[t][mm] *= f;
-      }
-    }
     uint4 pb[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-      for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[t][u][i] = fast_exp2(fmaf(s[t][u][i], a.scale, -w.m[t]));
-          w.l[t] += s[t][u][i];
-        }
-      // bf16 weights, as the values are: up to 2^-8 of each, in both directions
-      pb[t] = A::pack_weights(s[t]);
-    }
-#pragma unroll
-    for (int mm = 0; mm < A::DE; ++mm)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) w.acc[t][mm] = A::v_product(w.vf, mm, s[t], pb[t], w.acc[t][mm]);
+    if (w.weigh(s, pb, a, see, t0, ctx, ok, lane)) odd_sh = 1;
+    w.add_values(s, pb);
     if (tn < t_end) w.load_v(a, id_n, hk, tn, lane);
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
@@ -504,12 +575,7 @@ void tree_attention_kernel(AttnArgs a) {
     for (int i = 1; i < WAVES; ++i) m = fmaxf(m, m_sh[i][r]);
     const float f = w.m[t] == m ? 1.f : fast_exp2(w.m[t] - m);
     if (t > 0) __syncthreads();  // the last tile's rows have been read
-    float* o = &o_sh[wave][lane & 15][4 * A::DE * (lane >> 4)];
-#pragma unroll
-    for (int j = 0; j < 4 * A::DE; j += 4)
-      *reinterpret_cast<float4*>(o + j) =
-          make_float4(w.acc[t][j % A::DE][j / A::DE] * f, w.acc[t][(j + 1) % A::DE][(j + 1) / A::DE] * f,
-                      w.acc[t][(j + 2) % A::DE][(j + 2) / A::DE] * f, w.acc[t][(j + 3) % A::DE][(j + 3) / A::DE] * f);
+    w.put_sums(o_sh[wave], t, f, lane);
     __syncthreads();
     for (int i = tid; i < 16 * (D / 4); i += kThreadsOf) {
       const int rl = i / (D / 4);
@@ -530,22 +596,180 @@ void tree_attention_kernel(AttnArgs a) {
         v.z += p.z;
         v.w += p.w;
       }
-      const int node = (row0 + r2) / a.group;
-      if (odd_sh) add_odd<E>(a, b, hk, d, see_sh[node], t_begin, t_end, ctx, v);
-      if (alone) {
-        const bool none = total == 0 || see_sh[node] == 0 || l == 0.f;
-        const float inv = none ? 0.f : 1.f / l;
-        const int h = hk * a.group + (row0 + r2) - node * a.group;
-        const float4 o4 = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-        store_out<E>(a.out, (((int64_t)b * a.n + node) * a.heads + h) * D + d, o4);
-      } else {
-        const int64_t rec = ((((int64_t)b * a.c.kv_heads + hk) * a.n_rt + rt) * a.splits + sp) * ROWS + r2;
-        *reinterpret_cast<float4*>(a.acc + rec * D + d) = v;
-        if (d == 0) {
-          // (a node that is not there: no weight in any part)
-          *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mm, see_sh[node] == 0 ? 0.f : l);
+      end_row<E, D>(a, at, ROWS, row0 + r2, see_sh, odd_sh != 0, d, mm, l, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// many rows of one key head (bf16): shared heads under trees of more than a few nodes
+// ---------------------------------------------------------------------------
+//
+// The four waves of a block take a row tile each and the same entries, which come to LDS
+// once: 64 at a time, two buffers, by loads that go there directly (wave w brings the w-th
+// 16, whose page it looks up). From LDS on, a wave's lanes take what they would have loaded,
+// and all else is as above. Row tiles that load for themselves read everything once per
+// tile from the second-level and memory-side caches, at their 10 TB/s.
+//
+// A run of 16 entries of K has its 16-byte chunks rotated per entry (K's reads take one
+// chunk of 16 entries at a time); V lies as it is (its reads take whole entries).
+
+constexpr int kStageEntries = 64;
+
+template <int D>
+__device__ __forceinline__ int k_place(int entry, int chunk) {
+  if constexpr (D == 128) return chunk ^ (entry & 15);
+  if constexpr (D == 64) return chunk ^ (entry & 7) ^ ((entry >> 3) & 1);
+  return (chunk + (entry >> 2)) % (D / 8);
+}
+
+template <int LOADS>
+__device__ __forceinline__ void load_run(__amdgpu_buffer_rsrc_t rs, const int (&off)[LOADS], char* lds) {
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_t*)(lds + j * 1024), 16, off[j], 0, 0, 0);
+}
+
+template <int D, int RT>
+__global__ __launch_bounds__(64 * kAttnWaves, 2) void many_rows_attention_kernel(AttnArgs a) {
+  using A = Attn<Bf16, D, RT, kLoadKeep>;
+  constexpr int ROWS = A::ROWS;
+  constexpr int CPR = D / 8;          // chunks of an entry's head
+  constexpr int LOADS = CPR / 4;      // of a run of 16 entries: 64 chunks each
+  constexpr int kRun = 16 * D * 2;    // bytes of a run
+  constexpr int kBuf = kStageEntries * D * 2;
+  constexpr int kStage = 2 * kBuf;    // K, then V
+  static_assert(kAttnWaves * 16 == kStageEntries, "a run to each wave");
+  static_assert(kAttnWaves * 16 * A::LD * 4 <= 2 * kStage, "the end's rows fit the buffers");
+  __shared__ __attribute__((aligned(16))) char stage[2 * kStage];
+  __shared__ unsigned long long see_sh[64];
+  __shared__ int32_t parent_sh[64];
+  __shared__ int run_ok[2][kAttnWaves];  // whether a run of the stage has a page
+  __shared__ int odd_sh;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Block at;
+  int total;
+  if (!find_block(a, at, total)) return;
+  const int b = at.b, hk = at.hk, t_begin = at.t_begin, t_end = at.t_end, ctx = at.ctx;
+  at.tile = at.tile * kAttnWaves + wave;
+  const int32_t* table = a.c.table + (int64_t)b * a.c.table_ld;
+
+  int koff[LOADS], voff[LOADS];  // a lane's chunks of a run
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int slot = j * 64 + lane;
+    const int e = slot / CPR;
+    const int p = slot % CPR;
+    int c;  // the chunk whose place is p
+    if constexpr (D == 128)
+      c = p ^ (e & 15);
+    else if constexpr (D == 64)
+      c = p ^ (e & 7) ^ ((e >> 3) & 1);
+    else
+      c = (p + CPR - (e >> 2)) % CPR;
+    koff[j] = (e * (int)a.c.s_entry + c) * 16;
+    voff[j] = (e * (int)a.c.s_entry + p) * 16;
+  }
+  auto issue = [&](int t, int buf) {  // the stage at entry t
+    char* base = stage + buf * kStage;
+    const int tw = t + 16 * wave;
+    bool ok;
+    const int32_t page = page_of(a, table, tw, total, ok);
+    if (lane == 0) run_ok[buf][wave] = ok ? 1 : 0;
+    const __amdgpu_buffer_rsrc_t rk = A::run_rsrc(a.c.k, a, page, hk, tw);
+    const __amdgpu_buffer_rsrc_t rv = A::run_rsrc(a.c.v, a, page, hk, tw);
+    load_run<LOADS>(rk, koff, base + wave * kRun);
+    load_run<LOADS>(rv, voff, base + kBuf + wave * kRun);
+  };
+  if (t_begin < t_end) issue(t_begin, 0);
+
+  if (tid == 0) odd_sh = 0;
+  if (tid < a.n) parent_sh[tid] = a.parents ? a.parents[(int64_t)b * a.n + tid] : tid - 1;
+  __syncthreads();
+  if (tid < a.n) see_sh[tid] = ancestors(parent_sh, tid, a.n);
+  __syncthreads();
+
+  A w;
+  unsigned long long see[RT];
+  const int row0 = at.tile * ROWS;
+  w.take_rows(a, b, hk, row0, total > 0, see_sh, see, lane);
+
+  int buf = 0;
+  for (int t0 = t_begin; t0 < t_end; t0 += kStageEntries) {
+    // the stage has arrived, for every wave; and no wave reads the other buffer any more
+    wait_vmcnt<0>();
+    stage_barrier();
+    if (t0 + kStageEntries < t_end) issue(t0 + kStageEntries, buf ^ 1);
+    const char* base = stage + buf * kStage;
+    auto take_k = [&](int half) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int c = 0; c < A::KC; ++c) {
+          const int e = lane & 15;
+          const uint4 x = *reinterpret_cast<const uint4*>(base + (2 * half + u) * kRun + e * D * 2 +
+                                                          k_place<D>(e, 4 * c + (lane >> 4)) * 16);
+          w.kf[u][c][0] = x.x; w.kf[u][c][1] = x.y; w.kf[u][c][2] = x.z; w.kf[u][c][3] = x.w;
         }
-      }
+    };
+    auto take_v = [&](int half) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(base + kBuf + (2 * half + u) * kRun +
+                                                                (4 * (lane >> 4) + i) * D * 2 + (lane & 15) * A::VB);
+          if constexpr (A::VW == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            w.vf[4 * u + i][0] = x.x; w.vf[4 * u + i][1] = x.y; w.vf[4 * u + i][2] = x.z; w.vf[4 * u + i][3] = x.w;
+          } else {
+#pragma unroll
+            for (int k = 0; k < A::VW; ++k) w.vf[4 * u + i][k] = p[k];
+          }
+        }
+    };
+    take_k(0);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int t = t0 + half * A::KT;
+      if (t >= t_end) break;
+      take_v(half);  // (on the way while the scores are formed)
+      f32x4_t s[RT][2];
+      w.scores(s);
+      if (half == 0) take_k(1);  // (and while the weights are)
+      bool ok[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) ok[u] = __builtin_amdgcn_readfirstlane(run_ok[buf][2 * half + u]) != 0;
+      uint4 pb[RT];
+      if (w.weigh(s, pb, a, see, t, ctx, ok, lane)) odd_sh = 1;
+      w.add_values(s, pb);
+    }
+    buf ^= 1;
+  }
+
+  // each wave's rows, through its part of the buffers
+  __syncthreads();
+  float(*o)[A::LD] = reinterpret_cast<float(*)[A::LD]>(stage + wave * 16 * A::LD * 4);
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float l = w.l[t];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (t > 0) __syncthreads();  // the last tile's rows have been read
+    w.put_sums(o, t, 1.f, lane);
+    __syncthreads();
+    for (int i0 = 0; i0 < 16 * (D / 4); i0 += 64) {
+      const int i = i0 + lane;
+      const int rl = i / (D / 4);
+      const int d = 4 * (i % (D / 4));
+      const float lr = __shfl(l, rl, 64);
+      const float mr = __shfl(w.m[t], rl, 64);
+      const int row = row0 + 16 * t + rl;
+      if (row < a.rows)
+        end_row<Bf16, D>(a, at, ROWS, row, see_sh, odd_sh != 0, d, mr, lr, *reinterpret_cast<const float4*>(&o[rl][d]));
     }
   }
 }
@@ -568,7 +792,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int D) {
   const int hk = h / a.group;
   const int r = node * a.group + (h - hk * a.group);
   const int parts = (total + a.part - 1) / a.part;
-  const int64_t rec = (((b * a.c.kv_heads + hk) * a.n_rt + r / tile_rows) * a.splits) * tile_rows + r % tile_rows;
+  const int64_t rec = (((b * a.c.kv_heads + hk) * a.n_tiles + r / tile_rows) * a.splits) * tile_rows + r % tile_rows;
   float m = -INFINITY;
   for (int s = 0; s < parts; ++s) {
     const float2 ml = *reinterpret_cast<const float2*>(a.ml + (rec + (int64_t)s * tile_rows) * 2);
@@ -603,9 +827,17 @@ hipError_t launch_attn_k(const AttnArgs& a, int64_t blocks, hipStream_t stream) 
   return hipGetLastError();
 }
 
+constexpr int kManyTile = 32;
+
 template <typename E, int D>
 hipError_t launch_attn_d(const AttnArgs& a, int64_t blocks, hipStream_t stream) {
   constexpr int kHeadBytes = D * E::kBytes;
+  if constexpr (E::kBytes == 2 && (D == 64 || D == 96 || D == 128))
+    if (a.many) {
+      hipLaunchKernelGGL((many_rows_attention_kernel<D, kManyTile / 16>), dim3((unsigned)blocks), dim3(64 * kAttnWaves), 0,
+                         stream, a);
+      return hipGetLastError();
+    }
   constexpr int kMost = kHeadBytes <= kWideRow ? 4 : kHeadBytes <= kMiddleRow ? 2 : 1;  // 16 rows each
   switch (a.tile) {
     case 16:
@@ -654,6 +886,14 @@ int attn_tile_rows(int32_t rows, int32_t head_bytes, int64_t ways) {
   while (tile > 16 && (rows <= tile / 2 || ways * ((rows + tile - 1) / tile) < 512)) tile /= 2;
   return tile;
 }
+// Many rows: a block takes kAttnWaves tiles of kManyTile, where that leaves no part of the
+// chip idle (4 sequences of 500 entries, 80 rows of 4 heads of 64: 18 us, tiles of 16 rows 14).
+bool attn_many(int32_t rows, int32_t D, bool f32, int64_t ways) {
+  constexpr int kBlock = kAttnWaves * kManyTile;
+  return !f32 && rows > kBlock / 2 && (D == 64 || D == 96 || D == 128) && ways * ((rows + kBlock - 1) / kBlock) >= 256;
+}
+int attn_many_tile() { return kManyTile; }
+int attn_many_tiles() { return kAttnWaves; }
 // blocks: of one part each; entries: that a table's row has room for
 bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes) {
   return blocks <= 256 && entries <= 1536 && rows <= 16 && head_bytes <= kShortRow;

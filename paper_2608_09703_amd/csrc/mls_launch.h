@@ -519,7 +519,9 @@ struct AttnArgs {
   int32_t group;   // query heads of a key head
   int32_t rows;    // n * group: rows that read one key head
   int32_t tile;    // rows of a tile
-  int32_t n_rt;    // row tiles
+  int32_t n_rt;    // row tiles, or of many rows four at a time
+  int32_t n_tiles; // row tiles (of many rows a multiple of four)
+  int32_t many;    // attn_many: the waves of a block take a row tile each
   int32_t splits;  // parts of the entries
   int32_t part;    // entries of a part
   int32_t shorts;  // attn_short: one part, more waves to a block
@@ -641,6 +643,9 @@ hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t stream);
 // rows of a tile of tree attention, which read an entry's head once
 int attn_tile_rows(int32_t rows, int32_t head_bytes, int64_t ways);
+bool attn_many(int32_t rows, int32_t D, bool f32, int64_t ways);
+int attn_many_tile();   // rows of such a tile
+int attn_many_tiles();  // tiles of a block
 bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes);
 hipError_t launch_tree_attention(const AttnArgs& a, int32_t D, bool f32, hipStream_t stream);
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream);

@@ -78,6 +78,9 @@ CASES = [
     ("bf16", 128, 1, 2, 64, 128, [129, 200], "heads_first"),
     ("bf16", 64, 1, 8, 13, 16, [77], "heads_first"),  # more rows than a tile
     ("bf16", 96, 1, 1, 3, 16, [1500, 2, 700], "heads_first"),  # several parts
+    # more rows of a key head than a tile
+    ("bf16", 128, 1, 8, 9, 16, [0, 40, 127], "heads_first"),
+    ("bf16", 96, 1, 4, 40, 16, [900, 15], "padded"),
     ("f32", 64, 3, 4, 9, 32, [0, 1, 90, 333], "heads_first"),
     ("f32", 32, 1, 1, 33, 16, [47, 48], "entries_first"),
     ("f32", 96, 2, 1, 20, 16, [130], "heads_first"),
@@ -103,6 +106,41 @@ def test_against_the_oracle(case):
     _check(got, want, _bound(q, k, v, lengths, parents, dtype, want))
 
 
+WIDE = [
+    # tiles of 64 rows, of 32 and of 16
+    ("bf16", 32, 1, 1, 64, 16, [20, 300], "heads_first"), ("bf16", 64, 1, 2, 25, 16, [33, 290], "padded"),
+    ("bf16", 64, 2, 1, 20, 32, [7], "heads_first"), ("bf16", 96, 2, 1, 30, 16, [0, 520], "heads_first"),
+    ("bf16", 128, 1, 2, 16, 64, [15, 260, -1], "entries_first"), ("bf16", 192, 1, 1, 40, 16, [18, 280], "heads_first"),
+    ("bf16", 256, 1, 1, 20, 16, [270], "heads_first"), ("f32", 32, 1, 1, 50, 16, [16, 300], "heads_first"),
+    ("f32", 64, 1, 3, 11, 16, [31, 270], "heads_first"), ("f32", 96, 1, 1, 40, 16, [261], "heads_first"),
+    ("f32", 128, 1, 1, 20, 32, [9, 256], "padded"), ("f32", 192, 1, 1, 33, 16, [258], "heads_first"),
+    ("f32", 256, 1, 1, 18, 16, [12, 257], "heads_first"), ("bf16", 128, 3, 1, 5, 16, [300, 1], "heads_first"),
+    # more than 64 rows of a key head: a block's waves share the entries
+    ("bf16", 128, 1, 8, 9, 16, [0, 40, 127, 128], "heads_first"), ("bf16", 64, 2, 5, 33, 64, [63, 700, -1], "entries_first"),
+    ("bf16", 96, 1, 4, 40, 16, [900, 15], "padded"), ("bf16", 128, 1, 3, 64, 32, [64, 300], "heads_first"),
+    ("bf16", 64, 1, 8, 64, 16, [31, 255], "heads_first"), ("bf16", 96, 3, 5, 14, 16, [33], "heads_first"),
+    ("f32", 64, 1, 8, 17, 16, [40, 258], "heads_first"), ("bf16", 192, 1, 5, 20, 16, [50], "heads_first")]
+
+
+@pytest.mark.parametrize("room", [512 * 256, 1 << 21])
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "-".join(str(x) for x in c).replace(" ", ""))
+def test_wide_tables(case, room):
+    """Tables with room for many parts: the largest tiles of rows, and (the wider one) loads past the caches."""
+    dt, Dh, hk, group, n, page, lengths, layout = case
+    dtype = torch.bfloat16 if dt == "bf16" else torch.float32
+    rng = np.random.default_rng(sum(lengths) + 1000 * n + Dh)
+    c = Cache(rng, lengths, n, hk, Dh, page, dtype, layout=layout)
+    parents = tree(rng, c.B, n)
+    k, v = _fill(rng, c, dtype, parents)
+    table = torch.full((c.B, room // page), -1, dtype=torch.int32, device=DEV)
+    table[:, :c.per] = c.t_table
+    q = values(rng, (c.B, n, hk * group, Dh), dtype, 2.0)
+    got = D.tree_attention(torch.tensor(q, device=DEV).to(dtype), c.k[0], c.v[0], table, c.t_lengths,
+                           torch.tensor(parents, device=DEV))
+    want = O.attention(q, k, v, lengths, parents)
+    _check(got, want, _bound(q, k, v, lengths, parents, dtype, want))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_chain_strides_and_scale(dtype):
     """Without parents a node sees the earlier ones; q lies in a wider tensor; a scale of the caller's."""
@@ -119,9 +157,9 @@ def test_chain_strides_and_scale(dtype):
     assert torch.equal(got, D.tree_attention(qkv[:, :, 1], *c.layer(), torch.tensor(chain, device=DEV), scale=0.03))
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dtype,heads", [(torch.bfloat16, 2), (torch.float32, 2), (torch.bfloat16, 9)])
 @pytest.mark.parametrize("length", [3, 300])  # in one part, and in several
-def test_infinities_reach_the_rows_that_see_them_only(dtype, length):
+def test_infinities_reach_the_rows_that_see_them_only(dtype, heads, length):
     rng = np.random.default_rng(9)
     n = 8
     c = Cache(rng, [length], n, 1, 64, 16, dtype, wide=20)
@@ -134,8 +172,13 @@ def test_infinities_reach_the_rows_that_see_them_only(dtype, length):
             y[:, marks[i][0]] = marks[i][1]
         return y
     k, v = _fill(rng, c, dtype, parents, odd)
-    q = values(rng, (1, n, 2, 64), dtype)
-    got = D.tree_attention(torch.tensor(q, device=DEV).to(dtype), *c.layer(), torch.tensor(parents, device=DEV))
+    q = values(rng, (1, n, heads, 64), dtype)
+    table = c.t_table
+    if heads > 8:  # (room for many parts: a block's waves share the entries)
+        table = torch.full((1, 5000), -1, dtype=torch.int32, device=DEV)
+        table[:, :c.per] = c.t_table
+    got = D.tree_attention(torch.tensor(q, device=DEV).to(dtype), c.k[0], c.v[0], table, c.t_lengths,
+                           torch.tensor(parents, device=DEV))
     want = O.attention(q, k, v, [length], parents)
     assert np.isinf(want).any() and np.isnan(want).any() and np.isfinite(want).any()
     plain = [[np.where(np.isfinite(x), x, 0.0) for x in b] for b in v]
