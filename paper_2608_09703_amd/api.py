@@ -788,7 +788,8 @@ def _no_grad(name: str, *xs: Optional[torch.Tensor]):
 
 def _written(*xs: torch.Tensor):
     """Tells autograd of tensors that were written through their addresses."""
-    if not xs[0].is_inference():
+    xs = [x for x in xs if not x.is_inference()]
+    if xs:
         torch.autograd.graph.increment_version(xs)
 
 
@@ -819,8 +820,9 @@ def _kv_cache(name: str, k_pages, v_pages, page_table, lengths, all_layers: bool
         raise ValueError(f"{name}: page_table must be an int32 [B, pages of a sequence] tensor on the pages' device")
     Bt, width = t_shape
     _ints(name, "lengths", lengths, (Bt,), dev)
-    return B.KVCache(_dtype_code(dtype), shape[2], shape[1], shape[3], layers, shape[0], Bt, width, ld_layer,
-                     stride[0], stride[1], stride[2], t_stride[0] if Bt > 1 else width)
+    far = [s if n > 1 else 0 for n, s in zip((layers,) + tuple(shape), (ld_layer,) + tuple(stride))]
+    return B.KVCache(_dtype_code(dtype), shape[2], shape[1], shape[3], layers, shape[0], Bt, width, *far[:4],
+                     t_stride[0] if Bt > 1 else width)
 
 
 def _step_rows(name: str, x, what: str, c: B.KVCache, like, heads: Optional[int] = None):

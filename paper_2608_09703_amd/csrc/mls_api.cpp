@@ -2244,7 +2244,15 @@ mls_status validate_cache(const mls_kv_cache* c, int64_t layers_max) {
   for (int i = 0; i < 4; ++i) {
     if (lds[i] < 0 || lds[i] > (1ll << 48) || lds[i] * es % 16)
       return fail(MLS_INVALID_ARG, "strides must be multiples of 16 bytes");
-    if (counts[i] > 1 && lds[i] < c->head_dim) return fail(MLS_INVALID_ARG, "entries overlap");
+  }
+  // one after another by stride, each dimension steps over all of those inside it
+  int order[4] = {0, 1, 2, 3};
+  std::sort(order, order + 4, [&](int x, int y) { return lds[x] < lds[y]; });
+  __int128 span = c->head_dim;
+  for (int i : order) {
+    if (counts[i] == 1) continue;
+    if (lds[i] < span) return fail(MLS_INVALID_ARG, "entries overlap");
+    span += (__int128)(counts[i] - 1) * lds[i];
   }
   if (16 * c->ld_entry * es >= (1ll << 31)) return fail(MLS_UNSUPPORTED, "16 entries span 2 GiB or more");
   if (!c->k || !c->v || !c->page_table || !c->lengths)
@@ -2290,7 +2298,11 @@ mls_status validate_rows(const char* what, const void* p, int64_t es, int64_t ld
 
 // Parts of the entries: enough blocks for the chip where a batch has few sequences and
 // heads, and parts of kPartMost entries at most, so that one long sequence among short
-// ones does not run alone at the end.
+// ones does not run alone at the end. 4 sequences of up to 65,536 entries, 34 heads of 128,
+// 32 rows, parts of 1,024 / 2,048 / 4,096 / 8,192 entries: 956 / 877 / 838 / 845 us.
+// Blocks of many rows: two on a CU make one round of them. 16 sequences of 8,000 entries, 320
+// rows of each of two heads of 128, parts for 256 / 384 / 512 / 1,024 blocks: 147 / 108 / 95 /
+// 117 us; 256 rows of 4 heads of 96: 146 / 132 / 108 / 124.
 constexpr int64_t kAttnBlocks = 1024;
 constexpr int64_t kManyBlocks = 512;
 constexpr int64_t kPartLeast = 256;

@@ -272,3 +272,32 @@ def test_front_end_verification_and_quantization_shapes():
     for args in ((o, _m(torch.uint8, (7, 32)), ws, None), (o, W, _m(BF, (7,)), None)):
         with pytest.raises(TypeError):
             D._int8_plan(*args)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(ld_head=64), dict(ld_head=64 * 15), dict(ld_entry=128), dict(ld_page=1024), dict(ld_page=2048 - 64),
+    dict(ld_page=64, ld_head=9 * 64, ld_entry=64), dict(pages=0x7fffffff, ld_page=1 << 48, ld_head=1 << 48)])
+def test_entries_that_overlap(kw):
+    c = _cache(**kw)
+    _refused(B.MLS_INVALID_ARG, _write, c, text="overlap")
+    _refused(B.MLS_INVALID_ARG, _compact, c, text="overlap")
+    _refused(B.MLS_INVALID_ARG, B.tree_attention_workspace, c, 5, 4, text="overlap")
+
+
+@pytest.mark.parametrize("kw", [
+    dict(ld_head=64, ld_entry=128), dict(ld_page=64, ld_head=9 * 64, ld_entry=18 * 64), dict(ld_entry=72, ld_head=16 * 72, ld_page=32 * 72),
+    dict(pages=1, ld_page=0), dict(kv_heads=1, ld_head=0), dict(ld_head=15 * 64 * 2 + 64, ld_entry=128, ld_page=2 * (15 * 128 + 64)),
+    dict(pages=0x7fffffff, ld_page=1 << 48)])
+def test_dimensions_in_any_order(kw):
+    assert B.tree_attention_workspace(_cache(**kw), 5, 4) == 0
+
+
+def test_strides_of_single_layers_pages_and_heads_do_not_matter():
+    table, lengths = _m(I32, (3, 4)), _m(I32, (3,))
+    pages = _m(BF, (1, 1, 16, 64), stride=(3, 5, 64, 1))
+    k = _m(BF, (3, 5, 1, 64))
+    assert D._write_plan(k, k, pages, pages, table, lengths, None)[0].ld_head == 0
+    q = _m(BF, (3, 5, 4, 64))
+    assert D._attention_plan(q, pages, pages, table, lengths, None)[0].ld_page == 0
+    layers = _m(BF, (1, 9, 2, 16, 64), stride=(7, 2048, 1024, 64, 1))
+    assert D._compact_plan(layers, layers, table, lengths, _m(I32, (3, 5)), lengths)[0].ld_layer == 0
