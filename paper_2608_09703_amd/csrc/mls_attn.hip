@@ -7,11 +7,16 @@
 // over t < L and over the entries L + j of the nodes j on i's way to the root (i among
 // them). A row keeps a running maximum m and sum; w is taken relative to m, in base 2.
 //
+// What bounds it is the entries' bytes, read once per block of rows: 4 sequences of 65,536
+// entries, 34 heads of 128, one row: 698 us, 6.5 TB/s (a large copy: 4.9 TB/s, reads alone
+// about 6.6); 102 of 1,280 entries, 16 rows in 64 nodes' tree: 229 us with 17 heads, 5.5 TB/s.
+//
 // A block takes up to 64 rows (nodes x heads of one key head) and one part of the
 // entries; its waves take the part's tiles in turn, each for itself, and join their
 // sums at the end. Nothing goes through LDS on the way there, and no wave waits for
 // another: the two products are laid out so that each one's operands are what loads and
-// the other product leave in a lane's registers.
+// the other product leave in a lane's registers. (More rows than that read the entries
+// too often: a second kernel below, whose waves share them.)
 //   S^T = K Q^T   v_mfma 16x16x32: lane (g = lane / 16, r = lane % 16) brings 16 bytes of
 //                 entry r's head and 16 bytes of row r; it receives row r's scores with
 //                 entries 4 g .. 4 g + 3 of each 16.
@@ -44,8 +49,8 @@ constexpr int kShortWaves = 8;
 // passes it by this much (base 2): the weights stay below 2^8, which costs the sums nothing.
 constexpr float kMaxSlack = 8.f;
 // ... and a row's before its first entry: finite, so that a row that has none (every
-// score -inf) adds weights of 0 and no NaN.
-constexpr float kNoMax = -3e38f;
+// score -inf) adds weights of 0 and no NaN; the lowest number, so that no score is below it.
+constexpr float kNoMax = -3.40282347e38f;
 
 template <typename E>
 struct AttnTile;
@@ -609,7 +614,11 @@ void tree_attention_kernel(AttnArgs a) {
 // once: 64 at a time, two buffers, by loads that go there directly (wave w brings the w-th
 // 16, whose page it looks up). From LDS on, a wave's lanes take what they would have loaded,
 // and all else is as above. Row tiles that load for themselves read everything once per
-// tile from the second-level and memory-side caches, at their 10 TB/s.
+// tile from the second-level and memory-side caches, at their 10 TB/s: 16 sequences of 8,000
+// entries, 320 rows of each of two heads of 128: 126 -> 95 us (440 TFLOP/s); 256 rows of 4
+// heads of 96: 122 -> 108; 64 sequences of 2,000, 128 rows of 4 heads of 128: 98 -> 78. What
+// bounds it: the exponentials and masks between the two products, with two waves a SIMD to
+// hide them behind (matrix units 20 % busy, waves waiting 43 % of the time).
 //
 // A run of 16 entries of K has its 16-byte chunks rotated per entry (K's reads take one
 // chunk of 16 entries at a time); V lies as it is (its reads take whole entries).
@@ -887,7 +896,9 @@ int attn_tile_rows(int32_t rows, int32_t head_bytes, int64_t ways) {
   return tile;
 }
 // Many rows: a block takes kAttnWaves tiles of kManyTile, where that leaves no part of the
-// chip idle (4 sequences of 500 entries, 80 rows of 4 heads of 64: 18 us, tiles of 16 rows 14).
+// chip idle (4 sequences of 500 entries, 80 rows of 4 heads of 64: 18 us, tiles of 16 rows 14)
+// and its tiles are not half of them empty (64 rows of 16 heads of 64: 161 us, one tile of 64
+// rows 127).
 bool attn_many(int32_t rows, int32_t D, bool f32, int64_t ways) {
   constexpr int kBlock = kAttnWaves * kManyTile;
   return !f32 && rows > kBlock / 2 && (D == 64 || D == 96 || D == 128) && ways * ((rows + kBlock - 1) / kBlock) >= 256;

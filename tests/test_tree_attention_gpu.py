@@ -220,6 +220,23 @@ def test_scores_of_very_different_sizes():
     np.testing.assert_allclose(got.cpu().numpy(), want, rtol=0, atol=3 * 2.0 ** -23 * 4)
 
 
+def test_scores_near_the_lowest_number():
+    """Rows whose scores are all next to float32's lowest number still weigh them against one another."""
+    rng = np.random.default_rng(3)
+    c = Cache(rng, [20], 1, 1, 32, 16, torch.float32)
+    k, v = np.zeros((21, 1, 32)), values(rng, (21, 1, 32), torch.float32)
+    k[:, 0, 0] = np.float32(-2.3e19)
+    k[[4, 17], 0, 0] = np.float32(-2.2e19)
+    for t in range(21):
+        c.put(0, t, k[t], v[t])
+    q = torch.zeros(1, 1, 1, 32, device=DEV)
+    q[..., 0] = 1e19
+    got = D.tree_attention(q, *c.layer(), scale=1.0)[0, 0, 0].double().cpu().numpy()
+    # (in base 2 the scores are -3.32e38 and -3.17e38: all weight is on the two; two sums and a quotient in fp32)
+    want = (v[4, 0] + v[17, 0]) / 2
+    assert np.abs(got - want).max() <= 3 * 2.0 ** -24 * np.abs(v).max()
+
+
 def test_pages_that_are_not_there():
     rng = np.random.default_rng(12)
     n = 3
