@@ -13,6 +13,8 @@
 //  - STAGES K-tiles of RB bytes (64 or 32 bf16) are in flight; a K-tile is consumed after an
 //    explicit vmcnt wait and a plain s_barrier (no memory fence, so younger
 //    loads stay in flight across the barrier);
+//  - 8-bit integers (ET = I8) go the same way, 128 of them to a row of 128 bytes, through
+//    v_mfma_i32_32x32x32_i8 into 32-bit sums;
 //  - K of an MC operand is a multiple of a K-tile; K of KC operands too unless
 //    KTAIL is set, which takes any multiple of 8: the last K-tile's lanes past
 //    the row end get an offset outside the panel and read zero. The operand

@@ -154,7 +154,7 @@ __device__ __forceinline__ void for_wave_range(const float* logits, int V, F f) 
 
 // A row as a thread knows it: its distribution, and where it keeps few enough tokens the
 // list, whose entry i < n is thread i's (idx, p normalised; p is 0 for an entry that is not
-// kept). n is -1 for larger ones.
+// kept); n is -1 for larger ones.
 struct Opened {
   RowDist d;
   double norm;
@@ -259,13 +259,13 @@ __device__ __forceinline__ int open_large(const Settings& a, TreeShared& ts, int
   return r.norm == 0.0 ? 0 : n;
 }
 
-// Opens row `which` (0: the verifier's, 1: the draft's) of node blockIdx / batch-major in
-// the workspace, where the walk may want it: every node that the tree has, of the draft
-// those with a child.
+// Opens a row of one of the `ready` first nodes of each tree: the verifier's of every node
+// that the tree has (with its list), then the draft's of those that have a child (its record
+// and norm; the walk reads q at p's tokens only).
 template <int EPT>
 __global__ __launch_bounds__(kTreeThreads) void tree_rows_kernel(TreeVerifyArgs a) {
   __shared__ OpenShared os;
-  const int64_t row = blockIdx.x;  // [which][batch][ready]
+  const int64_t row = blockIdx.x;  // [verifier, draft][batch][ready]
   const int64_t half = a.batch * a.ready;
   const bool draft = row >= half;
   const int64_t in = draft ? row - half : row;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_rows_kernel(TreeVerifyArgs 
   const RowDist* rec = draft && a.dparams ? a.dparams + at : nullptr;
   const Settings set{a.V, a.inv_temp, 1.0 / (double)a.temperature, a.top_p};
   const Opened r = open_row<EPT>((draft ? a.draft : a.target) + at * a.V, rec, set, draft, os);
-  if ((int)threadIdx.x < r.n) {
+  if (!draft && (int)threadIdx.x < r.n) {
     a.list_idx[row * kMaxCand + threadIdx.x] = r.idx;
     a.list_p[row * kMaxCand + threadIdx.x] = r.p;
   }
@@ -647,7 +647,7 @@ static int tree_ready_nodes(int64_t batch, int64_t n) {
   return (int)(k < n ? k : n);
 }
 size_t tree_workspace(TreeVerifyArgs& a, void* workspace) {
-  const int64_t rows = 2 * a.batch * tree_ready_nodes(a.batch, a.n);
+  const int64_t lists = a.batch * tree_ready_nodes(a.batch, a.n);
   const int64_t entries = a.batch * ((a.V + 1) / 2 * 2);
   uintptr_t p = reinterpret_cast<uintptr_t>(workspace);
   auto take = [&](int64_t bytes) {
@@ -655,12 +655,12 @@ size_t tree_workspace(TreeVerifyArgs& a, void* workspace) {
     p += bytes;
     return reinterpret_cast<char*>(at);
   };
-  a.ready_rows = take(rows * sizeof(TreeRow));
-  a.list_p = reinterpret_cast<double*>(take(rows * kMaxCand * 8));
+  a.ready_rows = take(2 * lists * sizeof(TreeRow));
+  a.list_p = reinterpret_cast<double*>(take(lists * kMaxCand * 8));
   a.large_p = reinterpret_cast<double*>(take(entries * 8));
   a.large_p2 = reinterpret_cast<double*>(take(entries * 8));
   a.large_q = reinterpret_cast<double*>(take(entries * 8));
-  a.list_idx = reinterpret_cast<int32_t*>(take(rows * kMaxCand * 4));
+  a.list_idx = reinterpret_cast<int32_t*>(take(lists * kMaxCand * 4));
   a.large_idx = reinterpret_cast<int32_t*>(take(entries * 4));
   return (size_t)(p - reinterpret_cast<uintptr_t>(workspace));
 }
