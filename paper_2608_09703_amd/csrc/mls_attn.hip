@@ -51,6 +51,10 @@ constexpr float kMaxSlack = 8.f;
 // ... and a row's before its first entry: finite, so that a row that has none (every
 // score -inf) adds weights of 0 and no NaN; the lowest number, so that no score is below it.
 constexpr float kNoMax = -3.40282347e38f;
+// Up to here a fused multiply-add may take a row's maximum off the exact product: the two
+// roundings differ by 2^-5 at most, which all of the row's weights share. Beyond, the product
+// is rounded first, as the maximum's was.
+constexpr float kFusedMax = 1048576.f;
 
 template <typename E>
 struct AttnTile;
@@ -63,15 +67,30 @@ struct AttnTile<F32> {
   static constexpr int kSubs = 1;
 };
 
-// The nodes on the way from each node to the root (bit j: node j), 0 for a node that the
-// tree does not have. One thread per node.
-__device__ __forceinline__ unsigned long long ancestors(const int32_t* parents, int i, int n) {
-  unsigned long long m = 0;
+// A set of nodes, in two words. (Not in one of 64 bits: that is tested by a 64-bit shift, and
+// such a shift by a count in the last vector register that a kernel is given has now and then
+// shifted by register 0 instead, so that rows took part in nodes that they do not see.)
+struct Nodes {
+  uint32_t lo, hi;
+};
+__device__ __forceinline__ Nodes only_node(int j) {
+  const uint32_t bit = 1u << (j & 31);
+  return {j & 32 ? 0u : bit, j & 32 ? bit : 0u};
+}
+__device__ __forceinline__ bool meet(Nodes a, Nodes b) { return ((a.lo & b.lo) | (a.hi & b.hi)) != 0; }
+__device__ __forceinline__ bool none_of(Nodes a) { return (a.lo | a.hi) == 0; }
+
+// The nodes on the way from each node to the root, none for a node that the tree does not
+// have. One thread per node.
+__device__ __forceinline__ Nodes ancestors(const int32_t* parents, int i, int n) {
+  Nodes m = {0u, 0u};
   for (;;) {  // i falls with every step
-    m |= 1ull << i;
+    const Nodes x = only_node(i);
+    m.lo |= x.lo;
+    m.hi |= x.hi;
     const int p = parents[i];
     if (p == -1) return m;
-    if (p < 0 || p >= i) return 0;
+    if (p < 0 || p >= i) return {0u, 0u};
     i = p;
   }
 }
@@ -146,6 +165,7 @@ struct Attn {
   f32x4_t acc[RT][DE];
   float m[RT];
   float l[RT];
+  bool far;  // some row's maximum is beyond kFusedMax
 
   // The 16 entries from t0 on (head hk) in one pool: a scalar base, so that a lane's part
   // of any address is one 32-bit offset. (The host has checked that 16 entries span less
@@ -238,7 +258,7 @@ struct Attn {
   // Tiles in which not every row sees every entry: `see[t]` has the nodes that the lane's
   // row sees, `first` the node of the tile's entry 0 (below 0: context, which every row
   // sees); runs without a page and entries past the last node are seen by none.
-  __device__ __forceinline__ void mask(f32x4_t (&s)[RT][SUBS], const unsigned long long (&see)[RT], int first, int n,
+  __device__ __forceinline__ void mask(f32x4_t (&s)[RT][SUBS], const Nodes (&see)[RT], int first, int n,
                                        const bool (&page)[SUBS], int lane) {
     const int g4 = 4 * (lane >> 4);
 #pragma unroll
@@ -246,9 +266,10 @@ struct Attn {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int node = first + 16 * u + g4 + i;
+        const Nodes bit = only_node(node);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const bool in = page[u] && node < n && (node < 0 || ((see[t] >> (node & 63)) & 1));
+          const bool in = page[u] && node < n && (node < 0 || meet(see[t], bit));
           s[t][u][i] = in ? s[t][u][i] : -INFINITY;
         }
         // what no row sees is not used, whatever it holds
@@ -279,14 +300,15 @@ struct Attn {
 
   // Queries of the rows from row0 on, and the nodes they see.
   __device__ __forceinline__ void take_rows(const AttnArgs& a, int b, int hk, int row0, bool any,
-                                            const unsigned long long* nodes, unsigned long long (&see)[RT], int lane) {
+                                            const Nodes* nodes, Nodes (&see)[RT], int lane) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int r = row0 + 16 * t + (lane & 15);
       const bool in = r < a.rows && any;
       const int node = in ? r / a.group : 0;
       const int h = hk * a.group + (in ? r - node * a.group : 0);
-      see[t] = in ? nodes[node] : 0;
+      see[t] = {0u, 0u};
+      if (in) see[t] = nodes[node];
       const char* q = a.q + ((int64_t)b * a.q_batch + (int64_t)node * a.q_node + (int64_t)h * a.q_head) * 16;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
@@ -298,12 +320,13 @@ struct Attn {
 #pragma unroll
       for (int mm = 0; mm < DE; ++mm) acc[t][mm] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
+    far = false;
   }
 
   // The scores of the tile at entry t0 become weights (for bf16 products in pb), maxima and
   // sums of weights follow; true where nodes' values were infinite or NaN.
   __device__ __forceinline__ bool weigh(f32x4_t (&s)[RT][SUBS], uint4 (&pb)[RT], const AttnArgs& a,
-                                        const unsigned long long (&see)[RT], int t0, int ctx, const bool (&ok)[SUBS],
+                                        const Nodes (&see)[RT], int t0, int ctx, const bool (&ok)[SUBS],
                                         int lane) {
     bool odd = false;
     bool whole = t0 + KT <= ctx;
@@ -327,6 +350,7 @@ struct Attn {
       grow = grow || top[t] > m[t] + kMaxSlack;
     }
     if (__ballot(grow) != 0) {
+      bool beyond = false;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
@@ -334,10 +358,31 @@ struct Attn {
         const float mn = fmaxf(m[t], mx);
         const float f = m[t] == mn ? 1.f : fast_exp2(m[t] - mn);
         m[t] = mn;
+        beyond = beyond || (fabsf(mn) > kFusedMax && mn > kNoMax);
         l[t] *= f;
 #pragma unroll
         for (int mm = 0; mm < DE; ++mm) acc[t][mm] *= f;
       }
+      far = __ballot(beyond) != 0;
+    }
+    if (far) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y = s[t][u][i] * a.scale;
+            s[t][u][i] = y - m[t];
+          }
+    } else {
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][u][i] = fmaf(s[t][u][i], a.scale, -m[t]);
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -345,7 +390,7 @@ struct Attn {
       for (int u = 0; u < SUBS; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[t][u][i] = fast_exp2(fmaf(s[t][u][i], a.scale, -m[t]));
+          s[t][u][i] = fast_exp2(s[t][u][i]);
           l[t] += s[t][u][i];
         }
       // bf16 weights, as the values are: up to 2^-8 of each, in both directions
@@ -401,12 +446,12 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int64_t b) {
 // Adds the infinities and NaN among elements d .. d + 3 of the values of the nodes `see`
 // whose entries lie in [t_begin, t_end).
 template <typename E>
-__device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d, unsigned long long see, int t_begin,
+__device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d, Nodes see, int t_begin,
                                      int t_end, int ctx, float4& v) {
   for (int j = 0; j < a.n; ++j) {
     const int64_t t = (int64_t)ctx + j;
     const int64_t pg = t >> a.c.page_log2;
-    if (!((see >> j) & 1) || t < t_begin || t >= t_end || pg >= a.c.table_pages) continue;
+    if (!meet(see, only_node(j)) || t < t_begin || t >= t_end || pg >= a.c.table_pages) continue;
     const int32_t id = a.c.table[(int64_t)b * a.c.table_ld + pg];
     if (id < 0 || id >= a.c.pages) continue;
     const char* p = a.c.v + ((int64_t)id * a.c.s_page + (int64_t)hk * a.c.s_head +
@@ -442,12 +487,12 @@ struct Block {
 // (v; l the sum of weights, relative to mm).
 template <typename E, int D>
 __device__ __forceinline__ void end_row(const AttnArgs& a, const Block& at, int tile_rows, int row,
-                                        const unsigned long long* nodes, bool odd, int d, float mm, float l, float4 v) {
+                                        const Nodes* nodes, bool odd, int d, float mm, float l, float4 v) {
   const int node = row / a.group;
-  const unsigned long long see = nodes[node];
+  const Nodes see = nodes[node];
   if (odd) add_odd<E>(a, at.b, at.hk, d, see, at.t_begin, at.t_end, at.ctx, v);
   if (at.alone) {
-    const bool none = at.t_end == 0 || see == 0 || l == 0.f;
+    const bool none = at.t_end == 0 || none_of(see) || l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
     const int h = at.hk * a.group + row - node * a.group;
     store_out<E>(a.out, (((int64_t)at.b * a.n + node) * a.heads + h) * D + d,
@@ -458,7 +503,7 @@ __device__ __forceinline__ void end_row(const AttnArgs& a, const Block& at, int 
   const int64_t rec = (tile * a.splits + at.sp) * tile_rows + row % tile_rows;
   *reinterpret_cast<float4*>(a.acc + rec * D + d) = v;
   // (a node that is not there: no weight in any part)
-  if (d == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mm, see == 0 ? 0.f : l);
+  if (d == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mm, none_of(see) ? 0.f : l);
 }
 
 // The block's place, nodes and ancestors; false where it has nothing to do.
@@ -503,7 +548,7 @@ void tree_attention_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float o_sh[WAVES][16][A::LD];
   __shared__ float m_sh[WAVES][ROWS];
   __shared__ float l_sh[WAVES][ROWS];
-  __shared__ unsigned long long see_sh[64];
+  __shared__ Nodes see_sh[64];
   __shared__ int32_t parent_sh[64];
   __shared__ int odd_sh;  // some node's values were infinite or NaN
 
@@ -537,7 +582,7 @@ void tree_attention_kernel(AttnArgs a) {
   if (tid < a.n) see_sh[tid] = ancestors(parent_sh, tid, a.n);
   __syncthreads();
 
-  unsigned long long see[RT];
+  Nodes see[RT];
   const int row0 = at.tile * ROWS;
   w.take_rows(a, b, hk, row0, total > 0, see_sh, see, lane);
 
@@ -651,7 +696,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void many_rows_attention_kernel
   static_assert(kAttnWaves * 16 == kStageEntries, "a run to each wave");
   static_assert(kAttnWaves * 16 * A::LD * 4 <= 2 * kStage, "the end's rows fit the buffers");
   __shared__ __attribute__((aligned(16))) char stage[2 * kStage];
-  __shared__ unsigned long long see_sh[64];
+  __shared__ Nodes see_sh[64];
   __shared__ int32_t parent_sh[64];
   __shared__ int run_ok[2][kAttnWaves];  // whether a run of the stage has a page
   __shared__ int odd_sh;
@@ -702,7 +747,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, 2) void many_rows_attention_kernel
   __syncthreads();
 
   A w;
-  unsigned long long see[RT];
+  Nodes see[RT];
   const int row0 = at.tile * ROWS;
   w.take_rows(a, b, hk, row0, total > 0, see_sh, see, lane);
 

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_compact_kernel(CacheCompa
     const bool move = from >= 0 && to >= 0;
     const unsigned long long m = __ballot(move);
     if (move) {
-      const int at = __builtin_popcountll(m & ((1ull << j) - 1));
+      const int at = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
       from_sh[at] = from;
       to_sh[at] = to;
     }

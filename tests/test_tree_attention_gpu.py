@@ -141,6 +141,26 @@ def test_wide_tables(case, room):
     _check(got, want, _bound(q, k, v, lengths, parents, dtype, want))
 
 
+@pytest.mark.parametrize("Dh", [32, 64, 128])
+def test_many_calls_give_the_same_bits(Dh):
+    """Sequences whose nodes lie in a wave's third tile: every call is right, and equal to the first."""
+    rng = np.random.default_rng(64332 + Dh)
+    n, lengths = 64, [20, 300]
+    c = Cache(rng, lengths, n, 1, Dh, 16, torch.bfloat16)
+    parents = tree(rng, c.B, n)
+    k, v = _fill(rng, c, torch.bfloat16, parents)
+    table = torch.full((c.B, (1 << 20) // 16), -1, dtype=torch.int32, device=DEV)
+    table[:, :c.per] = c.t_table
+    q = values(rng, (c.B, n, 1, Dh), torch.bfloat16, 2.0)
+    args = (torch.tensor(q, device=DEV).to(torch.bfloat16), c.k[0], c.v[0], table, c.t_lengths,
+            torch.tensor(parents, device=DEV))
+    got = [D.tree_attention(*args) for _ in range(300)]
+    want = O.attention(q, k, v, lengths, parents)
+    _check(got[0], want, _bound(q, k, v, lengths, parents, torch.bfloat16, want))
+    for x in got[1:]:
+        assert torch.equal(x.view(torch.int16), got[0].view(torch.int16))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_chain_strides_and_scale(dtype):
     """Without parents a node sees the earlier ones; q lies in a wider tensor; a scale of the caller's."""
