@@ -324,3 +324,42 @@ def test_streams_graphs_and_repeats():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, D.tree_attention(q, *c.layer(), parents))
+
+
+@pytest.mark.parametrize("group,Dh,room", [(3, 128, 512 * 256), (1, 96, 1 << 21), (5, 64, 1 << 19)])
+def test_wide_tables_in_a_graph_and_on_two_streams(group, Dh, room):
+    """Replays follow new lengths, trees and queries; two calls at once do not share a workspace."""
+    rng = np.random.default_rng(group)
+    n, page, lengths = 40, 16, [290, 44]
+    c = Cache(rng, [310, 60], n, 1, Dh, page, torch.bfloat16)  # (room for the longer contexts below)
+    parents = tree(rng, c.B, n, absent=False)
+    _fill(rng, c, torch.bfloat16, parents)
+    table = torch.full((c.B, room // page), -1, dtype=torch.int32, device=DEV)
+    table[:, :c.per] = c.t_table
+    make = lambda: torch.tensor(values(rng, (c.B, n, group, Dh), torch.bfloat16), device=DEV).to(torch.bfloat16)  # noqa: E731
+    q, len_, par = make(), torch.tensor(lengths, dtype=torch.int32, device=DEV), torch.tensor(parents, device=DEV)
+    call = lambda x, ln, pr: D.tree_attention(x, c.k[0], c.v[0], table, ln, pr)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(q, len_, par)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call(q, len_, par)
+    for step in range(3):
+        q.copy_(make())
+        len_.copy_(torch.tensor([[290, 44], [310, 60], [-1, 7]][step], dtype=torch.int32))
+        par.copy_(torch.tensor(tree(rng, c.B, n), device=DEV))
+        g.replay()
+        assert torch.equal(out.view(torch.int16), call(q, len_, par).view(torch.int16))
+    other = make()
+    want = call(q, len_, par).clone(), call(other, len_, par).clone()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            b = call(other, len_, par)
+        a = call(q, len_, par)
+        torch.cuda.synchronize()
+        assert torch.equal(a.view(torch.int16), want[0].view(torch.int16))
+        assert torch.equal(b.view(torch.int16), want[1].view(torch.int16))
