@@ -447,9 +447,13 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
       for (int j = 0; j < rejected; ++j) x = fmax(x - qv, 0.0) * ts.scale[j];
       return x;
     }
-    for (int j = 0; j < rejected; ++j)
+    // (each factor is 1 over the mass left of the step before, which the last one alone is not; in
+    // the list's order, so that a token has the same bits here and there)
+    for (int j = 0; j < rejected; ++j) {
       if (ts.gone[j] == v) return 0.0;
-    return x * ts.scale[rejected - 1];
+      x *= ts.scale[j];
+    }
+    return x;
   };
   bool want_q = false;  // the row to open next: the draft's at this node, or the verifier's at a new one
   int i = 1;
