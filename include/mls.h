@@ -620,7 +620,7 @@ typedef struct mls_kv_cache {
  * device arrays [batch][n][kv_heads][head_dim] of the cache's dtype, 16-byte aligned, with
  * the given strides (elements, multiples of 16 bytes; the heads' elements are neighbours),
  * and must not overlap the pages. Nothing else is written; lengths stay as they are.
- * Asynchronous on stream.
+ * (n / 16 + 1) (kv_heads / 8), each rounded up, is below 2^24. Asynchronous on stream.
  */
 mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, const void* v, int64_t ld_batch,
                            int64_t ld_node, int64_t ld_head, const int32_t* counts, void* stream);
@@ -653,7 +653,9 @@ mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* pa
  * the cache's dtype, 16-byte aligned. n in 1..64, heads a multiple of kv_heads, head_dim
  * 32, 64, 96, 128, 192 or 256, scale finite and > 0. Sums are fp32; bf16 weights are rounded to bfloat16 for the
  * product with the values. Results depend on the table's width (entries are taken in parts),
- * and are the same bits on every call. Asynchronous on stream.
+ * and are the same bits on every call. Calls of 2^24 or more blocks (row tiles times parts of
+ * the entries, over all sequences and key heads), or of 2^34 or more results where there are
+ * parts to join, are refused. Asynchronous on stream.
  */
 mls_status mls_tree_attention_workspace(const mls_kv_cache* c, int64_t n, int64_t heads, size_t* bytes);
 mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, const void* q, int64_t ld_batch,
@@ -661,8 +663,8 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Verification of `batch` trees of n nodes (1..64), node 0 the last decided token. Device
- * arrays:
+ * Verification of `batch` trees (below 2^22) of n nodes (1..64), node 0 the last decided
+ * token. Device arrays:
  *   target_logits [batch][n][V]  the verifier's logits at each node
  *   tokens        [batch][n]     int32, node i's drafted token (node 0's is not used)
  *   parents       [batch][n]     int32, an earlier node; a node with any other parent is not
@@ -709,7 +711,8 @@ mls_status mls_quantize_rows(int64_t T, int64_t d, int64_t ld_x, int32_t dtype, 
  *   logits[t][v] = scale[t] W_scale[v] sum_k q[t][k] W[v][k],
  * the sum in 32-bit integers, exact. o [T][d] of dtype, W int8 [V][d], logits float32
  * [T][V], all contiguous and 16-byte aligned; W_scale float32 [V]. d is a multiple of 16, at
- * most 2^17. A row of o with an infinity or NaN gives NaN. Asynchronous on stream.
+ * most 2^17, and the tiles of the logits (64 x 32 to 192 x 128) number below 2^24. A row of o
+ * with an infinity or NaN gives NaN. Asynchronous on stream.
  */
 mls_status mls_head_logits_quantized_workspace(int64_t T, int64_t d, size_t* bytes);
 mls_status mls_head_logits_quantized(int64_t T, int64_t V, int64_t d, int32_t dtype, const void* o, const int8_t* W,

@@ -2222,6 +2222,10 @@ mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
 namespace {
 
 constexpr int64_t kMaxNodes = 64;  // nodes of a tree
+// A launch takes less than 2^32 threads along a dimension of its grid: blocks of 256, and
+// trees of a block of 1,024 each.
+constexpr int64_t kLaunchBlocks = (1ll << 24) - 1;
+constexpr int64_t kMaxTrees = (1ll << 22) - 1;
 
 mls_status validate_cache(const mls_kv_cache* c, int64_t layers_max) {
   if (!c) return fail(MLS_INVALID_ARG, "cache descriptor is NULL");
@@ -2343,8 +2347,10 @@ mls_status plan_attention(const mls_kv_cache* c, int64_t n, int64_t heads, AttnP
   pl.shorts = attn_short(base, cap, (int32_t)pl.rows, D * (c->dtype == MLS_BF16 ? 2 : 4));
   if (pl.shorts) pl.part = round_up(cap, 128);
   pl.splits = (cap + pl.part - 1) / pl.part;
-  if (base * pl.splits > 0x7fffff00 - 8 * pl.n_rt || c->batch * n * heads * (D / 4) > (1ll << 38))
+  if (round_up(c->batch * c->kv_heads * pl.splits, 8) * pl.n_rt > kLaunchBlocks)
     return fail(MLS_UNSUPPORTED, "%lld parts of the cache are more than one launch takes", (long long)(base * pl.splits));
+  if (pl.splits > 1 && c->batch * n * heads * (D / 4) > kLaunchBlocks * 256)
+    return fail(MLS_UNSUPPORTED, "%lld rows are more than one launch joins", (long long)(c->batch * n * heads));
   pl.once = pl.n_rt == 1 && c->batch * cap * c->kv_heads * D * (c->dtype == MLS_BF16 ? 4 : 8) > kMemorySideBytes;
   pl.records = pl.splits > 1 ? c->batch * c->kv_heads * pl.n_tiles * pl.splits * pl.tile : 0;
   pl.acc_bytes = align256((size_t)pl.records * D * 4);
@@ -2363,7 +2369,7 @@ size_t tree_ws_bytes(const mls_sampling* s, int64_t batch, int64_t n) {
 }
 
 mls_status validate_tree(int64_t batch, int64_t n) {
-  if (batch < 1 || batch > (1 << 24) || n < 1 || n > kMaxNodes)
+  if (batch < 1 || batch > kMaxTrees || n < 1 || n > kMaxNodes)
     return fail(MLS_INVALID_ARG, "batch=%lld n=%lld out of range", (long long)batch, (long long)n);
   return MLS_OK;
 }
@@ -2390,7 +2396,7 @@ mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, cons
   CacheWriteArgs a;
   memset(&a, 0, sizeof(a));
   a.c = cache_args(c);
-  if (n < 1 || n > (1ll << 30) || cache_write_blocks(n, a.c.kv_heads) > 0x7fffffff)
+  if (n < 1 || n > (1ll << 30) || cache_write_blocks(n, a.c.kv_heads) > kLaunchBlocks)
     return fail(MLS_INVALID_ARG, "n=%lld out of range", (long long)n);
   if ((st = validate_rows("k", k, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if ((st = validate_rows("v", v, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
@@ -2643,7 +2649,7 @@ mls_status mls_head_logits_quantized(int64_t T, int64_t V, int64_t d, int32_t dt
   head_i8_tile(T, V, &rows, &cols);
   a.n_tt = (int)((T + cols - 1) / cols);
   a.n_vt = (int)((V + rows - 1) / rows);
-  if ((int64_t)a.n_tt * a.n_vt > 0x7fffffff) return fail(MLS_INVALID_ARG, "T=%lld V=%lld out of range", (long long)T, (long long)V);
+  if ((int64_t)a.n_tt * a.n_vt > kLaunchBlocks) return fail(MLS_INVALID_ARG, "T=%lld V=%lld out of range", (long long)T, (long long)V);
   a.group_v = rows == 192 ? 4 : 8;
   QuantArgs z;
   memset(&z, 0, sizeof(z));

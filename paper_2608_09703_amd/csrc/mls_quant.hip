@@ -168,12 +168,23 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(QuantArgs 
       q[(int64_t)whole * N + i] = (int8_t)(s > 0.f ? quantize(widen(x[(int64_t)whole * N + i]), s) : 0);
 }
 
+// (a launch takes less than 2^32 threads: more rows go in pieces)
 template <typename E, int LANES, int C>
-hipError_t launch_quant(const QuantArgs& a, hipStream_t stream) {
+hipError_t launch_quant(const QuantArgs& all, hipStream_t stream) {
   constexpr int rows = kQuantThreads / LANES;
-  hipLaunchKernelGGL((quantize_rows_kernel<E, LANES, C>), dim3((unsigned)((a.T + rows - 1) / rows)),
-                     dim3(kQuantThreads), 0, stream, a);
-  return hipGetLastError();
+  constexpr int64_t piece = (int64_t)rows << 23;
+  for (int64_t t = 0; t < all.T; t += piece) {
+    QuantArgs a = all;
+    a.x = static_cast<const typename E::storage*>(all.x) + t * all.ld;
+    a.q += t * all.d;
+    a.scale += t;
+    a.T = all.T - t < piece ? all.T - t : piece;
+    hipLaunchKernelGGL((quantize_rows_kernel<E, LANES, C>), dim3((unsigned)((a.T + rows - 1) / rows)),
+                       dim3(kQuantThreads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename E>
