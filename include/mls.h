@@ -280,7 +280,7 @@ enum mls_junction_flags {
   MLS_JUNCTION_ACCUMULATE = 1u  /* backward: g_o += and g_e += instead of = */
 };
 typedef struct mls_junction {
-  int64_t T;           /* tokens, >= 1 */
+  int64_t T;           /* tokens, >= 1; below 2^26, of widths above 1024 2^25, above 2048 2^24 */
   int64_t d_prev;      /* width of o: a multiple of 8 in [8, 8192] */
   int64_t d_fresh;     /* width of e: a multiple of 8 in [8, 8192] */
   int32_t act_dtype;   /* mls_dtype of o, e and x */
@@ -507,7 +507,8 @@ typedef struct mls_sampling {
 /*
  * logits[t][v] = sum_k o[t][k] W[v][k] (fp32 row-major [T][V]) for o [T][d]
  * and W [V][d] of dtype (MLS_BF16: d a multiple of 8; MLS_F32: of 4), all
- * device arrays, 16-byte aligned. Asynchronous on stream.
+ * device arrays, 16-byte aligned; the tiles of the logits (64 x 32 to 192 x 128)
+ * number below 2^24. Asynchronous on stream.
  */
 mls_status mls_head_logits(int64_t T, int64_t V, int64_t d, int32_t dtype, const void* o,
                            const void* W, float* logits, void* stream);
@@ -553,8 +554,9 @@ mls_status mls_spec_verify_workspace(int64_t batch, int64_t gamma, size_t* bytes
  * MLS_ROW_PARAMS_BYTES from mls_sample on the same draft rows with the same
  * sampling settings; then the draft rows' distributions are not recomputed.
  * Outputs n_accepted, next_token: int32 [batch]; next_token is -1 where it is
- * to be drawn from a verifier row that keeps no token (see mls_sample).
- * Asynchronous on stream.
+ * to be drawn from a verifier row that keeps no token (see mls_sample). A call
+ * takes less than 2^22 sequences and, sampled, less than 2^22 rows (the drafts'
+ * without draft_params, and the verifier's). Asynchronous on stream.
  */
 mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
                            const float* draft_logits, const float* target_logits,

@@ -89,6 +89,10 @@ constexpr int64_t kRecordBudget = 1ll << 30;      // forward partial records of 
 constexpr int64_t kLogitSlabBudget = 16ll << 30;  // stored logits of one token chunk (all sub-models)
 constexpr int64_t kPanelMax = (1ll << 32) - 1;    // bytes one wide-GEMM operand may span
 constexpr int64_t kCus = 256;                     // compute units of the part
+// A launch takes less than 2^32 threads along a dimension of its grid (one of more runs a
+// part of them, and reports nothing): blocks of 256, and rows or trees of a block of 1,024.
+constexpr int64_t kLaunchBlocks = (1ll << 24) - 1;
+constexpr int64_t kLaunchRows = (1ll << 22) - 1;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxSplits = 16;                // K parts of a grad_h product
 // and of token log-probabilities', whose one chunk has a K of all of V for as little as
@@ -1557,6 +1561,10 @@ mls_status validate_junction(const mls_junction* j) {
   if (j->d_prev % 8 || j->d_fresh % 8)
     return fail(MLS_UNSUPPORTED, "junction widths %lld / %lld are not multiples of 8",
                 (long long)j->d_prev, (long long)j->d_fresh);
+  int tpr, cpl;  // threads of a row
+  if (!junction_shape(std::max(j->d_prev, j->d_fresh), &tpr, &cpl) || j->T * tpr >= 1ll << 32)
+    return fail(MLS_UNSUPPORTED, "T=%lld: more rows than one launch takes (2^26 up to 1,024 wide, 2^25 up to 2,048, 2^24)",
+                (long long)j->T);
   if ((j->act_dtype != MLS_BF16 && j->act_dtype != MLS_F32) ||
       (j->grad_dtype != MLS_BF16 && j->grad_dtype != MLS_F32))
     return fail(MLS_UNSUPPORTED, "junction dtypes %d / %d unsupported", j->act_dtype, j->grad_dtype);
@@ -2091,6 +2099,8 @@ mls_status mls_head_logits(int64_t T, int64_t V, int64_t d, int32_t dtype, const
   head_tile(wide, T, V, &rows, &cols);
   a.n_tt = (int)((T + cols - 1) / cols);
   a.n_vt = (int)((V + rows - 1) / rows);
+  if ((int64_t)a.n_tt * a.n_vt > kLaunchBlocks)
+    return fail(MLS_UNSUPPORTED, "T=%lld V=%lld: more tiles than one launch takes", (long long)T, (long long)V);
   // tile order (groups of vocabulary tiles), measured on the verifier's 714
   // rows with 192-row tiles: groups of 2 or 4 0.731-0.742 ms per decode step,
   // 6 0.756-0.759, 8 0.745-0.750, 16 0.753-0.758, 32 0.79-0.80
@@ -2140,7 +2150,7 @@ mls_status mls_sample(const mls_sampling* s, int64_t rows, const float* logits, 
 
 mls_status mls_spec_verify_workspace(int64_t batch, int64_t gamma, size_t* bytes) {
   g_last_error.clear();
-  if (batch < 1 || gamma < 0 || batch > (1 << 24) || gamma > 1024)
+  if (batch < 1 || gamma < 0 || batch > kLaunchRows || gamma > 1024)
     return fail(MLS_INVALID_ARG, "batch=%lld gamma=%lld out of range", (long long)batch, (long long)gamma);
   if (!bytes) return fail(MLS_INVALID_ARG, "bytes is NULL");
   *bytes = verify_ws_bytes(batch, gamma);
@@ -2156,7 +2166,7 @@ mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
   g_last_error.clear();
   mls_status st = validate_sampling(s);
   if (st != MLS_OK) return st;
-  if (batch < 1 || gamma < 0 || batch > (1 << 24) || gamma > 1024)
+  if (batch < 1 || gamma < 0 || batch > kLaunchRows || gamma > 1024)
     return fail(MLS_INVALID_ARG, "batch=%lld gamma=%lld out of range", (long long)batch, (long long)gamma);
   if (!target_logits || !n_accepted || !next_token || (gamma > 0 && (!draft_logits || !draft_tokens)))
     return fail(MLS_INVALID_ARG, "logits, draft tokens and outputs must be non-NULL");
@@ -2175,6 +2185,8 @@ mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
   // workspace: draft rows' records [gamma][batch], then the verifier rows' [batch][gamma + 1]
   RowDist* params = static_cast<RowDist*>(workspace);
   const bool have_draft = draft_params != nullptr && gamma > 0;
+  if (!s->greedy && batch * (gamma + 1) + (have_draft ? 0 : batch * gamma) > kLaunchRows)
+    return fail(MLS_UNSUPPORTED, "batch=%lld gamma=%lld: at most 2^22 - 1 rows a call", (long long)batch, (long long)gamma);
   if (!s->greedy) {
     RowParamArgs r;
     memset(&r, 0, sizeof(r));
@@ -2222,10 +2234,6 @@ mls_status mls_spec_verify(const mls_sampling* s, int64_t batch, int64_t gamma,
 namespace {
 
 constexpr int64_t kMaxNodes = 64;  // nodes of a tree
-// A launch takes less than 2^32 threads along a dimension of its grid: blocks of 256, and
-// trees of a block of 1,024 each.
-constexpr int64_t kLaunchBlocks = (1ll << 24) - 1;
-constexpr int64_t kMaxTrees = (1ll << 22) - 1;
 
 mls_status validate_cache(const mls_kv_cache* c, int64_t layers_max) {
   if (!c) return fail(MLS_INVALID_ARG, "cache descriptor is NULL");
@@ -2369,7 +2377,7 @@ size_t tree_ws_bytes(const mls_sampling* s, int64_t batch, int64_t n) {
 }
 
 mls_status validate_tree(int64_t batch, int64_t n) {
-  if (batch < 1 || batch > kMaxTrees || n < 1 || n > kMaxNodes)
+  if (batch < 1 || batch > kLaunchRows || n < 1 || n > kMaxNodes)
     return fail(MLS_INVALID_ARG, "batch=%lld n=%lld out of range", (long long)batch, (long long)n);
   return MLS_OK;
 }

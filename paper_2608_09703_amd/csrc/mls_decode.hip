@@ -423,16 +423,28 @@ hipError_t launch_head_logits_i8(const HeadArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_sample(const SampleArgs& a, int ept, hipStream_t stream) {
-  const dim3 grid((unsigned)a.rows);
-  switch (ept) {
-    case 16: hipLaunchKernelGGL(sample_kernel<16>, grid, dim3(kRowThreads), 0, stream, a); break;
-    case 32: hipLaunchKernelGGL(sample_kernel<32>, grid, dim3(kRowThreads), 0, stream, a); break;
-    case 48: hipLaunchKernelGGL(sample_kernel<48>, grid, dim3(kRowThreads), 0, stream, a); break;
-    case 64: hipLaunchKernelGGL(sample_kernel<64>, grid, dim3(kRowThreads), 0, stream, a); break;
-    default: return hipErrorInvalidValue;
+// (a launch takes less than 2^22 blocks of 1,024 threads: more rows go in pieces)
+hipError_t launch_sample(const SampleArgs& all, int ept, hipStream_t stream) {
+  constexpr int64_t kPiece = 1ll << 21;
+  for (int64_t r = 0; r < all.rows; r += kPiece) {
+    SampleArgs a = all;
+    a.rows = all.rows - r < kPiece ? all.rows - r : kPiece;
+    a.logits += r * a.V;
+    a.tokens += r;
+    if (a.u) a.u += r;
+    if (a.params) a.params += r;
+    const dim3 grid((unsigned)a.rows);
+    switch (ept) {
+      case 16: hipLaunchKernelGGL(sample_kernel<16>, grid, dim3(kRowThreads), 0, stream, a); break;
+      case 32: hipLaunchKernelGGL(sample_kernel<32>, grid, dim3(kRowThreads), 0, stream, a); break;
+      case 48: hipLaunchKernelGGL(sample_kernel<48>, grid, dim3(kRowThreads), 0, stream, a); break;
+      case 64: hipLaunchKernelGGL(sample_kernel<64>, grid, dim3(kRowThreads), 0, stream, a); break;
+      default: return hipErrorInvalidValue;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 hipError_t launch_row_params(const RowParamArgs& a, int ept, hipStream_t stream) {

@@ -17,10 +17,10 @@ namespace mls {
 namespace {
 
 template <typename E>
-__global__ __launch_bounds__(kThreads) void label_logits_kernel(RowArgs a) {
+__global__ __launch_bounds__(kThreads) void label_logits_kernel(RowArgs a, int64_t w0) {
   using S = typename E::storage;
   const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t w = w0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (w >= (int64_t)a.M * a.T) return;
   const int i = (int)(w / a.T);
   const int64_t t = w % a.T;
@@ -331,12 +331,18 @@ hipError_t launch_grad_logits(const GradArgs& a, hipStream_t stream) {
 
 hipError_t launch_label_logits(const RowArgs& a, bool f32, hipStream_t stream) {
   const int64_t waves = (int64_t)a.M * a.T;
-  dim3 grid((unsigned)((waves + 3) / 4));
-  if (f32)
-    hipLaunchKernelGGL(label_logits_kernel<F32>, grid, dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(label_logits_kernel<Bf16>, grid, dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  constexpr int64_t kPiece = 1ll << 25;  // of a launch, which takes less than 2^26 waves
+  for (int64_t w0 = 0; w0 < waves; w0 += kPiece) {
+    const int64_t n = waves - w0 < kPiece ? waves - w0 : kPiece;
+    dim3 grid((unsigned)((n + 3) / 4));
+    if (f32)
+      hipLaunchKernelGGL(label_logits_kernel<F32>, grid, dim3(kThreads), 0, stream, a, w0);
+    else
+      hipLaunchKernelGGL(label_logits_kernel<Bf16>, grid, dim3(kThreads), 0, stream, a, w0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <int MM>
