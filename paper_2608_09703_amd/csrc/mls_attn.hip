@@ -350,12 +350,13 @@ struct Attn {
       grow = grow || top[t] > m[t] + kMaxSlack;
     }
     if (__ballot(grow) != 0) {
+      // (each row by its own scores: its bits do not depend on what the other rows see)
       bool beyond = false;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = fmaxf(m[t], mx);
+        const float mn = mx > m[t] + kMaxSlack ? mx : m[t];
         const float f = m[t] == mn ? 1.f : fast_exp2(m[t] - mn);
         m[t] = mn;
         beyond = beyond || (fabsf(mn) > kFusedMax && mn > kNoMax);
@@ -368,14 +369,17 @@ struct Attn {
     if (far) {
 #pragma clang fp contract(off)
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
+      for (int t = 0; t < RT; ++t) {
+        const bool beyond = fabsf(m[t]) > kFusedMax;
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float y = s[t][u][i] * a.scale;
-            s[t][u][i] = y - m[t];
+            const float z = fmaf(s[t][u][i], a.scale, -m[t]);
+            s[t][u][i] = beyond ? y - m[t] : z;
           }
+      }
     } else {
 #pragma unroll
       for (int t = 0; t < RT; ++t)
@@ -467,10 +471,11 @@ __device__ __forceinline__ void add_odd(const AttnArgs& a, int b, int hk, int d,
         bits = __float_as_uint(e);
       x[i] = (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.f;
     }
-    v.x += x[0];
-    v.y += x[1];
-    v.z += x[2];
-    v.w += x[3];
+    // (nothing else: a zero keeps its sign)
+    v.x = x[0] != 0.f ? v.x + x[0] : v.x;
+    v.y = x[1] != 0.f ? v.y + x[1] : v.y;
+    v.z = x[2] != 0.f ? v.z + x[2] : v.z;
+    v.w = x[3] != 0.f ? v.w + x[3] : v.w;
   }
 }
 
