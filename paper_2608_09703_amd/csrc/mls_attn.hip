@@ -347,7 +347,7 @@ struct Attn {
 #pragma unroll
         for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][u][i]);
       top[t] *= a.scale;  // (above 0)
-      grow = grow || top[t] > m[t] + kMaxSlack;
+      grow = grow || top[t] >= m[t] + kMaxSlack;
     }
     if (__ballot(grow) != 0) {
       // (each row by its own scores: its bits do not depend on what the other rows see)
@@ -356,10 +356,10 @@ struct Attn {
       for (int t = 0; t < RT; ++t) {
         float mx = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = mx > m[t] + kMaxSlack ? mx : m[t];
+        const float mn = mx >= m[t] + kMaxSlack ? mx : m[t];
         const float f = m[t] == mn ? 1.f : fast_exp2(m[t] - mn);
         m[t] = mn;
-        beyond = beyond || (fabsf(mn) > kFusedMax && mn > kNoMax);
+        beyond = beyond || (fabsf(mn) > kFusedMax && (mn > kNoMax || mx == kNoMax));
         l[t] *= f;
 #pragma unroll
         for (int mm = 0; mm < DE; ++mm) acc[t][mm] *= f;
