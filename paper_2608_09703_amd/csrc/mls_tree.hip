@@ -43,17 +43,25 @@ constexpr int kAhead = 8;      // entries of a large list that a thread has in f
 constexpr int kMaxSlabs = 64;  // of kTreeThreads tokens: rows of up to 65,536
 static_assert(kMaxCand <= kTreeThreads, "a thread owns at most one token of a list");
 
+// What a row's weights are relative to: exp((logit - base) / temperature - top).
+struct Top {
+  double base;
+  double top;
+};
+
 // An opened row in the workspace; its list is idx[kMaxCand], p[kMaxCand].
 struct TreeRow {
   RowDist d;
   int32_t n;    // tokens of its list; -1: none, the row keeps more
   double norm;  // 1 / (sum of kept weights); 0: the row keeps no token
+  Top top;
 };
 
 struct Row {
   const float* logits;
   RowDist d;
   double norm;
+  Top top;
 };
 
 // How rows are sampled.
@@ -100,12 +108,12 @@ __device__ __forceinline__ double block_sum(double v, TreeShared& ts, int& turn)
   return block_sum(v, ts.red[turn]);
 }
 
-// exp(logit / temperature - m) of a kept token, 2e-14 off at most: with t the integer next
+// A kept token's weight, 2e-14 off at most: with t the integer next
 // to y / ln 2, 2^t times the exponential's series at y - t ln 2, whose first term left out
 // is 0.35^12 / 12!. A few of these per token are most of the arithmetic (the library's
 // exp and the division are three times as many operations).
-__device__ __forceinline__ double weight(const RowDist& d, float logit, double inv_temp) {
-  const double y = fma((double)logit, inv_temp, -(double)d.m);
+__device__ __forceinline__ double weight(const Top& t0, float logit, double inv_temp) {
+  const double y = fma((double)logit - t0.base, inv_temp, -t0.top);
   const double t = rint(y * 1.4426950408889634074);
   const double f = fma(t, -0.69314718055994530942, y);
   double e = 1.0 / 39916800.0;
@@ -124,7 +132,7 @@ __device__ __forceinline__ double weight(const RowDist& d, float logit, double i
 }
 __device__ __forceinline__ double prob_of(const Row& r, float logit, int v, const Settings& a) {
   if (r.norm == 0.0 || !kept_w(exp_weight(logit, a.inv_temp, r.d), v, r.d)) return 0.0;
-  return weight(r.d, logit, a.inv_temp64) * r.norm;
+  return weight(r.top, logit, a.inv_temp64) * r.norm;
 }
 __device__ __forceinline__ double prob(const Row& r, int v, const Settings& a) {
   return prob_of(r, r.logits[v], v, a);
@@ -158,10 +166,29 @@ __device__ __forceinline__ void for_wave_range(const float* logits, int V, F f) 
 struct Opened {
   RowDist d;
   double norm;
+  Top top;
   int n;
   int idx;
   double p;
 };
+
+// A row's weights are relative to its record's maximum, a rounded product: what it is off by is a
+// factor that all weights share, and norm takes out. Far from 0 that factor, e to the 2^-23 of
+// the maximum, would leave the numbers there are: there they are relative to the largest logit itself.
+constexpr float kFarTop = 16777216.f;
+__device__ __forceinline__ Top top_of(const float* logits, const RowDist& d, const Settings& a, double* red) {
+  if (!(fabsf(d.m) > kFarTop)) return Top{0.0, (double)d.m};
+  float x = -INFINITY;
+  for_wave_range(logits, a.V, [&](float l, int, bool in) { x = in ? fmaxf(x, l) : x; });
+  x = wave_max(x);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (double)x;
+  __syncthreads();
+  double m = red[0];
+#pragma unroll
+  for (int i = 1; i < kTreeWaves; ++i) m = fmax(m, red[i]);
+  __syncthreads();  // (the caller sums there next)
+  return Top{m, 0.0};
+}
 
 // Opens a row, its record given or found. Larger ones' weights are summed where `sum` asks
 // for it. All threads call it.
@@ -191,6 +218,7 @@ __device__ __forceinline__ Opened open_row(const float* logits, const RowDist* r
       n = kMaxCand + 1;
     }
   }
+  r.top = top_of(logits, r.d, a, os.red);
   r.n = n <= kMaxCand ? n : -1;
   r.idx = -1;
   r.p = 0.0;
@@ -198,13 +226,13 @@ __device__ __forceinline__ Opened open_row(const float* logits, const RowDist* r
   if (r.n >= 0) {
     if ((int)threadIdx.x < n) {
       r.idx = sh.ci[cand_slot(threadIdx.x)];
-      if (kept_w(sh.cw[cand_slot(threadIdx.x)], r.idx, r.d)) r.p = weight(r.d, logits[r.idx], a.inv_temp64);
+      if (kept_w(sh.cw[cand_slot(threadIdx.x)], r.idx, r.d)) r.p = weight(r.top, logits[r.idx], a.inv_temp64);
     }
     s = r.p;
   } else if (sum) {
     for_wave_range(logits, a.V, [&](float l, int v, bool in) {
       const bool k = in && kept_w(exp_weight(l, a.inv_temp, r.d), v, r.d);
-      if (__ballot(k) != 0 && k) s += weight(r.d, l, a.inv_temp64);
+      if (__ballot(k) != 0 && k) s += weight(r.top, l, a.inv_temp64);
     });
   }
   s = block_sum(s, os.red);
@@ -247,7 +275,7 @@ __device__ __forceinline__ int open_large(const Settings& a, TreeShared& ts, int
     if (m == 0) return;
     if (k) {
       const int pos = at + lanes_below(m);
-      const double w = weight(r.d, l, a.inv_temp64);
+      const double w = weight(r.top, l, a.inv_temp64);
       li[pos] = v;
       lr[pos] = w;
       s += w;
@@ -290,6 +318,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_rows_kernel(TreeVerifyArgs 
     t.d = r.d;
     t.n = r.n;
     t.norm = r.norm;
+    t.top = r.top;
     static_cast<TreeRow*>(a.ready_rows)[row] = t;
   }
 }
@@ -472,6 +501,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
         x.logits = logits;
         x.d = t.d;
         x.norm = t.norm;
+        x.top = t.top;
         xn = t.n;
         const bool in = !want_q && (int)threadIdx.x < xn;
         xi = in ? a.list_idx[at * kMaxCand + threadIdx.x] : -1;
@@ -481,6 +511,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
         x.logits = logits;
         x.d = o.d;
         x.norm = o.norm;
+        x.top = o.top;
         xn = o.n;
         xi = o.idx;
         xp = o.p;
