@@ -594,7 +594,8 @@ mls_status mls_spec_verify_noalloc(const mls_sampling* s, int64_t batch, int64_t
  * (a common prefix) as long as neither writes to it. A page number outside [0, pages) or
  * an entry past the table's row is not there: it is not read or written, and attention
  * leaves it out. Strides are in elements, and multiples of 16 bytes; k and v have the same.
- * Dimensions may lie in any order, each stepping over all of those inside it.
+ * Dimensions may lie in any order, each stepping over all of those inside it. k and v share no
+ * entry, unless nothing is written or both are to hold the same.
  */
 typedef struct mls_kv_cache {
   int32_t dtype;              /* mls_dtype of k and v */

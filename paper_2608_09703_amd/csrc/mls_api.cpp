@@ -2409,6 +2409,7 @@ mls_status mls_cache_write(const mls_kv_cache* c, int64_t n, const void* k, cons
   if ((st = validate_rows("k", k, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if ((st = validate_rows("v", v, es, ld_batch, ld_node, ld_head)) != MLS_OK) return st;
   if (!aligned(counts, 4)) return fail(MLS_INVALID_ARG, "misaligned pointer");
+  if (c->k == c->v && k != v) return fail(MLS_INVALID_ARG, "keys and values would be written to the same pages");
   const int64_t per = 16 / es;
   a.k = static_cast<const char*>(k);
   a.v = static_cast<const char*>(v);
