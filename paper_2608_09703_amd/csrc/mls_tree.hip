@@ -43,25 +43,19 @@ constexpr int kAhead = 8;      // entries of a large list that a thread has in f
 constexpr int kMaxSlabs = 64;  // of kTreeThreads tokens: rows of up to 65,536
 static_assert(kMaxCand <= kTreeThreads, "a thread owns at most one token of a list");
 
-// What a row's weights are relative to: exp((logit - base) / temperature - top).
-struct Top {
-  double base;
-  double top;
-};
-
 // An opened row in the workspace; its list is idx[kMaxCand], p[kMaxCand].
 struct TreeRow {
   RowDist d;
   int32_t n;    // tokens of its list; -1: none, the row keeps more
   double norm;  // 1 / (sum of kept weights); 0: the row keeps no token
-  Top top;
+  double top;
 };
 
 struct Row {
   const float* logits;
   RowDist d;
   double norm;
-  Top top;
+  double top;
 };
 
 // How rows are sampled.
@@ -108,12 +102,13 @@ __device__ __forceinline__ double block_sum(double v, TreeShared& ts, int& turn)
   return block_sum(v, ts.red[turn]);
 }
 
-// A kept token's weight, 2e-14 off at most: with t the integer next
+// exp(logit / temperature - top) of a kept token, 2e-14 off at most: with t the integer next
 // to y / ln 2, 2^t times the exponential's series at y - t ln 2, whose first term left out
 // is 0.35^12 / 12!. A few of these per token are most of the arithmetic (the library's
-// exp and the division are three times as many operations).
-__device__ __forceinline__ double weight(const Top& t0, float logit, double inv_temp) {
-  const double y = fma((double)logit - t0.base, inv_temp, -t0.top);
+// exp and the division are three times as many operations). (kMostLog: see top_of.)
+constexpr double kMostLog = 600.0;
+__device__ __forceinline__ double weight(double top, float logit, double inv_temp) {
+  const double y = fmin(fma((double)logit, inv_temp, -top), kMostLog);
   const double t = rint(y * 1.4426950408889634074);
   const double f = fma(t, -0.69314718055994530942, y);
   double e = 1.0 / 39916800.0;
@@ -166,18 +161,20 @@ __device__ __forceinline__ void for_wave_range(const float* logits, int V, F f) 
 struct Opened {
   RowDist d;
   double norm;
-  Top top;
+  double top;
   int n;
   int idx;
   double p;
 };
 
-// A row's weights are relative to its record's maximum, a rounded product: what it is off by is a
-// factor that all weights share, and norm takes out. Far from 0 that factor, e to the 2^-23 of
-// the maximum, would leave the numbers there are: there they are relative to the largest logit itself.
+// What a row's weights are relative to: its record's maximum, a float32 product. What that is off
+// by is a factor that all weights share, and norm takes out. Far from 0 this factor, e to the
+// 2^-23 of the maximum, would leave the numbers there are: there it is the largest logit's
+// product in 64 bits, from below. Where even that is more than e^kMostLog off (the maximum past
+// 2^60), the largest weights are kMostLog's, and neighbouring logits' are 0 beside them.
 constexpr float kFarTop = 16777216.f;
-__device__ __forceinline__ Top top_of(const float* logits, const RowDist& d, const Settings& a, double* red) {
-  if (!(fabsf(d.m) > kFarTop)) return Top{0.0, (double)d.m};
+__device__ __forceinline__ double top_of(const float* logits, const RowDist& d, const Settings& a, double* red) {
+  if (!(fabsf(d.m) > kFarTop)) return (double)d.m;
   float x = -INFINITY;
   for_wave_range(logits, a.V, [&](float l, int, bool in) { x = in ? fmaxf(x, l) : x; });
   x = wave_max(x);
@@ -187,7 +184,8 @@ __device__ __forceinline__ Top top_of(const float* logits, const RowDist& d, con
 #pragma unroll
   for (int i = 1; i < kTreeWaves; ++i) m = fmax(m, red[i]);
   __syncthreads();  // (the caller sums there next)
-  return Top{m, 0.0};
+  m *= a.inv_temp64;
+  return m - fabs(m) * 0x1p-52;
 }
 
 // Opens a row, its record given or found. Larger ones' weights are summed where `sum` asks
