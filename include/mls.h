@@ -650,12 +650,13 @@ mls_status mls_cache_compact(const mls_kv_cache* c, int64_t n, const int32_t* pa
  * holds each node's parent: -1 for one behind the context, else an earlier node. A node
  * with any other parent, or below such a node, is not there: its rows are zeros, and no
  * node attends to it. One that has nothing to attend to, or whose scores are all -inf, gives
- * zeros too. Keys and values that a row does not attend to do not matter to it, whatever they
- * hold.
+ * zeros too. Keys and values that a row does not attend to do not change a bit of it, whatever
+ * they hold. Where the value of a node that it attends to is infinite or NaN, so is that
+ * element of the result (of a row that is not zeros), even if the weight is 0.
  * q [batch][n][heads][head_dim] has strides like mls_cache_write's k; out is contiguous, of
  * the cache's dtype, 16-byte aligned. n in 1..64, heads a multiple of kv_heads, head_dim
- * 32, 64, 96, 128, 192 or 256, scale finite and > 0. Sums are fp32; bf16 weights are rounded to bfloat16 for the
- * product with the values. Results depend on the table's width (entries are taken in parts),
+ * 32, 64, 96, 128, 192 or 256, scale finite and > 0. Sums are fp32; bf16 weights are rounded
+ * to bfloat16 for the product with the values. Results depend on the table's width (entries are taken in parts),
  * and are the same bits on every call. Calls of 2^24 or more blocks (row tiles times parts of
  * the entries, over all sequences and key heads), or of 2^34 or more results where there are
  * parts to join, are refused. Asynchronous on stream.
@@ -682,8 +683,9 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
  * the next child is tried. Without draft_logits q(x) is 1 and p loses x. Where no child is
  * taken, next_token is drawn from p with u_sample, as mls_sample draws. Greedy mode takes
  * the first child that is the verifier's argmax and ends with the argmax (the uniforms,
- * draft_logits and the workspace may be NULL). A chain gives mls_spec_verify's results.
- * Probabilities are formed in 64 bits; which tokens top_p keeps is mls_sample's choice.
+ * draft_logits and the workspace may be NULL). Probabilities are formed in 64 bits; which tokens
+ * top_p keeps is mls_sample's choice. A chain gives mls_spec_verify's results, except where a
+ * uniform lies within float32's roundings of a threshold (that one has probabilities in 32 bits).
  * draft_params (may be NULL): [batch][n] records of MLS_ROW_PARAMS_BYTES from mls_sample on
  * the draft's rows with the same settings; records of nodes without children are not used.
  * Outputs: n_accepted int32 [batch], the drafted tokens taken; path int32 [batch][n], the
@@ -712,7 +714,8 @@ mls_status mls_quantize_rows(int64_t T, int64_t d, int64_t ld_x, int32_t dtype, 
  * mls_head_logits with the head's weights as 8-bit integers (mls_quantize_rows of W [V][d],
  * once, when a server loads them): the rows of o are made 8-bit integers q, scale alike, and
  *   logits[t][v] = scale[t] W_scale[v] sum_k q[t][k] W[v][k],
- * the sum in 32-bit integers, exact. o [T][d] of dtype, W int8 [V][d], logits float32
+ * the sum in 32-bit integers, exact; then it, the product with scale[t] and that with W_scale[v]
+ * are rounded to float32 in turn. o [T][d] of dtype, W int8 [V][d], logits float32
  * [T][V], all contiguous and 16-byte aligned; W_scale float32 [V]. d is a multiple of 16, at
  * most 2^17, and the tiles of the logits (64 x 32 to 192 x 128) number below 2^24. A row of o
  * with an infinity or NaN gives NaN. Asynchronous on stream.

@@ -997,8 +997,9 @@ def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
     the tree does not have (nor any below it), whose rows are zeros. Without ``parents`` the nodes are a chain, and
     ``n = 1`` is a decoding step without a draft. Up to 64 nodes; ``heads`` is a multiple of the pages' ``kv_heads``
     (consecutive heads share one); ``head_dim`` 32, 64, 96, 128, 192 or 256; ``scale`` is ``head_dim ** -0.5`` by
-    itself. bf16 or float32, sums in float32; the weights of bf16 values are rounded to bf16. The entries are taken
-    in parts as the table's width has it, so pass the columns that are in use.
+    itself. bf16 or float32, sums in float32; the weights of bf16 values are rounded to bf16. What a node does not
+    attend to does not change a bit of its result, whatever it holds. The entries are taken in parts as the table's
+    width has it, so pass the columns that are in use.
     """
     _no_grad("tree_attention", q, k_pages, v_pages)
     c, n, heads, ld, default, ws_bytes = _attention_plan(_meta(q), _meta(k_pages), _meta(v_pages),

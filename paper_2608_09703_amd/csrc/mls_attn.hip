@@ -9,7 +9,9 @@
 //
 // What bounds it is the entries' bytes, read once per block of rows: 4 sequences of 65,536
 // entries, 34 heads of 128, one row: 698 us, 6.5 TB/s (a large copy: 4.9 TB/s, reads alone
-// about 6.6); 102 of 1,280 entries, 16 rows in 64 nodes' tree: 229 us with 17 heads, 5.5 TB/s.
+// about 6.6); 102 of up to 1,536 entries, 16 nodes, 24 heads of 96: 227 us, 5.4 TB/s. float32: 102
+// of 1,280, 24 heads of 96: 440 us with one node (5.5 TB/s), 471 with 16; 4 of 32,768, 34 heads of
+// 128: 821 us with one node, 988 with 32 (4.6 TB/s, 74 TFLOP/s).
 //
 // A block takes up to 64 rows (nodes x heads of one key head) and one part of the
 // entries; its waves take the part's tiles in turn, each for itself, and join their
@@ -397,7 +399,9 @@ struct Attn {
           s[t][u][i] = fast_exp2(s[t][u][i]);
           l[t] += s[t][u][i];
         }
-      // bf16 weights, as the values are: up to 2^-8 of each, in both directions
+      // bf16 weights, as the values are: up to 2^-8 of each, in both directions. (A weight's two
+      // halves would be two products. 102 trees of 16 nodes: results 2.3e-3 off those in 64 bits,
+      // with float32 weights 1.7e-3, which is the results' own rounding.)
       pb[t] = pack_weights(s[t]);
     }
     return odd;
@@ -667,8 +671,9 @@ void tree_attention_kernel(AttnArgs a) {
 // tile from the second-level and memory-side caches, at their 10 TB/s: 16 sequences of 8,000
 // entries, 320 rows of each of two heads of 128: 126 -> 95 us (440 TFLOP/s); 256 rows of 4
 // heads of 96: 122 -> 108; 64 sequences of 2,000, 128 rows of 4 heads of 128: 98 -> 78. What
-// bounds it: the exponentials and masks between the two products, with two waves a SIMD to
-// hide them behind (matrix units 20 % busy, waves waiting 43 % of the time).
+// bounds it: the exponentials, sums and packing between the two products, with two waves a SIMD
+// to hide them behind (matrix units 20 % busy, waves waiting 43 % of the time); masks are in
+// the tiles with nodes or missing pages alone.
 //
 // A run of 16 entries of K has its 16-byte chunks rotated per entry (K's reads take one
 // chunk of 16 entries at a time); V lies as it is (its reads take whole entries).
@@ -955,7 +960,13 @@ bool attn_many(int32_t rows, int32_t D, bool f32, int64_t ways) {
 }
 int attn_many_tile() { return kManyTile; }
 int attn_many_tiles() { return kAttnWaves; }
-// blocks: of one part each; entries: that a table's row has room for
+// blocks: of one part each; entries: that a table's row has room for. With it / without, us:
+// 16 blocks, heads of 64: 511 entries 7.0 / 9.2, 1,023 9.6 / 10.3, 1,343 11.2 / 10.9, 2,047 14.9 / 12.1;
+// 16 blocks, heads of 128: 511 10.3 / 11.5, 767 12.3 / 11.9, 1,535 19.0 / 13.5;
+// 256 blocks: heads of 64, 511 7.9 / 11.9, 1,535 19.1 / 22.4, 3,071 32.7 / 36.0, of 96, 1,535 27.0 / 30.0;
+// heads of 64, 1,343 entries: 384 blocks 24.0 / 27.7, 1,024 59.0 / 54.4.
+// One border for all: the widest heads of few blocks lose above 700 entries, many blocks would
+// still gain beyond it.
 bool attn_short(int64_t blocks, int64_t entries, int32_t rows, int32_t head_bytes) {
   return blocks <= 256 && entries <= 1536 && rows <= 16 && head_bytes <= kShortRow;
 }

@@ -526,7 +526,7 @@ struct AttnArgs {
   int32_t part;    // entries of a part
   int32_t shorts;  // attn_short: one part, more waves to a block
   int32_t once;    // entries are read once, and then not for long
-  float* acc;      // [batch][kv_heads][n_rt][splits][tile rows][D] partial sums, if splits > 1
+  float* acc;      // [batch][kv_heads][n_tiles][splits][tile rows][D] partial sums, if splits > 1
   float* ml;       // and [..][tile rows][2]: their maximum and sum of weights
 };
 // Verification of a tree of drafted tokens.

@@ -673,7 +673,8 @@ hipError_t launch_tree_ept(const TreeVerifyArgs& a, hipStream_t stream) {
 }  // namespace
 
 // Rows opened beforehand: a block each, one on a CU. 102 trees of 16 nodes at V = 49,152
-// (with the walk): 256 rows 228 us, 512 211, 1,024 184, 2,048 213, 4,096 229.
+// (with the walk): 256 rows 228 us, 512 211, 1,024 184, 2,048 213, 4,096 229. Half of them are the
+// draft's: without a draft 512 are opened (the same trees, nucleus 0.9: 91 us).
 constexpr int64_t kReadyRows = 1024;
 static int tree_ready_nodes(int64_t batch, int64_t n) {
   const int64_t k = kReadyRows / (2 * batch);
