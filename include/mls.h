@@ -679,7 +679,8 @@ mls_status mls_tree_attention(const mls_kv_cache* c, int64_t n, int64_t heads, c
  *                                drawn, each by itself; NULL: children without probabilities
  * The walk starts at node 0. At node c with p = the verifier's sampling distribution (as
  * mls_sample has it) and q the draft's, child x of c, in node order, is taken when u_accept
- * q(x) < p(x); otherwise p becomes max(0, p - q) over its sum (p itself where that is 0), and
+ * q(x) < p(x); otherwise p becomes max(0, p - q) over its sum (p itself where that is 0; a
+ * difference below 2^-42 of p is none), and
  * the next child is tried. Without draft_logits q(x) is 1 and p loses x. Where no child is
  * taken, next_token is drawn from p with u_sample, as mls_sample draws. Greedy mode takes
  * the first child that is the verifier's argmax and ends with the argmax (the uniforms,

@@ -133,6 +133,14 @@ __device__ __forceinline__ double prob(const Row& r, int v, const Settings& a) {
   return prob_of(r, r.logits[v], v, a);
 }
 
+// max(0, p - q) of a token. Where both are the same number, formed on two ways (weights 2e-14 off, sums
+// in another order, a fused multiply-add), it is none: rows that are alike have nothing left, and
+// no distribution of roundings.
+__device__ __forceinline__ double left_of(double p, double q) {
+  const double d = p - q;
+  return d > p * 0x1p-42 ? d : 0.0;
+}
+
 // Calls f(logit, v, in) for the wave's range of the row, 64 tokens after 64 in index order,
 // kAhead loads in flight.
 template <class F>
@@ -471,7 +479,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
     if (x == 0.0 || rejected == 0) return x;
     if (a.draft) {
       const double qv = prob(q, v, set);
-      for (int j = 0; j < rejected; ++j) x = fmax(x - qv, 0.0) * ts.scale[j];
+      for (int j = 0; j < rejected; ++j) x = left_of(x, qv) * ts.scale[j];
       return x;
     }
     // (each factor is 1 over the mass left of the step before, which the last one alone is not; in
@@ -587,7 +595,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
       // what is left of p, over its mass (no mass left: p stays as it was)
       double s = 0.0;
       if (n >= 0) {
-        const double w = a.draft ? fmax(r - qi, 0.0) : idx == x ? 0.0 : r;
+        const double w = a.draft ? left_of(r, qi) : idx == x ? 0.0 : r;
         s = block_sum(w, ts, turn);
         if (s > 0.0) r = w * (1.0 / s);
       } else {
@@ -606,7 +614,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_verify_kernel(TreeVerifyArg
 #pragma unroll
           for (int u = 0; u < kAhead; ++u) {
             const int k = k0 + u * kTreeThreads;
-            const double y = a.draft ? fmax(w[u] * over - qw[u], 0.0) : v[u] == x ? 0.0 : w[u] * over;
+            const double y = a.draft ? left_of(w[u] * over, qw[u]) : v[u] == x ? 0.0 : w[u] * over;
             if (k < N) {
               s += y;
               lr2[k] = y;
