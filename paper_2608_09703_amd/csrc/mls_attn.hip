@@ -963,7 +963,7 @@ int attn_many_tiles() { return kAttnWaves; }
 // blocks: of one part each; entries: that a table's row has room for. With it / without, us:
 // 16 blocks, heads of 64: 511 entries 7.0 / 9.2, 1,023 9.6 / 10.3, 1,343 11.2 / 10.9, 2,047 14.9 / 12.1;
 // 16 blocks, heads of 128: 511 10.3 / 11.5, 767 12.3 / 11.9, 1,535 19.0 / 13.5;
-// 256 blocks: heads of 64, 511 7.9 / 11.9, 1,535 19.1 / 22.4, 3,071 32.7 / 36.0, of 96, 1,535 27.0 / 30.0;
+// 256 blocks: heads of 64, 511 7.9 / 11.9, 1,535 19.1 / 22.4, 2,047 24.4 / 27.3, of 96, 1,535 27.0 / 30.0;
 // heads of 64, 1,343 entries: 384 blocks 24.0 / 27.7, 1,024 59.0 / 54.4.
 // One border for all: the widest heads of few blocks lose above 700 entries, many blocks would
 // still gain beyond it.
